@@ -324,6 +324,184 @@ int llmcad_commit_path(const llmcad_config* cfg, void* k_cache, void* v_cache, i
                        int32_t prefix_len, const int32_t* path, const int32_t* accept_len, int32_t n,
                        void* stream);
 
+/*
+ * Several requests behind one shared prefix.
+ *
+ * A server answers many requests whose prompts begin alike (a system prompt, a
+ * document, worked examples).  The prefix's keys and values are kept once, in a
+ * KV cache as above (llmcad_prefill writes it); what a request adds -- its own
+ * prompt, its accepted tokens -- lies in pages of LLMCAD_PAGE slots, each a KV
+ * cache of capacity LLMCAD_PAGE:
+ *   k_pages bf16 [L][n_pages][Hkv][LLMCAD_PAGE][Dh]
+ *   v_pages bf16 [L][n_pages][Hkv][Dh][LLMCAD_PAGE]
+ * Slot s is entry s % LLMCAD_PAGE of page s / LLMCAD_PAGE.  Token t of request
+ * b (t counts from the end of the prefix) lies in page block_table[b][t /
+ * LLMCAD_PAGE].  A step adds rows to the requests: request b, which holds
+ * held[b] tokens, gets rows [row_start[b], row_start[b + 1]) -- one token, a
+ * chain, or a token tree (parent as in llmcad_verify_tree, counted within the
+ * request) of at most LLMCAD_MAX_NODES nodes; none, if it sits the step out.
+ * Row i of a request is its token held + i, at position prefix_len + held +
+ * depth(i), and sees the prefix, the request's held tokens, its ancestors and
+ * itself.  Rows [row_start[B], n_rows) are padding (a step captured in a graph
+ * has a fixed n_rows): no operator reads or writes theirs.
+ *
+ * A step is llmcad_batch_plan once, llmcad_batch_store and
+ * llmcad_batch_attention in every layer, and llmcad_batch_commit after the
+ * target has answered.  Lengths, tables and trees are device arrays, so that a
+ * step can be captured and replayed while requests grow.
+ *
+ * The configuration gives L, H, Dh and theta; n_kv_heads (Hkv) divides H, and
+ * query head h reads K/V head h / (H / Hkv).  Pointers to bf16 data, plans and
+ * workspaces are 16-byte aligned, row strides multiples of 8 elements.
+ */
+#define LLMCAD_PAGE 64
+#define LLMCAD_MAX_REQUESTS 1024
+
+/* Status of a request in a plan. */
+#define LLMCAD_PLAN_OK 0
+#define LLMCAD_PLAN_BAD_LENGTHS 1 /* row_start does not rise from 0 to at most n_rows in steps of at most
+                                     LLMCAD_MAX_NODES, or a length is negative: no request is placed */
+#define LLMCAD_PLAN_NO_PAGES 2    /* the request's rows need pages past its table or the free list, or an
+                                     entry of either is not in [0, n_pages): the request is not placed */
+#define LLMCAD_PLAN_BAD_TREE 3    /* its parents are not a tree (-1 for the first row, then earlier rows) */
+
+/* Bytes of a plan (0 if the configuration or a size is invalid: 1 <= n_requests
+ * <= LLMCAD_MAX_REQUESTS, 1 <= n_rows <= 2 LLMCAD_MAX_REQUESTS LLMCAD_MAX_NODES). */
+size_t llmcad_batch_plan_bytes(const llmcad_config* cfg, int32_t n_requests, int32_t n_rows);
+
+/* Byte offset and size of a plan's arrays: 0 slot int32 [n_rows] (-1: the row
+ * has none), 1 position int32 [n_rows], 2 mask uint32 [n_rows][4] (bit j: row j
+ * of the request is the row or an ancestor), 3 rotary table fp32
+ * [n_rows][Dh/2][2] (cos, sin of position theta^(-2j/Dh), computed in 64 bits),
+ * 4 status int32 [n_requests] (LLMCAD_PLAN_*), 5 pages taken int32 [1]. */
+int llmcad_batch_plan_region(const llmcad_config* cfg, int32_t n_requests, int32_t n_rows, int32_t which, size_t* offset,
+                             size_t* bytes);
+
+/*
+ * The plan of a step, built on the device from the requests' lengths.
+ *
+ * row_start int32 [n_requests + 1], held int32 [n_requests], parent int32
+ * [n_rows] (NULL: chains), block_table int32 [n_requests][max_pages],
+ * free_pages int32 [n_free] (device arrays).  Requests take the pages that
+ * their rows need beyond those they hold from free_pages in the order of the
+ * requests; block_table receives them, and "pages taken" their number: the
+ * caller's free list begins behind them in the next step.  Where the free list
+ * is too short, the requests whose share lies within it are placed and the
+ * others are not (status LLMCAD_PLAN_NO_PAGES, their shares stay counted in
+ * "pages taken", which then exceeds n_free).  A request that is not placed has
+ * slot -1, position 0 and an empty mask in its rows, its table row is left as
+ * it was, and the other operators leave its rows out.  Calling again with the
+ * same arguments gives the same plan.
+ *
+ * Errors (checked on the host, nothing enqueued): LLMCAD_EARG for a NULL or
+ * unaligned pointer or a size out of range, LLMCAD_ECAPACITY for prefix_len not
+ * in [0, 2^30], LLMCAD_EWORKSPACE for plan_bytes below llmcad_batch_plan_bytes.
+ */
+int llmcad_batch_plan(const llmcad_config* cfg, int32_t n_requests, int32_t n_rows, const int32_t* row_start,
+                      const int32_t* held, const int32_t* parent, int32_t prefix_len, int32_t* block_table,
+                      int32_t max_pages, const int32_t* free_pages, int32_t n_free, int32_t n_pages, void* plan,
+                      size_t plan_bytes, void* stream);
+
+/*
+ * Rotary embedding of a layer's queries and keys, and the write of its keys and
+ * values into the pages.
+ *
+ * q bf16 [n_rows][H][Dh], k and v bf16 [n_rows][Hkv][Dh], rows q_stride,
+ * k_stride and v_stride elements apart (a fused projection's output is taken as
+ * it is).  q_out bf16 [n_rows][H][Dh] receives the turned queries (rotate-half
+ * pairing; it may be q itself if q_stride is H Dh), the row's slot of layer
+ * `layer` the turned key and the value; each is rounded to bf16 once.  Rows
+ * without a slot are left out.
+ *
+ * Errors: LLMCAD_EARG (a NULL or unaligned pointer, a stride that is no
+ * multiple of 8, a layer or size out of range), LLMCAD_ESHAPE (n_kv_heads does
+ * not divide H, a stride shorter than a row), LLMCAD_EWORKSPACE (plan_bytes).
+ */
+int llmcad_batch_store(const llmcad_config* cfg, int32_t n_kv_heads, int32_t layer, const void* q, int64_t q_stride,
+                       const void* k, int64_t k_stride, const void* v, int64_t v_stride, void* q_out, void* k_pages,
+                       void* v_pages, int32_t n_pages, const void* plan, size_t plan_bytes, int32_t n_requests,
+                       int32_t n_rows, void* stream);
+
+/* Bytes of llmcad_batch_attention's workspace (0 if an argument is invalid).  It
+ * need not be cleared; calls that share one must not overlap. */
+size_t llmcad_batch_workspace_bytes(const llmcad_config* cfg, int32_t n_kv_heads, int32_t n_requests, int32_t n_rows);
+
+/*
+ * A layer's attention of every row to the shared prefix (read once for all
+ * requests), to its request's held tokens and to its own branch:
+ *   out[r][h] = sum_t softmax_t(q[r][h] . k[t] / sqrt(Dh)) v[t].
+ * q bf16 [n_rows][H][Dh] after the rotary embedding, rows q_stride apart; out
+ * bf16 [n_rows][H][Dh].  k_cache / v_cache hold the prefix in slots [0,
+ * prefix_len) (layouts as above with Hkv heads; not read if prefix_len is 0).
+ * Softmax and sums in fp32; the probabilities enter the value product in bf16
+ * or finer.  A held token whose table entry is not in [0, n_pages) counts as
+ * absent; a row that sees nothing gets zeros; what lies in slots that a row does
+ * not see (Inf and NaN too) does not reach it.  Rows of no request, or of one
+ * that the plan did not place, are left as they were.
+ *
+ * Errors: as llmcad_batch_store; LLMCAD_ECAPACITY unless 0 <= prefix_len <=
+ * capacity and capacity is a positive multiple of 64 (with a prefix);
+ * LLMCAD_EWORKSPACE for a plan or workspace that is too small.
+ */
+int llmcad_batch_attention(const llmcad_config* cfg, int32_t n_kv_heads, int32_t layer, const void* q, int64_t q_stride,
+                           const void* k_cache, const void* v_cache, int32_t capacity, int32_t prefix_len,
+                           const void* k_pages, const void* v_pages, int32_t n_pages, const int32_t* block_table,
+                           int32_t max_pages, const void* plan, size_t plan_bytes, int32_t n_requests, int32_t n_rows,
+                           void* out, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Rollback of every request to its verified sequence (llmcad_commit_path, in
+ * pages): in every layer and K/V head the keys and values of row path[k] move
+ * to row k, k = 1 .. accept_len[b], of request b.  path int32 [n_rows]: request
+ * b's path from entry row_start[b] on, counted within the request, its first
+ * entry the root's 0; accept_len int32 [n_requests] (device arrays).  The
+ * request then holds held[b] + accept_len[b] + 1 tokens.  plan is the step's.
+ * accept_len not in [1, rows of the request) moves nothing, nor does an entry
+ * path[k] that is not in (k, rows of the request).
+ *
+ * Errors: as llmcad_batch_store.
+ */
+int llmcad_batch_commit(const llmcad_config* cfg, int32_t n_kv_heads, void* k_pages, void* v_pages, int32_t n_pages,
+                        const void* plan, size_t plan_bytes, int32_t n_requests, int32_t n_rows, const int32_t* path,
+                        const int32_t* accept_len, void* stream);
+
+/* Most alternatives llmcad_token_scores returns per row. */
+#define LLMCAD_TOP_MAX 64
+
+/* Bytes of llmcad_token_scores' workspace (0 if an argument is invalid).  It
+ * need not be cleared; calls that share one must not overlap. */
+size_t llmcad_token_scores_workspace_bytes(int32_t n_rows, int32_t vocab, int32_t k);
+
+/*
+ * Scores of logits rows: how likely given tokens are under them, how certain
+ * they are, and what else they hold likely.
+ *
+ * logits [n_rows][vocab], rows row_stride elements apart, fp32 (bits 32; what
+ * the passes return) or bf16 (bits 16), 1 <= vocab <= 2^24.
+ *   lse fp32 [n_rows]      log sum_t exp(logit_t)
+ *   entropy fp32 [n_rows]  -sum_t p_t log p_t, p = exp(logit - lse)
+ *   logprob fp32 [n_tokens] log p of tokens[i] under row row_of[i] (NULL: row i,
+ *                          n_tokens = n_rows; a tree's draft tokens go under
+ *                          their parents' rows).  A negative token ("none") gets
+ *                          0, one past the vocabulary or a row not in [0,
+ *                          n_rows) NaN.
+ *   top_token int32, top_logprob fp32 [n_rows][k] the k most likely tokens, most
+ *                          likely first, the lower token first among equal
+ *                          logits; tokens with a logit of -inf are none, and
+ *                          entries past the last are -1 and -inf.
+ * 0 <= k <= LLMCAD_TOP_MAX (0: top_token and top_logprob are not read).  Sums in
+ * fp32.  A row of nothing but -inf has lse -inf, entropy 0 and log probabilities
+ * -inf; a row with a NaN or +inf has NaN everywhere and no alternatives (-1).
+ *
+ * Errors (checked on the host, nothing enqueued): LLMCAD_EARG (a NULL or
+ * unaligned pointer, bits, a count or k out of range), LLMCAD_ESHAPE (vocab out
+ * of range, row_stride < vocab), LLMCAD_EWORKSPACE.
+ */
+int llmcad_token_scores(const void* logits, int32_t bits, int64_t row_stride, int32_t n_rows, int32_t vocab,
+                        const int32_t* tokens, const int32_t* row_of, int32_t n_tokens, float* logprob, float* entropy,
+                        float* lse, int32_t k, int32_t* top_token, float* top_logprob, void* workspace,
+                        size_t workspace_bytes, void* stream);
+
 /* Static text for a status code. */
 const char* llmcad_status_string(int status);
 

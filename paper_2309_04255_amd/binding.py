@@ -37,6 +37,15 @@ SYMBOLS = (
     "llmcad_commit_path",
     "llmcad_extend_tree",
     "llmcad_extend_tree_candidates",
+    "llmcad_batch_plan_bytes",
+    "llmcad_batch_plan_region",
+    "llmcad_batch_plan",
+    "llmcad_batch_store",
+    "llmcad_batch_workspace_bytes",
+    "llmcad_batch_attention",
+    "llmcad_batch_commit",
+    "llmcad_token_scores_workspace_bytes",
+    "llmcad_token_scores",
     "llmcad_status_string",
     "llmcad_workspace_region",
     "llmcad_split_plan",
@@ -106,7 +115,7 @@ def _load():
             f"{_LIB_PATH} is missing: build it with `python -m paper_2309_04255_amd.build` "
             "(there is no fallback implementation)")
     lib = ctypes.CDLL(_LIB_PATH)
-    P, I32, SZ = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t
+    P, I32, I64, SZ = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
     CFG = ctypes.POINTER(LlmcadConfig)
     I32P = ctypes.POINTER(ctypes.c_int32)
     sig = {
@@ -126,6 +135,16 @@ def _load():
         "llmcad_extend_tree": (ctypes.c_int, [CFG, P, P, P, I32, I32, I32P, I32P, I32, I32, P, P, SZ, P]),
         "llmcad_extend_tree_candidates": (ctypes.c_int, [CFG, P, P, P, I32, I32, I32P, I32P, I32, I32, ctypes.c_float,
                                                          P, P, P, SZ, P]),
+        "llmcad_batch_plan_bytes": (SZ, [CFG, I32, I32]),
+        "llmcad_batch_plan_region": (ctypes.c_int, [CFG, I32, I32, I32, ctypes.POINTER(SZ), ctypes.POINTER(SZ)]),
+        "llmcad_batch_plan": (ctypes.c_int, [CFG, I32, I32, P, P, P, I32, P, I32, P, I32, I32, P, SZ, P]),
+        "llmcad_batch_store": (ctypes.c_int, [CFG, I32, I32, P, I64, P, I64, P, I64, P, P, P, I32, P, SZ, I32, I32, P]),
+        "llmcad_batch_workspace_bytes": (SZ, [CFG, I32, I32, I32]),
+        "llmcad_batch_attention": (ctypes.c_int, [CFG, I32, I32, P, I64, P, P, I32, I32, P, P, I32, P, I32, P, SZ, I32,
+                                                  I32, P, P, SZ, P]),
+        "llmcad_batch_commit": (ctypes.c_int, [CFG, I32, P, P, I32, P, SZ, I32, I32, P, P, P]),
+        "llmcad_token_scores_workspace_bytes": (SZ, [I32, I32, I32]),
+        "llmcad_token_scores": (ctypes.c_int, [P, I32, I64, I32, I32, P, P, I32, P, P, P, I32, P, P, P, SZ, P]),
         "llmcad_status_string": (ctypes.c_char_p, [ctypes.c_int]),
         "llmcad_workspace_region": (ctypes.c_int, [CFG, I32, I32, ctypes.POINTER(SZ),
                                                    ctypes.POINTER(SZ)]),
@@ -345,6 +364,205 @@ def commit_path(cfg, k_cache, v_cache, prefix_len: int, path, accept_len, n: int
     return rc
 
 
+# ---- several requests behind one shared prefix (see the header's section)
+
+PAGE = 64  # LLMCAD_PAGE, slots of a page
+MAX_REQUESTS = 1024
+TOP_MAX = 64  # LLMCAD_TOP_MAX
+PLAN_OK = 0
+PLAN_BAD_LENGTHS = 1
+PLAN_NO_PAGES = 2
+PLAN_BAD_TREE = 3
+_PLAN_REGIONS = ("slot", "position", "mask", "rope", "status", "taken")
+
+
+def _on_device(what, first, *others):
+    """The device every tensor of a call lies on (ValueError if they differ or one is not on a GPU)."""
+    dev = first.device
+    if dev.type != "cuda":
+        raise ValueError(f"{what}: the tensors must be on a GPU")
+    for t in others:
+        if t is not None and t.device != dev:
+            raise ValueError(f"{what}: tensors on {dev} and {t.device}")
+    return dev
+
+
+def _enqueue(fn, dev, stream, args):
+    """fn(*args, stream) with dev the current device (a launch goes to the current device's kernels)."""
+    if dev.index == torch.cuda.current_device():
+        return fn(*args, (stream or torch.cuda.current_stream()).cuda_stream)
+    with torch.cuda.device(dev):
+        return fn(*args, (stream or torch.cuda.current_stream()).cuda_stream)
+
+
+def _want(what, name, t, dtype, *shape):
+    """t is a contiguous tensor of dtype and shape (None: any size)."""
+    if t.dtype != dtype or t.dim() != len(shape) or not t.is_contiguous() or \
+            any(w is not None and w != s for w, s in zip(shape, t.shape)):
+        raise ValueError(f"{what}: {name} must be a contiguous {dtype} tensor of shape "
+                         f"{tuple('any' if w is None else w for w in shape)}, got {t.dtype} {tuple(t.shape)}")
+
+
+def _want_rows(what, name, t, n, heads, dh):
+    """t is bf16 [n, heads, dh] whose rows are contiguous (any distance between them); returns that distance."""
+    if t.dtype != torch.bfloat16 or t.shape != (n, heads, dh) or t.stride(2) != 1 or \
+            (heads > 1 and t.stride(1) != dh):
+        raise ValueError(f"{what}: {name} must be bfloat16 [{n}, {heads}, {dh}] with contiguous rows, "
+                         f"got {t.dtype} {tuple(t.shape)}")
+    return t.stride(0) if n > 1 else heads * dh
+
+
+def batch_plan_bytes(cfg, n_requests: int, n_rows: int) -> int:
+    return _lib.llmcad_batch_plan_bytes(ctypes.byref(cfg), int(n_requests), int(n_rows))
+
+
+def batch_plan_views(cfg, n_requests: int, n_rows: int, plan) -> dict:
+    """The arrays of a plan as views of its buffer: slot, position int32 [n_rows], mask int32
+    [n_rows, 4], rope float32 [n_rows, Dh/2, 2], status int32 [n_requests], taken int32 [1]."""
+    shapes = {"slot": (n_rows,), "position": (n_rows,), "mask": (n_rows, 4), "rope": (n_rows, cfg.head_dim // 2, 2),
+              "status": (n_requests,), "taken": (1,)}
+    views, off, size = {}, ctypes.c_size_t(), ctypes.c_size_t()
+    for which, name in enumerate(_PLAN_REGIONS):
+        _check(_lib.llmcad_batch_plan_region(ctypes.byref(cfg), int(n_requests), int(n_rows), which, ctypes.byref(off),
+                                             ctypes.byref(size)), "llmcad_batch_plan_region")
+        part = plan[off.value:off.value + size.value].view(torch.float32 if name == "rope" else torch.int32)
+        views[name] = part.view(shapes[name])
+    return views
+
+
+def batch_plan(cfg, row_start, held, parent, prefix_len: int, block_table, free_pages, n_pages: int, plan,
+               n_rows: int, stream=None):
+    """Build a step's plan on the device (see llmcad_batch_plan): row_start [B + 1], held [B], parent
+    [n_rows] or None, block_table [B, max_pages] (updated), free_pages [n_free], all int32; plan a uint8
+    tensor of batch_plan_bytes."""
+    what = "batch_plan"
+    dev = _on_device(what, row_start, held, parent, block_table, free_pages, plan)
+    B = held.shape[0]
+    _want(what, "row_start", row_start, torch.int32, B + 1)
+    _want(what, "held", held, torch.int32, B)
+    _want(what, "block_table", block_table, torch.int32, B, None)
+    _want(what, "free_pages", free_pages, torch.int32, None)
+    _want(what, "plan", plan, torch.uint8, None)
+    if parent is not None:
+        _want(what, "parent", parent, torch.int32, None)
+        if parent.shape[0] < n_rows:
+            raise ValueError("batch_plan: parent must have an entry for every row")
+    _check(_enqueue(_lib.llmcad_batch_plan, dev, stream,
+                    (ctypes.byref(cfg), B, int(n_rows), row_start.data_ptr(), held.data_ptr(),
+                     parent.data_ptr() if parent is not None else None, int(prefix_len), block_table.data_ptr(),
+                     block_table.shape[1], free_pages.data_ptr(), free_pages.shape[0], int(n_pages), plan.data_ptr(),
+                     plan.shape[0])), "llmcad_batch_plan")
+
+
+def _want_pages(what, cfg, n_kv_heads, k_pages, v_pages):
+    n_pages = k_pages.shape[1]
+    _want(what, "k_pages", k_pages, torch.bfloat16, cfg.n_layers, n_pages, n_kv_heads, PAGE, cfg.head_dim)
+    _want(what, "v_pages", v_pages, torch.bfloat16, cfg.n_layers, n_pages, n_kv_heads, cfg.head_dim, PAGE)
+    return n_pages
+
+
+def batch_store(cfg, n_kv_heads: int, layer: int, q, k, v, q_out, k_pages, v_pages, plan, n_requests: int,
+                stream=None):
+    """Rotary embedding of q [N, H, Dh] (to q_out) and k [N, Hkv, Dh], and the write of k and v into the
+    layer's pages at the plan's slots (see llmcad_batch_store).  q, k and v may be slices of one fused
+    projection; q_out may be q."""
+    what = "batch_store"
+    dev = _on_device(what, q, k, v, q_out, k_pages, v_pages, plan)
+    N, H, Dh = q.shape[0], cfg.n_heads, cfg.head_dim
+    qs = _want_rows(what, "q", q, N, H, Dh)
+    ks = _want_rows(what, "k", k, N, n_kv_heads, Dh)
+    vs = _want_rows(what, "v", v, N, n_kv_heads, Dh)
+    _want(what, "q_out", q_out, torch.bfloat16, N, H, Dh)
+    _want(what, "plan", plan, torch.uint8, None)
+    n_pages = _want_pages(what, cfg, n_kv_heads, k_pages, v_pages)
+    _check(_enqueue(_lib.llmcad_batch_store, dev, stream,
+                    (ctypes.byref(cfg), int(n_kv_heads), int(layer), q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs,
+                     q_out.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), n_pages, plan.data_ptr(), plan.shape[0],
+                     int(n_requests), N)), "llmcad_batch_store")
+
+
+def batch_workspace_bytes(cfg, n_kv_heads: int, n_requests: int, n_rows: int) -> int:
+    return _lib.llmcad_batch_workspace_bytes(ctypes.byref(cfg), int(n_kv_heads), int(n_requests), int(n_rows))
+
+
+def batch_attention(cfg, n_kv_heads: int, layer: int, q, k_cache, v_cache, prefix_len: int, k_pages, v_pages,
+                    block_table, plan, out, workspace, stream=None):
+    """Attention of the rows q [N, H, Dh] (after the rotary embedding) to the shared prefix in slots
+    [0, prefix_len) of k_cache [L, Hkv, cap, Dh] / v_cache [L, Hkv, Dh, cap] (None without a prefix), to
+    their requests' pages and branches (see llmcad_batch_attention); out [N, H, Dh]."""
+    what = "batch_attention"
+    dev = _on_device(what, q, k_cache, v_cache, k_pages, v_pages, block_table, plan, out, workspace)
+    N, H, Dh = q.shape[0], cfg.n_heads, cfg.head_dim
+    qs = _want_rows(what, "q", q, N, H, Dh)
+    _want(what, "out", out, torch.bfloat16, N, H, Dh)
+    _want(what, "block_table", block_table, torch.int32, None, None)
+    _want(what, "plan", plan, torch.uint8, None)
+    _want(what, "workspace", workspace, torch.uint8, None)
+    n_pages = _want_pages(what, cfg, n_kv_heads, k_pages, v_pages)
+    cap = 0
+    if k_cache is not None and v_cache is not None:
+        cap = k_cache.shape[2] if k_cache.dim() == 4 else 0
+        _want(what, "k_cache", k_cache, torch.bfloat16, cfg.n_layers, n_kv_heads, cap, Dh)
+        _want(what, "v_cache", v_cache, torch.bfloat16, cfg.n_layers, n_kv_heads, Dh, cap)
+    _check(_enqueue(_lib.llmcad_batch_attention, dev, stream,
+                    (ctypes.byref(cfg), int(n_kv_heads), int(layer), q.data_ptr(), qs,
+                     k_cache.data_ptr() if cap else None, v_cache.data_ptr() if cap else None, cap, int(prefix_len),
+                     k_pages.data_ptr(), v_pages.data_ptr(), n_pages, block_table.data_ptr(), block_table.shape[1],
+                     plan.data_ptr(), plan.shape[0], block_table.shape[0], N, out.data_ptr(), workspace.data_ptr(),
+                     workspace.shape[0])), "llmcad_batch_attention")
+
+
+def batch_commit(cfg, n_kv_heads: int, k_pages, v_pages, plan, n_requests: int, path, accept_len, stream=None):
+    """Rollback of every request to its verified sequence (see llmcad_batch_commit): path int32 [n_rows],
+    accept_len int32 [n_requests], on the device."""
+    what = "batch_commit"
+    dev = _on_device(what, k_pages, v_pages, plan, path, accept_len)
+    _want(what, "path", path, torch.int32, None)
+    _want(what, "accept_len", accept_len, torch.int32, n_requests)
+    _want(what, "plan", plan, torch.uint8, None)
+    n_pages = _want_pages(what, cfg, n_kv_heads, k_pages, v_pages)
+    _check(_enqueue(_lib.llmcad_batch_commit, dev, stream,
+                    (ctypes.byref(cfg), int(n_kv_heads), k_pages.data_ptr(), v_pages.data_ptr(), n_pages, plan.data_ptr(),
+                     plan.shape[0], int(n_requests), path.shape[0], path.data_ptr(), accept_len.data_ptr())),
+           "llmcad_batch_commit")
+
+
+def token_scores_workspace_bytes(n_rows: int, vocab: int, k: int) -> int:
+    return _lib.llmcad_token_scores_workspace_bytes(int(n_rows), int(vocab), int(k))
+
+
+def token_scores(logits, tokens, k: int = 0, row_of=None, workspace=None, stream=None) -> dict:
+    """Scores of logits [n, V] (float32 or bfloat16, any distance between rows): {"logprob" of tokens
+    (int32; under row row_of[i], or row i), "entropy", "lse", "top_token" [n, k], "top_logprob" [n, k]}
+    (see llmcad_token_scores).  tokens may be None.  The outputs are new tensors of `stream`."""
+    what = "token_scores"
+    dev = _on_device(what, logits, tokens, row_of, workspace)
+    if logits.dim() != 2 or logits.dtype not in (torch.float32, torch.bfloat16) or \
+            (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise ValueError("token_scores: logits must be float32 or bfloat16 [n, V] with contiguous rows")
+    n, V = logits.shape
+    m = 0
+    if tokens is not None:
+        m = tokens.shape[0] if tokens.dim() == 1 else -1
+        _want(what, "tokens", tokens, torch.int32, n if row_of is None else m)
+        if row_of is not None:
+            _want(what, "row_of", row_of, torch.int32, m)
+    with torch.cuda.device(dev), torch.cuda.stream(stream):
+        if workspace is None:
+            workspace = torch.zeros(token_scores_workspace_bytes(n, V, k), dtype=torch.uint8, device=dev)
+        _want(what, "workspace", workspace, torch.uint8, None)
+        floats = torch.empty(m + 2 * n, dtype=torch.float32, device=dev)
+        top = torch.empty((2, n, k), dtype=torch.int32, device=dev)
+        base, tp = floats.data_ptr(), top.data_ptr()
+        _check(_lib.llmcad_token_scores(
+            logits.data_ptr(), 32 if logits.dtype == torch.float32 else 16, logits.stride(0) if n > 1 else V,
+            n, V, tokens.data_ptr() if m else None, row_of.data_ptr() if m and row_of is not None else
+            None, m, base, base + 4 * m, base + 4 * (m + n), int(k), tp, tp + 4 * n * k, workspace.data_ptr(),
+            workspace.shape[0], torch.cuda.current_stream().cuda_stream), "llmcad_token_scores")
+    return {"logprob": floats[:m], "entropy": floats[m:m + n], "lse": floats[m + n:], "top_token": top[0],
+            "top_logprob": top[1].view(torch.float32)}
+
+
 def workspace_region(cfg, n: int, which: int):
     off, size = ctypes.c_size_t(), ctypes.c_size_t()
     _check(_lib.llmcad_workspace_region(ctypes.byref(cfg), int(n), int(which), ctypes.byref(off),
@@ -451,6 +669,29 @@ class Session:
                     self.logits, self.workspace)
         return self.logits[: n - first]
 
+    def score_tree(self, tree_tokens, parent, k=0):
+        """Scores of the last verify_tree (with logits) over this tree: token_scores of its rows, "logprob"
+        being the log probability of every node's token after its parent's branch (the root's entry is 0:
+        nothing here predicts it)."""
+        n = len(tree_tokens)
+        host = np.stack([np.asarray(tree_tokens, dtype=np.int32), np.maximum(np.asarray(parent, dtype=np.int32), 0)])
+        host[0, 0] = -1
+        given = torch.from_numpy(host).to(self.device)
+        return token_scores(self.logits[:n], given[0], k, row_of=given[1])
+
+    def score(self, tokens, start_pos=0, k=0):
+        """Takes tokens in as prefill does and scores every position: {"logprob" [n] of the next token of
+        `tokens` (the last entry is 0), "entropy", "lse" [n], "top_token", "top_logprob" [n, k]}."""
+        tokens = np.asarray(tokens, dtype=np.int32)
+        following = torch.from_numpy(np.append(tokens[1:], np.int32(-1))).to(self.device)
+        parts = []
+        for off in range(0, len(tokens), self.max_n):
+            chunk = tokens[off:off + self.max_n]
+            rows = self.extend(start_pos + off, chunk, np.arange(-1, len(chunk) - 1), 0)
+            parts.append(token_scores(rows, following[off:off + len(chunk)], k))
+        self.check("scoring pass")
+        return {name: torch.cat([p[name] for p in parts]) for name in parts[0]}
+
     def extend_candidates(self, prefix_len, tree_tokens, parent, first, threshold):
         """Forward of nodes [first, n) with candidate summaries; returns one parsed
         record per computed row (synchronises; checks the device status)."""
@@ -495,3 +736,68 @@ class Session:
         acc = int(self.accept_len.item())
         return (self.logits[:n].cpu(), [int(x) for x in self.path[: acc + 1].cpu()], acc,
                 int(self.next_token.item()))
+
+
+class Batch:
+    """Several requests behind one shared prefix: the page pool, block tables and the step's plan and
+    workspace for a model of `shape` (device buffers owned here), with the prefix in k_cache / v_cache
+    (a Session's, or any of that layout with n_kv_heads heads; None: no prefix).
+
+    A step: plan(row_start, held, parent), then per layer store and attention, then commit with the
+    verified paths.  Lengths are the caller's: after a step request b holds held[b] + its accepted rows.
+    Pages go out in the order of `free_pages`; advance(pages taken) drops the ones a plan handed out,
+    release(b) takes back a finished request's."""
+
+    def __init__(self, shape, n_requests: int, n_rows: int, n_pages: int, max_pages: int, prefix_len: int = 0,
+                 k_cache=None, v_cache=None, n_kv_heads=None, device="cuda"):
+        self.cfg = make_config(shape)
+        rc = check_config(self.cfg)
+        if rc != OK:
+            raise LlmcadError(rc, "config")
+        dev = torch.device(device)
+        self.n_requests, self.n_rows, self.n_pages = int(n_requests), int(n_rows), int(n_pages)
+        self.n_kv_heads = int(n_kv_heads or shape.n_heads)
+        self.prefix_len, self.k_cache, self.v_cache = int(prefix_len), k_cache, v_cache
+        L, Dh = shape.n_layers, shape.head_dim
+        size = batch_plan_bytes(self.cfg, self.n_requests, self.n_rows)
+        work = batch_workspace_bytes(self.cfg, self.n_kv_heads, self.n_requests, self.n_rows)
+        if size == 0 or work == 0:
+            raise LlmcadError(EARG, "batch sizes")
+        self.k_pages = torch.zeros((L, self.n_pages, self.n_kv_heads, PAGE, Dh), dtype=torch.bfloat16, device=dev)
+        self.v_pages = torch.zeros((L, self.n_pages, self.n_kv_heads, Dh, PAGE), dtype=torch.bfloat16, device=dev)
+        self.block_table = torch.full((self.n_requests, int(max_pages)), -1, dtype=torch.int32, device=dev)
+        self.free_pages = torch.arange(self.n_pages, dtype=torch.int32, device=dev)
+        self.plan_buffer = torch.zeros(size, dtype=torch.uint8, device=dev)
+        self.workspace = torch.zeros(work, dtype=torch.uint8, device=dev)
+        for name, view in batch_plan_views(self.cfg, self.n_requests, self.n_rows, self.plan_buffer).items():
+            setattr(self, name, view)  # slot, position, mask, rope, status, taken
+
+    def plan(self, row_start, held, parent=None):
+        batch_plan(self.cfg, row_start, held, parent, self.prefix_len, self.block_table, self.free_pages,
+                   self.n_pages, self.plan_buffer, self.n_rows)
+
+    def store(self, layer, q, k, v, q_out):
+        batch_store(self.cfg, self.n_kv_heads, layer, q, k, v, q_out, self.k_pages, self.v_pages, self.plan_buffer,
+                    self.n_requests)
+
+    def attention(self, layer, q, out):
+        batch_attention(self.cfg, self.n_kv_heads, layer, q, self.k_cache, self.v_cache, self.prefix_len, self.k_pages,
+                        self.v_pages, self.block_table, self.plan_buffer, out, self.workspace)
+
+    def commit(self, path, accept_len):
+        batch_commit(self.cfg, self.n_kv_heads, self.k_pages, self.v_pages, self.plan_buffer, self.n_requests, path,
+                     accept_len)
+
+    def advance(self, taken=None):
+        """Drops the pages that the last plan handed out from the free list (taken: their number if the
+        caller has it; read from the device otherwise).  Raises if a request was not placed."""
+        taken = int(self.taken.item()) if taken is None else int(taken)
+        if taken > self.free_pages.shape[0]:
+            raise RuntimeError(f"the step needs {taken} pages and {self.free_pages.shape[0]} are free")
+        self.free_pages = self.free_pages[taken:].clone()
+
+    def release(self, request: int):
+        """Takes back the pages of a finished request."""
+        row = self.block_table[request]
+        self.free_pages = torch.cat([self.free_pages, row[row >= 0]])
+        row.fill_(-1)

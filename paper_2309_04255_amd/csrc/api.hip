@@ -16,6 +16,7 @@
 
 #include <mutex>
 
+#include "batch.h"
 #include "kernels.h"
 #include "layout.h"
 #include "llmcad.h"
@@ -73,6 +74,12 @@ struct TimedLaunch {
     if (on) (void)hipEventRecord(g_timing.ev[2 * slot + 1], st);
   }
 };
+
+}  // namespace
+
+void llmcad::keep_hip_error(hipError_t e) { g_last_error = e; }
+
+namespace {
 
 #define HIP_TRY(expr)                 \
   do {                                \

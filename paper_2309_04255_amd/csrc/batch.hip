@@ -1,0 +1,418 @@
+// A step of several requests behind one shared prefix, around its attention:
+// the plan (pages, slots, positions, ancestor masks, rotary table), the rotary
+// embedding with the write of the new keys and values into pages, and the
+// rollback to the accepted rows.
+#include "batch.h"
+
+namespace llmcad {
+
+namespace {
+
+constexpr int kThreads = 256;
+
+// Sum of a pair of 64-bit values over the workgroup, in every thread.
+__device__ __forceinline__ void block_sum(long long (&v)[4], long long* lds) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) v[i] += __shfl_xor(v[i], off, kWave);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0)
+    for (int i = 0; i < 4; ++i) lds[(threadIdx.x >> 6) * 4 + i] = v[i];
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[i] = 0;
+    for (int w = 0; w < kThreads / kWave; ++w) v[i] += lds[w * 4 + i];
+  }
+  __syncthreads();
+}
+
+// One workgroup per request.  Every workgroup reads all requests' lengths (a
+// few KiB) and sums what lies before its own, so that nothing is handed from
+// one workgroup to another and the launch needs no counters.
+__global__ __launch_bounds__(kThreads) void plan_kernel(PlanArgs a) {
+  __shared__ long long sums[4 * kThreads / kWave];
+  __shared__ int up[128];
+  __shared__ uint32_t anc[128][4];
+  __shared__ int pos_s[128];
+  __shared__ int page_s[4];
+  __shared__ int bad_s;
+  const int b = blockIdx.x, tid = threadIdx.x, B = a.B;
+  constexpr int PER = kMaxRequests / kThreads;
+  int n[PER], held[PER];
+  int bad = 0;
+  // pages wanted before request b and in all, pages held in all, (row, page) pairs in all
+  long long v[4] = {0, 0, 0, 0};
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int r = tid + i * kThreads;
+    n[i] = held[i] = 0;
+    if (r < B) {
+      const int lo = ldg(a.row_start + r), hi = ldg(a.row_start + r + 1);
+      const int h = ldg(a.held + r);
+      if (lo < 0 || hi < lo || (long long)hi - lo > LLMCAD_MAX_NODES || hi > a.N || h < 0 || (r == 0 && lo != 0)) {
+        bad = 1;
+      } else {
+        n[i] = hi - lo;
+        held[i] = h;
+      }
+      const long long need = ((long long)held[i] + n[i] + kPage - 1) / kPage - ((long long)held[i] + kPage - 1) / kPage;
+      long long pages = ((long long)held[i] + n[i] + kPage - 1) / kPage;
+      if (pages > a.max_pages) pages = a.max_pages;
+      if (r < b) v[0] += need;
+      v[1] += need;
+      if (n[i] > 0) v[2] += pages;
+      v[3] += pages * n[i];
+    }
+  }
+  const bool invalid = __syncthreads_or(bad) != 0;
+  block_sum(v, sums);
+  const long long need_before = v[0];
+  // The length of a run of pages: see kSplitRuns and kSplitRows; at least two
+  // pages, 32 keys for each of a workgroup's four waves.
+  long long chunk = 2;
+  const long long c1 = (v[2] + kSplitRuns - 1) / kSplitRuns;
+  const long long room = a.N > kSplitRows ? a.N : kSplitRows;
+  const long long c2 = (v[3] + room - 1) / room;
+  if (c1 > chunk) chunk = c1;
+  if (c2 > chunk) chunk = c2;
+  const long long taken = v[1];
+  // runs before request b and in all, partial rows before it
+  long long w[4] = {0, 0, 0, 0};
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int r = tid + i * kThreads;
+    if (r < B && n[i] > 0) {
+      long long pages = ((long long)held[i] + n[i] + kPage - 1) / kPage;
+      if (pages > a.max_pages) pages = a.max_pages;
+      const long long ns = (pages + chunk - 1) / chunk;
+      if (r < b) {
+        w[0] += ns;
+        w[2] += ns * n[i];
+      }
+      w[1] += ns;
+    }
+  }
+  block_sum(w, sums);
+  const int row0 = invalid ? 0 : ldg(a.row_start + b);
+  const int nb = invalid ? 0 : ldg(a.row_start + b + 1) - row0;
+  const int hb = invalid ? 0 : ldg(a.held + b);
+  const long long end = (long long)hb + nb;
+  const int first_new = (int)(((long long)hb + kPage - 1) / kPage);
+  const int need = (int)((end + kPage - 1) / kPage) - first_new;
+  int ns = 0;
+  if (nb > 0) {
+    long long pages = (end + kPage - 1) / kPage;
+    if (pages > a.max_pages) pages = a.max_pages;
+    ns = (int)((pages + chunk - 1) / chunk);
+  }
+
+  // Pages: the one the first new row shares with held tokens, then free ones.
+  if (tid == 0) bad_s = 0;
+  __syncthreads();
+  int st = LLMCAD_PLAN_OK;
+  if (invalid) st = LLMCAD_PLAN_BAD_LENGTHS;
+  else if (nb > 0 && (end > (long long)a.max_pages * kPage || need_before + need > a.n_free)) st = LLMCAD_PLAN_NO_PAGES;
+  const int col0 = hb / kPage;  // table column of the first new row
+  if (st == LLMCAD_PLAN_OK && nb > 0 && tid < 4) {
+    const int col = col0 + tid;
+    int id = -1;
+    if ((long long)col * kPage < end) {
+      id = col < first_new ? ldg(a.table + (size_t)b * a.max_pages + col)
+                           : ldg(a.free_pages + need_before + (col - first_new));
+      if (id < 0 || id >= a.n_pages) bad_s = 1;
+    }
+    page_s[tid] = id;
+  }
+  __syncthreads();
+  if (st == LLMCAD_PLAN_OK && bad_s) st = LLMCAD_PLAN_NO_PAGES;
+
+  // Parents, then ancestors-or-self by pointer jumping (7 rounds cover 128 rows).
+  int parent = -1;
+  bad = 0;
+  if (st == LLMCAD_PLAN_OK && tid < nb) {
+    parent = a.parent ? ldg(a.parent + row0 + tid) : tid - 1;
+    if (tid == 0 ? parent != -1 : (parent < 0 || parent >= tid)) bad = 1;
+  }
+  if (__syncthreads_or(bad)) st = LLMCAD_PLAN_BAD_TREE;
+  const bool placed = st == LLMCAD_PLAN_OK;
+  if (placed && tid < 4 && nb > 0) {
+    const int col = col0 + tid;
+    if (col >= first_new && (long long)col * kPage < end) stg(a.table + (size_t)b * a.max_pages + col, page_s[tid]);
+  }
+  if (placed && tid < nb) {
+    up[tid] = parent;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) anc[tid][j] = (tid >> 5) == j ? 1u << (tid & 31) : 0u;
+  }
+  __syncthreads();
+  for (int round = 0; round < 7; ++round) {
+    uint32_t m[4] = {0, 0, 0, 0};
+    int next = -1;
+    const bool on = placed && tid < nb && up[tid] >= 0;
+    if (on) {
+      const int p = up[tid];
+      next = up[p];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) m[j] = anc[p][j];
+    }
+    __syncthreads();
+    if (on) {
+      up[tid] = next;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) anc[tid][j] |= m[j];
+    }
+    __syncthreads();
+  }
+  if (!invalid && tid < nb) {
+    const int row = row0 + tid;
+    int slot = -1, pos = 0;
+    uint32_t m[4] = {0, 0, 0, 0};
+    if (placed) {
+      int seen = 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        m[j] = anc[tid][j];
+        seen += __popc(m[j]);
+      }
+      const int at = hb + tid;
+      slot = page_s[at / kPage - col0] * kPage + at % kPage;
+      pos = a.prefix_len + hb + seen - 1;
+    }
+    pos_s[tid] = pos;
+    stg(a.slot + row, slot);
+    stg(a.position + row, pos);
+    stg(a.row_req + row, placed ? b : -1);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) stg(a.mask + (size_t)row * 4 + j, m[j]);
+  }
+  __syncthreads();
+
+  // Rotary table: the angle in turns, position theta^(-2j/Dh) / 2 pi, reduced
+  // in 64 bits (a far position times an fp32 frequency is off by whole
+  // degrees); what is left, in [-1/2, 1/2], is split into an fp32 value and its
+  // remainder, which enters to first order.
+  const int half = a.Dh / 2, j = tid % half;
+  const double turns = exp2(-(2.0 * a.log2_theta / a.Dh) * j) * 0.15915494309189533577;
+  for (int i = tid / half; i < nb; i += kThreads / half) {
+    const double t = (double)pos_s[i] * turns;
+    const double f = t - rint(t);
+    const float x = (float)f;
+    const float rest = (float)(f - (double)x) * 6.2831853f;
+    float sn, cs;
+    sincospif(2.0f * x, &sn, &cs);
+    float* o = a.rope + ((size_t)(row0 + i) * half + j) * 2;
+    stg(o, cs - rest * sn);
+    stg(o + 1, sn + rest * cs);
+  }
+  // Rows behind the last request (all of them if the lengths are not valid).
+  const int total = invalid ? 0 : ldg(a.row_start + B);
+  for (int row = total + b * kThreads + tid; row < a.N; row += B * kThreads) {
+    stg(a.slot + row, -1);
+    stg(a.position + row, 0);
+    stg(a.row_req + row, -1);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) stg(a.mask + (size_t)row * 4 + k, 0u);
+  }
+  for (size_t e = (size_t)total * half + (size_t)b * kThreads + tid; e < (size_t)a.N * half; e += (size_t)B * kThreads) {
+    stg(a.rope + 2 * e, 1.0f);
+    stg(a.rope + 2 * e + 1, 0.0f);
+  }
+  if (tid == 0) {
+    BatchRequest r;
+    r.row0 = row0;
+    r.n = placed ? nb : 0;
+    r.held = hb;
+    r.splits = ns;
+    r.part0 = (int)w[2];
+    r.pad[0] = r.pad[1] = r.pad[2] = 0;
+    stg(a.req + b, r);
+    stg(a.status + b, st);
+    if (b == 0) {
+      stg(a.head + PLAN_UNITS, (int)(invalid ? 0 : w[1]));
+      stg(a.head + PLAN_CHUNK, (int)(chunk < (1 << 30) ? chunk : (1 << 30)));
+      stg(a.head + PLAN_TAKEN, (int)(invalid ? 0 : taken));
+    }
+  }
+  if (!invalid)
+    for (int s = tid; s < ns; s += kThreads) stg(a.units + w[0] + s, b << 16 | s);
+}
+
+}  // namespace
+
+hipError_t launch_batch_plan(const PlanArgs& a, hipStream_t st) {
+  plan_kernel<<<dim3(a.B), dim3(kThreads), 0, st>>>(a);
+  return hipGetLastError();
+}
+
+namespace {
+
+// ---------------------------------------------------------------- store
+//
+// Rows of 64 per workgroup and head.  A lane turns 8 dims of a row's first
+// half with their partners of the second (rotate-half pairing).  A V row
+// becomes a column of its page: the rows meet in LDS, and eight rows whose
+// slots are one aligned piece of eight leave as 16 bytes; the others (a
+// piece's ends, single tokens) as single entries.
+constexpr int kStoreRows = 64;
+
+__device__ __forceinline__ void turn8(const bf16* src, bf16* dst, const float* rope, int half) {
+  const bf16x8 a = ldg((const bf16x8*)src), b = ldg((const bf16x8*)(src + half));
+  bf16x8 x, y;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const f32x4 cs = ldg((const f32x4*)rope + e);  // cos, sin of two pairs
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const float p = bf2f(a[2 * e + u]), q = bf2f(b[2 * e + u]), c = cs[2 * u], s = cs[2 * u + 1];
+      x[2 * e + u] = f2bf(p * c - q * s);
+      y[2 * e + u] = f2bf(q * c + p * s);
+    }
+  }
+  stg((bf16x8*)dst, x);
+  stg((bf16x8*)(dst + half), y);
+}
+
+template <int DH>
+__global__ __launch_bounds__(kThreads) void store_kernel(StoreArgs a) {
+  __shared__ int slot_s[kStoreRows];
+  __shared__ int full_s[kStoreRows];
+  __shared__ uint16_t vt[kStoreRows][DH + 2];
+  const int r0 = blockIdx.x * kStoreRows, h = blockIdx.y, tid = threadIdx.x;
+  const int rows = a.N - r0 < kStoreRows ? a.N - r0 : kStoreRows;
+  constexpr int HALF = DH / 2, LANES = HALF / 8;  // lanes per row
+  if (tid < kStoreRows) {
+    int s = tid < rows ? ldg(a.slot + r0 + tid) : -1;
+    if (s >= a.n_pages * kPage) s = -1;
+    slot_s[tid] = s;
+  }
+  __syncthreads();
+  if (h < a.H) {  // a query head
+    for (int e = tid; e < rows * LANES; e += kThreads) {
+      const int i = e / LANES, c = 8 * (e % LANES);
+      if (slot_s[i] < 0) continue;
+      const size_t row = (size_t)r0 + i;
+      turn8(a.q + row * a.q_stride + (size_t)h * DH + c, a.q_out + (row * a.H + h) * DH + c,
+            a.rope + (row * HALF + c) * 2, HALF);
+    }
+    return;
+  }
+  const int kh = h - a.H;
+  for (int e = tid; e < rows * LANES; e += kThreads) {
+    const int i = e / LANES, c = 8 * (e % LANES), s = slot_s[i];
+    if (s < 0) continue;
+    const size_t row = (size_t)r0 + i;
+    turn8(a.k + row * a.k_stride + (size_t)kh * DH + c,
+          a.k_pages + (((size_t)(s / kPage) * a.Hkv + kh) * kPage + s % kPage) * DH + c,
+          a.rope + (row * HALF + c) * 2, HALF);
+  }
+  for (int e = tid; e < rows * (DH / 8); e += kThreads) {
+    const int i = e / (DH / 8), c = 8 * (e % (DH / 8));
+    if (slot_s[i] < 0) continue;
+    const bf16x8 v = ldg((const bf16x8*)(a.v + ((size_t)r0 + i) * a.v_stride + (size_t)kh * DH + c));
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const bf16 x = v[u];  // (a bit cast of the vector's element itself takes element 0)
+      vt[i][c + u] = __builtin_bit_cast(uint16_t, x);
+    }
+  }
+  if (tid < kStoreRows) {
+    const int s = slot_s[tid], first = tid - (s & 7);
+    int full = s >= 0 && first >= 0 && first + 8 <= kStoreRows;
+    for (int u = 0; u < 8 && full; ++u) full = slot_s[first + u] == (s & ~7) + u;
+    full_s[tid] = full;
+  }
+  __syncthreads();
+  for (int e = tid; e < rows * DH; e += kThreads) {
+    const int i = e / DH, c = e % DH, s = slot_s[i];
+    if (s < 0) continue;
+    bf16* dst = a.v_pages + (((size_t)(s / kPage) * a.Hkv + kh) * DH + c) * kPage + s % kPage;
+    if (full_s[i]) {
+      if (s & 7) continue;
+      bf16x8 v;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) v[u] = __builtin_bit_cast(bf16, vt[i + u][c]);
+      stg((bf16x8*)dst, v);
+    } else {
+      stg(dst, __builtin_bit_cast(bf16, vt[i][c]));
+    }
+  }
+}
+
+// ---------------------------------------------------------------- rollback
+//
+// As llmcad_commit_path, in pages.  Accepted row path[k] moves to row k, and
+// path[k] > k: a row that a move writes is never the source of a later one, so
+// a thread that moves its piece of the rows in the order of k needs no other
+// thread's and no copy in between (in batches: eight loads, then their eight
+// stores).  A thread's piece is 16 bytes of a K row or one dim of V^T.
+constexpr int kCommitBatch = 8;
+
+template <class T>
+__device__ __forceinline__ void move_rows(T* base, size_t page_step, int slot_step, const int* src, const int* dst, int len) {
+  for (int k0 = 0; k0 < len; k0 += kCommitBatch) {
+    T v[kCommitBatch];
+#pragma unroll
+    for (int u = 0; u < kCommitBatch; ++u) {
+      const int s = k0 + u < len ? src[k0 + u] : -1;
+      if (s >= 0) v[u] = ldg(base + (size_t)(s / kPage) * page_step + (s % kPage) * slot_step);
+    }
+#pragma unroll
+    for (int u = 0; u < kCommitBatch; ++u) {
+      const int s = k0 + u < len ? src[k0 + u] : -1;
+      if (s >= 0) {
+        const int d = dst[k0 + u];
+        stg(base + (size_t)(d / kPage) * page_step + (d % kPage) * slot_step, v[u]);
+      }
+    }
+  }
+}
+
+__global__ __launch_bounds__(kThreads) void commit_kernel(CommitArgs a) {
+  __shared__ int src_s[128], dst_s[128];  // slots of the moves k = 1 .. len
+  const int b = blockIdx.y, tid = threadIdx.x, dh = a.Dh;
+  const BatchRequest r = ldg(a.req + b);
+  const int len = ldg(a.accept_len + b);
+  if (len < 1 || len >= r.n) return;  // (nothing moves, or not the outcome of a tree of n rows)
+  const int limit = a.n_pages * kPage;
+  if (tid < len) {
+    const int k = tid + 1, p = ldg(a.path + r.row0 + k);
+    const int dst = ldg(a.slot + r.row0 + k);
+    int src = p > k && p < r.n ? ldg(a.slot + r.row0 + p) : -1;  // (in place already, or no row of the tree)
+    if (dst < 0 || dst >= limit || src >= limit) src = -1;
+    src_s[tid] = src;
+    dst_s[tid] = dst;
+  }
+  __syncthreads();
+  const int kp = dh / 8, per = kp + dh;  // pieces of a (layer, K/V head): K's, V^T's
+  const long long e = (long long)blockIdx.x * kThreads + tid;
+  const long long lh = e / per;
+  if (lh >= (long long)a.L * a.Hkv) return;
+  const int c = (int)(e % per);
+  const size_t page = (size_t)a.Hkv * kPage * dh;  // elements of a page
+  const size_t at = (size_t)(lh / a.Hkv) * a.n_pages * page + (size_t)(lh % a.Hkv) * kPage * dh;
+  if (c < dh)
+    move_rows(a.v_pages + at + (size_t)c * kPage, page, 1, src_s, dst_s, len);
+  else
+    move_rows((bf16x8*)(a.k_pages + at) + (c - dh), page / 8, kp, src_s, dst_s, len);
+}
+
+}  // namespace
+
+hipError_t launch_batch_store(const StoreArgs& a, hipStream_t st) {
+  const dim3 grid(cdiv(a.N, kStoreRows), a.H + a.Hkv);
+  if (a.Dh == 128)
+    store_kernel<128><<<grid, dim3(kThreads), 0, st>>>(a);
+  else
+    store_kernel<64><<<grid, dim3(kThreads), 0, st>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_batch_commit(const CommitArgs& a, hipStream_t st) {
+  const long long pieces = (long long)a.L * a.Hkv * (a.Dh + a.Dh / 8);
+  commit_kernel<<<dim3((unsigned)((pieces + kThreads - 1) / kThreads), a.B), dim3(kThreads), 0, st>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace llmcad

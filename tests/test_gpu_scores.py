@@ -1,0 +1,145 @@
+"""Token scores (llmcad_token_scores) against their float64 statement (oracle/batch.py).
+
+Tolerances: a logit enters exactly; lse and log probabilities are m + log S with S a sum of fp32
+exponentials (each within 2^-22, the sum of up to 2^18 of them in chains of at most 2^9 additions and
+14 joins: 2^-14 at the worst, 2^-20 in the mean of random roundings), the difference x - m rounded
+once: 2^-18 absolute and 2^-22 of the value.  The entropy adds products p (x - m) of size up to about
+100: 2^-15."""
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import batch as ob
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def binding():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2309_04255_amd import binding
+
+    return binding
+
+
+def _check(binding, logits, tokens, k, row_of=None, **kw):
+    dev = lambda a: None if a is None else torch.tensor(np.asarray(a), dtype=torch.int32, device="cuda")  # noqa: E731
+    got = binding.token_scores(logits, dev(tokens), k, row_of=dev(row_of), **kw)
+    torch.cuda.synchronize()
+    x = logits.float().cpu().numpy().astype(np.float64)
+    want = ob.token_scores(x, [] if tokens is None else tokens, row_of if tokens is not None else [], k)
+    np.testing.assert_array_equal(got["top_token"].cpu().numpy(), want["top_token"])
+    for name, atol in (("lse", 2.0 ** -18), ("logprob", 2.0 ** -18), ("top_logprob", 2.0 ** -18), ("entropy", 2.0 ** -15)):
+        np.testing.assert_allclose(got[name].cpu().numpy(), want[name], rtol=2.0 ** -22, atol=atol, err_msg=name)
+    return got
+
+
+def _logits(n, V, dtype=torch.float32, seed=0, scale=3.0, stride=None, shift=0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    x = (torch.randn(n, V, device="cuda", generator=g) * scale).to(dtype)
+    buf = torch.zeros(n * (stride or V) + shift, dtype=dtype, device="cuda")
+    view = torch.as_strided(buf, (n, V), (stride or V, 1), shift)
+    view.copy_(x)
+    return view
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n,V,k", [(1, 1, 1), (3, 2, 5), (2, 63, 64), (5, 1000, 7), (31, 1998, 8), (2, 16384, 64), (2, 16385, 1),
+                                   (4, 32000, 20), (1, 50257, 0), (2, 131075, 64), (1, 262144, 33)])
+def test_scores(binding, dtype, n, V, k):
+    rng = np.random.default_rng(V)
+    _check(binding, _logits(n, V, dtype), rng.integers(0, V, n), k)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("shift,extra", [(1, 3), (3, 5), (7, 1), (0, 9)])
+def test_rows_off_any_alignment(binding, dtype, shift, extra):
+    V = 4001
+    _check(binding, _logits(6, V, dtype, stride=V + extra, shift=shift), np.arange(6) * 100, 16)
+
+
+@pytest.mark.parametrize("order", ["constant", "rising", "falling", "two_values", "late_peaks"])
+@pytest.mark.parametrize("V", [700, 20000, 70000])
+def test_orders_and_ties(binding, order, V):
+    x = torch.arange(V, dtype=torch.float64, device="cuda")
+    x = {"constant": torch.zeros_like(x) + 1.5, "rising": x * (8.0 / V), "falling": -x * (8.0 / V), "two_values": (x % 2),
+         "late_peaks": torch.where(x > V - 3000, 5.0 + x / V, torch.sin(x))}[order]
+    logits = x.to(torch.float32)[None].repeat(2, 1).contiguous()
+    if order == "rising":
+        logits = torch.round(logits * 64) / 64  # (long runs of ties)
+    _check(binding, logits, [0, V - 1], 64)
+
+
+def test_special_rows(binding):
+    inf, V = float("inf"), 3000
+    x = _logits(10, V)
+    x[0] = -inf
+    x[1, 5:] = -inf
+    x[2, 77] = float("nan")
+    x[3, 2999] = inf
+    x[4] = torch.finfo(torch.float32).min
+    x[5, 100:] = torch.finfo(torch.float32).min
+    x[6] = float("nan")
+    x[7, :] = -inf
+    x[7, 2000] = 3.0
+    x[8] = 1e30
+    x[8, 3] = -1e30
+    x[9, ::2] = 0.0
+    x[9, 1::2] = -0.0
+    _check(binding, x, [0, 4, 3, 1, 9, 99, 0, 2000, 3, 8], 9)
+
+
+def test_given_tokens_of_a_tree(binding):
+    x = _logits(7, 997)
+    _check(binding, x, [5, 996, -1, 0, 3, 900, 997, 5, 5, 1 << 30], 3, row_of=[0, 0, 1, 6, 6, 2, 3, -1, 7, 0])
+    _check(binding, x, [1] * 3000, 2, row_of=[i % 8 for i in range(3000)])
+    _check(binding, x, None, 4)
+    _check(binding, x, [1, 2, 3, 4, 5, 6, -3], 0)
+
+
+def test_near_certain_row(binding):
+    x = torch.full((1, 32000), -30.0, device="cuda")
+    x[0, 123] = 10.0
+    got = _check(binding, x, [123], 2)
+    assert float(got["logprob"][0]) <= 0.0
+
+
+def test_in_a_graph_and_on_a_stream(binding):
+    x = _logits(9, 32000)
+    tok = torch.arange(9, dtype=torch.int32, device="cuda")
+    ws = torch.zeros(binding.token_scores_workspace_bytes(9, 32000, 5), dtype=torch.uint8, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = binding.token_scores(x, tok, 5, workspace=ws)
+    for turn in range(3):
+        x.copy_(_logits(9, 32000, seed=turn + 10))
+        want = binding.token_scores(x, tok, 5)
+        graph.replay()
+        torch.cuda.synchronize()
+        for name in want:
+            assert torch.equal(got[name], want[name]), (turn, name)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    other = binding.token_scores(x, tok, 5, stream=side)
+    side.synchronize()
+    assert torch.equal(other["logprob"], want["logprob"])
+
+
+def test_refusals(binding):
+    x = _logits(2, 100)
+    tok = torch.zeros(2, dtype=torch.int32, device="cuda")
+    for bad in (x.double(), x[0], x.t(), x.cpu()):
+        with pytest.raises(ValueError):
+            binding.token_scores(bad, tok)
+    for bad in (tok.long(), tok[:1], tok[None]):
+        with pytest.raises(ValueError):
+            binding.token_scores(x, bad)
+    with pytest.raises(ValueError):
+        binding.token_scores(x, tok, row_of=tok[:1])
+    for k in (-1, 65):
+        with pytest.raises((binding.LlmcadError, RuntimeError, ValueError)):
+            binding.token_scores(x, tok, k)
+    with pytest.raises(binding.LlmcadError):
+        binding.token_scores(x, tok, 3, workspace=torch.zeros(8, dtype=torch.uint8, device="cuda"))
