@@ -157,18 +157,17 @@ __device__ __forceinline__ void add_nonfinite(const KeyStep<DH>& taken, uint32_t
   }
 }
 
-// Workgroup (x, y): K/V head y, run x of keys: the first KP x (row blocks of all
-// rows) take the prefix's key splits, the others the plan's runs of pages, one
+// Workgroup (x, y): K/V head y, run x of keys: the first KP x `blocks` (row blocks of
+// all rows; 0 if wide_kernel has the prefix) take the prefix's key splits, the others the plan's runs of pages, one
 // block of 16 (row, query head) pairs after the other.  The four waves take
 // every fourth 32-key step and meet in LDS.
 template <int DH>
-__global__ __launch_bounds__(kThreads) void split_kernel(AttnArgs a) {
+__global__ __launch_bounds__(kThreads) void split_kernel(AttnArgs a, int blocks) {
   __shared__ float o_s[kWaves][16][DH + 4];
   __shared__ float ml_s[kWaves][16][2];
   constexpr int NS = KeyStep<DH>::NS, NB = KeyStep<DH>::NB;
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, g = lane >> 4, wave = wave_index();
   const int kh = blockIdx.y, group = a.H / a.Hkv;
-  const int blocks = (int)(((long long)a.N * group + 15) / 16);
   int x = blockIdx.x;
   const bool prefix = x < a.KP * blocks;
   int row0, n, held = 0, lim, first, last;  // rows, visible key range, steps [first, last)
@@ -289,6 +288,174 @@ __global__ __launch_bounds__(kThreads) void split_kernel(AttnArgs a) {
   }
 }
 
+// The prefix for many rows: 128 (row, query head) pairs of a K/V head per
+// workgroup, 32 per wave, over one key split.  Tiles of 64 keys are shared
+// through LDS in fragment order (every access is 16 bytes per lane, lane by
+// lane): while a tile is computed the next one is on its way to registers, and
+// it goes to the other buffer before the barrier.
+//
+// The running maximum is only a reference point: any value near it serves, so
+// the output is rescaled only when some score exceeds it by 2^kSlack, and
+// until then no lane needs another's scores.  The sums are per lane, joined at
+// the end.  Probabilities (up to 2^kSlack) enter the value product in bf16, half
+// a step of 2^-8 each.
+constexpr int kTileKeys = 64;
+constexpr int kTileRows = 128;
+constexpr float kSlack = 8.0f;
+
+template <int DH>
+__global__ __launch_bounds__(kThreads, 2) void wide_kernel(AttnArgs a) {
+  constexpr int NS = KeyStep<DH>::NS, NB = KeyStep<DH>::NB, LOADS = KeyStep<DH>::LOADS;
+  constexpr int PER = LOADS / 2;  // fragments per wave and tile: K of a step, or V^T of a step
+  constexpr int TILE = 2 * LOADS * 1024;
+  __shared__ __align__(16) char lds[2][TILE];
+  const int lane = threadIdx.x & 63, li = lane & 15, g = lane >> 4, wave = wave_index();
+  const int group = a.H / a.Hkv, pairs = a.N * group, tiles = up_div(pairs, kTileRows);
+  // workgroup w runs on XCD w % 8: each XCD gets a contiguous share of the units,
+  // tile by tile of one (head, split), so that its keys are read into one L2
+  const int units = tiles * a.KP * a.Hkv, per_xcd = up_div(units, 8);
+  const int u = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
+  if ((int)(blockIdx.x >> 3) >= per_xcd || u >= units) return;
+  const int tile = u % tiles, split = u / tiles % a.KP, kh = u / tiles / a.KP;
+  const int ktiles = up_div(a.P, kTileKeys), per = up_div(ktiles, a.KP);
+  const int first = split * per, last = first + per < ktiles ? first + per : ktiles;
+
+  bf16x8 qf[2][NS];
+#pragma unroll
+  for (int rb = 0; rb < 2; ++rb) {
+    const int pr0 = tile * kTileRows + wave * 32 + rb * 16 + li, pr = pr0 < pairs ? pr0 : pairs - 1;
+    const bf16* q = a.q + (size_t)(pr / group) * a.q_stride + (size_t)(kh * group + pr % group) * DH + 8 * g;
+#pragma unroll
+    for (int s = 0; s < NS; ++s) qf[rb][s] = ldg((const bf16x8*)(q + 32 * s));
+  }
+  // this wave's part of a tile: waves 0 and 2 the keys of its two steps, 1 and 3 the values
+  const bool values = (wave & 1) != 0;
+  const int key = 32 * (wave >> 1);
+  const bf16* src = values ? a.vc + ((size_t)kh * DH + li) * a.cap + key + 8 * g + (size_t)first * kTileKeys
+                           : a.kc + ((size_t)kh * a.cap + key + 8 * (li >> 2) + (li & 3) + (size_t)first * kTileKeys) * DH + 8 * g;
+  const size_t advance = values ? kTileKeys : (size_t)kTileKeys * DH;
+  const int lds_at = ((wave >> 1) * LOADS + (values ? 2 * NS : 0)) * 1024 + lane * 16;
+  bf16x8 stage[PER];
+  auto fetch = [&]() {
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+      const size_t off = values ? (size_t)e * 16 * a.cap : (size_t)((e / NS) * 4 * DH + (e % NS) * 32);
+      stage[e] = ldg((const bf16x8*)(src + off));
+    }
+    src += advance;
+  };
+  auto put = [&](int t) {  // (tile t)
+    char* at = lds[t & 1] + lds_at;
+    const int valid = a.P - (t * kTileKeys + key + 8 * g);  // (values of keys past the prefix: zeros)
+    if (values && (t + 1) * kTileKeys > a.P) {
+#pragma unroll
+      for (int e = 0; e < PER; ++e)
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (i >= valid) stage[e][i] = (bf16)0.0f;
+    }
+#pragma unroll
+    for (int e = 0; e < PER; ++e) lds_st<bf16x8>(at + e * 1024, stage[e]);
+  };
+
+  float m[2], neg_m[2], l[2];
+  f32x4 o[2][NB];
+#pragma unroll
+  for (int rb = 0; rb < 2; ++rb) {
+    m[rb] = -INFINITY;
+    neg_m[rb] = 0.0f;
+    l[rb] = 0.0f;
+#pragma unroll
+    for (int db = 0; db < NB; ++db) o[rb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  if (first < last) {
+    fetch();
+    put(first);
+  }
+  __syncthreads();
+  for (int t = first; t < last; ++t) {
+    if (t + 1 < last) fetch();
+    const char* at = lds[t & 1] + lane * 16;
+    f32x4 sc[2][4];  // [row block][step, key block]
+#pragma unroll
+    for (int sb = 0; sb < 4; ++sb) {
+#pragma unroll
+      for (int rb = 0; rb < 2; ++rb) sc[rb][sb] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int s = 0; s < NS; ++s) {
+        const bf16x8 k = lds_ld<bf16x8>(at + ((sb >> 1) * LOADS + (sb & 1) * NS + s) * 1024);
+#pragma unroll
+        for (int rb = 0; rb < 2; ++rb) sc[rb][sb] = mfma16x16x32(k, qf[rb][s], sc[rb][sb]);
+      }
+    }
+    if ((t + 1) * kTileKeys > a.P) {
+      const int valid = a.P - t * kTileKeys;
+#pragma unroll
+      for (int sb = 0; sb < 4; ++sb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (32 * (sb >> 1) + 8 * g + 4 * (sb & 1) + i >= valid)
+#pragma unroll
+            for (int rb = 0; rb < 2; ++rb) sc[rb][sb][i] = -INFINITY;
+    }
+    float mx[2];
+    bool grow = false;
+#pragma unroll
+    for (int rb = 0; rb < 2; ++rb) {
+      mx[rb] = sc[rb][0][0];
+#pragma unroll
+      for (int e = 1; e < 16; ++e) mx[rb] = fmaxf(mx[rb], sc[rb][e >> 2][e & 3]);
+      mx[rb] *= a.scale_log2;
+      grow |= mx[rb] > m[rb] + kSlack;
+    }
+    if (__any(grow)) {
+#pragma unroll
+      for (int rb = 0; rb < 2; ++rb) {
+        const float m_new = fmaxf(m[rb], col4_max(mx[rb]));
+        const float m_use = m_new == -INFINITY ? 0.0f : m_new;
+        const float alpha = __builtin_amdgcn_exp2f(m[rb] - m_use);
+        m[rb] = m_new;
+        neg_m[rb] = -m_use;
+        l[rb] *= alpha;
+#pragma unroll
+        for (int db = 0; db < NB; ++db) o[rb][db] = o[rb][db] * alpha;
+      }
+    }
+    bf16x8 p[2][2];
+#pragma unroll
+    for (int rb = 0; rb < 2; ++rb)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float v = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[rb][e >> 2][e & 3], a.scale_log2, neg_m[rb]));
+        l[rb] += v;
+        p[rb][e >> 3][e & 7] = f2bf(v);
+      }
+#pragma unroll
+    for (int st = 0; st < 2; ++st)
+#pragma unroll
+      for (int db = 0; db < NB; ++db) {
+        const bf16x8 v = lds_ld<bf16x8>(at + (st * LOADS + 2 * NS + db) * 1024);
+#pragma unroll
+        for (int rb = 0; rb < 2; ++rb) o[rb][db] = mfma16x16x32(v, p[rb][st], o[rb][db]);
+      }
+    if (t + 1 < last) put(t + 1);
+    __syncthreads();
+  }
+#pragma unroll
+  for (int rb = 0; rb < 2; ++rb) {
+    const int pr = tile * kTileRows + wave * 32 + rb * 16 + li;
+    const float sum = col4_sum(l[rb]);
+    if (pr >= pairs) continue;
+    const size_t at = ((size_t)split * a.N + pr / group) * a.H + kh * group + pr % group;
+#pragma unroll
+    for (int db = 0; db < NB; ++db) stg((f32x4*)(a.part_o + at * DH + 16 * db + 4 * g), o[rb][db]);
+    if (g == 0) {
+      stg(a.part_ml + at * 2, m[rb]);
+      stg(a.part_ml + at * 2 + 1, sum);
+    }
+  }
+}
+
 // A wave per (row, head): its partial results in the order of their keys.
 template <int DH>
 __global__ __launch_bounds__(kThreads) void join_kernel(AttnArgs a) {
@@ -323,29 +490,43 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttnArgs a) {
 
 }  // namespace
 
+// Few pairs of rows and heads per K/V head: the waves share 16 of them and split the keys; many:
+// the waves split the pairs and share the keys.
+static bool wide_prefix(int N, int H, int Hkv) { return (long long)N * (H / Hkv) > 64; }
+
 int prefix_splits(int N, int H, int Hkv, int P) {
   if (P <= 0) return 0;
-  const int steps = cdiv(P, 32), tiles = cdiv(N * (H / Hkv), 16) * Hkv;
-  int KP = cdiv(512, tiles);
-  if (KP > cdiv(steps, 4)) KP = cdiv(steps, 4);
+  int KP, most;
+  if (wide_prefix(N, H, Hkv)) {
+    KP = 512 / (cdiv(N * (H / Hkv), kTileRows) * Hkv);
+    most = cdiv(P, 2 * kTileKeys);
+  } else {
+    KP = cdiv(512, cdiv(N * (H / Hkv), 16) * Hkv);
+    most = cdiv(P, 128);
+  }
+  if (KP > most) KP = most;
   if (KP > max_prefix_splits(N)) KP = max_prefix_splits(N);
   return KP < 1 ? 1 : KP;
 }
 
-hipError_t launch_batch_attention(const AttnArgs& a, hipStream_t st) {
-  const int blocks = (int)(((long long)a.N * (a.H / a.Hkv) + 15) / 16);
+template <int DH>
+static hipError_t launch_attention(const AttnArgs& a, hipStream_t st) {
+  const int group = a.H / a.Hkv;
+  const bool wide = a.KP > 0 && wide_prefix(a.N, a.H, a.Hkv);
+  const int blocks = wide || a.KP == 0 ? 0 : cdiv(a.N * group, 16);
   const long long most = (long long)a.B * cdiv(a.max_pages, 2);  // (a run has two pages or more)
   const int units = most < plan_max_units(a.B) ? (int)most : plan_max_units(a.B);
-  const dim3 grid(a.KP * blocks + units, a.Hkv);
-  const dim3 join((unsigned)(((long long)a.N * a.H + kWaves - 1) / kWaves));
-  if (a.Dh == 128) {
-    split_kernel<128><<<grid, dim3(kThreads), 0, st>>>(a);
-    join_kernel<128><<<join, dim3(kThreads), 0, st>>>(a);
-  } else {
-    split_kernel<64><<<grid, dim3(kThreads), 0, st>>>(a);
-    join_kernel<64><<<join, dim3(kThreads), 0, st>>>(a);
+  if (wide) {
+    const int wu = cdiv(a.N * group, kTileRows) * a.KP * a.Hkv;
+    wide_kernel<DH><<<dim3(cdiv(wu, 8) * 8), dim3(kThreads), 0, st>>>(a);
   }
+  split_kernel<DH><<<dim3(a.KP * blocks + units, a.Hkv), dim3(kThreads), 0, st>>>(a, blocks);
+  join_kernel<DH><<<dim3((unsigned)(((long long)a.N * a.H + kWaves - 1) / kWaves)), dim3(kThreads), 0, st>>>(a);
   return hipGetLastError();
+}
+
+hipError_t launch_batch_attention(const AttnArgs& a, hipStream_t st) {
+  return a.Dh == 128 ? launch_attention<128>(a, st) : launch_attention<64>(a, st);
 }
 
 }  // namespace llmcad
