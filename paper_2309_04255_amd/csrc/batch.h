@@ -129,7 +129,9 @@ struct AttnArgs {
   float* part_ml;  // their running maximum (log2 domain) and sum [..][H][2]
   int B, N, H, Hkv, Dh;
   float scale_log2;
-  int KP;  // key splits of the prefix
+  int KP;     // key splits of the prefix
+  int wide;   // its rows in tiles of 128 pairs (else 16)
+  int merge;  // runs of a request's pages per workgroup
 };
 hipError_t launch_batch_attention(const AttnArgs& a, hipStream_t st);
 // Key splits of the prefix (the workspace holds max_prefix_splits(N) at most).

@@ -5,8 +5,10 @@
 //
 // over the prefix [0, P), the tokens its request holds and the rows of the
 // request that its mask names.  The prefix's keys and values are read for all
-// requests at once; a request's own for its rows at once.  Both leave partial
-// results (maximum, sum, unnormalised output), which a second launch joins.
+// requests at once; a request's own for its rows at once.  Every workgroup
+// takes a run of keys for some (row, query head) pairs of one K/V head and
+// leaves partial results (maximum, sum, unnormalised output), which a second
+// launch joins.
 //
 // As in the verification pass, S^T = K q^T and O^T = V^T P^T run on the matrix
 // cores with K and V^T taken from memory in fragment order: K block b of a
@@ -20,276 +22,115 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWaves = 4;
+constexpr int kTileKeys = kPage;  // keys of a tile: two 32-key steps, one page
+constexpr float kSlack = 8.0f;
 
 __device__ __forceinline__ int up_div(int x, int a) { return (x + a - 1) / a; }
 
-// One 32-key step's operands of a wave: K block b, 32-dim step s at f[b NS + s],
-// V^T 16-dim block db at f[2 NS + db].
+// Fragments of a 32-key step: K block b, 32-dim step s at b NS + s; V^T 16-dim
+// block db at 2 NS + db.
 template <int DH>
-struct KeyStep {
+struct Frags {
   static constexpr int NS = DH / 32, NB = DH / 16, LOADS = 2 * NS + NB;
-  bf16x8 f[LOADS];
 };
 
-// k: K row of the step's first key (rows DH apart); vt: its entry in V^T row 0
-// (rows vs apart).
-template <int DH>
-__device__ __forceinline__ void load_step(KeyStep<DH>& R, const bf16* k, const bf16* vt, int vs) {
-  const int lane = threadIdx.x & 63, li = lane & 15, g = lane >> 4;
-  constexpr int NS = KeyStep<DH>::NS, NB = KeyStep<DH>::NB;
-#pragma unroll
-  for (int b = 0; b < 2; ++b)
-#pragma unroll
-    for (int s = 0; s < NS; ++s)
-      R.f[b * NS + s] = ldg((const bf16x8*)(k + (size_t)(8 * (li >> 2) + 4 * b + (li & 3)) * DH + 32 * s + 8 * g));
-#pragma unroll
-  for (int db = 0; db < NB; ++db) R.f[2 * NS + db] = ldg((const bf16x8*)(vt + (size_t)(16 * db + li) * vs + 8 * g));
-}
-
-// Running softmax of 16 rows: lane (li, g) holds row li's maximum and sum, and
-// dims 16 db + 4 g + i of its output.
-template <int DH>
-struct RowState {
-  float m, l;
-  f32x4 o[DH / 16];
+// What a workgroup works on.
+struct Unit {
+  int kh;            // K/V head
+  int row0, pairs;   // first row, (row, query head of the group) pairs
+  int pair0;         // first pair of a tile unit
+  int first, last;   // tiles of kTileKeys keys
+  int lim;           // keys at or past it are not there
+  int held;          // keys from it on are the request's rows, seen by mask (the prefix: lim)
+  const int* table;  // pages, or null: the prefix
+  size_t part;       // partial row of row0
 };
 
-// One step for 16 rows.  vis: bit e set if the lane's row sees key 8 g + e; p:
-// the lane's probabilities against the new maximum.
-template <int DH>
-__device__ __forceinline__ void attend(const KeyStep<DH>& R, const bf16x8 (&qf)[DH / 32], uint32_t vis, float scale_log2,
-                                       RowState<DH>& st, float (&p)[8]) {
-  constexpr int NS = KeyStep<DH>::NS, NB = KeyStep<DH>::NB;
-  f32x4 sc[2];
-#pragma unroll
-  for (int b = 0; b < 2; ++b) {
-    sc[b] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int s = 0; s < NS; ++s) sc[b] = mfma16x16x32(R.f[b * NS + s], qf[s], sc[b]);
+// Where a tile's keys and values lie: K rows of the head DH apart, V^T rows vs.
+struct TileAt {
+  const bf16* k;
+  const bf16* v;
+  int vs;
+  bool there;
+};
+__device__ __forceinline__ TileAt prefix_tile(const AttnArgs& a, const Unit& u, int t) {
+  return {a.kc + ((size_t)u.kh * a.cap + (size_t)t * kTileKeys) * a.Dh, a.vc + (size_t)u.kh * a.Dh * a.cap + (size_t)t * kTileKeys,
+          a.cap, true};
+}
+__device__ __forceinline__ TileAt page_tile(const AttnArgs& a, const Unit& u, int id) {
+  const bool there = id >= 0 && id < a.n_pages;  // (otherwise: any page, and none of its keys)
+  const size_t at = ((size_t)(there ? id : 0) * a.Hkv + u.kh) * kPage * a.Dh;
+  return {a.kp + at, a.vp + at, kPage, there};
+}
+// Page ids of a run, 64 at a time in the lanes of a wave.
+struct PageIds {
+  int ids, base;
+  __device__ void start(const Unit& u, int t) {
+    base = t;
+    const int at = t + (int)(threadIdx.x & 63);
+    ids = at < u.last ? ldg(u.table + at) : -1;
   }
-  float sv[8], mx = -INFINITY;
+  __device__ int get(const Unit& u, int t) {
+    if (t - base >= kWave) start(u, t);
+    return __builtin_amdgcn_readlane(ids, t - base);
+  }
+};
+
+// Which of the 8 keys from `key` on a row sees, by its mask (keys before held
+// are tokens all rows of the request see).
+__device__ __forceinline__ uint32_t seen8(const uint32_t (&anc)[4], int key, int held, int lim) {
+  uint32_t vis = 0;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    sv[e] = (vis >> e) & 1u ? sc[e >> 2][e & 3] * scale_log2 : -INFINITY;
-    mx = fmaxf(mx, sv[e]);
+    const int t = key + e - held;
+    const uint32_t w = t < 32 ? anc[0] : t < 64 ? anc[1] : t < 96 ? anc[2] : anc[3];
+    const bool sees = key + e < lim && (t < 0 || (t < LLMCAD_MAX_NODES && ((w >> (t & 31)) & 1u)));
+    vis |= sees ? 1u << e : 0u;
   }
-  mx = col4_max(mx);
-  const float m_new = fmaxf(st.m, mx);
-  const float m_use = m_new == -INFINITY ? 0.0f : m_new;
-  const float alpha = __builtin_amdgcn_exp2f(st.m - m_use);
-  bf16x8 ph, pl;
-  float sum = 0.0f;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    p[e] = __builtin_amdgcn_exp2f(sv[e] - m_use);
-    ph[e] = f2bf(p[e]);
-    pl[e] = f2bf(p[e] - bf2f(ph[e]));
-    sum += p[e];
-  }
-  st.l = st.l * alpha + col4_sum(sum);
-  st.m = m_new;
-#pragma unroll
-  for (int db = 0; db < NB; ++db) {
-    st.o[db] = st.o[db] * alpha;
-    st.o[db] = mfma16x16x32(R.f[2 * NS + db], ph, st.o[db]);
-    st.o[db] = mfma16x16x32(R.f[2 * NS + db], pl, st.o[db]);
-  }
+  return vis;
 }
 
-// Values of keys that no row may read count as zeros (0 x NaN is NaN): the
-// lane's keys 8 g + e with e >= valid.
-template <int DH>
-__device__ __forceinline__ void clear_values(KeyStep<DH>& R, int valid) {
-#pragma unroll
-  for (int db = 0; db < KeyStep<DH>::NB; ++db)
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (e >= valid) R.f[2 * KeyStep<DH>::NS + db][e] = (bf16)0.0f;
-}
-
-// A step whose keys some rows see and others do not: an Inf or NaN among its
-// values would reach the others as 0 x Inf.  Such values are left out of the
-// product (true: there are some)...
-template <int DH>
-__device__ __forceinline__ bool take_out_nonfinite(KeyStep<DH>& R, KeyStep<DH>& taken) {
+// Keys that some rows see and others do not: an Inf or NaN among their values
+// would reach the others as 0 x Inf.  Such values are left out of the product
+// O^T += V^T P^T, and a product of their indicators with the rows' sight tells
+// which outputs they belong to.
+typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
+__device__ __forceinline__ bool nonfinite(const bf16x8& v) {
+  const u16x8 x = __builtin_bit_cast(u16x8, v) & (uint16_t)0x7f80;
   bool any = false;
 #pragma unroll
-  for (int db = 0; db < KeyStep<DH>::NB; ++db)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const bf16 v = R.f[2 * KeyStep<DH>::NS + db][e];
-      any |= (__builtin_bit_cast(uint16_t, v) & 0x7f80) == 0x7f80;
-    }
-  if (!__any(any)) return false;
-#pragma unroll
-  for (int db = 0; db < KeyStep<DH>::NB; ++db)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int f = 2 * KeyStep<DH>::NS + db;
-      const bf16 v = R.f[f][e];
-      const bool bad = (__builtin_bit_cast(uint16_t, v) & 0x7f80) == 0x7f80;
-      taken.f[f][e] = bad ? v : (bf16)0.0f;
-      if (bad) R.f[f][e] = (bf16)0.0f;
-    }
-  return true;
+  for (int e = 0; e < 8; ++e) any |= x[e] == 0x7f80;
+  return any;
 }
-// ... and added for the rows that see them: the value of dim 16 db + 4 g + i at
-// key 8 k + e is held by lane (4 g + i, k), row li's probability by lane (li, k).
-template <int DH>
-__device__ __forceinline__ void add_nonfinite(const KeyStep<DH>& taken, uint32_t vis, const float (&p)[8], RowState<DH>& st) {
-  const int lane = threadIdx.x & 63, li = lane & 15, g = lane >> 4;
-#pragma unroll 1
-  for (int k = 0; k < 4; ++k) {
-    const uint32_t sees = (uint32_t)__shfl((int)vis, 16 * k + li, kWave);
+// v without its Inf and NaN; o with what they give the rows that see them.
+__device__ __forceinline__ f32x4 take_nonfinite(bf16x8& v, uint32_t vis, f32x4 o) {
+  constexpr uint16_t one = 0x3f80;  // (bf16 1)
+  const u16x8 x = __builtin_bit_cast(u16x8, v);
+  u16x8 up, down, sees, kept;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float pe = __shfl(p[e], 16 * k + li, kWave);
-#pragma unroll
-      for (int db = 0; db < KeyStep<DH>::NB; ++db) {
-        const float mine = bf2f(taken.f[2 * KeyStep<DH>::NS + db][e]);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float v = __shfl(mine, 16 * k + 4 * g + i, kWave);
-          if (((sees >> e) & 1u) && v != 0.0f) st.o[db][i] += pe * v;
-        }
-      }
-    }
+  for (int e = 0; e < 8; ++e) {
+    const bool bad = (x[e] & 0x7f80) == 0x7f80, nan = bad && (x[e] & 0x7f);
+    up[e] = bad && (nan || !(x[e] & 0x8000)) ? one : (uint16_t)0;
+    down[e] = bad && (nan || (x[e] & 0x8000)) ? one : (uint16_t)0;
+    sees[e] = (vis >> e) & 1u ? one : (uint16_t)0;
+    kept[e] = bad ? (uint16_t)0 : x[e];
   }
+  v = __builtin_bit_cast(bf16x8, kept);
+  const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+  const bf16x8 s = __builtin_bit_cast(bf16x8, sees);
+  const f32x4 ups = mfma16x16x32(__builtin_bit_cast(bf16x8, up), s, zero);
+  const f32x4 downs = mfma16x16x32(__builtin_bit_cast(bf16x8, down), s, zero);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (ups[i] > 0.0f) o[i] += INFINITY;
+    if (downs[i] > 0.0f) o[i] -= INFINITY;
+  }
+  return o;
 }
 
-// Workgroup (x, y): K/V head y, run x of keys: the first KP x `blocks` (row blocks of
-// all rows; 0 if wide_kernel has the prefix) take the prefix's key splits, the others the plan's runs of pages, one
-// block of 16 (row, query head) pairs after the other.  The four waves take
-// every fourth 32-key step and meet in LDS.
-template <int DH>
-__global__ __launch_bounds__(kThreads) void split_kernel(AttnArgs a, int blocks) {
-  __shared__ float o_s[kWaves][16][DH + 4];
-  __shared__ float ml_s[kWaves][16][2];
-  constexpr int NS = KeyStep<DH>::NS, NB = KeyStep<DH>::NB;
-  const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, g = lane >> 4, wave = wave_index();
-  const int kh = blockIdx.y, group = a.H / a.Hkv;
-  int x = blockIdx.x;
-  const bool prefix = x < a.KP * blocks;
-  int row0, n, held = 0, lim, first, last;  // rows, visible key range, steps [first, last)
-  size_t part;                              // partial row of row 0
-  const int* table = nullptr;
-  if (prefix) {
-    const int split = x / blocks;
-    row0 = 0;
-    n = a.N;
-    lim = a.P;
-    const int steps = up_div(a.P, 32), per = up_div(steps, a.KP);
-    first = split * per;
-    last = first + per < steps ? first + per : steps;
-    part = (size_t)split * a.N;
-  } else {
-    x -= a.KP * blocks;
-    if (x >= ldg(a.head + PLAN_UNITS)) return;
-    const int u = ldg(a.units + x);
-    const BatchRequest r = ldg(a.req + (u >> 16));
-    if (r.n == 0) return;
-    const int run = u & 0xffff, chunk = ldg(a.head + PLAN_CHUNK);
-    row0 = r.row0;
-    n = r.n;
-    held = r.held;
-    lim = r.held + r.n;
-    table = a.table + (size_t)(u >> 16) * a.max_pages;
-    const int room = a.max_pages < (1 << 25) ? a.max_pages * 2 : 1 << 26;  // (steps of the table)
-    const int steps = up_div(lim, 32) < room ? up_div(lim, 32) : room;
-    const long long f = (long long)run * chunk * 2, t = f + (long long)chunk * 2;
-    first = f < steps ? (int)f : steps;
-    last = t < steps ? (int)t : steps;
-    part = (size_t)a.KP * a.N + r.part0 + (size_t)run * r.n;
-  }
-  const int pairs = n * group;
-  const int b0 = prefix ? x % blocks : 0, b1 = prefix ? b0 + 1 : up_div(pairs, 16);
-  for (int blk = b0; blk < b1; ++blk) {
-    const int pr = 16 * blk + li < pairs ? 16 * blk + li : pairs - 1;
-    const size_t row = (size_t)row0 + pr / group;
-    const int head = kh * group + pr % group;
-    bf16x8 qf[NS];
-#pragma unroll
-    for (int s = 0; s < NS; ++s) qf[s] = ldg((const bf16x8*)(a.q + row * a.q_stride + (size_t)head * DH + 32 * s + 8 * g));
-    uint32_t anc[4] = {0, 0, 0, 0};
-    if (!prefix)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) anc[j] = ldg(a.mask + row * 4 + j);
-    RowState<DH> st;
-    st.m = -INFINITY;
-    st.l = 0.0f;
-#pragma unroll
-    for (int db = 0; db < NB; ++db) st.o[db] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int j = first + wave; j < last; j += kWaves) {
-      const int key0 = 32 * j;
-      KeyStep<DH> R;
-      if (prefix) {
-        load_step<DH>(R, a.kc + ((size_t)kh * a.cap + key0) * DH, a.vc + (size_t)kh * DH * a.cap + key0, a.cap);
-      } else {
-        const int id = wave_uniform(ldg(table + key0 / kPage));
-        if (id < 0 || id >= a.n_pages) continue;
-        const size_t page = ((size_t)id * a.Hkv + kh) * kPage * DH;
-        load_step<DH>(R, a.kp + page + (size_t)(key0 % kPage) * DH, a.vp + page + key0 % kPage, kPage);
-      }
-      uint32_t vis = 0;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int key = key0 + 8 * g + e;
-        bool sees = key < lim;
-        if (!prefix && key >= held) {
-          const int t = key - held;
-          sees = sees && t < LLMCAD_MAX_NODES && ((anc[(t >> 5) & 3] >> (t & 31)) & 1u);
-        }
-        vis |= sees ? 1u << e : 0u;
-      }
-      if (key0 + 32 > lim) clear_values<DH>(R, lim - (key0 + 8 * g));
-      float pr_[8];
-      if (!prefix && key0 + 32 > held) {
-        KeyStep<DH> taken;
-        const bool some = take_out_nonfinite<DH>(R, taken);
-        attend<DH>(R, qf, vis, a.scale_log2, st, pr_);
-        if (some) add_nonfinite<DH>(taken, vis, pr_, st);
-      } else {
-        attend<DH>(R, qf, vis, a.scale_log2, st, pr_);
-      }
-    }
-    // the four waves' states, joined in wave order
-    __syncthreads();
-#pragma unroll
-    for (int db = 0; db < NB; ++db)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) o_s[wave][li][16 * db + 4 * g + i] = st.o[db][i];
-    if (g == 0) {
-      ml_s[wave][li][0] = st.m;
-      ml_s[wave][li][1] = st.l;
-    }
-    __syncthreads();
-    for (int e = tid; e < 16 * DH; e += kThreads) {
-      const int i = e / DH, c = e % DH, p = 16 * blk + i;
-      if (p >= pairs) continue;
-      float m = -INFINITY;
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) m = fmaxf(m, ml_s[w][i][0]);
-      const float mu = m == -INFINITY ? 0.0f : m;
-      float l = 0.0f, o = 0.0f;
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) {
-        const float f = __builtin_amdgcn_exp2f(ml_s[w][i][0] - mu);
-        l += f * ml_s[w][i][1];
-        o += f * o_s[w][i][c];
-      }
-      const size_t at = (part + p / group) * a.H + kh * group + p % group;
-      stg(a.part_o + at * DH + c, o);
-      if (c == 0) {
-        stg(a.part_ml + at * 2, m);
-        stg(a.part_ml + at * 2 + 1, l);
-      }
-    }
-    __syncthreads();
-  }
-}
-
-// The prefix for many rows: 128 (row, query head) pairs of a K/V head per
-// workgroup, 32 per wave, over one key split.  Tiles of 64 keys are shared
+// ---------------------------------------------------------------- many rows
+//
+// 64 RB pairs per workgroup, 16 RB per wave.  Tiles of 64 keys are shared
 // through LDS in fragment order (every access is 16 bytes per lane, lane by
 // lane): while a tile is computed the next one is on its way to registers, and
 // it goes to the other buffer before the barrier.
@@ -299,55 +140,46 @@ __global__ __launch_bounds__(kThreads) void split_kernel(AttnArgs a, int blocks)
 // until then no lane needs another's scores.  The sums are per lane, joined at
 // the end.  Probabilities (up to 2^kSlack) enter the value product in bf16, half
 // a step of 2^-8 each.
-constexpr int kTileKeys = 64;
-constexpr int kTileRows = 128;
-constexpr float kSlack = 8.0f;
-
-template <int DH>
-__global__ __launch_bounds__(kThreads, 2) void wide_kernel(AttnArgs a) {
-  constexpr int NS = KeyStep<DH>::NS, NB = KeyStep<DH>::NB, LOADS = KeyStep<DH>::LOADS;
+template <int DH, int RB, bool PAGED>
+__device__ __forceinline__ void tile_unit(const AttnArgs& a, const Unit& u, char* lds) {
+  constexpr int NS = Frags<DH>::NS, NB = Frags<DH>::NB, LOADS = Frags<DH>::LOADS;
   constexpr int PER = LOADS / 2;  // fragments per wave and tile: K of a step, or V^T of a step
   constexpr int TILE = 2 * LOADS * 1024;
-  __shared__ __align__(16) char lds[2][TILE];
   const int lane = threadIdx.x & 63, li = lane & 15, g = lane >> 4, wave = wave_index();
-  const int group = a.H / a.Hkv, pairs = a.N * group, tiles = up_div(pairs, kTileRows);
-  // workgroup w runs on XCD w % 8: each XCD gets a contiguous share of the units,
-  // tile by tile of one (head, split), so that its keys are read into one L2
-  const int units = tiles * a.KP * a.Hkv, per_xcd = up_div(units, 8);
-  const int u = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
-  if ((int)(blockIdx.x >> 3) >= per_xcd || u >= units) return;
-  const int tile = u % tiles, split = u / tiles % a.KP, kh = u / tiles / a.KP;
-  const int ktiles = up_div(a.P, kTileKeys), per = up_div(ktiles, a.KP);
-  const int first = split * per, last = first + per < ktiles ? first + per : ktiles;
+  const int group = a.H / a.Hkv;
+  auto pair_of = [&](int rb) { return u.pair0 + (wave * RB + rb) * 16 + li; };
+  auto clamped = [&](int rb) { return pair_of(rb) < u.pairs ? pair_of(rb) : u.pairs - 1; };
 
-  bf16x8 qf[2][NS];
+  bf16x8 qf[RB][NS];
 #pragma unroll
-  for (int rb = 0; rb < 2; ++rb) {
-    const int pr0 = tile * kTileRows + wave * 32 + rb * 16 + li, pr = pr0 < pairs ? pr0 : pairs - 1;
-    const bf16* q = a.q + (size_t)(pr / group) * a.q_stride + (size_t)(kh * group + pr % group) * DH + 8 * g;
+  for (int rb = 0; rb < RB; ++rb) {
+    const int pr = clamped(rb);
+    const bf16* q = a.q + (size_t)(u.row0 + pr / group) * a.q_stride + (size_t)(u.kh * group + pr % group) * DH + 8 * g;
 #pragma unroll
     for (int s = 0; s < NS; ++s) qf[rb][s] = ldg((const bf16x8*)(q + 32 * s));
   }
   // this wave's part of a tile: waves 0 and 2 the keys of its two steps, 1 and 3 the values
   const bool values = (wave & 1) != 0;
   const int key = 32 * (wave >> 1);
-  const bf16* src = values ? a.vc + ((size_t)kh * DH + li) * a.cap + key + 8 * g + (size_t)first * kTileKeys
-                           : a.kc + ((size_t)kh * a.cap + key + 8 * (li >> 2) + (li & 3) + (size_t)first * kTileKeys) * DH + 8 * g;
-  const size_t advance = values ? kTileKeys : (size_t)kTileKeys * DH;
   const int lds_at = ((wave >> 1) * LOADS + (values ? 2 * NS : 0)) * 1024 + lane * 16;
+  PageIds pages;
+  if (PAGED) pages.start(u, u.first);
   bf16x8 stage[PER];
-  auto fetch = [&]() {
+  bool there, next_there = true;
+  auto fetch = [&](int t) {
+    const TileAt at = PAGED ? page_tile(a, u, pages.get(u, t)) : prefix_tile(a, u, t);
+    next_there = at.there;
+    const bf16* src = values ? at.v + (size_t)li * at.vs + key + 8 * g : at.k + (key + 8 * (li >> 2) + (li & 3)) * DH + 8 * g;
 #pragma unroll
     for (int e = 0; e < PER; ++e) {
-      const size_t off = values ? (size_t)e * 16 * a.cap : (size_t)((e / NS) * 4 * DH + (e % NS) * 32);
+      const size_t off = values ? (size_t)e * 16 * at.vs : (size_t)((e / NS) * 4 * DH + (e % NS) * 32);
       stage[e] = ldg((const bf16x8*)(src + off));
     }
-    src += advance;
   };
-  auto put = [&](int t) {  // (tile t)
-    char* at = lds[t & 1] + lds_at;
-    const int valid = a.P - (t * kTileKeys + key + 8 * g);  // (values of keys past the prefix: zeros)
-    if (values && (t + 1) * kTileKeys > a.P) {
+  auto put = [&](int t) {
+    char* at = lds + (t & 1) * TILE + lds_at;
+    if (values && ((t + 1) * kTileKeys > u.lim || !next_there)) {  // (values of keys that are not there: zeros)
+      const int valid = next_there ? u.lim - (t * kTileKeys + key + 8 * g) : 0;
 #pragma unroll
       for (int e = 0; e < PER; ++e)
 #pragma unroll
@@ -358,50 +190,62 @@ __global__ __launch_bounds__(kThreads, 2) void wide_kernel(AttnArgs a) {
     for (int e = 0; e < PER; ++e) lds_st<bf16x8>(at + e * 1024, stage[e]);
   };
 
-  float m[2], neg_m[2], l[2];
-  f32x4 o[2][NB];
+  float m[RB], neg_m[RB], l[RB];
+  f32x4 o[RB][NB];
 #pragma unroll
-  for (int rb = 0; rb < 2; ++rb) {
+  for (int rb = 0; rb < RB; ++rb) {
     m[rb] = -INFINITY;
     neg_m[rb] = 0.0f;
     l[rb] = 0.0f;
 #pragma unroll
     for (int db = 0; db < NB; ++db) o[rb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  if (first < last) {
-    fetch();
-    put(first);
+  if (u.first < u.last) {
+    fetch(u.first);
+    put(u.first);
   }
+  there = next_there;
   __syncthreads();
-  for (int t = first; t < last; ++t) {
-    if (t + 1 < last) fetch();
-    const char* at = lds[t & 1] + lane * 16;
-    f32x4 sc[2][4];  // [row block][step, key block]
+  for (int t = u.first; t < u.last; ++t) {
+    if (t + 1 < u.last) fetch(t + 1);
+    const char* at = lds + (t & 1) * TILE + lane * 16;
+    f32x4 sc[RB][4];  // [row block][step, key block]
 #pragma unroll
     for (int sb = 0; sb < 4; ++sb) {
 #pragma unroll
-      for (int rb = 0; rb < 2; ++rb) sc[rb][sb] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int rb = 0; rb < RB; ++rb) sc[rb][sb] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int s = 0; s < NS; ++s) {
         const bf16x8 k = lds_ld<bf16x8>(at + ((sb >> 1) * LOADS + (sb & 1) * NS + s) * 1024);
 #pragma unroll
-        for (int rb = 0; rb < 2; ++rb) sc[rb][sb] = mfma16x16x32(k, qf[rb][s], sc[rb][sb]);
+        for (int rb = 0; rb < RB; ++rb) sc[rb][sb] = mfma16x16x32(k, qf[rb][s], sc[rb][sb]);
       }
     }
-    if ((t + 1) * kTileKeys > a.P) {
-      const int valid = a.P - t * kTileKeys;
+    const bool masked = (t + 1) * kTileKeys > u.held || !there;  // (not every row sees every key)
+    uint32_t vis[RB][2];
+    if (masked) {
 #pragma unroll
-      for (int sb = 0; sb < 4; ++sb)
+      for (int rb = 0; rb < RB; ++rb) {
+        uint32_t anc[4] = {0, 0, 0, 0};
+        if (PAGED) {
+          const size_t row = (size_t)u.row0 + clamped(rb) / group;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (32 * (sb >> 1) + 8 * g + 4 * (sb & 1) + i >= valid)
+          for (int j = 0; j < 4; ++j) anc[j] = ldg(a.mask + row * 4 + j);
+        }
 #pragma unroll
-            for (int rb = 0; rb < 2; ++rb) sc[rb][sb][i] = -INFINITY;
+        for (int st = 0; st < 2; ++st) {
+          vis[rb][st] = there ? seen8(anc, t * kTileKeys + 32 * st + 8 * g, u.held, u.lim) : 0u;
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (!((vis[rb][st] >> e) & 1u)) sc[rb][2 * st + (e >> 2)][e & 3] = -INFINITY;
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
     }
-    float mx[2];
+    float mx[RB];
     bool grow = false;
 #pragma unroll
-    for (int rb = 0; rb < 2; ++rb) {
+    for (int rb = 0; rb < RB; ++rb) {
       mx[rb] = sc[rb][0][0];
 #pragma unroll
       for (int e = 1; e < 16; ++e) mx[rb] = fmaxf(mx[rb], sc[rb][e >> 2][e & 3]);
@@ -410,7 +254,7 @@ __global__ __launch_bounds__(kThreads, 2) void wide_kernel(AttnArgs a) {
     }
     if (__any(grow)) {
 #pragma unroll
-      for (int rb = 0; rb < 2; ++rb) {
+      for (int rb = 0; rb < RB; ++rb) {
         const float m_new = fmaxf(m[rb], col4_max(mx[rb]));
         const float m_use = m_new == -INFINITY ? 0.0f : m_new;
         const float alpha = __builtin_amdgcn_exp2f(m[rb] - m_use);
@@ -421,38 +265,272 @@ __global__ __launch_bounds__(kThreads, 2) void wide_kernel(AttnArgs a) {
         for (int db = 0; db < NB; ++db) o[rb][db] = o[rb][db] * alpha;
       }
     }
-    bf16x8 p[2][2];
+    bf16x8 p[RB][2];
 #pragma unroll
-    for (int rb = 0; rb < 2; ++rb)
+    for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
         const float v = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[rb][e >> 2][e & 3], a.scale_log2, neg_m[rb]));
         l[rb] += v;
         p[rb][e >> 3][e & 7] = f2bf(v);
       }
+    bool bad = false;
+    if (PAGED && masked) {
 #pragma unroll
-    for (int st = 0; st < 2; ++st)
+      for (int e = 0; e < 2 * NB; ++e) bad |= nonfinite(lds_ld<bf16x8>(at + ((e / NB) * LOADS + 2 * NS + e % NB) * 1024));
+    }
+    if (PAGED && __any(bad)) {
 #pragma unroll
-      for (int db = 0; db < NB; ++db) {
-        const bf16x8 v = lds_ld<bf16x8>(at + (st * LOADS + 2 * NS + db) * 1024);
+      for (int st = 0; st < 2; ++st)
 #pragma unroll
-        for (int rb = 0; rb < 2; ++rb) o[rb][db] = mfma16x16x32(v, p[rb][st], o[rb][db]);
-      }
-    if (t + 1 < last) put(t + 1);
+        for (int db = 0; db < NB; ++db) {
+          bf16x8 v = lds_ld<bf16x8>(at + (st * LOADS + 2 * NS + db) * 1024);
+#pragma unroll
+          for (int rb = 0; rb < RB; ++rb) {
+            bf16x8 kept = v;
+            o[rb][db] = take_nonfinite(kept, vis[rb][st], o[rb][db]);
+            o[rb][db] = mfma16x16x32(kept, p[rb][st], o[rb][db]);
+          }
+          __builtin_amdgcn_sched_barrier(0);  // (one block's values at a time: the registers)
+        }
+    } else {
+#pragma unroll
+      for (int st = 0; st < 2; ++st)
+#pragma unroll
+        for (int db = 0; db < NB; ++db) {
+          const bf16x8 v = lds_ld<bf16x8>(at + (st * LOADS + 2 * NS + db) * 1024);
+#pragma unroll
+          for (int rb = 0; rb < RB; ++rb) o[rb][db] = mfma16x16x32(v, p[rb][st], o[rb][db]);
+        }
+    }
+    if (t + 1 < u.last) put(t + 1);
+    there = next_there;
     __syncthreads();
   }
 #pragma unroll
-  for (int rb = 0; rb < 2; ++rb) {
-    const int pr = tile * kTileRows + wave * 32 + rb * 16 + li;
+  for (int rb = 0; rb < RB; ++rb) {
+    const int pr = pair_of(rb);
     const float sum = col4_sum(l[rb]);
-    if (pr >= pairs) continue;
-    const size_t at = ((size_t)split * a.N + pr / group) * a.H + kh * group + pr % group;
+    if (pr >= u.pairs) continue;
+    const size_t at = (u.part + pr / group) * a.H + u.kh * group + pr % group;
 #pragma unroll
     for (int db = 0; db < NB; ++db) stg((f32x4*)(a.part_o + at * DH + 16 * db + 4 * g), o[rb][db]);
     if (g == 0) {
       stg(a.part_ml + at * 2, m[rb]);
       stg(a.part_ml + at * 2 + 1, sum);
     }
+  }
+}
+
+// ---------------------------------------------------------------- few rows
+//
+// 16 pairs at a time: the waves take every fourth 32-key step each and meet in
+// LDS.  What such a unit takes is the time of its loads, so a wave fetches a
+// step while it computes another, and the probabilities enter the value
+// product as two bf16 halves (about 16 bits): the matrix cores have the time.
+template <int DH>
+struct KeyStep {
+  bf16x8 f[Frags<DH>::LOADS];
+};
+
+template <int DH>
+__device__ __forceinline__ void load_step(KeyStep<DH>& R, const TileAt& at, int key) {
+  const int lane = threadIdx.x & 63, li = lane & 15, g = lane >> 4;
+  constexpr int NS = Frags<DH>::NS, NB = Frags<DH>::NB;
+#pragma unroll
+  for (int b = 0; b < 2; ++b)
+#pragma unroll
+    for (int s = 0; s < NS; ++s)
+      R.f[b * NS + s] = ldg((const bf16x8*)(at.k + (key + 8 * (li >> 2) + 4 * b + (li & 3)) * DH + 32 * s + 8 * g));
+#pragma unroll
+  for (int db = 0; db < NB; ++db) R.f[2 * NS + db] = ldg((const bf16x8*)(at.v + (size_t)(16 * db + li) * at.vs + key + 8 * g));
+}
+
+template <int DH>
+__device__ __forceinline__ void narrow_unit(const AttnArgs& a, const Unit& u, int pair0, char* lds) {
+  constexpr int NS = Frags<DH>::NS, NB = Frags<DH>::NB;
+  float(*o_s)[16][DH + 4] = (float(*)[16][DH + 4])lds;
+  float(*ml_s)[16][2] = (float(*)[16][2])(lds + sizeof(float) * kWaves * 16 * (DH + 4));
+  const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, g = lane >> 4, wave = wave_index();
+  const int group = a.H / a.Hkv;
+  const int pr = pair0 + li < u.pairs ? pair0 + li : u.pairs - 1;
+  const size_t row = (size_t)u.row0 + pr / group;
+  const int j0 = 2 * u.first + wave, j1 = u.last * kTileKeys <= u.lim ? 2 * u.last : (u.lim + 31) / 32;
+  PageIds pages;
+  if (u.table) pages.start(u, u.first);
+  KeyStep<DH> A, B;
+  bool there_a = false, there_b = false;
+  auto fetch = [&](KeyStep<DH>& R, bool& there, int j) {
+    const TileAt at = u.table ? page_tile(a, u, pages.get(u, j >> 1)) : prefix_tile(a, u, j >> 1);
+    there = at.there;
+    load_step<DH>(R, at, 32 * (j & 1));
+  };
+  if (j0 < j1) fetch(A, there_a, j0);
+  bf16x8 qf[NS];
+#pragma unroll
+  for (int s = 0; s < NS; ++s)
+    qf[s] = ldg((const bf16x8*)(a.q + row * a.q_stride + (size_t)(u.kh * group + pr % group) * DH + 32 * s + 8 * g));
+  uint32_t anc[4] = {0, 0, 0, 0};
+  if (u.table)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) anc[j] = ldg(a.mask + row * 4 + j);
+  float m = -INFINITY, l = 0.0f;
+  f32x4 o[NB];
+#pragma unroll
+  for (int db = 0; db < NB; ++db) o[db] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  auto compute = [&](KeyStep<DH>& R, bool there, int j) {
+    if (!there) return;
+    f32x4 sc[2];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      sc[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int s = 0; s < NS; ++s) sc[b] = mfma16x16x32(R.f[b * NS + s], qf[s], sc[b]);
+    }
+    const bool masked = 32 * (j + 1) > u.held;
+    const uint32_t vis = masked ? seen8(anc, 32 * j + 8 * g, u.held, u.lim) : 0xffu;
+    float sv[8], mx = -INFINITY;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      sv[e] = (vis >> e) & 1u ? sc[e >> 2][e & 3] * a.scale_log2 : -INFINITY;
+      mx = fmaxf(mx, sv[e]);
+    }
+    if (__any(mx > m + kSlack)) {  // (the reference point moves)
+      const float m_new = fmaxf(m, col4_max(mx));
+      const float alpha = m_new == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - m_new);
+      m = m_new;
+      l *= alpha;
+#pragma unroll
+      for (int db = 0; db < NB; ++db) o[db] = o[db] * alpha;
+    }
+    const float m_use = m == -INFINITY ? 0.0f : m;
+    bf16x8 ph, pl;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float p = __builtin_amdgcn_exp2f(sv[e] - m_use);
+      l += p;
+      ph[e] = f2bf(p);
+      pl[e] = f2bf(p - bf2f(ph[e]));
+    }
+    bool bad = false;
+    if (masked) {
+      const int valid = u.lim - (32 * j + 8 * g);
+#pragma unroll
+      for (int db = 0; db < NB; ++db) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (e >= valid) R.f[2 * NS + db][e] = (bf16)0.0f;
+        bad |= nonfinite(R.f[2 * NS + db]);
+      }
+    }
+    if (__any(bad))
+#pragma unroll
+      for (int db = 0; db < NB; ++db) {
+        o[db] = take_nonfinite(R.f[2 * NS + db], vis, o[db]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+    for (int db = 0; db < NB; ++db) {
+      o[db] = mfma16x16x32(R.f[2 * NS + db], ph, o[db]);
+      o[db] = mfma16x16x32(R.f[2 * NS + db], pl, o[db]);
+    }
+  };
+  for (int j = j0; j < j1; j += 2 * kWaves) {
+    if (j + kWaves < j1) fetch(B, there_b, j + kWaves);
+    compute(A, there_a, j);
+    if (j + 2 * kWaves < j1) fetch(A, there_a, j + 2 * kWaves);
+    if (j + kWaves < j1) compute(B, there_b, j + kWaves);
+  }
+  // the four waves' states, joined in wave order
+  l = col4_sum(l);
+#pragma unroll
+  for (int db = 0; db < NB; ++db)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o_s[wave][li][16 * db + 4 * g + i] = o[db][i];
+  if (g == 0) {
+    ml_s[wave][li][0] = m;
+    ml_s[wave][li][1] = l;
+  }
+  __syncthreads();
+  for (int e = tid; e < 16 * DH; e += kThreads) {
+    const int i = e / DH, c = e % DH, p = pair0 + i;
+    if (p >= u.pairs) break;
+    float mm = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) mm = fmaxf(mm, ml_s[w][i][0]);
+    const float mu = mm == -INFINITY ? 0.0f : mm;
+    float ll = 0.0f, oo = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float f = __builtin_amdgcn_exp2f(ml_s[w][i][0] - mu);
+      ll += f * ml_s[w][i][1];
+      oo += f * o_s[w][i][c];
+    }
+    const size_t at = (u.part + p / group) * a.H + u.kh * group + p % group;
+    stg(a.part_o + at * DH + c, oo);
+    if (c == 0) {
+      stg(a.part_ml + at * 2, mm);
+      stg(a.part_ml + at * 2 + 1, ll);
+    }
+  }
+  __syncthreads();
+}
+
+// The launch's workgroups: the prefix's units first (they are the longest),
+// then a.merge runs of a request's pages each.
+template <int DH>
+__global__ __launch_bounds__(kThreads, 2) void unit_kernel(AttnArgs a, int prefix_units, int row_tiles) {
+  constexpr int kTileBytes = 4 * Frags<DH>::LOADS * 1024, kJoinBytes = kWaves * 16 * (DH + 6) * 4;
+  __shared__ __align__(16) char lds[kTileBytes > kJoinBytes ? kTileBytes : kJoinBytes];
+  const int group = a.H / a.Hkv;
+  Unit u;
+  // workgroup w runs on XCD w % 8: each XCD gets a contiguous share of the prefix's
+  // units, row tile by row tile of one (head, split), so that its keys are read
+  // into one L2
+  const int padded = up_div(prefix_units, 8) * 8;
+  if ((int)blockIdx.x < padded) {
+    const int x = (blockIdx.x & 7) * (padded / 8) + (blockIdx.x >> 3);
+    if (x >= prefix_units) return;
+    const int split = x / row_tiles % a.KP, tiles = up_div(a.P, kTileKeys), per = up_div(tiles, a.KP);
+    u.kh = x / row_tiles / a.KP;
+    u.row0 = 0;
+    u.pairs = a.N * group;
+    u.first = split * per < tiles ? split * per : tiles;
+    u.last = u.first + per < tiles ? u.first + per : tiles;
+    u.lim = u.held = a.P;
+    u.table = nullptr;
+    u.part = (size_t)split * a.N;
+    const int tile = x % row_tiles;
+    u.pair0 = 128 * tile;
+    if (a.wide)
+      tile_unit<DH, 2, false>(a, u, lds);
+    else
+      narrow_unit<DH>(a, u, 16 * tile, lds);
+    return;
+  }
+  const int x = blockIdx.x - padded, run_of = x / a.Hkv;
+  u.kh = x % a.Hkv;
+  if (run_of >= ldg(a.head + PLAN_UNITS)) return;
+  const int unit = ldg(a.units + run_of), run = unit & 0xffff;
+  const BatchRequest r = ldg(a.req + (unit >> 16));
+  if (r.n == 0 || run % a.merge != 0) return;
+  const int chunk = ldg(a.head + PLAN_CHUNK);
+  u.row0 = r.row0;
+  u.pairs = r.n * group;
+  u.held = r.held;
+  u.lim = r.held + r.n;
+  u.table = a.table + (size_t)(unit >> 16) * a.max_pages;
+  const int tiles = up_div(u.lim, kTileKeys) < a.max_pages ? up_div(u.lim, kTileKeys) : a.max_pages;
+  const long long f = (long long)run * chunk, t = f + (long long)chunk * a.merge;
+  u.first = f < tiles ? (int)f : tiles;
+  u.last = t < tiles ? (int)t : tiles;
+  u.part = (size_t)a.KP * a.N + r.part0 + (size_t)(run / a.merge) * r.n;
+  u.pair0 = 0;
+  if (u.pairs <= 16) {
+    narrow_unit<DH>(a, u, 0, lds);
+  } else {
+    for (; u.pair0 < u.pairs; u.pair0 += 64) tile_unit<DH, 1, true>(a, u, lds);
   }
 }
 
@@ -466,7 +544,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttnArgs a) {
   const int b = ldg(a.row_req + row);
   if (b < 0) return;  // (no request's row: left as it was)
   const BatchRequest r = ldg(a.req + b);
-  const int parts = a.KP + r.splits;
+  const int parts = a.KP + up_div(r.splits, a.merge);
   constexpr int PER = DH / 64;
   float m = -INFINITY, l = 0.0f, o[PER];
 #pragma unroll
@@ -488,41 +566,35 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttnArgs a) {
   for (int i = 0; i < PER; ++i) stg(a.out + item * DH + lane * PER + i, f2bf(o[i] * inv));
 }
 
-}  // namespace
-
 // Few pairs of rows and heads per K/V head: the waves share 16 of them and split the keys; many:
 // the waves split the pairs and share the keys.
-static bool wide_prefix(int N, int H, int Hkv) { return (long long)N * (H / Hkv) > 64; }
+bool wide_prefix(int N, int H, int Hkv) { return (long long)N * (H / Hkv) > 64; }
+
+template <int DH>
+hipError_t launch_attention(AttnArgs a, hipStream_t st) {
+  a.wide = wide_prefix(a.N, a.H, a.Hkv);
+  // The plan cuts the requests' pages for 8 K/V heads; more heads make enough
+  // workgroups of longer runs.
+  a.merge = a.Hkv <= 8 ? 1 : cdiv(a.Hkv, 12);
+  const int row_tiles = cdiv(a.N * (a.H / a.Hkv), a.wide ? 128 : 16), prefix_units = row_tiles * a.KP * a.Hkv;
+  const long long most = (long long)a.B * cdiv(a.max_pages, 2);  // (a run has two pages or more)
+  const int runs = most < plan_max_units(a.B) ? (int)most : plan_max_units(a.B);
+  unit_kernel<DH><<<dim3(cdiv(prefix_units, 8) * 8 + runs * a.Hkv), dim3(kThreads), 0, st>>>(a, prefix_units, row_tiles);
+  join_kernel<DH><<<dim3((unsigned)(((long long)a.N * a.H + kWaves - 1) / kWaves)), dim3(kThreads), 0, st>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace
 
 int prefix_splits(int N, int H, int Hkv, int P) {
   if (P <= 0) return 0;
-  int KP, most;
-  if (wide_prefix(N, H, Hkv)) {
-    KP = 512 / (cdiv(N * (H / Hkv), kTileRows) * Hkv);
-    most = cdiv(P, 2 * kTileKeys);
-  } else {
-    KP = cdiv(512, cdiv(N * (H / Hkv), 16) * Hkv);
-    most = cdiv(P, 128);
-  }
+  const int pairs = N * (H / Hkv);
+  const bool wide = wide_prefix(N, H, Hkv);
+  int KP = wide ? 512 / (cdiv(pairs, 128) * Hkv) : cdiv(512, cdiv(pairs, 16) * Hkv);
+  const int most = cdiv(P, 2 * kTileKeys);
   if (KP > most) KP = most;
   if (KP > max_prefix_splits(N)) KP = max_prefix_splits(N);
   return KP < 1 ? 1 : KP;
-}
-
-template <int DH>
-static hipError_t launch_attention(const AttnArgs& a, hipStream_t st) {
-  const int group = a.H / a.Hkv;
-  const bool wide = a.KP > 0 && wide_prefix(a.N, a.H, a.Hkv);
-  const int blocks = wide || a.KP == 0 ? 0 : cdiv(a.N * group, 16);
-  const long long most = (long long)a.B * cdiv(a.max_pages, 2);  // (a run has two pages or more)
-  const int units = most < plan_max_units(a.B) ? (int)most : plan_max_units(a.B);
-  if (wide) {
-    const int wu = cdiv(a.N * group, kTileRows) * a.KP * a.Hkv;
-    wide_kernel<DH><<<dim3(cdiv(wu, 8) * 8), dim3(kThreads), 0, st>>>(a);
-  }
-  split_kernel<DH><<<dim3(a.KP * blocks + units, a.Hkv), dim3(kThreads), 0, st>>>(a, blocks);
-  join_kernel<DH><<<dim3((unsigned)(((long long)a.N * a.H + kWaves - 1) / kWaves)), dim3(kThreads), 0, st>>>(a);
-  return hipGetLastError();
 }
 
 hipError_t launch_batch_attention(const AttnArgs& a, hipStream_t st) {
