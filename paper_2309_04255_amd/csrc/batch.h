@@ -130,7 +130,6 @@ struct AttnArgs {
   int B, N, H, Hkv, Dh;
   float scale_log2;
   int KP;     // key splits of the prefix
-  int wide;   // its rows in tiles of 128 pairs (else 16)
   int merge;  // runs of a request's pages per workgroup
 };
 hipError_t launch_batch_attention(const AttnArgs& a, hipStream_t st);

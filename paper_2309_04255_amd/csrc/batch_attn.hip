@@ -76,6 +76,12 @@ struct PageIds {
   }
 };
 
+// Direct global -> LDS copy of 16 bytes per lane: lane l's land at lds + 16 l
+// (lds the same in every lane).
+__device__ __forceinline__ void dma16(const void* src, char* lds) {
+  __builtin_amdgcn_global_load_lds((const LLMCAD_GLOBAL void*)src, (__attribute__((address_space(3))) void*)lds, 16, 0, 0);
+}
+
 // Which of the 8 keys from `key` on a row sees, by its mask (keys before held
 // are tokens all rows of the request see).
 __device__ __forceinline__ uint32_t seen8(const uint32_t (&anc)[4], int key, int held, int lim) {
@@ -132,8 +138,12 @@ __device__ __forceinline__ f32x4 take_nonfinite(bf16x8& v, uint32_t vis, f32x4 o
 //
 // 64 RB pairs per workgroup, 16 RB per wave.  Tiles of 64 keys are shared
 // through LDS in fragment order (every access is 16 bytes per lane, lane by
-// lane): while a tile is computed the next one is on its way to registers, and
-// it goes to the other buffer before the barrier.
+// lane), keys and values in two buffers each.  A turn of the loop takes the
+// values of tile t and the keys of tile t + 1: the scores of the next tile and
+// the exponentials of this one need different units, and their instructions
+// alternate.  Meanwhile the values of t + 1 and the keys of t + 2 are on their
+// way to registers; they go to the buffers that this turn does not read, so one
+// barrier per turn does.
 //
 // The running maximum is only a reference point: any value near it serves, so
 // the output is rescaled only when some score exceeds it by 2^kSlack, and
@@ -141,88 +151,74 @@ __device__ __forceinline__ f32x4 take_nonfinite(bf16x8& v, uint32_t vis, f32x4 o
 // the end.  Probabilities (up to 2^kSlack) enter the value product in bf16, half
 // a step of 2^-8 each.
 template <int DH, int RB, bool PAGED>
-__device__ __forceinline__ void tile_unit(const AttnArgs& a, const Unit& u, char* lds) {
-  constexpr int NS = Frags<DH>::NS, NB = Frags<DH>::NB, LOADS = Frags<DH>::LOADS;
-  constexpr int PER = LOADS / 2;  // fragments per wave and tile: K of a step, or V^T of a step
-  constexpr int TILE = 2 * LOADS * 1024;
-  const int lane = threadIdx.x & 63, li = lane & 15, g = lane >> 4, wave = wave_index();
-  const int group = a.H / a.Hkv;
-  auto pair_of = [&](int rb) { return u.pair0 + (wave * RB + rb) * 16 + li; };
-  auto clamped = [&](int rb) { return pair_of(rb) < u.pairs ? pair_of(rb) : u.pairs - 1; };
+struct TileWork {
+  static constexpr int NS = Frags<DH>::NS, NB = Frags<DH>::NB;
+  static constexpr int PER = 2 * NS;              // fragments a wave fetches per tile: K of a step, or V^T of a step
+  static constexpr int HALF = 2 * PER * 1024;     // a tile's keys, or its values
+  static_assert(2 * NS == NB, "as many key as value fragments");
+  typedef f32x4 Scores[RB][4];  // [row block][step, key block]
 
+  const AttnArgs& a;
+  const Unit& u;
+  char* lds;  // keys of even tiles, of odd tiles, values of even, of odd
+  int lane, li, g, wave, group;
   bf16x8 qf[RB][NS];
-#pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    const int pr = clamped(rb);
-    const bf16* q = a.q + (size_t)(u.row0 + pr / group) * a.q_stride + (size_t)(u.kh * group + pr % group) * DH + 8 * g;
-#pragma unroll
-    for (int s = 0; s < NS; ++s) qf[rb][s] = ldg((const bf16x8*)(q + 32 * s));
-  }
-  // this wave's part of a tile: waves 0 and 2 the keys of its two steps, 1 and 3 the values
-  const bool values = (wave & 1) != 0;
-  const int key = 32 * (wave >> 1);
-  const int lds_at = ((wave >> 1) * LOADS + (values ? 2 * NS : 0)) * 1024 + lane * 16;
-  PageIds pages;
-  if (PAGED) pages.start(u, u.first);
-  bf16x8 stage[PER];
-  bool there, next_there = true;
-  auto fetch = [&](int t) {
-    const TileAt at = PAGED ? page_tile(a, u, pages.get(u, t)) : prefix_tile(a, u, t);
-    next_there = at.there;
-    const bf16* src = values ? at.v + (size_t)li * at.vs + key + 8 * g : at.k + (key + 8 * (li >> 2) + (li & 3)) * DH + 8 * g;
-#pragma unroll
-    for (int e = 0; e < PER; ++e) {
-      const size_t off = values ? (size_t)e * 16 * at.vs : (size_t)((e / NS) * 4 * DH + (e % NS) * 32);
-      stage[e] = ldg((const bf16x8*)(src + off));
-    }
-  };
-  auto put = [&](int t) {
-    char* at = lds + (t & 1) * TILE + lds_at;
-    if (values && ((t + 1) * kTileKeys > u.lim || !next_there)) {  // (values of keys that are not there: zeros)
-      const int valid = next_there ? u.lim - (t * kTileKeys + key + 8 * g) : 0;
-#pragma unroll
-      for (int e = 0; e < PER; ++e)
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (i >= valid) stage[e][i] = (bf16)0.0f;
-    }
-#pragma unroll
-    for (int e = 0; e < PER; ++e) lds_st<bf16x8>(at + e * 1024, stage[e]);
-  };
-
   float m[RB], neg_m[RB], l[RB];
   f32x4 o[RB][NB];
-#pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    m[rb] = -INFINITY;
-    neg_m[rb] = 0.0f;
-    l[rb] = 0.0f;
-#pragma unroll
-    for (int db = 0; db < NB; ++db) o[rb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
+  uint32_t vis[RB][2];
+  bool masked, there;
+  PageIds pages;
+  uint32_t lane_k, lane_v;  // byte offsets of the lane's part of a tile's fragments
+
+  __device__ __forceinline__ TileWork(const AttnArgs& a_, const Unit& u_, char* lds_) : a(a_), u(u_), lds(lds_) {
+    lane = threadIdx.x & 63;
+    li = lane & 15;
+    g = lane >> 4;
+    wave = wave_index();
+    group = a.H / a.Hkv;
   }
-  if (u.first < u.last) {
-    fetch(u.first);
-    put(u.first);
+  __device__ __forceinline__ int pair_of(int rb) const { return u.pair0 + (wave * RB + rb) * 16 + li; }
+  __device__ __forceinline__ int clamped(int rb) const { return pair_of(rb) < u.pairs ? pair_of(rb) : u.pairs - 1; }
+  // waves 0 and 2 fetch the keys of a tile's two steps, 1 and 3 the values
+  __device__ __forceinline__ bool values() const { return (wave & 1) != 0; }
+  __device__ __forceinline__ int key_of() const { return 32 * (wave >> 1); }
+
+  // copies this wave's part of tile t straight to LDS
+  __device__ __forceinline__ void fetch(int t) {
+    const TileAt at = PAGED ? page_tile(a, u, pages.get(u, t)) : prefix_tile(a, u, t);
+    char* to = lds + ((values() ? 2 : 0) + (t & 1)) * HALF + (wave >> 1) * PER * 1024;
+    if (values()) {
+#pragma unroll
+      for (int e = 0; e < PER; ++e) dma16((const char*)(at.v + (size_t)e * 16 * at.vs) + lane_v, to + e * 1024);
+    } else {
+#pragma unroll
+      for (int e = 0; e < PER; ++e) dma16((const char*)(at.k + (e / NS) * 4 * DH + (e % NS) * 32) + lane_k, to + e * 1024);
+    }
   }
-  there = next_there;
-  __syncthreads();
-  for (int t = u.first; t < u.last; ++t) {
-    if (t + 1 < u.last) fetch(t + 1);
-    const char* at = lds + (t & 1) * TILE + lane * 16;
-    f32x4 sc[RB][4];  // [row block][step, key block]
+
+  // scores of tile t (its keys in LDS)
+  __device__ __forceinline__ void scores(Scores& sc, int t) {
+    const char* at = lds + (t & 1) * HALF + lane * 16;
 #pragma unroll
     for (int sb = 0; sb < 4; ++sb) {
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) sc[rb][sb] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int s = 0; s < NS; ++s) {
-        const bf16x8 k = lds_ld<bf16x8>(at + ((sb >> 1) * LOADS + (sb & 1) * NS + s) * 1024);
+        const bf16x8 k = lds_ld<bf16x8>(at + (sb * NS + s) * 1024);
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) sc[rb][sb] = mfma16x16x32(k, qf[rb][s], sc[rb][sb]);
       }
     }
-    const bool masked = (t + 1) * kTileKeys > u.held || !there;  // (not every row sees every key)
-    uint32_t vis[RB][2];
+  }
+  // the mask of tile t, and a new reference point where its scores need one
+  __device__ __forceinline__ void look(Scores& sc, int t) {
+    there = true;
+    if (PAGED) {
+      const int id = pages.get(u, t);
+      there = id >= 0 && id < a.n_pages;
+    }
+    masked = (t + 1) * kTileKeys > u.held || !there;  // (not every row sees every key)
     if (masked) {
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) {
@@ -238,7 +234,6 @@ __device__ __forceinline__ void tile_unit(const AttnArgs& a, const Unit& u, char
 #pragma unroll
           for (int e = 0; e < 8; ++e)
             if (!((vis[rb][st] >> e) & 1u)) sc[rb][2 * st + (e >> 2)][e & 3] = -INFINITY;
-          __builtin_amdgcn_sched_barrier(0);
         }
       }
     }
@@ -265,26 +260,56 @@ __device__ __forceinline__ void tile_unit(const AttnArgs& a, const Unit& u, char
         for (int db = 0; db < NB; ++db) o[rb][db] = o[rb][db] * alpha;
       }
     }
-    bf16x8 p[RB][2];
+  }
+  __device__ __forceinline__ bf16x8 value(int t, int st, int db) const {
+    return lds_ld<bf16x8>(lds + (2 + (t & 1)) * HALF + (st * NB + db) * 1024 + lane * 16);
+  }
+  // Values of keys that are not there count as zeros (what lies there may be NaN).
+  __device__ __forceinline__ void clear_absent(int t) {
+#pragma unroll 1
+    for (int st = 0; st < 2; ++st) {
+      const int valid = there ? u.lim - (t * kTileKeys + 32 * st + 8 * g) : 0;
+      if (__any(valid < 8)) {
+        char* at = lds + (2 + (t & 1)) * HALF + st * NB * 1024 + lane * 16;
+#pragma unroll 1
+        for (int db = wave; db < NB; db += kWaves) {
+          bf16x8 v = lds_ld<bf16x8>(at + db * 1024);
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const float v = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[rb][e >> 2][e & 3], a.scale_log2, neg_m[rb]));
-        l[rb] += v;
-        p[rb][e >> 3][e & 7] = f2bf(v);
+          for (int e = 0; e < 8; ++e)
+            if (e >= valid) v[e] = (bf16)0.0f;
+          lds_st<bf16x8>(at + db * 1024, v);
+        }
       }
+    }
+    __syncthreads();
+  }
+  // Tile t's probabilities and its part of the output; the next tile's scores.
+  __device__ __forceinline__ void turn(Scores& sc, Scores& next, int t) {
+    const bool more = t + 1 < u.last;
+    if (values() ? more : t + 2 < u.last) fetch(values() ? t + 1 : t + 2);
     bool bad = false;
     if (PAGED && masked) {
 #pragma unroll
-      for (int e = 0; e < 2 * NB; ++e) bad |= nonfinite(lds_ld<bf16x8>(at + ((e / NB) * LOADS + 2 * NS + e % NB) * 1024));
+      for (int e = 0; e < 2 * NB; ++e) bad |= nonfinite(value(t, e / NB, e % NB));
     }
+    scores(next, t + 1);  // (past the last tile: of what lies there, not used)
+    bf16x8 p[RB][2];
+#pragma unroll
+    for (int st = 0; st < 2; ++st)
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float v = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[rb][2 * st + (e >> 2)][e & 3], a.scale_log2, neg_m[rb]));
+          l[rb] += v;
+          p[rb][st][e] = f2bf(v);
+        }
     if (PAGED && __any(bad)) {
 #pragma unroll
       for (int st = 0; st < 2; ++st)
 #pragma unroll
         for (int db = 0; db < NB; ++db) {
-          bf16x8 v = lds_ld<bf16x8>(at + (st * LOADS + 2 * NS + db) * 1024);
+          const bf16x8 v = value(t, st, db);
 #pragma unroll
           for (int rb = 0; rb < RB; ++rb) {
             bf16x8 kept = v;
@@ -298,28 +323,72 @@ __device__ __forceinline__ void tile_unit(const AttnArgs& a, const Unit& u, char
       for (int st = 0; st < 2; ++st)
 #pragma unroll
         for (int db = 0; db < NB; ++db) {
-          const bf16x8 v = lds_ld<bf16x8>(at + (st * LOADS + 2 * NS + db) * 1024);
+          const bf16x8 v = value(t, st, db);
 #pragma unroll
           for (int rb = 0; rb < RB; ++rb) o[rb][db] = mfma16x16x32(v, p[rb][st], o[rb][db]);
         }
     }
-    if (t + 1 < u.last) put(t + 1);
-    there = next_there;
     __syncthreads();
-  }
-#pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    const int pr = pair_of(rb);
-    const float sum = col4_sum(l[rb]);
-    if (pr >= u.pairs) continue;
-    const size_t at = (u.part + pr / group) * a.H + u.kh * group + pr % group;
-#pragma unroll
-    for (int db = 0; db < NB; ++db) stg((f32x4*)(a.part_o + at * DH + 16 * db + 4 * g), o[rb][db]);
-    if (g == 0) {
-      stg(a.part_ml + at * 2, m[rb]);
-      stg(a.part_ml + at * 2 + 1, sum);
+    if (more) {
+      look(next, t + 1);
+      if (masked && ((t + 2) * kTileKeys > u.lim || !there)) clear_absent(t + 1);
     }
   }
+
+  __device__ __forceinline__ void run() {
+    if (PAGED) pages.start(u, u.first);
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      m[rb] = -INFINITY;
+      neg_m[rb] = 0.0f;
+      l[rb] = 0.0f;
+#pragma unroll
+      for (int db = 0; db < NB; ++db) o[rb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    if (u.first < u.last) {
+      lane_k = ((key_of() + 8 * (li >> 2) + (li & 3)) * DH + 8 * g) * 2;
+      lane_v = ((uint32_t)li * (PAGED ? kPage : a.cap) + key_of() + 8 * g) * 2;
+      fetch(u.first);
+      if (!values() && u.first + 1 < u.last) fetch(u.first + 1);
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        const int pr = clamped(rb);
+        const bf16* q = a.q + (size_t)(u.row0 + pr / group) * a.q_stride + (size_t)(u.kh * group + pr % group) * DH + 8 * g;
+#pragma unroll
+        for (int s = 0; s < NS; ++s) qf[rb][s] = ldg((const bf16x8*)(q + 32 * s));
+      }
+      __syncthreads();
+      Scores A, B;
+      scores(A, u.first);
+      // (the first turn overwrites this tile's keys: every wave has read them)
+      __syncthreads();
+      look(A, u.first);
+      if (masked && ((u.first + 1) * kTileKeys > u.lim || !there)) clear_absent(u.first);
+      for (int t = u.first; t < u.last; t += 2) {
+        turn(A, B, t);
+        if (t + 1 < u.last) turn(B, A, t + 1);
+      }
+    }
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      const int pr = pair_of(rb);
+      const float sum = col4_sum(l[rb]);
+      if (pr >= u.pairs) continue;
+      const size_t at = (u.part + pr / group) * a.H + u.kh * group + pr % group;
+#pragma unroll
+      for (int db = 0; db < NB; ++db) stg((f32x4*)(a.part_o + at * DH + 16 * db + 4 * g), o[rb][db]);
+      if (g == 0) {
+        stg(a.part_ml + at * 2, m[rb]);
+        stg(a.part_ml + at * 2 + 1, sum);
+      }
+    }
+  }
+};
+
+template <int DH, int RB, bool PAGED>
+__device__ __forceinline__ void tile_unit(const AttnArgs& a, const Unit& u, char* lds) {
+  TileWork<DH, RB, PAGED> w(a, u, lds);
+  w.run();
 }
 
 // ---------------------------------------------------------------- few rows
@@ -477,36 +546,48 @@ __device__ __forceinline__ void narrow_unit(const AttnArgs& a, const Unit& u, in
   __syncthreads();
 }
 
-// The launch's workgroups: the prefix's units first (they are the longest),
-// then a.merge runs of a request's pages each.
+// Unit x of the prefix: (K/V head, key split, row tile), row tiles fastest.
+// Workgroup w runs on XCD w % 8: each XCD gets a contiguous share of the units, so
+// that a (head, split)'s keys are read into one L2.
+__device__ __forceinline__ bool prefix_unit(const AttnArgs& a, int w, int units, int row_tiles, Unit& u, int& tile) {
+  const int share = up_div(units, 8), x = (w & 7) * share + (w >> 3);
+  if ((w >> 3) >= share || x >= units) return false;
+  const int split = x / row_tiles % a.KP, tiles = up_div(a.P, kTileKeys), per = up_div(tiles, a.KP);
+  tile = x % row_tiles;
+  u.kh = x / row_tiles / a.KP;
+  u.row0 = 0;
+  u.pairs = a.N * (a.H / a.Hkv);
+  u.first = split * per < tiles ? split * per : tiles;
+  u.last = u.first + per < tiles ? u.first + per : tiles;
+  u.lim = u.held = a.P;
+  u.table = nullptr;
+  u.part = (size_t)split * a.N;
+  u.pair0 = 0;
+  return true;
+}
+
+template <int DH>
+__global__ __launch_bounds__(kThreads, 2) void prefix_kernel(AttnArgs a, int units, int row_tiles) {
+  __shared__ __align__(16) char lds[4 * Frags<DH>::LOADS * 1024];
+  Unit u;
+  int tile;
+  if (!prefix_unit(a, blockIdx.x, units, row_tiles, u, tile)) return;
+  u.pair0 = 128 * tile;
+  tile_unit<DH, 2, false>(a, u, lds);
+}
+
+// Workgroups of few rows of the prefix first, then a.merge runs of a request's
+// pages each.
 template <int DH>
 __global__ __launch_bounds__(kThreads, 2) void unit_kernel(AttnArgs a, int prefix_units, int row_tiles) {
   constexpr int kTileBytes = 4 * Frags<DH>::LOADS * 1024, kJoinBytes = kWaves * 16 * (DH + 6) * 4;
   __shared__ __align__(16) char lds[kTileBytes > kJoinBytes ? kTileBytes : kJoinBytes];
   const int group = a.H / a.Hkv;
   Unit u;
-  // workgroup w runs on XCD w % 8: each XCD gets a contiguous share of the prefix's
-  // units, row tile by row tile of one (head, split), so that its keys are read
-  // into one L2
   const int padded = up_div(prefix_units, 8) * 8;
   if ((int)blockIdx.x < padded) {
-    const int x = (blockIdx.x & 7) * (padded / 8) + (blockIdx.x >> 3);
-    if (x >= prefix_units) return;
-    const int split = x / row_tiles % a.KP, tiles = up_div(a.P, kTileKeys), per = up_div(tiles, a.KP);
-    u.kh = x / row_tiles / a.KP;
-    u.row0 = 0;
-    u.pairs = a.N * group;
-    u.first = split * per < tiles ? split * per : tiles;
-    u.last = u.first + per < tiles ? u.first + per : tiles;
-    u.lim = u.held = a.P;
-    u.table = nullptr;
-    u.part = (size_t)split * a.N;
-    const int tile = x % row_tiles;
-    u.pair0 = 128 * tile;
-    if (a.wide)
-      tile_unit<DH, 2, false>(a, u, lds);
-    else
-      narrow_unit<DH>(a, u, 16 * tile, lds);
+    int tile;
+    if (prefix_unit(a, blockIdx.x, prefix_units, row_tiles, u, tile)) narrow_unit<DH>(a, u, 16 * tile, lds);
     return;
   }
   const int x = blockIdx.x - padded, run_of = x / a.Hkv;
@@ -572,14 +653,19 @@ bool wide_prefix(int N, int H, int Hkv) { return (long long)N * (H / Hkv) > 64; 
 
 template <int DH>
 hipError_t launch_attention(AttnArgs a, hipStream_t st) {
-  a.wide = wide_prefix(a.N, a.H, a.Hkv);
+  const bool wide = wide_prefix(a.N, a.H, a.Hkv);
   // The plan cuts the requests' pages for 8 K/V heads; more heads make enough
   // workgroups of longer runs.
   a.merge = a.Hkv <= 8 ? 1 : cdiv(a.Hkv, 12);
-  const int row_tiles = cdiv(a.N * (a.H / a.Hkv), a.wide ? 128 : 16), prefix_units = row_tiles * a.KP * a.Hkv;
+  const int row_tiles = cdiv(a.N * (a.H / a.Hkv), wide ? 128 : 16);
+  int units = row_tiles * a.KP * a.Hkv;
   const long long most = (long long)a.B * cdiv(a.max_pages, 2);  // (a run has two pages or more)
   const int runs = most < plan_max_units(a.B) ? (int)most : plan_max_units(a.B);
-  unit_kernel<DH><<<dim3(cdiv(prefix_units, 8) * 8 + runs * a.Hkv), dim3(kThreads), 0, st>>>(a, prefix_units, row_tiles);
+  if (wide && units > 0) {
+    prefix_kernel<DH><<<dim3(cdiv(units, 8) * 8), dim3(kThreads), 0, st>>>(a, units, row_tiles);
+    units = 0;
+  }
+  unit_kernel<DH><<<dim3(cdiv(units, 8) * 8 + runs * a.Hkv), dim3(kThreads), 0, st>>>(a, units, row_tiles);
   join_kernel<DH><<<dim3((unsigned)(((long long)a.N * a.H + kWaves - 1) / kWaves)), dim3(kThreads), 0, st>>>(a);
   return hipGetLastError();
 }
