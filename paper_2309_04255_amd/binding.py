@@ -7,6 +7,7 @@ fails loudly if the library has not been built.
 """
 
 import ctypes
+import functools
 import os
 
 import numpy as np
@@ -376,31 +377,39 @@ PLAN_BAD_TREE = 3
 _PLAN_REGIONS = ("slot", "position", "mask", "rope", "status", "taken")
 
 
+# The current stream's handle: torch.cuda.current_stream() builds an object for it, which takes a
+# quarter of a small call's host time (2.7 us; 0.06 us this way).
+_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+    (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+
+
 def _on_device(what, first, *others):
-    """The device every tensor of a call lies on (ValueError if they differ or one is not on a GPU)."""
-    dev = first.device
-    if dev.type != "cuda":
-        raise ValueError(f"{what}: the tensors must be on a GPU")
+    """The index of the GPU that every tensor of a call lies on (ValueError if they differ or one is on none)."""
+    dev = first.get_device()
     for t in others:
-        if t is not None and t.device != dev:
-            raise ValueError(f"{what}: tensors on {dev} and {t.device}")
+        if t is not None and t.get_device() != dev:
+            raise ValueError(f"{what}: tensors on {first.device} and {t.device}")
+    if dev < 0:
+        raise ValueError(f"{what}: the tensors must be on a GPU")
     return dev
 
 
 def _enqueue(fn, dev, stream, args):
     """fn(*args, stream) with dev the current device (a launch goes to the current device's kernels)."""
-    if dev.index == torch.cuda.current_device():
-        return fn(*args, (stream or torch.cuda.current_stream()).cuda_stream)
+    if dev == torch.cuda.current_device():
+        return fn(*args, _current_stream(dev) if stream is None else stream.cuda_stream)
     with torch.cuda.device(dev):
-        return fn(*args, (stream or torch.cuda.current_stream()).cuda_stream)
+        return fn(*args, _current_stream(dev) if stream is None else stream.cuda_stream)
 
 
 def _want(what, name, t, dtype, *shape):
     """t is a contiguous tensor of dtype and shape (None: any size)."""
-    if t.dtype != dtype or t.dim() != len(shape) or not t.is_contiguous() or \
-            any(w is not None and w != s for w, s in zip(shape, t.shape)):
-        raise ValueError(f"{what}: {name} must be a contiguous {dtype} tensor of shape "
-                         f"{tuple('any' if w is None else w for w in shape)}, got {t.dtype} {tuple(t.shape)}")
+    got = t.shape
+    if t.dtype is dtype and t.is_contiguous() and \
+            (got == shape or (len(got) == len(shape) and all(w is None or w == s for w, s in zip(shape, got)))):
+        return
+    raise ValueError(f"{what}: {name} must be a contiguous {dtype} tensor of shape "
+                     f"{tuple('any' if w is None else w for w in shape)}, got {t.dtype} {tuple(got)}")
 
 
 def _want_rows(what, name, t, n, heads, dh):
@@ -416,18 +425,36 @@ def batch_plan_bytes(cfg, n_requests: int, n_rows: int) -> int:
     return _lib.llmcad_batch_plan_bytes(ctypes.byref(cfg), int(n_requests), int(n_rows))
 
 
+@functools.lru_cache(maxsize=64)
+def _plan_parts(head_dim, n_requests, n_rows):
+    """A plan's int32 words in pieces: (their lengths, the piece of every array)."""
+    cfg = LlmcadConfig(1, head_dim, 1, head_dim, 1, 1, 1e-6, 10000.0, 16)  # (the layout depends on head_dim alone)
+    off, size, spans = ctypes.c_size_t(), ctypes.c_size_t(), []
+    for which in range(len(_PLAN_REGIONS)):
+        _check(_lib.llmcad_batch_plan_region(ctypes.byref(cfg), n_requests, n_rows, which, ctypes.byref(off),
+                                             ctypes.byref(size)), "llmcad_batch_plan_region")
+        spans.append((off.value // 4, off.value // 4 + size.value // 4, which))
+    lengths, piece, at = [], {}, 0
+    for lo, hi, which in sorted(spans):
+        lengths += [lo - at, hi - lo]
+        piece[_PLAN_REGIONS[which]] = len(lengths) - 1
+        at = hi
+    lengths.append(batch_plan_bytes(cfg, n_requests, n_rows) // 4 - at)
+    return lengths, piece
+
+
 def batch_plan_views(cfg, n_requests: int, n_rows: int, plan) -> dict:
     """The arrays of a plan as views of its buffer: slot, position int32 [n_rows], mask int32
     [n_rows, 4], rope float32 [n_rows, Dh/2, 2], status int32 [n_requests], taken int32 [1]."""
-    shapes = {"slot": (n_rows,), "position": (n_rows,), "mask": (n_rows, 4), "rope": (n_rows, cfg.head_dim // 2, 2),
-              "status": (n_requests,), "taken": (1,)}
-    views, off, size = {}, ctypes.c_size_t(), ctypes.c_size_t()
-    for which, name in enumerate(_PLAN_REGIONS):
-        _check(_lib.llmcad_batch_plan_region(ctypes.byref(cfg), int(n_requests), int(n_rows), which, ctypes.byref(off),
-                                             ctypes.byref(size)), "llmcad_batch_plan_region")
-        part = plan[off.value:off.value + size.value].view(torch.float32 if name == "rope" else torch.int32)
-        views[name] = part.view(shapes[name])
-    return views
+    lengths, piece = _plan_parts(cfg.head_dim, n_requests, n_rows)
+    words = plan.view(torch.int32)
+    if words.shape[0] != sum(lengths):  # (a larger buffer)
+        words = words[:sum(lengths)]
+    parts = words.split(lengths)
+    return {"slot": parts[piece["slot"]], "position": parts[piece["position"]],
+            "mask": parts[piece["mask"]].view(n_rows, 4),
+            "rope": parts[piece["rope"]].view(torch.float32).view(n_rows, cfg.head_dim // 2, 2),
+            "status": parts[piece["status"]], "taken": parts[piece["taken"]]}
 
 
 def batch_plan(cfg, row_start, held, parent, prefix_len: int, block_table, free_pages, n_pages: int, plan,
@@ -537,30 +564,38 @@ def token_scores(logits, tokens, k: int = 0, row_of=None, workspace=None, stream
     (see llmcad_token_scores).  tokens may be None.  The outputs are new tensors of `stream`."""
     what = "token_scores"
     dev = _on_device(what, logits, tokens, row_of, workspace)
-    if logits.dim() != 2 or logits.dtype not in (torch.float32, torch.bfloat16) or \
+    fp32 = logits.dtype is torch.float32
+    if logits.dim() != 2 or not (fp32 or logits.dtype is torch.bfloat16) or \
             (logits.shape[1] > 1 and logits.stride(1) != 1):
         raise ValueError("token_scores: logits must be float32 or bfloat16 [n, V] with contiguous rows")
     n, V = logits.shape
+    k = int(k)
+    if not 0 <= k <= TOP_MAX:
+        raise ValueError(f"token_scores: k must be in [0, {TOP_MAX}]")
     m = 0
     if tokens is not None:
         m = tokens.shape[0] if tokens.dim() == 1 else -1
         _want(what, "tokens", tokens, torch.int32, n if row_of is None else m)
         if row_of is not None:
             _want(what, "row_of", row_of, torch.int32, m)
-    with torch.cuda.device(dev), torch.cuda.stream(stream):
-        if workspace is None:
-            workspace = torch.zeros(token_scores_workspace_bytes(n, V, k), dtype=torch.uint8, device=dev)
+    if stream is not None or dev != torch.cuda.current_device():
+        with torch.cuda.device(dev), torch.cuda.stream(stream):
+            return token_scores(logits, tokens, k, row_of, workspace)
+    if workspace is None:
+        workspace = torch.zeros(token_scores_workspace_bytes(n, V, k), dtype=torch.uint8, device=logits.device)
+    else:
         _want(what, "workspace", workspace, torch.uint8, None)
-        floats = torch.empty(m + 2 * n, dtype=torch.float32, device=dev)
-        top = torch.empty((2, n, k), dtype=torch.int32, device=dev)
-        base, tp = floats.data_ptr(), top.data_ptr()
-        _check(_lib.llmcad_token_scores(
-            logits.data_ptr(), 32 if logits.dtype == torch.float32 else 16, logits.stride(0) if n > 1 else V,
-            n, V, tokens.data_ptr() if m else None, row_of.data_ptr() if m and row_of is not None else
-            None, m, base, base + 4 * m, base + 4 * (m + n), int(k), tp, tp + 4 * n * k, workspace.data_ptr(),
-            workspace.shape[0], torch.cuda.current_stream().cuda_stream), "llmcad_token_scores")
-    return {"logprob": floats[:m], "entropy": floats[m:m + n], "lse": floats[m + n:], "top_token": top[0],
-            "top_logprob": top[1].view(torch.float32)}
+    out = torch.empty(m + 2 * n + 2 * n * k, dtype=torch.float32, device=logits.device)
+    at = out.data_ptr()
+    top = at + 4 * (m + 2 * n)
+    _check(_lib.llmcad_token_scores(
+        logits.data_ptr(), 32 if fp32 else 16, logits.stride(0) if n > 1 else V, n, V,
+        tokens.data_ptr() if m else None, row_of.data_ptr() if m and row_of is not None else None, m, at, at + 4 * m,
+        at + 4 * (m + n), k, top, top + 4 * n * k, workspace.data_ptr(), workspace.shape[0],
+        _current_stream(dev)), "llmcad_token_scores")
+    logprob, entropy, lse, token, value = out.split((m, n, n, n * k, n * k))
+    return {"logprob": logprob, "entropy": entropy, "lse": lse, "top_token": token.view(torch.int32).view(n, k),
+            "top_logprob": value.view(n, k)}
 
 
 def workspace_region(cfg, n: int, which: int):

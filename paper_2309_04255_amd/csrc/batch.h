@@ -94,6 +94,7 @@ struct StoreArgs {
   const int* slot;
   const float* rope;
   int N, H, Hkv, Dh, n_pages;
+  int heads_per;  // heads that a workgroup turns (the launch sets it)
 };
 hipError_t launch_batch_store(const StoreArgs& a, hipStream_t st);
 

@@ -250,66 +250,59 @@ namespace {
 
 // ---------------------------------------------------------------- store
 //
-// Rows of 64 per workgroup and head.  A lane turns 8 dims of a row's first
-// half with their partners of the second (rotate-half pairing).  A V row
-// becomes a column of its page: the rows meet in LDS, and eight rows whose
-// slots are one aligned piece of eight leave as 16 bytes; the others (a
-// piece's ends, single tokens) as single entries.
+// Two kinds of workgroups.  The first turn queries and keys: 256 threads hold the
+// cosines and sines of kTurnRows rows (a lane those of 8 dims and their partners
+// in the second half, rotate-half pairing) and go through `a.heads_per` heads.
+// The others write values: a V row becomes a column of its page, so 64 rows of a
+// head meet in LDS, and eight rows whose slots are one aligned piece of eight
+// leave as 16 bytes; the others (a piece's ends, single tokens) as single entries.
 constexpr int kStoreRows = 64;
 
-__device__ __forceinline__ void turn8(const bf16* src, bf16* dst, const float* rope, int half) {
-  const bf16x8 a = ldg((const bf16x8*)src), b = ldg((const bf16x8*)(src + half));
-  bf16x8 x, y;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const f32x4 cs = ldg((const f32x4*)rope + e);  // cos, sin of two pairs
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const float p = bf2f(a[2 * e + u]), q = bf2f(b[2 * e + u]), c = cs[2 * u], s = cs[2 * u + 1];
-      x[2 * e + u] = f2bf(p * c - q * s);
-      y[2 * e + u] = f2bf(q * c + p * s);
-    }
-  }
-  stg((bf16x8*)dst, x);
-  stg((bf16x8*)(dst + half), y);
+__device__ __forceinline__ int slot_of(const StoreArgs& a, int row) {
+  const int s = row < a.N ? ldg(a.slot + row) : -1;
+  return s < a.n_pages * kPage ? s : -1;
 }
 
 template <int DH>
-__global__ __launch_bounds__(kThreads) void store_kernel(StoreArgs a) {
+__device__ __forceinline__ void turn_rows(const StoreArgs& a, int block, int heads0) {
+  constexpr int HALF = DH / 2, LANES = HALF / 8, ROWS = kThreads / LANES;
+  const int row = block * ROWS + threadIdx.x / LANES, c = 8 * (threadIdx.x % LANES);
+  const int s = slot_of(a, row);
+  if (s < 0) return;
+  f32x4 cs[4];  // cos, sin of two pairs each
+#pragma unroll
+  for (int e = 0; e < 4; ++e) cs[e] = ldg((const f32x4*)(a.rope + ((size_t)row * HALF + c) * 2) + e);
+  const int heads1 = heads0 + a.heads_per < a.H + a.Hkv ? heads0 + a.heads_per : a.H + a.Hkv;
+#pragma unroll 4
+  for (int h = heads0; h < heads1; ++h) {
+    const int kh = h - a.H;
+    const bf16* src = kh < 0 ? a.q + (size_t)row * a.q_stride + (size_t)h * DH : a.k + (size_t)row * a.k_stride + (size_t)kh * DH;
+    bf16* dst = kh < 0 ? a.q_out + ((size_t)row * a.H + h) * DH
+                       : a.k_pages + (((size_t)(s / kPage) * a.Hkv + kh) * kPage + s % kPage) * DH;
+    const bf16x8 p = ldg((const bf16x8*)(src + c)), q = ldg((const bf16x8*)(src + c + HALF));
+    bf16x8 x, y;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float u = bf2f(p[e]), v = bf2f(q[e]), co = cs[e >> 1][2 * (e & 1)], si = cs[e >> 1][2 * (e & 1) + 1];
+      x[e] = f2bf(u * co - v * si);
+      y[e] = f2bf(v * co + u * si);
+    }
+    stg((bf16x8*)(dst + c), x);
+    stg((bf16x8*)(dst + c + HALF), y);
+  }
+}
+
+template <int DH>
+__device__ __forceinline__ void write_values(const StoreArgs& a, int block, int kh) {
   __shared__ int slot_s[kStoreRows];
   __shared__ int full_s[kStoreRows];
   __shared__ uint16_t vt[kStoreRows][DH + 2];
-  const int r0 = blockIdx.x * kStoreRows, h = blockIdx.y, tid = threadIdx.x;
+  const int r0 = block * kStoreRows, tid = threadIdx.x;
   const int rows = a.N - r0 < kStoreRows ? a.N - r0 : kStoreRows;
-  constexpr int HALF = DH / 2, LANES = HALF / 8;  // lanes per row
-  if (tid < kStoreRows) {
-    int s = tid < rows ? ldg(a.slot + r0 + tid) : -1;
-    if (s >= a.n_pages * kPage) s = -1;
-    slot_s[tid] = s;
-  }
-  __syncthreads();
-  if (h < a.H) {  // a query head
-    for (int e = tid; e < rows * LANES; e += kThreads) {
-      const int i = e / LANES, c = 8 * (e % LANES);
-      if (slot_s[i] < 0) continue;
-      const size_t row = (size_t)r0 + i;
-      turn8(a.q + row * a.q_stride + (size_t)h * DH + c, a.q_out + (row * a.H + h) * DH + c,
-            a.rope + (row * HALF + c) * 2, HALF);
-    }
-    return;
-  }
-  const int kh = h - a.H;
-  for (int e = tid; e < rows * LANES; e += kThreads) {
-    const int i = e / LANES, c = 8 * (e % LANES), s = slot_s[i];
-    if (s < 0) continue;
-    const size_t row = (size_t)r0 + i;
-    turn8(a.k + row * a.k_stride + (size_t)kh * DH + c,
-          a.k_pages + (((size_t)(s / kPage) * a.Hkv + kh) * kPage + s % kPage) * DH + c,
-          a.rope + (row * HALF + c) * 2, HALF);
-  }
+  if (tid < kStoreRows) slot_s[tid] = slot_of(a, r0 + tid);
+#pragma unroll 4
   for (int e = tid; e < rows * (DH / 8); e += kThreads) {
     const int i = e / (DH / 8), c = 8 * (e % (DH / 8));
-    if (slot_s[i] < 0) continue;
     const bf16x8 v = ldg((const bf16x8*)(a.v + ((size_t)r0 + i) * a.v_stride + (size_t)kh * DH + c));
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
@@ -317,6 +310,7 @@ __global__ __launch_bounds__(kThreads) void store_kernel(StoreArgs a) {
       vt[i][c + u] = __builtin_bit_cast(uint16_t, x);
     }
   }
+  __syncthreads();
   if (tid < kStoreRows) {
     const int s = slot_s[tid], first = tid - (s & 7);
     int full = s >= 0 && first >= 0 && first + 8 <= kStoreRows;
@@ -338,6 +332,15 @@ __global__ __launch_bounds__(kThreads) void store_kernel(StoreArgs a) {
       stg(dst, __builtin_bit_cast(bf16, vt[i][c]));
     }
   }
+}
+
+template <int DH>
+__global__ __launch_bounds__(kThreads) void store_kernel(StoreArgs a, int turn_blocks, int head_blocks) {
+  const int x = blockIdx.x, turns = turn_blocks * head_blocks;
+  if (x < turns)
+    turn_rows<DH>(a, x % turn_blocks, x / turn_blocks * a.heads_per);
+  else
+    write_values<DH>(a, (x - turns) / a.Hkv, (x - turns) % a.Hkv);
 }
 
 // ---------------------------------------------------------------- rollback
@@ -385,33 +388,41 @@ __global__ __launch_bounds__(kThreads) void commit_kernel(CommitArgs a) {
     dst_s[tid] = dst;
   }
   __syncthreads();
-  const int kp = dh / 8, per = kp + dh;  // pieces of a (layer, K/V head): K's, V^T's
-  const long long e = (long long)blockIdx.x * kThreads + tid;
-  const long long lh = e / per;
-  if (lh >= (long long)a.L * a.Hkv) return;
-  const int c = (int)(e % per);
+  const int kp = dh / 8, per = kp + dh;  // pieces of a (layer, K/V head): V^T's, K's
   const size_t page = (size_t)a.Hkv * kPage * dh;  // elements of a page
-  const size_t at = (size_t)(lh / a.Hkv) * a.n_pages * page + (size_t)(lh % a.Hkv) * kPage * dh;
-  if (c < dh)
-    move_rows(a.v_pages + at + (size_t)c * kPage, page, 1, src_s, dst_s, len);
-  else
-    move_rows((bf16x8*)(a.k_pages + at) + (c - dh), page / 8, kp, src_s, dst_s, len);
+  const long long pieces = (long long)a.L * a.Hkv * per;
+  for (long long e = (long long)blockIdx.x * kThreads + tid; e < pieces; e += (long long)gridDim.x * kThreads) {
+    const long long lh = e / per;
+    const int c = (int)(e % per);
+    const size_t at = (size_t)(lh / a.Hkv) * a.n_pages * page + (size_t)(lh % a.Hkv) * kPage * dh;
+    if (c < dh)
+      move_rows(a.v_pages + at + (size_t)c * kPage, page, 1, src_s, dst_s, len);
+    else
+      move_rows((bf16x8*)(a.k_pages + at) + (c - dh), page / 8, kp, src_s, dst_s, len);
+  }
 }
 
 }  // namespace
 
-hipError_t launch_batch_store(const StoreArgs& a, hipStream_t st) {
-  const dim3 grid(cdiv(a.N, kStoreRows), a.H + a.Hkv);
+hipError_t launch_batch_store(const StoreArgs& args, hipStream_t st) {
+  StoreArgs a = args;
+  const int turn_blocks = cdiv(a.N, kThreads / (a.Dh / 16)), heads = a.H + a.Hkv;
+  // heads per workgroup: enough workgroups for the chip, up to eight heads on one table row
+  a.heads_per = (int)((long long)turn_blocks * heads / 1024);
+  a.heads_per = a.heads_per < 1 ? 1 : a.heads_per > 8 ? 8 : a.heads_per;
+  const int head_blocks = cdiv(heads, a.heads_per);
+  const dim3 grid(turn_blocks * head_blocks + cdiv(a.N, kStoreRows) * a.Hkv);
   if (a.Dh == 128)
-    store_kernel<128><<<grid, dim3(kThreads), 0, st>>>(a);
+    store_kernel<128><<<grid, dim3(kThreads), 0, st>>>(a, turn_blocks, head_blocks);
   else
-    store_kernel<64><<<grid, dim3(kThreads), 0, st>>>(a);
+    store_kernel<64><<<grid, dim3(kThreads), 0, st>>>(a, turn_blocks, head_blocks);
   return hipGetLastError();
 }
 
 hipError_t launch_batch_commit(const CommitArgs& a, hipStream_t st) {
   const long long pieces = (long long)a.L * a.Hkv * (a.Dh + a.Dh / 8);
-  commit_kernel<<<dim3((unsigned)((pieces + kThreads - 1) / kThreads), a.B), dim3(kThreads), 0, st>>>(a);
+  const int all = (int)((pieces + kThreads - 1) / kThreads);
+  commit_kernel<<<dim3(all, a.B), dim3(kThreads), 0, st>>>(a);
   return hipGetLastError();
 }
 

@@ -1,33 +1,33 @@
 // Scores of logits rows: log probabilities of given tokens, the entropy, the
 // normaliser and the most likely tokens.
 //
-// One pass over a row: every thread keeps the running maximum m of its values,
-// the sum S of exp(x - m) and T of exp(x - m) (x - m), rescaled when m grows;
-// joined over the workgroup, lse = m + log S and the entropy is log S - T / S.
-// The k largest values come out of the same pass.  The first tile of the row
-// gives a lower bound of the k-th largest value (the k-th largest of 256
-// groups' maxima: about as many values as k lie above it in the tile); every
-// value from the bound on joins a list in LDS, which is sorted at the end by
-// counting for each entry those before it.  A row whose later tiles hold more
-// than the list does (values in rising order, say) is read once more in steps
-// that cut the list back to its k best.
+// One pass over a row, the next tile's loads in flight while one is computed:
+// every thread keeps the running maximum m of its values, the sum S of exp(x - m)
+// and T of exp(x - m) (x - m), rescaled when m grows; joined over the workgroup,
+// lse = m + log S and the entropy is log S - T / S.  The k largest values come out
+// of the same pass.  The first tile gives a lower bound of the k-th largest value
+// (the k-th largest of 256 groups' maxima: about as many values as k lie above it
+// in the tile); every value from the bound on joins a list in LDS.  After 2, 4, 8
+// .. tiles the list's k-th best becomes the bound, so that a row adds about
+// k log(tiles) entries; at the end the list is sorted by counting for each entry
+// those before it.  A row whose later tiles hold more than the list does (values
+// in rising order, say) is read once more in steps that cut the list back to its
+// k best.
 #include "batch.h"
 
 namespace llmcad {
 
 namespace {
 
-constexpr int kScoreThreads = 1024;
-constexpr int kScoreWaves = kScoreThreads / kWave;
-constexpr int kPer = 16;                           // values per thread and tile
-constexpr int kTile = kPer * kScoreThreads;
+constexpr int kPieces = 4;  // 16-byte pieces of a row per thread and tile
 constexpr int kList = 2048;
+constexpr int kGroups = 256;
 constexpr float kLowest = -3.402823466e38f;        // (finite: x - m stays a number for rows of -inf)
 constexpr float kLog2e = 1.4426950408889634f;
 
 struct ScoreLds {
-  float m[kScoreWaves], s[kScoreWaves], t[kScoreWaves];
-  float group[256];
+  float m[16], s[16], t[16];  // by wave
+  __align__(16) float group[kGroups];
   float bound;
   int count;
   uint64_t list[kList];  // ordered value bits << 32 | ~token: larger is better, ties to the lower token
@@ -43,71 +43,113 @@ __device__ __forceinline__ float unordered(uint32_t u) {
   return __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u);
 }
 
-// Values [i0, i0 + N) of the row (i0 may be negative, i0 + N past V: -inf
-// there); 16-byte loads where all of them are the row's (row + i0 is then
-// 16-byte aligned).
-template <bool BF16>
-__device__ __forceinline__ void load16(const void* row, long i0, int V, float* x) {
-  constexpr int N = BF16 ? 8 : 4;
-  if (i0 >= 0 && i0 + N <= V) {
-    if (BF16) {
-      const bf16x8 v = ldg((const bf16x8*)((const bf16*)row + i0));
-#pragma unroll
-      for (int e = 0; e < N; ++e) x[e] = bf2f(v[e]);
-    } else {
-      const f32x4 v = ldg((const f32x4*)((const float*)row + i0));
-#pragma unroll
-      for (int e = 0; e < N; ++e) x[e] = v[e];
-    }
-    return;
-  }
-#pragma unroll
-  for (int e = 0; e < N; ++e) {
-    const long i = i0 + e;
-    x[e] = -INFINITY;
-    if (i >= 0 && i < V) x[e] = BF16 ? bf2f(ldg((const bf16*)row + i)) : ldg((const float*)row + i);
-  }
-}
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-template <bool BF16>
-__device__ __forceinline__ void load_tile(const void* row, long base, int V, float (&x)[kPer]) {
-  constexpr int N = BF16 ? 8 : 4;
+// A thread's part of the tile at base: pieces of 16 bytes, kPieces of them a
+// workgroup's width apart, as they lie in memory.  (row + base is 16-byte aligned;
+// what lies outside the row, before its first or behind its last value, reads as
+// -inf and is not touched.)
+template <bool BF16, int THREADS>
+struct Tile {
+  static constexpr int N = BF16 ? 8 : 4;             // values per piece
+  static constexpr int PER = N * kPieces;            // values per thread
+  static constexpr int SIZE = PER * THREADS;
+  u32x4 raw[kPieces];
+
+  __device__ static __forceinline__ long at(long base, int piece) { return base + (long)N * (piece * THREADS + (int)threadIdx.x); }
+  __device__ __forceinline__ void load(const char* row, long base, int V) {
+    constexpr int ES = 16 / N;
+    if (base >= 0 && base + SIZE <= V) {
 #pragma unroll
-  for (int v = 0; v < kPer / N; ++v)
-    load16<BF16>(row, base + (long)v * N * kScoreThreads + N * threadIdx.x, V, x + v * N);
-}
-// Token of value e of this thread's tile at base.
-template <bool BF16>
-__device__ __forceinline__ long tile_token(long base, int e) {
-  constexpr int N = BF16 ? 8 : 4;
-  return base + (long)(e / N) * N * kScoreThreads + N * threadIdx.x + e % N;
-}
+      for (int v = 0; v < kPieces; ++v) raw[v] = ldg((const u32x4*)(row + at(base, v) * ES));
+      return;
+    }
+#pragma unroll
+    for (int v = 0; v < kPieces; ++v) {
+      const long i0 = at(base, v);
+      const uint32_t none = BF16 ? 0xff80ff80u : 0xff800000u;
+      u32x4 x = {none, none, none, none};
+      if (i0 >= 0 && i0 + N <= V) {
+        x = ldg((const u32x4*)(row + i0 * ES));
+      } else if (i0 < V) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+          const long i = i0 + e;
+          if (i < 0 || i >= V) continue;
+          if (BF16) {
+            const uint32_t bits = ldg((const uint16_t*)row + i);
+            x[e / 2] = e & 1 ? (x[e / 2] & 0xffffu) | bits << 16 : (x[e / 2] & 0xffff0000u) | bits;
+          } else {
+            x[e & 3] = ldg((const uint32_t*)row + i);
+          }
+        }
+      }
+      raw[v] = x;
+    }
+  }
+  __device__ __forceinline__ float value(int e) const {  // value e of the thread's PER
+    const uint32_t w = raw[e / N][BF16 ? (e % N) / 2 : e % N];
+    return __uint_as_float(!BF16 ? w : e & 1 ? w & 0xffff0000u : w << 16);
+  }
+  __device__ static __forceinline__ long token(long base, int e) { return at(base, e / N) + e % N; }
+};
 
 template <bool BF16>
 __device__ __forceinline__ float value_at(const void* row, int i) {
   return BF16 ? bf2f(ldg((const bf16*)row + i)) : ldg((const float*)row + i);
 }
 
-// The list's k best, sorted, in L.keep (0: no entry).  All threads call it.
+// The list's k best, sorted, in L.keep (0: no entry).  All threads call it;
+// groups of neighbouring lanes count for one entry together.
+template <int THREADS>
 __device__ __forceinline__ void keep_best(ScoreLds& L, int count, int k) {
   if (threadIdx.x < k) L.keep[threadIdx.x] = 0;
   __syncthreads();
-  for (int i = threadIdx.x; i < count; i += kScoreThreads) {
-    const uint64_t mine = L.list[i];
+  int share = kWave;  // lanes per entry
+  while (share > 1 && count * share > THREADS) share >>= 1;
+  const int part = threadIdx.x & (share - 1);
+  for (int i0 = 0; i0 < count; i0 += THREADS / share) {
+    const int i = i0 + threadIdx.x / share;
+    const uint64_t mine = i < count ? L.list[i] : 0;
     int before = 0;
-    for (int j = 0; j < count; ++j) before += L.list[j] > mine ? 1 : 0;
-    if (before < k) L.keep[before] = mine;
+    if (i < count)
+      for (int j = part; j < count; j += share) before += L.list[j] > mine ? 1 : 0;
+    for (int off = share >> 1; off >= 1; off >>= 1) before += __shfl_xor(before, off, kWave);
+    if (i < count && part == 0 && before < k) L.keep[before] = mine;
+  }
+  __syncthreads();
+}
+
+// The list's k-th best value (L.bound), if it has k entries.  All threads call it.
+template <int THREADS>
+__device__ __forceinline__ void raise_bound(ScoreLds& L, int k) {
+  __syncthreads();
+  const int count = L.count;
+  __syncthreads();  // (nobody adds before all have read the count)
+  if (count >= k && count <= kList) {
+    int share = kWave;
+    while (share > 1 && count * share > THREADS) share >>= 1;
+    const int part = threadIdx.x & (share - 1);
+    for (int i0 = 0; i0 < count; i0 += THREADS / share) {
+      const int i = i0 + threadIdx.x / share;
+      const uint64_t mine = i < count ? L.list[i] : 0;
+      int before = 0;
+      if (i < count)
+        for (int j = part; j < count; j += share) before += L.list[j] > mine ? 1 : 0;
+      for (int off = share >> 1; off >= 1; off >>= 1) before += __shfl_xor(before, off, kWave);
+      if (i < count && part == 0 && before == k - 1) L.bound = unordered((uint32_t)(mine >> 32));
+    }
   }
   __syncthreads();
 }
 
 // The k best of a row whose list overflowed.
-template <bool BF16>
+template <bool BF16, int THREADS>
 __device__ __attribute__((noinline)) void best_in_steps(const void* row, int V, int k, ScoreLds& L) {
   uint64_t least = 0;  // the k-th best so far: later entries must be larger
   __syncthreads();
   if (threadIdx.x == 0) L.count = 0;
-  for (long i0 = 0; i0 < V; i0 += kScoreThreads) {
+  for (long i0 = 0; i0 < V; i0 += THREADS) {
     __syncthreads();
     const long i = i0 + threadIdx.x;
     if (i < V) {
@@ -117,19 +159,20 @@ __device__ __attribute__((noinline)) void best_in_steps(const void* row, int V, 
     }
     __syncthreads();
     const int count = L.count;
-    if (count > kList - kScoreThreads) {
-      keep_best(L, count, k);
+    if (count > kList - THREADS) {
+      keep_best<THREADS>(L, count, k);
       if (threadIdx.x < k) L.list[threadIdx.x] = L.keep[threadIdx.x];
       if (threadIdx.x == 0) L.count = k;
       least = L.keep[k - 1];
     }
   }
   __syncthreads();
-  keep_best(L, L.count, k);
+  keep_best<THREADS>(L, L.count, k);
 }
 
-template <bool BF16>
-__global__ __launch_bounds__(kScoreThreads) void scores_kernel(ScoresArgs a) {
+template <bool BF16, int THREADS>
+__global__ __launch_bounds__(THREADS) void scores_kernel(ScoresArgs a) {
+  typedef Tile<BF16, THREADS> T_;
   __shared__ ScoreLds L;
   const int r = blockIdx.x, tid = threadIdx.x, wave = tid >> 6, V = a.V, k = a.k;
   constexpr int ESIZE = BF16 ? 2 : 4;
@@ -141,15 +184,15 @@ __global__ __launch_bounds__(kScoreThreads) void scores_kernel(ScoresArgs a) {
     L.bound = -INFINITY;
   }
   float m = kLowest, S = 0.0f, T = 0.0f, bound = -INFINITY;
-  float x[kPer], nx[kPer];
-  load_tile<BF16>(row, -lead, V, nx);
-  for (long base = -lead; base < V; base += kTile) {
+  T_ tile, ahead;
+  ahead.load(row, -lead, V);
+  int done = 0;  // tiles
+  for (long base = -lead; base < V; base += T_::SIZE) {
+    tile = ahead;
+    if (base + T_::SIZE < V) ahead.load(row, base + T_::SIZE, V);
+    float top = tile.value(0);
 #pragma unroll
-    for (int e = 0; e < kPer; ++e) x[e] = nx[e];
-    if (base + kTile < V) load_tile<BF16>(row, base + kTile, V, nx);
-    float top = x[0];
-#pragma unroll
-    for (int e = 1; e < kPer; ++e) top = fmaxf(top, x[e]);
+    for (int e = 1; e < T_::PER; ++e) top = fmaxf(top, tile.value(e));
     const float grown = fmaxf(m, top);
     const float step = fmaxf(m - grown, -1e4f);  // (0 where the maximum stays)
     const float alpha = __builtin_amdgcn_exp2f(step * kLog2e);
@@ -157,38 +200,51 @@ __global__ __launch_bounds__(kScoreThreads) void scores_kernel(ScoresArgs a) {
     S = alpha * S;
     m = grown;
 #pragma unroll
-    for (int e = 0; e < kPer; ++e) {
-      const float d = x[e] - m;  // (NaN for NaN and +inf: S tells)
+    for (int e = 0; e < T_::PER; ++e) {
+      const float d = tile.value(e) - m;  // (NaN for NaN and +inf: S tells)
       const float p = __builtin_amdgcn_exp2f(d * kLog2e);
       S += p;
       T += p * fmaxf(d, -1e4f);  // (0 (-inf) is no number)
     }
     if (k > 0) {
-      if (base <= 0) {  // the first tile: the bound
-        float g = top;
-        g = fmaxf(g, __shfl_xor(g, 1, kWave));
-        g = fmaxf(g, __shfl_xor(g, 2, kWave));
-        if ((tid & 3) == 0) L.group[tid >> 2] = g;
-        __syncthreads();
-        if (tid < 256) {
-          const float mine = L.group[tid];
-          int before = 0;
-          for (int j = 0; j < 256; ++j) {
-            const float o = L.group[j];
-            before += o > mine || (o == mine && j < tid) ? 1 : 0;
-          }
-          if (before == k - 1) L.bound = mine;
-        }
-        __syncthreads();
-        bound = L.bound;
-      }
-      if (top >= bound && top > -INFINITY) {
+      if (done == 0) {  // the first tile: the bound
+        constexpr int PER_GROUP = THREADS / kGroups;
+        float gm = top;
 #pragma unroll
-        for (int e = 0; e < kPer; ++e)
-          if (x[e] >= bound && x[e] > -INFINITY) {
-            const int at = atomicAdd(&L.count, 1);
-            if (at < kList) L.list[at] = (uint64_t)ordered(x[e]) << 32 | (uint32_t)~(uint32_t)tile_token<BF16>(base, e);
-          }
+        for (int off = 1; off < PER_GROUP; off <<= 1) gm = fmaxf(gm, __shfl_xor(gm, off, kWave));
+        const int group = tid / PER_GROUP, part = tid % PER_GROUP;
+        if (part == 0) L.group[group] = gm;
+        __syncthreads();
+        int before = 0;  // the groups before this one, a share of them per lane
+#pragma unroll 4
+        for (int j = part * (kGroups / PER_GROUP); j < (part + 1) * (kGroups / PER_GROUP); j += 4) {
+          const f32x4 o = *(const f32x4*)&L.group[j];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) before += o[e] > gm || (o[e] == gm && j + e < group) ? 1 : 0;
+        }
+#pragma unroll
+        for (int off = 1; off < PER_GROUP; off <<= 1) before += __shfl_xor(before, off, kWave);
+        if (part == 0 && before == k - 1) L.bound = gm;
+        __syncthreads();
+        bound = fmaxf(L.bound, kLowest);  // (-inf is no alternative)
+      }
+      if (__any(top >= bound)) {
+#pragma unroll
+        for (int e = 0; e < T_::PER; ++e) {
+          const float x = tile.value(e);
+          const uint64_t hits = __ballot(x >= bound);
+          if (hits == 0) continue;
+          const int lane = tid & 63, first = __ffsll((unsigned long long)hits) - 1;
+          int at = 0;
+          if (lane == first) at = atomicAdd(&L.count, __popcll(hits));
+          at = __builtin_amdgcn_readlane(at, first) + __popcll(hits & ((1ull << lane) - 1));
+          if (x >= bound && at < kList) L.list[at] = (uint64_t)ordered(x) << 32 | (uint32_t)~(uint32_t)T_::token(base, e);
+        }
+      }
+      ++done;
+      if (done > 1 && (done & (done - 1)) == 0 && base + T_::SIZE < V) {
+        raise_bound<THREADS>(L, k);
+        bound = fmaxf(L.bound, kLowest);
       }
     }
   }
@@ -209,9 +265,9 @@ __global__ __launch_bounds__(kScoreThreads) void scores_kernel(ScoresArgs a) {
   }
   __syncthreads();
   m = kLowest;
-  for (int w = 0; w < kScoreWaves; ++w) m = fmaxf(m, L.m[w]);
+  for (int w = 0; w < (THREADS / kWave); ++w) m = fmaxf(m, L.m[w]);
   S = T = 0.0f;
-  for (int w = 0; w < kScoreWaves; ++w) {
+  for (int w = 0; w < (THREADS / kWave); ++w) {
     const float d = fmaxf(L.m[w] - m, -1e4f), e = __builtin_amdgcn_exp2f(d * kLog2e);
     T += e * (L.t[w] + L.s[w] * d);
     S += e * L.s[w];
@@ -234,7 +290,7 @@ __global__ __launch_bounds__(kScoreThreads) void scores_kernel(ScoresArgs a) {
   if (a.row_of == nullptr) {
     if (tid == 0 && r < a.m) score(r);
   } else {
-    for (int q = tid; q < a.m; q += kScoreThreads) {
+    for (int q = tid; q < a.m; q += THREADS) {
       const int of = ldg(a.row_of + q);
       if (of == r) score(q);
       else if (r == 0 && (of < 0 || of >= a.n)) stg(a.logprob + q, (float)NAN);
@@ -245,9 +301,9 @@ __global__ __launch_bounds__(kScoreThreads) void scores_kernel(ScoresArgs a) {
   if (bad) {
     if (tid < k) L.keep[tid] = 0;
   } else if (count <= kList) {
-    keep_best(L, count, k);
+    keep_best<THREADS>(L, count, k);
   } else {
-    best_in_steps<BF16>(row, V, k, L);
+    best_in_steps<BF16, THREADS>(row, V, k, L);
   }
   if (tid < k) {
     const uint64_t e = L.keep[tid];
@@ -259,10 +315,19 @@ __global__ __launch_bounds__(kScoreThreads) void scores_kernel(ScoresArgs a) {
 }  // namespace
 
 hipError_t launch_token_scores(const ScoresArgs& a, hipStream_t st) {
-  if (a.bf16_in)
-    scores_kernel<true><<<dim3(a.n), dim3(kScoreThreads), 0, st>>>(a);
-  else
-    scores_kernel<false><<<dim3(a.n), dim3(kScoreThreads), 0, st>>>(a);
+  // Up to a row per CU: 16 waves on each row; more rows: 8 waves, so that a CU
+  // reads one row while it closes another.
+  if (a.n <= 256) {
+    if (a.bf16_in)
+      scores_kernel<true, 1024><<<dim3(a.n), dim3(1024), 0, st>>>(a);
+    else
+      scores_kernel<false, 1024><<<dim3(a.n), dim3(1024), 0, st>>>(a);
+  } else {
+    if (a.bf16_in)
+      scores_kernel<true, 512><<<dim3(a.n), dim3(512), 0, st>>>(a);
+    else
+      scores_kernel<false, 512><<<dim3(a.n), dim3(512), 0, st>>>(a);
+  }
   return hipGetLastError();
 }
 
