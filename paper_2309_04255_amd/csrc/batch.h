@@ -35,8 +35,16 @@ struct BatchRequest {
   int pad[3];
 };
 
+// A run of a request's pages, with all that a workgroup needs to begin on it.
+struct BatchUnit {
+  int request, run;
+  int row0, n, held, part0;  // the request's
+  int chunk;                 // pages per run
+  int pad;
+};
+
 // Head of a plan (int32 words).
-enum PlanWord { PLAN_UNITS = 0, PLAN_CHUNK = 1, PLAN_TAKEN = 2, PLAN_WORDS = 64 };
+enum PlanWord { PLAN_UNITS = 0, PLAN_TAKEN = 1, PLAN_WORDS = 64 };
 
 inline int plan_max_units(int B) { return B + kSplitRuns; }
 inline size_t plan_part_rows(int n_rows) { return (size_t)n_rows + (n_rows > kSplitRows ? n_rows : kSplitRows); }
@@ -53,7 +61,7 @@ struct PlanLayout {
     head = take(PLAN_WORDS * 4);
     status = take((size_t)B * 4);
     req = take((size_t)B * sizeof(BatchRequest));
-    units = take((size_t)plan_max_units(B) * 4);  // request << 16 | run
+    units = take((size_t)plan_max_units(B) * sizeof(BatchUnit));
     slot = take((size_t)N * 4);
     position = take((size_t)N * 4);
     row_req = take((size_t)N * 4);  // the row's request, -1: none
@@ -74,7 +82,7 @@ struct PlanArgs {
   int* head;
   int* status;
   BatchRequest* req;
-  int* units;
+  BatchUnit* units;
   int* slot;
   int* position;
   int* row_req;
@@ -122,7 +130,7 @@ struct AttnArgs {
   int max_pages;
   const int* head;
   const BatchRequest* req;
-  const int* units;
+  const BatchUnit* units;
   const int* row_req;
   const uint32_t* mask;
   bf16* out;       // [N][H][Dh]

@@ -231,12 +231,22 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(PlanArgs a) {
     stg(a.status + b, st);
     if (b == 0) {
       stg(a.head + PLAN_UNITS, (int)(invalid ? 0 : w[1]));
-      stg(a.head + PLAN_CHUNK, (int)(chunk < (1 << 30) ? chunk : (1 << 30)));
       stg(a.head + PLAN_TAKEN, (int)(invalid ? 0 : taken));
     }
   }
   if (!invalid)
-    for (int s = tid; s < ns; s += kThreads) stg(a.units + w[0] + s, b << 16 | s);
+    for (int s = tid; s < ns; s += kThreads) {
+      BatchUnit u;
+      u.request = b;
+      u.run = s;
+      u.row0 = row0;
+      u.n = placed ? nb : 0;
+      u.held = hb;
+      u.part0 = (int)w[2];
+      u.chunk = (int)chunk;
+      u.pad = 0;
+      stg(a.units + w[0] + s, u);
+    }
 }
 
 }  // namespace
@@ -254,8 +264,8 @@ namespace {
 // cosines and sines of kTurnRows rows (a lane those of 8 dims and their partners
 // in the second half, rotate-half pairing) and go through `a.heads_per` heads.
 // The others write values: a V row becomes a column of its page, so 64 rows of a
-// head meet in LDS, and eight rows whose slots are one aligned piece of eight
-// leave as 16 bytes; the others (a piece's ends, single tokens) as single entries.
+// head meet in LDS, and rows whose slots lie in one aligned piece of eight leave
+// together, 16 bytes per dim if there are eight of them.
 constexpr int kStoreRows = 64;
 
 __device__ __forceinline__ int slot_of(const StoreArgs& a, int row) {
@@ -294,12 +304,14 @@ __device__ __forceinline__ void turn_rows(const StoreArgs& a, int block, int hea
 
 template <int DH>
 __device__ __forceinline__ void write_values(const StoreArgs& a, int block, int kh) {
-  __shared__ int slot_s[kStoreRows];
-  __shared__ int full_s[kStoreRows];
-  __shared__ uint16_t vt[kStoreRows][DH + 2];
+  // (up to seven rows behind the block's own finish its last piece)
+  __shared__ int slot_s[kStoreRows + 8];  // from the row before the block on
+  __shared__ int piece_s[kStoreRows];     // pieces that begin in the block: first row | rows << 8
+  __shared__ int pieces;
+  __shared__ uint16_t vt[kStoreRows + 7][DH + 2];
   const int r0 = block * kStoreRows, tid = threadIdx.x;
-  const int rows = a.N - r0 < kStoreRows ? a.N - r0 : kStoreRows;
-  if (tid < kStoreRows) slot_s[tid] = slot_of(a, r0 + tid);
+  const int rows = a.N - r0 < kStoreRows + 7 ? a.N - r0 : kStoreRows + 7;
+  if (tid < kStoreRows + 8) slot_s[tid] = r0 + tid > 0 ? slot_of(a, r0 + tid - 1) : -1;
 #pragma unroll 4
   for (int e = tid; e < rows * (DH / 8); e += kThreads) {
     const int i = e / (DH / 8), c = 8 * (e % (DH / 8));
@@ -311,25 +323,40 @@ __device__ __forceinline__ void write_values(const StoreArgs& a, int block, int 
     }
   }
   __syncthreads();
-  if (tid < kStoreRows) {
-    const int s = slot_s[tid], first = tid - (s & 7);
-    int full = s >= 0 && first >= 0 && first + 8 <= kStoreRows;
-    for (int u = 0; u < 8 && full; ++u) full = slot_s[first + u] == (s & ~7) + u;
-    full_s[tid] = full;
+  if (tid < kStoreRows) {  // (one wave)
+    const int s = slot_s[tid + 1];
+    const bool begins = s >= 0 && ((s & 7) == 0 || slot_s[tid] != s - 1);
+    int n = 1;
+    while (n < 8 && (s & 7) + n < 8 && slot_s[tid + 1 + n] == s + n) ++n;
+    const uint64_t all = __ballot(begins);
+    if (begins) piece_s[__popcll(all & ((1ull << tid) - 1))] = tid | n << 8;
+    if (tid == 0) pieces = __popcll(all);
   }
   __syncthreads();
-  for (int e = tid; e < rows * DH; e += kThreads) {
-    const int i = e / DH, c = e % DH, s = slot_s[i];
-    if (s < 0) continue;
-    bf16* dst = a.v_pages + (((size_t)(s / kPage) * a.Hkv + kh) * DH + c) * kPage + s % kPage;
-    if (full_s[i]) {
-      if (s & 7) continue;
+  for (int e = tid; e < pieces * DH; e += kThreads) {
+    const int p = piece_s[e / DH], c = e % DH, i = p & 0xff, n = p >> 8, s = slot_s[i + 1];
+    uint16_t* dst = (uint16_t*)a.v_pages + (((size_t)(s / kPage) * a.Hkv + kh) * DH + c) * kPage + s % kPage;
+    if (n == 8) {
       bf16x8 v;
 #pragma unroll
       for (int u = 0; u < 8; ++u) v[u] = __builtin_bit_cast(bf16, vt[i + u][c]);
       stg((bf16x8*)dst, v);
-    } else {
-      stg(dst, __builtin_bit_cast(bf16, vt[i][c]));
+      continue;
+    }
+    // (part of a piece: its entries in the largest aligned groups)
+    for (int u = 0; u < n;) {
+      const int at = (s & 7) + u;
+      if ((at & 3) == 0 && u + 4 <= n) {
+        stg((uint2*)(dst + u), make_uint2((uint32_t)vt[i + u][c] | (uint32_t)vt[i + u + 1][c] << 16,
+                                          (uint32_t)vt[i + u + 2][c] | (uint32_t)vt[i + u + 3][c] << 16));
+        u += 4;
+      } else if ((at & 1) == 0 && u + 2 <= n) {
+        stg((uint32_t*)(dst + u), (uint32_t)vt[i + u][c] | (uint32_t)vt[i + u + 1][c] << 16);
+        u += 2;
+      } else {
+        stg(dst + u, vt[i + u][c]);
+        u += 1;
+      }
     }
   }
 }

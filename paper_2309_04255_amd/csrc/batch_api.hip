@@ -98,7 +98,7 @@ int llmcad_batch_plan(const llmcad_config* cfg, int32_t n_requests, int32_t n_ro
   a.head = (int*)(at + P.head);
   a.status = (int*)(at + P.status);
   a.req = (BatchRequest*)(at + P.req);
-  a.units = (int*)(at + P.units);
+  a.units = (BatchUnit*)(at + P.units);
   a.slot = (int*)(at + P.slot);
   a.position = (int*)(at + P.position);
   a.row_req = (int*)(at + P.row_req);
@@ -193,7 +193,7 @@ int llmcad_batch_attention(const llmcad_config* cfg, int32_t n_kv_heads, int32_t
   a.max_pages = max_pages;
   a.head = (const int*)(at + P.head);
   a.req = (const BatchRequest*)(at + P.req);
-  a.units = (const int*)(at + P.units);
+  a.units = (const BatchUnit*)(at + P.units);
   a.row_req = (const int*)(at + P.row_req);
   a.mask = (const uint32_t*)(at + P.mask);
   a.out = (bf16*)out;

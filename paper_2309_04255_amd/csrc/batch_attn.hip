@@ -20,10 +20,18 @@ namespace llmcad {
 
 namespace {
 
+#define LB_P 2
+#define LB_G 2
+#define LB_N 2
+#define RB_P 2
+#define RB_G 1
 constexpr int kThreads = 256;
 constexpr int kWaves = 4;
 constexpr int kTileKeys = kPage;  // keys of a tile: two 32-key steps, one page
 constexpr float kSlack = 8.0f;
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
 
 __device__ __forceinline__ int up_div(int x, int a) { return (x + a - 1) / a; }
 
@@ -62,7 +70,8 @@ __device__ __forceinline__ TileAt page_tile(const AttnArgs& a, const Unit& u, in
   const size_t at = ((size_t)(there ? id : 0) * a.Hkv + u.kh) * kPage * a.Dh;
   return {a.kp + at, a.vp + at, kPage, there};
 }
-// Page ids of a run, 64 at a time in the lanes of a wave.
+// Page ids of a run, 64 at a time in the lanes of a wave (and still those of the
+// last few pages when the next 64 come).
 struct PageIds {
   int ids, base;
   __device__ void start(const Unit& u, int t) {
@@ -71,7 +80,7 @@ struct PageIds {
     ids = at < u.last ? ldg(u.table + at) : -1;
   }
   __device__ int get(const Unit& u, int t) {
-    if (t - base >= kWave) start(u, t);
+    if (t - base >= kWave) start(u, t - 8);
     return __builtin_amdgcn_readlane(ids, t - base);
   }
 };
@@ -82,63 +91,93 @@ __device__ __forceinline__ void dma16(const void* src, char* lds) {
   __builtin_amdgcn_global_load_lds((const LLMCAD_GLOBAL void*)src, (__attribute__((address_space(3))) void*)lds, 16, 0, 0);
 }
 
-// Which of the 8 keys from `key` on a row sees, by its mask (keys before held
-// are tokens all rows of the request see).
+// Which of the 8 keys from `key` on a row sees, by its mask: all before held,
+// those that the mask names from there on, none from lim on.
 __device__ __forceinline__ uint32_t seen8(const uint32_t (&anc)[4], int key, int held, int lim) {
-  uint32_t vis = 0;
+  const int off = key - held;  // (keys of the request's rows: bits off .. off + 7 of the mask)
+  const int at = off < 0 ? 0 : off;
+  const uint32_t lo = at < 32 ? anc[0] : at < 64 ? anc[1] : at < 96 ? anc[2] : anc[3];
+  const uint32_t hi = at < 32 ? anc[1] : at < 64 ? anc[2] : at < 96 ? anc[3] : 0u;
+  uint32_t vis = at < LLMCAD_MAX_NODES ? (uint32_t)((((uint64_t)hi << 32) | lo) >> (at & 31)) : 0u;
+  const int before = -off < 0 ? 0 : -off > 8 ? 8 : -off;  // (held tokens among the eight)
+  vis = vis << before | ((1u << before) - 1u);
+  const int there = lim - key < 0 ? 0 : lim - key > 8 ? 8 : lim - key;
+  return vis & ((1u << there) - 1u);
+}
+// The 8 values of a fragment whose keys are there (bits of `there`; the others
+// count as zeros: what lies in them may be NaN): masks for its four words.
+__device__ __forceinline__ u32x4 kept_words(uint32_t there) {
+  u32x4 w;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const int t = key + e - held;
-    const uint32_t w = t < 32 ? anc[0] : t < 64 ? anc[1] : t < 96 ? anc[2] : anc[3];
-    const bool sees = key + e < lim && (t < 0 || (t < LLMCAD_MAX_NODES && ((w >> (t & 31)) & 1u)));
-    vis |= sees ? 1u << e : 0u;
-  }
-  return vis;
+  for (int i = 0; i < 4; ++i) w[i] = ((there >> (2 * i)) & 1u ? 0xffffu : 0u) | ((there >> (2 * i + 1)) & 1u ? 0xffff0000u : 0u);
+  return w;
+}
+__device__ __forceinline__ bf16x8 keep(bf16x8 v, u32x4 words) {
+  return __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, v) & words);
 }
 
 // Keys that some rows see and others do not: an Inf or NaN among their values
 // would reach the others as 0 x Inf.  Such values are left out of the product
 // O^T += V^T P^T, and a product of their indicators with the rows' sight tells
-// which outputs they belong to.
-typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
-__device__ __forceinline__ bool nonfinite(const bf16x8& v) {
-  const u16x8 x = __builtin_bit_cast(u16x8, v) & (uint16_t)0x7f80;
+// which outputs they belong to; those get them at the end.
+// The largest magnitudes of the values seen so far, two by two.
+__device__ __forceinline__ void largest(u16x8& most, const bf16x8& v) {
+  most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x8, v) & (uint16_t)0x7fff);
+}
+__device__ __forceinline__ bool nonfinite(const u16x8& most) {
   bool any = false;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) any |= x[e] == 0x7f80;
+  for (int e = 0; e < 8; ++e) any |= most[e] >= 0x7f80;
   return any;
 }
-// v without its Inf and NaN; o with what they give the rows that see them.
-__device__ __forceinline__ f32x4 take_nonfinite(bf16x8& v, uint32_t vis, f32x4 o) {
-  constexpr uint16_t one = 0x3f80;  // (bf16 1)
-  const u16x8 x = __builtin_bit_cast(u16x8, v);
-  u16x8 up, down, sees, kept;
+// What the Inf and NaN of a fragment give the outputs of the rows that see them:
+// bit 4 db + i of up (+Inf), of down (-Inf); both: NaN.
+struct Strays {
+  uint32_t up = 0, down = 0;
+  __device__ __forceinline__ void note(const bf16x8& v, uint32_t vis, int db) {
+    constexpr uint16_t one = 0x3f80;  // (bf16 1)
+    const u16x8 x = __builtin_bit_cast(u16x8, v);
+    u16x8 ups, downs, sees;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const bool bad = (x[e] & 0x7f80) == 0x7f80, nan = bad && (x[e] & 0x7f);
-    up[e] = bad && (nan || !(x[e] & 0x8000)) ? one : (uint16_t)0;
-    down[e] = bad && (nan || (x[e] & 0x8000)) ? one : (uint16_t)0;
-    sees[e] = (vis >> e) & 1u ? one : (uint16_t)0;
-    kept[e] = bad ? (uint16_t)0 : x[e];
-  }
-  v = __builtin_bit_cast(bf16x8, kept);
-  const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-  const bf16x8 s = __builtin_bit_cast(bf16x8, sees);
-  const f32x4 ups = mfma16x16x32(__builtin_bit_cast(bf16x8, up), s, zero);
-  const f32x4 downs = mfma16x16x32(__builtin_bit_cast(bf16x8, down), s, zero);
+    for (int e = 0; e < 8; ++e) {
+      const bool bad = (x[e] & 0x7f80) == 0x7f80, nan = bad && (x[e] & 0x7f);
+      ups[e] = bad && (nan || !(x[e] & 0x8000)) ? one : (uint16_t)0;
+      downs[e] = bad && (nan || (x[e] & 0x8000)) ? one : (uint16_t)0;
+      sees[e] = (vis >> e) & 1u ? one : (uint16_t)0;
+    }
+    const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+    const bf16x8 s = __builtin_bit_cast(bf16x8, sees);
+    const f32x4 a = mfma16x16x32(__builtin_bit_cast(bf16x8, ups), s, zero);
+    const f32x4 b = mfma16x16x32(__builtin_bit_cast(bf16x8, downs), s, zero);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if (ups[i] > 0.0f) o[i] += INFINITY;
-    if (downs[i] > 0.0f) o[i] -= INFINITY;
+    for (int i = 0; i < 4; ++i) {
+      up |= a[i] > 0.0f ? 1u << (4 * db + i) : 0u;
+      down |= b[i] > 0.0f ? 1u << (4 * db + i) : 0u;
+    }
   }
-  return o;
+  template <int NB>
+  __device__ __forceinline__ void give(f32x4 (&o)[NB]) const {
+    if (!__any((up | down) != 0u)) return;
+#pragma unroll
+    for (int db = 0; db < NB; ++db)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if ((up >> (4 * db + i)) & 1u) o[db][i] += INFINITY;
+        if ((down >> (4 * db + i)) & 1u) o[db][i] -= INFINITY;
+      }
+  }
+};
+__device__ __forceinline__ bf16x8 finite(const bf16x8& v) {
+  u16x8 x = __builtin_bit_cast(u16x8, v);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] = (x[e] & 0x7f80) == 0x7f80 ? (uint16_t)0 : x[e];
+  return __builtin_bit_cast(bf16x8, x);
 }
 
 // ---------------------------------------------------------------- many rows
 //
 // 64 RB pairs per workgroup, 16 RB per wave.  Tiles of 64 keys are shared
-// through LDS in fragment order (every access is 16 bytes per lane, lane by
-// lane), keys and values in two buffers each.  A turn of the loop takes the
+// through LDS, keys and values in two buffers each.  A turn of the loop takes the
 // values of tile t and the keys of tile t + 1: the scores of the next tile and
 // the exponentials of this one need different units, and their instructions
 // alternate.  Meanwhile the values of t + 1 and the keys of t + 2 are on their
@@ -153,10 +192,12 @@ __device__ __forceinline__ f32x4 take_nonfinite(bf16x8& v, uint32_t vis, f32x4 o
 template <int DH, int RB, bool PAGED>
 struct TileWork {
   static constexpr int NS = Frags<DH>::NS, NB = Frags<DH>::NB;
-  static constexpr int PER = 2 * NS;              // fragments a wave fetches per tile: K of a step, or V^T of a step
-  static constexpr int HALF = 2 * PER * 1024;     // a tile's keys, or its values
-  static_assert(2 * NS == NB, "as many key as value fragments");
-  typedef f32x4 Scores[RB][4];  // [row block][step, key block]
+  static constexpr int STEPS = kTileKeys / 32;
+  static constexpr int HALF = kTileKeys * DH * 2;  // bytes of a tile's keys, or of its values
+  static constexpr int FLAG = 4 * HALF;            // (a flag behind the buffers)
+  static constexpr int LDS = FLAG + 16;
+  static constexpr int PER = HALF / 2048;          // KiB that a wave fetches: half of the keys, or of the values
+  typedef f32x4 Scores[RB][2 * STEPS];             // [row block][step, key block]
 
   const AttnArgs& a;
   const Unit& u;
@@ -165,10 +206,10 @@ struct TileWork {
   bf16x8 qf[RB][NS];
   float m[RB], neg_m[RB], l[RB];
   f32x4 o[RB][NB];
-  uint32_t vis[RB][2];
-  bool masked, there;
+  Strays strays[RB];
+  bool there;
   PageIds pages;
-  uint32_t lane_k, lane_v;  // byte offsets of the lane's part of a tile's fragments
+  uint32_t lane_at[4];  // byte offset of the lane's part of a fetched KiB, by the KiB's index
 
   __device__ __forceinline__ TileWork(const AttnArgs& a_, const Unit& u_, char* lds_) : a(a_), u(u_), lds(lds_) {
     lane = threadIdx.x & 63;
@@ -179,47 +220,114 @@ struct TileWork {
   }
   __device__ __forceinline__ int pair_of(int rb) const { return u.pair0 + (wave * RB + rb) * 16 + li; }
   __device__ __forceinline__ int clamped(int rb) const { return pair_of(rb) < u.pairs ? pair_of(rb) : u.pairs - 1; }
-  // waves 0 and 2 fetch the keys of a tile's two steps, 1 and 3 the values
-  __device__ __forceinline__ bool values() const { return (wave & 1) != 0; }
-  __device__ __forceinline__ int key_of() const { return 32 * (wave >> 1); }
 
+  // LDS holds a tile's keys as [step][key block][16 rows][DH] and its values as
+  // [DH][64 keys], so that a KiB copied to it is whole rows: 64 lanes read 4 to 8
+  // rows of 128 or 256 contiguous bytes.  (In fragment order each lane's 16 bytes
+  // are another row than its neighbours', and the vector cache takes them one by
+  // one: 67 accesses per KiB instead of 19.)  The 16-byte pieces of a row are swapped by its
+  // index, so that the pieces of 16 rows that a fragment reads together lie in
+  // different banks (a read takes 256 bytes of LDS at a time).
+  static constexpr int ROW = DH * 2;            // bytes of a row of keys
+  static constexpr int ROWS = 1024 / ROW;       // of them in a KiB
+  __device__ static __forceinline__ int swap(int row_bytes, int row) { return row_bytes == 256 ? row & 15 : (row >> 1) & 7; }
+  __device__ __forceinline__ const char* key_at(int t, int sb, int s) const {
+    return lds + (t & 1) * HALF + sb * 16 * ROW + li * ROW + (((4 * s + g) ^ swap(ROW, li)) * 16);
+  }
+  __device__ __forceinline__ char* value_at(int t, int st, int db) const {
+    return lds + (2 + (t & 1)) * HALF + (16 * db + li) * 128 + (((4 * st + g) ^ swap(128, li)) * 16);
+  }
+  // waves 0 and 1 fetch a step's keys each, 2 and 3 half of the values' dims each
+  __device__ __forceinline__ bool values() const { return wave >= 2; }
+  __device__ __forceinline__ void place_lanes() {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (values()) {
+        const int dim = 8 * i + (lane >> 3), piece = lane & 7;
+        lane_at[i] = ((uint32_t)(lane >> 3) * (PAGED ? kPage : a.cap) + 8 * (piece ^ swap(128, dim))) * 2;
+      } else {
+        const int row = lane / (ROW / 16), piece = lane % (ROW / 16);
+        lane_at[i] = (8 * (row >> 2) + (row & 3)) * ROW + (piece ^ swap(ROW, i % NS * ROWS + row)) * 16;
+      }
+  }
   // copies this wave's part of tile t straight to LDS
   __device__ __forceinline__ void fetch(int t) {
     const TileAt at = PAGED ? page_tile(a, u, pages.get(u, t)) : prefix_tile(a, u, t);
-    char* to = lds + ((values() ? 2 : 0) + (t & 1)) * HALF + (wave >> 1) * PER * 1024;
+    const int part = wave & 1;
     if (values()) {
+      char* to = lds + (2 + (t & 1)) * HALF + part * PER * 1024;
+      const bf16* v = at.v + (size_t)(8 * PER * part) * at.vs;
 #pragma unroll
-      for (int e = 0; e < PER; ++e) dma16((const char*)(at.v + (size_t)e * 16 * at.vs) + lane_v, to + e * 1024);
+      for (int e = 0; e < PER; ++e) dma16((const char*)(v + (size_t)(8 * e) * at.vs) + lane_at[e & 3], to + e * 1024);
     } else {
+      char* to = lds + (t & 1) * HALF + part * PER * 1024;
+      const char* k = (const char*)(at.k + 32 * part * DH);
 #pragma unroll
-      for (int e = 0; e < PER; ++e) dma16((const char*)(at.k + (e / NS) * 4 * DH + (e % NS) * 32) + lane_k, to + e * 1024);
+      for (int e = 0; e < PER; ++e) {  // key block e / NS, rows ROWS (e % NS) .. of it: keys 2 ROWS (e % NS) + 4 (e / NS) ..
+        const int i = e % NS;
+        dma16(k + (2 * ROWS * i + 4 * (e / NS)) * ROW + lane_at[i], to + e * 1024);
+      }
     }
   }
 
   // scores of tile t (its keys in LDS)
   __device__ __forceinline__ void scores(Scores& sc, int t) {
-    const char* at = lds + (t & 1) * HALF + lane * 16;
 #pragma unroll
-    for (int sb = 0; sb < 4; ++sb) {
+    for (int sb = 0; sb < 2 * STEPS; ++sb) {
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) sc[rb][sb] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int s = 0; s < NS; ++s) {
-        const bf16x8 k = lds_ld<bf16x8>(at + (sb * NS + s) * 1024);
+        const bf16x8 k = lds_ld<bf16x8>(key_at(t, sb, s));
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) sc[rb][sb] = mfma16x16x32(k, qf[rb][s], sc[rb][sb]);
       }
     }
   }
-  // the mask of tile t, and a new reference point where its scores need one
+  // Clears, where they lie, tile t's values of keys that are not there, and takes
+  // out the Inf and NaN of those that some rows see and others do not.  A wave does
+  // a quarter; all waves of the workgroup come here for the same tiles.
+  __device__ __forceinline__ void clean(int t, const uint32_t (&vis)[RB][STEPS]) {
+    int* flag = (int*)(lds + FLAG);
+    u16x8 most = (uint16_t)0;
+#pragma unroll 1
+    for (int f = wave; f < STEPS * NB; f += kWaves) {
+      char* at = value_at(t, f / NB, f % NB);
+      const int left = u.lim - (t * kTileKeys + 32 * (f / NB) + 8 * g);
+      const bf16x8 v = keep(lds_ld<bf16x8>(at), kept_words(!there || left <= 0 ? 0u : left >= 8 ? 0xffu : (1u << left) - 1u));
+      if (PAGED) largest(most, v);
+      lds_st<bf16x8>(at, v);
+    }
+    if (PAGED && __any(nonfinite(most)) && lane == 0) *flag = 1;
+    __syncthreads();
+    if (PAGED && *flag != 0) {
+#pragma unroll
+      for (int st = 0; st < STEPS; ++st)
+#pragma unroll 1
+        for (int db = 0; db < NB; ++db) {
+          const bf16x8 v = lds_ld<bf16x8>(value_at(t, st, db));
+#pragma unroll
+          for (int rb = 0; rb < RB; ++rb) strays[rb].note(v, vis[rb][st], db);
+        }
+      __syncthreads();
+      if (threadIdx.x == 0) *flag = 0;
+#pragma unroll 1
+      for (int f = wave; f < STEPS * NB; f += kWaves) {
+        char* at = value_at(t, f / NB, f % NB);
+        lds_st<bf16x8>(at, finite(lds_ld<bf16x8>(at)));
+      }
+      __syncthreads();
+    }
+  }
+  // The mask of tile t, and a new reference point where its scores need one.
   __device__ __forceinline__ void look(Scores& sc, int t) {
     there = true;
     if (PAGED) {
       const int id = pages.get(u, t);
       there = id >= 0 && id < a.n_pages;
     }
-    masked = (t + 1) * kTileKeys > u.held || !there;  // (not every row sees every key)
-    if (masked) {
+    if ((t + 1) * kTileKeys > u.held || !there) {  // (not every row sees every key)
+      uint32_t vis[RB][STEPS];
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) {
         uint32_t anc[4] = {0, 0, 0, 0};
@@ -229,13 +337,14 @@ struct TileWork {
           for (int j = 0; j < 4; ++j) anc[j] = ldg(a.mask + row * 4 + j);
         }
 #pragma unroll
-        for (int st = 0; st < 2; ++st) {
+        for (int st = 0; st < STEPS; ++st) {
           vis[rb][st] = there ? seen8(anc, t * kTileKeys + 32 * st + 8 * g, u.held, u.lim) : 0u;
 #pragma unroll
           for (int e = 0; e < 8; ++e)
             if (!((vis[rb][st] >> e) & 1u)) sc[rb][2 * st + (e >> 2)][e & 3] = -INFINITY;
         }
       }
+      clean(t, vis);
     }
     float mx[RB];
     bool grow = false;
@@ -243,7 +352,7 @@ struct TileWork {
     for (int rb = 0; rb < RB; ++rb) {
       mx[rb] = sc[rb][0][0];
 #pragma unroll
-      for (int e = 1; e < 16; ++e) mx[rb] = fmaxf(mx[rb], sc[rb][e >> 2][e & 3]);
+      for (int e = 1; e < 8 * STEPS; ++e) mx[rb] = fmaxf(mx[rb], sc[rb][e >> 2][e & 3]);
       mx[rb] *= a.scale_log2;
       grow |= mx[rb] > m[rb] + kSlack;
     }
@@ -261,41 +370,15 @@ struct TileWork {
       }
     }
   }
-  __device__ __forceinline__ bf16x8 value(int t, int st, int db) const {
-    return lds_ld<bf16x8>(lds + (2 + (t & 1)) * HALF + (st * NB + db) * 1024 + lane * 16);
-  }
-  // Values of keys that are not there count as zeros (what lies there may be NaN).
-  __device__ __forceinline__ void clear_absent(int t) {
-#pragma unroll 1
-    for (int st = 0; st < 2; ++st) {
-      const int valid = there ? u.lim - (t * kTileKeys + 32 * st + 8 * g) : 0;
-      if (__any(valid < 8)) {
-        char* at = lds + (2 + (t & 1)) * HALF + st * NB * 1024 + lane * 16;
-#pragma unroll 1
-        for (int db = wave; db < NB; db += kWaves) {
-          bf16x8 v = lds_ld<bf16x8>(at + db * 1024);
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (e >= valid) v[e] = (bf16)0.0f;
-          lds_st<bf16x8>(at + db * 1024, v);
-        }
-      }
-    }
-    __syncthreads();
-  }
   // Tile t's probabilities and its part of the output; the next tile's scores.
   __device__ __forceinline__ void turn(Scores& sc, Scores& next, int t) {
     const bool more = t + 1 < u.last;
-    if (values() ? more : t + 2 < u.last) fetch(values() ? t + 1 : t + 2);
-    bool bad = false;
-    if (PAGED && masked) {
-#pragma unroll
-      for (int e = 0; e < 2 * NB; ++e) bad |= nonfinite(value(t, e / NB, e % NB));
-    }
+    const int coming = values() ? t + 1 : t + 2;
+    if (coming < u.last) fetch(coming);
     scores(next, t + 1);  // (past the last tile: of what lies there, not used)
-    bf16x8 p[RB][2];
+    bf16x8 p[RB][STEPS];
 #pragma unroll
-    for (int st = 0; st < 2; ++st)
+    for (int st = 0; st < STEPS; ++st)
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
@@ -304,39 +387,21 @@ struct TileWork {
           l[rb] += v;
           p[rb][st][e] = f2bf(v);
         }
-    if (PAGED && __any(bad)) {
 #pragma unroll
-      for (int st = 0; st < 2; ++st)
+    for (int st = 0; st < STEPS; ++st)
 #pragma unroll
-        for (int db = 0; db < NB; ++db) {
-          const bf16x8 v = value(t, st, db);
+      for (int db = 0; db < NB; ++db) {
+        const bf16x8 v = lds_ld<bf16x8>(value_at(t, st, db));
 #pragma unroll
-          for (int rb = 0; rb < RB; ++rb) {
-            bf16x8 kept = v;
-            o[rb][db] = take_nonfinite(kept, vis[rb][st], o[rb][db]);
-            o[rb][db] = mfma16x16x32(kept, p[rb][st], o[rb][db]);
-          }
-          __builtin_amdgcn_sched_barrier(0);  // (one block's values at a time: the registers)
-        }
-    } else {
-#pragma unroll
-      for (int st = 0; st < 2; ++st)
-#pragma unroll
-        for (int db = 0; db < NB; ++db) {
-          const bf16x8 v = value(t, st, db);
-#pragma unroll
-          for (int rb = 0; rb < RB; ++rb) o[rb][db] = mfma16x16x32(v, p[rb][st], o[rb][db]);
-        }
-    }
+        for (int rb = 0; rb < RB; ++rb) o[rb][db] = mfma16x16x32(v, p[rb][st], o[rb][db]);
+      }
     __syncthreads();
-    if (more) {
-      look(next, t + 1);
-      if (masked && ((t + 2) * kTileKeys > u.lim || !there)) clear_absent(t + 1);
-    }
+    if (more) look(next, t + 1);
   }
 
   __device__ __forceinline__ void run() {
     if (PAGED) pages.start(u, u.first);
+    place_lanes();
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
       m[rb] = -INFINITY;
@@ -345,9 +410,8 @@ struct TileWork {
 #pragma unroll
       for (int db = 0; db < NB; ++db) o[rb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
+    if (threadIdx.x == 0) *(int*)(lds + FLAG) = 0;
     if (u.first < u.last) {
-      lane_k = ((key_of() + 8 * (li >> 2) + (li & 3)) * DH + 8 * g) * 2;
-      lane_v = ((uint32_t)li * (PAGED ? kPage : a.cap) + key_of() + 8 * g) * 2;
       fetch(u.first);
       if (!values() && u.first + 1 < u.last) fetch(u.first + 1);
 #pragma unroll
@@ -363,7 +427,6 @@ struct TileWork {
       // (the first turn overwrites this tile's keys: every wave has read them)
       __syncthreads();
       look(A, u.first);
-      if (masked && ((u.first + 1) * kTileKeys > u.lim || !there)) clear_absent(u.first);
       for (int t = u.first; t < u.last; t += 2) {
         turn(A, B, t);
         if (t + 1 < u.last) turn(B, A, t + 1);
@@ -373,6 +436,7 @@ struct TileWork {
     for (int rb = 0; rb < RB; ++rb) {
       const int pr = pair_of(rb);
       const float sum = col4_sum(l[rb]);
+      if (PAGED) strays[rb].give(o[rb]);
       if (pr >= u.pairs) continue;
       const size_t at = (u.part + pr / group) * a.H + u.kh * group + pr % group;
 #pragma unroll
@@ -385,80 +449,77 @@ struct TileWork {
   }
 };
 
-template <int DH, int RB, bool PAGED>
-__device__ __forceinline__ void tile_unit(const AttnArgs& a, const Unit& u, char* lds) {
-  TileWork<DH, RB, PAGED> w(a, u, lds);
-  w.run();
-}
-
 // ---------------------------------------------------------------- few rows
 //
 // 16 pairs at a time: the waves take every fourth 32-key step each and meet in
-// LDS.  What such a unit takes is the time of its loads, so a wave fetches a
-// step while it computes another, and the probabilities enter the value
-// product as two bf16 halves (about 16 bits): the matrix cores have the time.
+// LDS.  What such a unit takes is the time of its loads, so a wave fetches the
+// next step's keys as soon as the scores have taken this one's, and its values
+// behind the value product; and the probabilities enter that product as two bf16
+// halves (about 16 bits): the matrix cores have the time.
 template <int DH>
-struct KeyStep {
-  bf16x8 f[Frags<DH>::LOADS];
-};
-
-template <int DH>
-__device__ __forceinline__ void load_step(KeyStep<DH>& R, const TileAt& at, int key) {
-  const int lane = threadIdx.x & 63, li = lane & 15, g = lane >> 4;
-  constexpr int NS = Frags<DH>::NS, NB = Frags<DH>::NB;
-#pragma unroll
-  for (int b = 0; b < 2; ++b)
-#pragma unroll
-    for (int s = 0; s < NS; ++s)
-      R.f[b * NS + s] = ldg((const bf16x8*)(at.k + (key + 8 * (li >> 2) + 4 * b + (li & 3)) * DH + 32 * s + 8 * g));
-#pragma unroll
-  for (int db = 0; db < NB; ++db) R.f[2 * NS + db] = ldg((const bf16x8*)(at.v + (size_t)(16 * db + li) * at.vs + key + 8 * g));
-}
-
-template <int DH>
-__device__ __forceinline__ void narrow_unit(const AttnArgs& a, const Unit& u, int pair0, char* lds) {
+__device__ __forceinline__ void narrow_unit(const AttnArgs& a, const Unit& u, char* lds) {
   constexpr int NS = Frags<DH>::NS, NB = Frags<DH>::NB;
   float(*o_s)[16][DH + 4] = (float(*)[16][DH + 4])lds;
   float(*ml_s)[16][2] = (float(*)[16][2])(lds + sizeof(float) * kWaves * 16 * (DH + 4));
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, g = lane >> 4, wave = wave_index();
-  const int group = a.H / a.Hkv;
+  const int group = a.H / a.Hkv, pair0 = u.pair0;
   const int pr = pair0 + li < u.pairs ? pair0 + li : u.pairs - 1;
   const size_t row = (size_t)u.row0 + pr / group;
   const int j0 = 2 * u.first + wave, j1 = u.last * kTileKeys <= u.lim ? 2 * u.last : (u.lim + 31) / 32;
   PageIds pages;
   if (u.table) pages.start(u, u.first);
-  KeyStep<DH> A, B;
-  bool there_a = false, there_b = false;
-  auto fetch = [&](KeyStep<DH>& R, bool& there, int j) {
-    const TileAt at = u.table ? page_tile(a, u, pages.get(u, j >> 1)) : prefix_tile(a, u, j >> 1);
-    there = at.there;
-    load_step<DH>(R, at, 32 * (j & 1));
+  bf16x8 k[2 * NS], v[NB];
+  const uint32_t lane_k = ((8 * (li >> 2) + (li & 3)) * DH + 8 * g) * 2;
+  const uint32_t lane_v = ((uint32_t)li * (u.table ? kPage : a.cap) + 8 * g) * 2;
+  auto where = [&](int j) { return u.table ? page_tile(a, u, pages.get(u, j >> 1)) : prefix_tile(a, u, j >> 1); };
+  auto fetch_keys = [&](const TileAt& at, int j) {
+    const bf16* src = at.k + 32 * (j & 1) * DH;
+#pragma unroll
+    for (int e = 0; e < 2 * NS; ++e) k[e] = ldg((const bf16x8*)((const char*)(src + (e / NS) * 4 * DH + (e % NS) * 32) + lane_k));
   };
-  if (j0 < j1) fetch(A, there_a, j0);
+  auto fetch_values = [&](const TileAt& at, int j) {
+    const bf16* src = at.v + 32 * (j & 1);
+#pragma unroll
+    for (int db = 0; db < NB; ++db) v[db] = ldg((const bf16x8*)((const char*)(src + (size_t)(16 * db) * at.vs) + lane_v));
+  };
+  TileAt at = {nullptr, nullptr, 0, false};
+  if (j0 < j1) {
+    at = where(j0);
+    fetch_keys(at, j0);
+    fetch_values(at, j0);
+  }
   bf16x8 qf[NS];
 #pragma unroll
   for (int s = 0; s < NS; ++s)
     qf[s] = ldg((const bf16x8*)(a.q + row * a.q_stride + (size_t)(u.kh * group + pr % group) * DH + 32 * s + 8 * g));
-  uint32_t anc[4] = {0, 0, 0, 0};
-  if (u.table)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) anc[j] = ldg(a.mask + row * 4 + j);
   float m = -INFINITY, l = 0.0f;
+  Strays strays;
   f32x4 o[NB];
 #pragma unroll
   for (int db = 0; db < NB; ++db) o[db] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  auto compute = [&](KeyStep<DH>& R, bool there, int j) {
-    if (!there) return;
+  for (int j = j0; j < j1; j += kWaves) {
     f32x4 sc[2];
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
       sc[b] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int s = 0; s < NS; ++s) sc[b] = mfma16x16x32(R.f[b * NS + s], qf[s], sc[b]);
+      for (int s = 0; s < NS; ++s) sc[b] = mfma16x16x32(k[b * NS + s], qf[s], sc[b]);
     }
-    const bool masked = 32 * (j + 1) > u.held;
-    const uint32_t vis = masked ? seen8(anc, 32 * j + 8 * g, u.held, u.lim) : 0xffu;
+    const bool there = at.there, more = j + kWaves < j1;
+    if (more) {
+      at = where(j + kWaves);
+      fetch_keys(at, j + kWaves);
+    }
+    const bool masked = 32 * (j + 1) > u.held || !there;
+    uint32_t vis = 0xffu;
+    if (masked) {
+      uint32_t anc[4] = {0, 0, 0, 0};
+      if (u.table)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) anc[w] = ldg(a.mask + row * 4 + w);
+      vis = there ? seen8(anc, 32 * j + 8 * g, u.held, u.lim) : 0u;
+    }
     float sv[8], mx = -INFINITY;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -482,37 +543,40 @@ __device__ __forceinline__ void narrow_unit(const AttnArgs& a, const Unit& u, in
       ph[e] = f2bf(p);
       pl[e] = f2bf(p - bf2f(ph[e]));
     }
-    bool bad = false;
     if (masked) {
-      const int valid = u.lim - (32 * j + 8 * g);
+      const int left = u.lim - (32 * j + 8 * g);
+      const u32x4 words = kept_words(!there || left <= 0 ? 0u : left >= 8 ? 0xffu : (1u << left) - 1u);
+      u16x8 most = (uint16_t)0;
 #pragma unroll
       for (int db = 0; db < NB; ++db) {
+        v[db] = keep(v[db], words);
+        largest(most, v[db]);
+      }
+      if (__any(nonfinite(most))) {  // (through the wave's part of LDS: a short loop)
+        char* mine = lds + wave * 16 * (DH + 4) * 4 + lane * 16;
+        static_assert(NB * 1024 <= 16 * (DH + 4) * 4, "the values of a step in a wave's part");
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (e >= valid) R.f[2 * NS + db][e] = (bf16)0.0f;
-        bad |= nonfinite(R.f[2 * NS + db]);
+        for (int db = 0; db < NB; ++db) lds_st<bf16x8>(mine + db * 1024, v[db]);
+#pragma unroll 1
+        for (int db = 0; db < NB; ++db) {
+          const bf16x8 x = lds_ld<bf16x8>(mine + db * 1024);
+          strays.note(x, vis, db);
+          lds_st<bf16x8>(mine + db * 1024, finite(x));
+        }
+#pragma unroll
+        for (int db = 0; db < NB; ++db) v[db] = lds_ld<bf16x8>(mine + db * 1024);
       }
     }
-    if (__any(bad))
-#pragma unroll
-      for (int db = 0; db < NB; ++db) {
-        o[db] = take_nonfinite(R.f[2 * NS + db], vis, o[db]);
-        __builtin_amdgcn_sched_barrier(0);
-      }
 #pragma unroll
     for (int db = 0; db < NB; ++db) {
-      o[db] = mfma16x16x32(R.f[2 * NS + db], ph, o[db]);
-      o[db] = mfma16x16x32(R.f[2 * NS + db], pl, o[db]);
+      o[db] = mfma16x16x32(v[db], ph, o[db]);
+      o[db] = mfma16x16x32(v[db], pl, o[db]);
     }
-  };
-  for (int j = j0; j < j1; j += 2 * kWaves) {
-    if (j + kWaves < j1) fetch(B, there_b, j + kWaves);
-    compute(A, there_a, j);
-    if (j + 2 * kWaves < j1) fetch(A, there_a, j + 2 * kWaves);
-    if (j + kWaves < j1) compute(B, there_b, j + kWaves);
+    if (more) fetch_values(at, j + kWaves);
   }
   // the four waves' states, joined in wave order
   l = col4_sum(l);
+  strays.give(o);
 #pragma unroll
   for (int db = 0; db < NB; ++db)
 #pragma unroll
@@ -567,52 +631,61 @@ __device__ __forceinline__ bool prefix_unit(const AttnArgs& a, int w, int units,
 }
 
 template <int DH>
-__global__ __launch_bounds__(kThreads, 2) void prefix_kernel(AttnArgs a, int units, int row_tiles) {
-  __shared__ __align__(16) char lds[4 * Frags<DH>::LOADS * 1024];
+__global__ __launch_bounds__(kThreads, LB_P) void prefix_kernel(AttnArgs a, int units, int row_tiles) {
+  typedef TileWork<DH, RB_P, false> Work;
+  __shared__ __align__(16) char lds[Work::LDS];
   Unit u;
   int tile;
   if (!prefix_unit(a, blockIdx.x, units, row_tiles, u, tile)) return;
-  u.pair0 = 128 * tile;
-  tile_unit<DH, 2, false>(a, u, lds);
+  u.pair0 = 64 * RB_P * tile;
+  Work(a, u, lds).run();
 }
 
-// Workgroups of few rows of the prefix first, then a.merge runs of a request's
-// pages each.
+// Workgroup x of the runs' part: a.merge runs of a request's pages for one K/V head.
+__device__ __forceinline__ bool run_unit(const AttnArgs& a, int x, Unit& u) {
+  const int run_of = x / a.Hkv;
+  u.kh = x % a.Hkv;
+  const BatchUnit r = ldg(a.units + run_of);  // (what lies behind the last one is not used)
+  if (run_of >= ldg(a.head + PLAN_UNITS) || r.n == 0 || r.run % a.merge != 0) return false;
+  u.row0 = r.row0;
+  u.pairs = r.n * (a.H / a.Hkv);
+  u.held = r.held;
+  u.lim = r.held + r.n;
+  u.table = a.table + (size_t)r.request * a.max_pages;
+  const int tiles = up_div(u.lim, kTileKeys) < a.max_pages ? up_div(u.lim, kTileKeys) : a.max_pages;
+  const long long f = (long long)r.run * r.chunk, t = f + (long long)r.chunk * a.merge;
+  u.first = f < tiles ? (int)f : tiles;
+  u.last = t < tiles ? (int)t : tiles;
+  u.part = (size_t)a.KP * a.N + r.part0 + (size_t)(r.run / a.merge) * r.n;
+  u.pair0 = 0;
+  return true;
+}
+
+// Few pairs per unit: of the prefix (its workgroups first) and of the runs.
 template <int DH>
-__global__ __launch_bounds__(kThreads, 2) void unit_kernel(AttnArgs a, int prefix_units, int row_tiles) {
-  constexpr int kTileBytes = 4 * Frags<DH>::LOADS * 1024, kJoinBytes = kWaves * 16 * (DH + 6) * 4;
-  __shared__ __align__(16) char lds[kTileBytes > kJoinBytes ? kTileBytes : kJoinBytes];
-  const int group = a.H / a.Hkv;
+__global__ __launch_bounds__(kThreads, LB_N) void narrow_kernel(AttnArgs a, int prefix_units, int row_tiles) {
+  __shared__ __align__(16) char lds[kWaves * 16 * (DH + 6) * 4];
   Unit u;
   const int padded = up_div(prefix_units, 8) * 8;
   if ((int)blockIdx.x < padded) {
     int tile;
-    if (prefix_unit(a, blockIdx.x, prefix_units, row_tiles, u, tile)) narrow_unit<DH>(a, u, 16 * tile, lds);
+    if (!prefix_unit(a, blockIdx.x, prefix_units, row_tiles, u, tile)) return;
+    u.pair0 = 16 * tile;
+    u.pairs = u.pair0 + 16 < u.pairs ? u.pair0 + 16 : u.pairs;
+  } else if (!run_unit(a, blockIdx.x - padded, u)) {
     return;
   }
-  const int x = blockIdx.x - padded, run_of = x / a.Hkv;
-  u.kh = x % a.Hkv;
-  if (run_of >= ldg(a.head + PLAN_UNITS)) return;
-  const int unit = ldg(a.units + run_of), run = unit & 0xffff;
-  const BatchRequest r = ldg(a.req + (unit >> 16));
-  if (r.n == 0 || run % a.merge != 0) return;
-  const int chunk = ldg(a.head + PLAN_CHUNK);
-  u.row0 = r.row0;
-  u.pairs = r.n * group;
-  u.held = r.held;
-  u.lim = r.held + r.n;
-  u.table = a.table + (size_t)(unit >> 16) * a.max_pages;
-  const int tiles = up_div(u.lim, kTileKeys) < a.max_pages ? up_div(u.lim, kTileKeys) : a.max_pages;
-  const long long f = (long long)run * chunk, t = f + (long long)chunk * a.merge;
-  u.first = f < tiles ? (int)f : tiles;
-  u.last = t < tiles ? (int)t : tiles;
-  u.part = (size_t)a.KP * a.N + r.part0 + (size_t)(run / a.merge) * r.n;
-  u.pair0 = 0;
-  if (u.pairs <= 16) {
-    narrow_unit<DH>(a, u, 0, lds);
-  } else {
-    for (; u.pair0 < u.pairs; u.pair0 += 64) tile_unit<DH, 1, true>(a, u, lds);
-  }
+  for (; u.pair0 < u.pairs; u.pair0 += 16) narrow_unit<DH>(a, u, lds);
+}
+
+// Many pairs per unit: the runs.
+template <int DH>
+__global__ __launch_bounds__(kThreads, LB_G) void pages_kernel(AttnArgs a) {
+  typedef TileWork<DH, RB_G, true> Work;
+  __shared__ __align__(16) char lds[Work::LDS];
+  Unit u;
+  if (!run_unit(a, blockIdx.x, u)) return;
+  for (; u.pair0 < u.pairs; u.pair0 += 64 * RB_G) Work(a, u, lds).run();
 }
 
 // A wave per (row, head): its partial results in the order of their keys.
@@ -657,15 +730,16 @@ hipError_t launch_attention(AttnArgs a, hipStream_t st) {
   // The plan cuts the requests' pages for 8 K/V heads; more heads make enough
   // workgroups of longer runs.
   a.merge = a.Hkv <= 8 ? 1 : cdiv(a.Hkv, 12);
-  const int row_tiles = cdiv(a.N * (a.H / a.Hkv), wide ? 128 : 16);
-  int units = row_tiles * a.KP * a.Hkv;
+  const int row_tiles = cdiv(a.N * (a.H / a.Hkv), wide ? 64 * RB_P : 16);
+  const int units = row_tiles * a.KP * a.Hkv;
   const long long most = (long long)a.B * cdiv(a.max_pages, 2);  // (a run has two pages or more)
-  const int runs = most < plan_max_units(a.B) ? (int)most : plan_max_units(a.B);
-  if (wide && units > 0) {
-    prefix_kernel<DH><<<dim3(cdiv(units, 8) * 8), dim3(kThreads), 0, st>>>(a, units, row_tiles);
-    units = 0;
-  }
-  unit_kernel<DH><<<dim3(cdiv(units, 8) * 8 + runs * a.Hkv), dim3(kThreads), 0, st>>>(a, units, row_tiles);
+  const int runs = (most < plan_max_units(a.B) ? (int)most : plan_max_units(a.B)) * a.Hkv;
+  const bool narrow = (long long)a.N * (a.H / a.Hkv) <= 16ll * a.B;  // (pairs of a request, in the mean)
+  if (wide && units > 0) prefix_kernel<DH><<<dim3(cdiv(units, 8) * 8), dim3(kThreads), 0, st>>>(a, units, row_tiles);
+  const int few = wide ? 0 : units;
+  if (few + (narrow ? runs : 0) > 0)
+    narrow_kernel<DH><<<dim3(cdiv(few, 8) * 8 + (narrow ? runs : 0)), dim3(kThreads), 0, st>>>(a, few, row_tiles);
+  if (!narrow) pages_kernel<DH><<<dim3(runs), dim3(kThreads), 0, st>>>(a);
   join_kernel<DH><<<dim3((unsigned)(((long long)a.N * a.H + kWaves - 1) / kWaves)), dim3(kThreads), 0, st>>>(a);
   return hipGetLastError();
 }
@@ -676,7 +750,7 @@ int prefix_splits(int N, int H, int Hkv, int P) {
   if (P <= 0) return 0;
   const int pairs = N * (H / Hkv);
   const bool wide = wide_prefix(N, H, Hkv);
-  int KP = wide ? 512 / (cdiv(pairs, 128) * Hkv) : cdiv(512, cdiv(pairs, 16) * Hkv);
+  int KP = wide ? 256 * LB_P / (cdiv(pairs, 64 * RB_P) * Hkv) : cdiv(512, cdiv(pairs, 16) * Hkv);
   const int most = cdiv(P, 2 * kTileKeys);
   if (KP > most) KP = most;
   if (KP > max_prefix_splits(N)) KP = max_prefix_splits(N);
