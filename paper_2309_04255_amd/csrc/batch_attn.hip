@@ -21,10 +21,11 @@ namespace llmcad {
 namespace {
 
 #define LB_P 2
-#define LB_G 2
+#define LB_G 3
 #define LB_N 2
 #define RB_P 2
 #define RB_G 1
+#define ST_G 1
 constexpr int kThreads = 256;
 constexpr int kWaves = 4;
 constexpr int kTileKeys = kPage;  // keys of a tile: two 32-key steps, one page
@@ -189,19 +190,21 @@ __device__ __forceinline__ bf16x8 finite(const bf16x8& v) {
 // until then no lane needs another's scores.  The sums are per lane, joined at
 // the end.  Probabilities (up to 2^kSlack) enter the value product in bf16, half
 // a step of 2^-8 each.
-template <int DH, int RB, bool PAGED>
+template <int DH, int RB, int STEPS, bool PAGED, bool JOIN>
 struct TileWork {
   static constexpr int NS = Frags<DH>::NS, NB = Frags<DH>::NB;
-  static constexpr int STEPS = kTileKeys / 32;
-  static constexpr int HALF = kTileKeys * DH * 2;  // bytes of a tile's keys, or of its values
-  static constexpr int FLAG = 4 * HALF;            // (a flag behind the buffers)
+  static constexpr int KEYS = 32 * STEPS;       // of a tile: a page, or half of one
+  static constexpr int PARTS = kTileKeys / KEYS;
+  static constexpr int HALF = KEYS * DH * 2;    // bytes of a tile's keys, or of its values
+  static constexpr int FLAG = 4 * HALF;         // (a flag behind the buffers)
   static constexpr int LDS = FLAG + 16;
-  static constexpr int PER = HALF / 2048;          // KiB that a wave fetches: half of the keys, or of the values
-  typedef f32x4 Scores[RB][2 * STEPS];             // [row block][step, key block]
+  static constexpr int PER = HALF / 2048;       // KiB that a wave fetches: half of the keys, or of the values
+  typedef f32x4 Scores[RB][2 * STEPS];          // [row block][step, key block]
 
   const AttnArgs& a;
   const Unit& u;
   char* lds;  // keys of even tiles, of odd tiles, values of even, of odd
+  int first, last;  // tiles
   int lane, li, g, wave, group;
   bf16x8 qf[RB][NS];
   float m[RB], neg_m[RB], l[RB];
@@ -209,6 +212,7 @@ struct TileWork {
   Strays strays[RB];
   bool there;
   PageIds pages;
+  int own_row[RB], own_n[RB], own_parts[RB];  // JOIN: partial results of the row's own keys (rows own_row + p own_n), how many (-1: no request's row)
   uint32_t lane_at[4];  // byte offset of the lane's part of a fetched KiB, by the KiB's index
 
   __device__ __forceinline__ TileWork(const AttnArgs& a_, const Unit& u_, char* lds_) : a(a_), u(u_), lds(lds_) {
@@ -217,25 +221,30 @@ struct TileWork {
     g = lane >> 4;
     wave = wave_index();
     group = a.H / a.Hkv;
+    first = u.first * PARTS;
+    const int end = (u.lim + KEYS - 1) / KEYS;
+    last = u.last * PARTS < end ? u.last * PARTS : end;
   }
   __device__ __forceinline__ int pair_of(int rb) const { return u.pair0 + (wave * RB + rb) * 16 + li; }
   __device__ __forceinline__ int clamped(int rb) const { return pair_of(rb) < u.pairs ? pair_of(rb) : u.pairs - 1; }
 
   // LDS holds a tile's keys as [step][key block][16 rows][DH] and its values as
-  // [DH][64 keys], so that a KiB copied to it is whole rows: 64 lanes read 4 to 8
-  // rows of 128 or 256 contiguous bytes.  (In fragment order each lane's 16 bytes
+  // [DH][KEYS], so that a KiB copied to it is whole rows: 64 lanes read 4 to 16
+  // rows of 64 to 256 contiguous bytes.  (In fragment order each lane's 16 bytes
   // are another row than its neighbours', and the vector cache takes them one by
   // one: 67 accesses per KiB instead of 19.)  The 16-byte pieces of a row are swapped by its
   // index, so that the pieces of 16 rows that a fragment reads together lie in
   // different banks (a read takes 256 bytes of LDS at a time).
-  static constexpr int ROW = DH * 2;            // bytes of a row of keys
-  static constexpr int ROWS = 1024 / ROW;       // of them in a KiB
-  __device__ static __forceinline__ int swap(int row_bytes, int row) { return row_bytes == 256 ? row & 15 : (row >> 1) & 7; }
+  static constexpr int ROW = DH * 2, VROW = KEYS * 2;  // bytes of a row of keys, of values
+  static constexpr int ROWS = 1024 / ROW, DIMS = 1024 / VROW;  // of them in a KiB
+  __device__ static __forceinline__ int swap(int row_bytes, int row) {
+    return row_bytes == 256 ? row & 15 : row_bytes == 128 ? (row >> 1) & 7 : (row >> 2) & 3;
+  }
   __device__ __forceinline__ const char* key_at(int t, int sb, int s) const {
     return lds + (t & 1) * HALF + sb * 16 * ROW + li * ROW + (((4 * s + g) ^ swap(ROW, li)) * 16);
   }
   __device__ __forceinline__ char* value_at(int t, int st, int db) const {
-    return lds + (2 + (t & 1)) * HALF + (16 * db + li) * 128 + (((4 * st + g) ^ swap(128, li)) * 16);
+    return lds + (2 + (t & 1)) * HALF + (16 * db + li) * VROW + (((4 * st + g) ^ swap(VROW, li)) * 16);
   }
   // waves 0 and 1 fetch a step's keys each, 2 and 3 half of the values' dims each
   __device__ __forceinline__ bool values() const { return wave >= 2; }
@@ -243,8 +252,8 @@ struct TileWork {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
       if (values()) {
-        const int dim = 8 * i + (lane >> 3), piece = lane & 7;
-        lane_at[i] = ((uint32_t)(lane >> 3) * (PAGED ? kPage : a.cap) + 8 * (piece ^ swap(128, dim))) * 2;
+        const int dim = lane / (VROW / 16), piece = lane % (VROW / 16);
+        lane_at[i] = ((uint32_t)dim * (PAGED ? kPage : a.cap) + 8 * (piece ^ swap(VROW, i * DIMS + dim))) * 2;
       } else {
         const int row = lane / (ROW / 16), piece = lane % (ROW / 16);
         lane_at[i] = (8 * (row >> 2) + (row & 3)) * ROW + (piece ^ swap(ROW, i % NS * ROWS + row)) * 16;
@@ -252,16 +261,16 @@ struct TileWork {
   }
   // copies this wave's part of tile t straight to LDS
   __device__ __forceinline__ void fetch(int t) {
-    const TileAt at = PAGED ? page_tile(a, u, pages.get(u, t)) : prefix_tile(a, u, t);
-    const int part = wave & 1;
+    const TileAt at = PAGED ? page_tile(a, u, pages.get(u, t / PARTS)) : prefix_tile(a, u, t / PARTS);
+    const int key = t % PARTS * KEYS, part = wave & 1;
     if (values()) {
       char* to = lds + (2 + (t & 1)) * HALF + part * PER * 1024;
-      const bf16* v = at.v + (size_t)(8 * PER * part) * at.vs;
+      const bf16* v = at.v + key + (size_t)(DIMS * PER * part) * at.vs;
 #pragma unroll
-      for (int e = 0; e < PER; ++e) dma16((const char*)(v + (size_t)(8 * e) * at.vs) + lane_at[e & 3], to + e * 1024);
-    } else {
+      for (int e = 0; e < PER; ++e) dma16((const char*)(v + (size_t)(DIMS * e) * at.vs) + lane_at[e & 3], to + e * 1024);
+    } else {  // (a part: a step's keys, or with tiles of one step a key block's)
       char* to = lds + (t & 1) * HALF + part * PER * 1024;
-      const char* k = (const char*)(at.k + 32 * part * DH);
+      const char* k = (const char*)(at.k + (key + (STEPS == 2 ? 32 : 4) * part) * DH);
 #pragma unroll
       for (int e = 0; e < PER; ++e) {  // key block e / NS, rows ROWS (e % NS) .. of it: keys 2 ROWS (e % NS) + 4 (e / NS) ..
         const int i = e % NS;
@@ -293,7 +302,7 @@ struct TileWork {
 #pragma unroll 1
     for (int f = wave; f < STEPS * NB; f += kWaves) {
       char* at = value_at(t, f / NB, f % NB);
-      const int left = u.lim - (t * kTileKeys + 32 * (f / NB) + 8 * g);
+      const int left = u.lim - (t * KEYS + 32 * (f / NB) + 8 * g);
       const bf16x8 v = keep(lds_ld<bf16x8>(at), kept_words(!there || left <= 0 ? 0u : left >= 8 ? 0xffu : (1u << left) - 1u));
       if (PAGED) largest(most, v);
       lds_st<bf16x8>(at, v);
@@ -323,10 +332,10 @@ struct TileWork {
   __device__ __forceinline__ void look(Scores& sc, int t) {
     there = true;
     if (PAGED) {
-      const int id = pages.get(u, t);
+      const int id = pages.get(u, t / PARTS);
       there = id >= 0 && id < a.n_pages;
     }
-    if ((t + 1) * kTileKeys > u.held || !there) {  // (not every row sees every key)
+    if ((t + 1) * KEYS > u.held || !there) {  // (not every row sees every key)
       uint32_t vis[RB][STEPS];
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) {
@@ -338,7 +347,7 @@ struct TileWork {
         }
 #pragma unroll
         for (int st = 0; st < STEPS; ++st) {
-          vis[rb][st] = there ? seen8(anc, t * kTileKeys + 32 * st + 8 * g, u.held, u.lim) : 0u;
+          vis[rb][st] = there ? seen8(anc, t * KEYS + 32 * st + 8 * g, u.held, u.lim) : 0u;
 #pragma unroll
           for (int e = 0; e < 8; ++e)
             if (!((vis[rb][st] >> e) & 1u)) sc[rb][2 * st + (e >> 2)][e & 3] = -INFINITY;
@@ -372,9 +381,9 @@ struct TileWork {
   }
   // Tile t's probabilities and its part of the output; the next tile's scores.
   __device__ __forceinline__ void turn(Scores& sc, Scores& next, int t) {
-    const bool more = t + 1 < u.last;
+    const bool more = t + 1 < last;
     const int coming = values() ? t + 1 : t + 2;
-    if (coming < u.last) fetch(coming);
+    if (coming < last) fetch(coming);
     scores(next, t + 1);  // (past the last tile: of what lies there, not used)
     bf16x8 p[RB][STEPS];
 #pragma unroll
@@ -399,9 +408,51 @@ struct TileWork {
     if (more) look(next, t + 1);
   }
 
+  // The rows' outputs, from this unit (all of the prefix) and the partial results
+  // that an earlier launch left of their own keys.
+  __device__ __forceinline__ void join() {
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      const int pr = pair_of(rb), h = u.kh * group + clamped(rb) % group;
+      float sum = col4_sum(l[rb]), most = m[rb];
+      for (int p = 0; __any(p < own_parts[rb]); ++p) {
+        if (p >= own_parts[rb]) continue;
+        const size_t at = ((size_t)a.KP * a.N + own_row[rb] + (size_t)p * own_n[rb]) * a.H + h;
+        const float pm = ldg(a.part_ml + at * 2), pl = ldg(a.part_ml + at * 2 + 1);
+        const float mm = fmaxf(most, pm), mu = mm == -INFINITY ? 0.0f : mm;
+        const float fa = __builtin_amdgcn_exp2f(most - mu), fb = __builtin_amdgcn_exp2f(pm - mu);
+        sum = fa * sum + fb * pl;
+        most = mm;
+#pragma unroll
+        for (int db = 0; db < NB; ++db) {
+          const f32x4 x = ldg((const f32x4*)(a.part_o + at * DH + 16 * db + 4 * g));
+          o[rb][db] = o[rb][db] * fa + x * fb;
+        }
+      }
+      if (own_parts[rb] < 0) continue;
+      const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+      bf16* out = a.out + ((size_t)(pr / group) * a.H + h) * DH + 4 * g;
+#pragma unroll
+      for (int db = 0; db < NB; ++db) {
+        bf16x4 y;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = f2bf(o[rb][db][i] * inv);
+        stg((bf16x4*)(out + 16 * db), y);
+      }
+    }
+  }
   __device__ __forceinline__ void run() {
     if (PAGED) pages.start(u, u.first);
     place_lanes();
+    if (JOIN)
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        const int row = clamped(rb) / group, b = pair_of(rb) < u.pairs ? ldg(a.row_req + row) : -1;
+        const BatchRequest r = ldg(a.req + (b < 0 ? 0 : b));
+        own_row[rb] = r.part0 + row - r.row0;
+        own_n[rb] = r.n;
+        own_parts[rb] = b < 0 ? -1 : up_div(r.splits, a.merge);
+      }
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
       m[rb] = -INFINITY;
@@ -411,9 +462,9 @@ struct TileWork {
       for (int db = 0; db < NB; ++db) o[rb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
     if (threadIdx.x == 0) *(int*)(lds + FLAG) = 0;
-    if (u.first < u.last) {
-      fetch(u.first);
-      if (!values() && u.first + 1 < u.last) fetch(u.first + 1);
+    if (first < last) {
+      fetch(first);
+      if (!values() && u.first + 1 < last) fetch(first + 1);
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) {
         const int pr = clamped(rb);
@@ -423,14 +474,18 @@ struct TileWork {
       }
       __syncthreads();
       Scores A, B;
-      scores(A, u.first);
+      scores(A, first);
       // (the first turn overwrites this tile's keys: every wave has read them)
       __syncthreads();
-      look(A, u.first);
-      for (int t = u.first; t < u.last; t += 2) {
+      look(A, first);
+      for (int t = first; t < last; t += 2) {
         turn(A, B, t);
-        if (t + 1 < u.last) turn(B, A, t + 1);
+        if (t + 1 < last) turn(B, A, t + 1);
       }
+    }
+    if (JOIN) {
+      join();
+      return;
     }
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
@@ -630,9 +685,10 @@ __device__ __forceinline__ bool prefix_unit(const AttnArgs& a, int w, int units,
   return true;
 }
 
-template <int DH>
+// (JOIN: one split, and what is left of the rows' own keys was computed before)
+template <int DH, bool JOIN>
 __global__ __launch_bounds__(kThreads, LB_P) void prefix_kernel(AttnArgs a, int units, int row_tiles) {
-  typedef TileWork<DH, RB_P, false> Work;
+  typedef TileWork<DH, RB_P, 2, false, JOIN> Work;
   __shared__ __align__(16) char lds[Work::LDS];
   Unit u;
   int tile;
@@ -681,7 +737,7 @@ __global__ __launch_bounds__(kThreads, LB_N) void narrow_kernel(AttnArgs a, int 
 // Many pairs per unit: the runs.
 template <int DH>
 __global__ __launch_bounds__(kThreads, LB_G) void pages_kernel(AttnArgs a) {
-  typedef TileWork<DH, RB_G, true> Work;
+  typedef TileWork<DH, RB_G, ST_G, true, false> Work;
   __shared__ __align__(16) char lds[Work::LDS];
   Unit u;
   if (!run_unit(a, blockIdx.x, u)) return;
@@ -735,11 +791,16 @@ hipError_t launch_attention(AttnArgs a, hipStream_t st) {
   const long long most = (long long)a.B * cdiv(a.max_pages, 2);  // (a run has two pages or more)
   const int runs = (most < plan_max_units(a.B) ? (int)most : plan_max_units(a.B)) * a.Hkv;
   const bool narrow = (long long)a.N * (a.H / a.Hkv) <= 16ll * a.B;  // (pairs of a request, in the mean)
-  if (wide && units > 0) prefix_kernel<DH><<<dim3(cdiv(units, 8) * 8), dim3(kThreads), 0, st>>>(a, units, row_tiles);
   const int few = wide ? 0 : units;
   if (few + (narrow ? runs : 0) > 0)
     narrow_kernel<DH><<<dim3(cdiv(few, 8) * 8 + (narrow ? runs : 0)), dim3(kThreads), 0, st>>>(a, few, row_tiles);
   if (!narrow) pages_kernel<DH><<<dim3(runs), dim3(kThreads), 0, st>>>(a);
+  const dim3 grid(cdiv(units, 8) * 8);
+  if (wide && a.KP == 1) {
+    prefix_kernel<DH, true><<<grid, dim3(kThreads), 0, st>>>(a, units, row_tiles);
+    return hipGetLastError();
+  }
+  if (wide && units > 0) prefix_kernel<DH, false><<<grid, dim3(kThreads), 0, st>>>(a, units, row_tiles);
   join_kernel<DH><<<dim3((unsigned)(((long long)a.N * a.H + kWaves - 1) / kWaves)), dim3(kThreads), 0, st>>>(a);
   return hipGetLastError();
 }
