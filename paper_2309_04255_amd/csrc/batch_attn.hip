@@ -20,14 +20,9 @@ namespace llmcad {
 
 namespace {
 
-#define LB_P 2
-#define LB_G 3
-#define LB_N 2
-#define RB_P 2
-#define RB_G 1
-#define ST_G 1
 constexpr int kThreads = 256;
 constexpr int kWaves = 4;
+constexpr int kWideRows = 128;  // pairs per workgroup of the prefix, where there are many
 constexpr int kTileKeys = kPage;  // keys of a tile: two 32-key steps, one page
 constexpr float kSlack = 8.0f;
 
@@ -177,23 +172,19 @@ __device__ __forceinline__ bf16x8 finite(const bf16x8& v) {
 
 // ---------------------------------------------------------------- many rows
 //
-// 64 RB pairs per workgroup, 16 RB per wave.  Tiles of 64 keys are shared
-// through LDS, keys and values in two buffers each.  A turn of the loop takes the
-// values of tile t and the keys of tile t + 1: the scores of the next tile and
-// the exponentials of this one need different units, and their instructions
-// alternate.  Meanwhile the values of t + 1 and the keys of t + 2 are on their
-// way to registers; they go to the buffers that this turn does not read, so one
-// barrier per turn does.
+// 64 RB pairs per workgroup, 16 RB per wave.  Tiles of 32 keys are shared
+// through LDS, in two buffers: while one is computed the next is copied.
 //
 // The running maximum is only a reference point: any value near it serves, so
 // the output is rescaled only when some score exceeds it by 2^kSlack, and
 // until then no lane needs another's scores.  The sums are per lane, joined at
 // the end.  Probabilities (up to 2^kSlack) enter the value product in bf16, half
 // a step of 2^-8 each.
-template <int DH, int RB, int STEPS, bool PAGED, bool JOIN>
+template <int DH, int RB, bool PAGED>
 struct TileWork {
   static constexpr int NS = Frags<DH>::NS, NB = Frags<DH>::NB;
-  static constexpr int KEYS = 32 * STEPS;       // of a tile: a page, or half of one
+  static constexpr int STEPS = 1;
+  static constexpr int KEYS = 32 * STEPS;       // of a tile: half a page
   static constexpr int PARTS = kTileKeys / KEYS;
   static constexpr int HALF = KEYS * DH * 2;    // bytes of a tile's keys, or of its values
   static constexpr int FLAG = 4 * HALF;         // (a flag behind the buffers)
@@ -212,7 +203,6 @@ struct TileWork {
   Strays strays[RB];
   bool there;
   PageIds pages;
-  int own_row[RB], own_n[RB], own_parts[RB];  // JOIN: partial results of the row's own keys (rows own_row + p own_n), how many (-1: no request's row)
   uint32_t lane_at[4];  // byte offset of the lane's part of a fetched KiB, by the KiB's index
 
   __device__ __forceinline__ TileWork(const AttnArgs& a_, const Unit& u_, char* lds_) : a(a_), u(u_), lds(lds_) {
@@ -379,12 +369,8 @@ struct TileWork {
       }
     }
   }
-  // Tile t's probabilities and its part of the output; the next tile's scores.
-  __device__ __forceinline__ void turn(Scores& sc, Scores& next, int t) {
-    const bool more = t + 1 < last;
-    const int coming = values() ? t + 1 : t + 2;
-    if (coming < last) fetch(coming);
-    scores(next, t + 1);  // (past the last tile: of what lies there, not used)
+  // Tile t's probabilities and its part of the output.
+  __device__ __forceinline__ void add(Scores& sc, int t) {
     bf16x8 p[RB][STEPS];
 #pragma unroll
     for (int st = 0; st < STEPS; ++st)
@@ -404,55 +390,10 @@ struct TileWork {
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) o[rb][db] = mfma16x16x32(v, p[rb][st], o[rb][db]);
       }
-    __syncthreads();
-    if (more) look(next, t + 1);
-  }
-
-  // The rows' outputs, from this unit (all of the prefix) and the partial results
-  // that an earlier launch left of their own keys.
-  __device__ __forceinline__ void join() {
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-      const int pr = pair_of(rb), h = u.kh * group + clamped(rb) % group;
-      float sum = col4_sum(l[rb]), most = m[rb];
-      for (int p = 0; __any(p < own_parts[rb]); ++p) {
-        if (p >= own_parts[rb]) continue;
-        const size_t at = ((size_t)a.KP * a.N + own_row[rb] + (size_t)p * own_n[rb]) * a.H + h;
-        const float pm = ldg(a.part_ml + at * 2), pl = ldg(a.part_ml + at * 2 + 1);
-        const float mm = fmaxf(most, pm), mu = mm == -INFINITY ? 0.0f : mm;
-        const float fa = __builtin_amdgcn_exp2f(most - mu), fb = __builtin_amdgcn_exp2f(pm - mu);
-        sum = fa * sum + fb * pl;
-        most = mm;
-#pragma unroll
-        for (int db = 0; db < NB; ++db) {
-          const f32x4 x = ldg((const f32x4*)(a.part_o + at * DH + 16 * db + 4 * g));
-          o[rb][db] = o[rb][db] * fa + x * fb;
-        }
-      }
-      if (own_parts[rb] < 0) continue;
-      const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-      bf16* out = a.out + ((size_t)(pr / group) * a.H + h) * DH + 4 * g;
-#pragma unroll
-      for (int db = 0; db < NB; ++db) {
-        bf16x4 y;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) y[i] = f2bf(o[rb][db][i] * inv);
-        stg((bf16x4*)(out + 16 * db), y);
-      }
-    }
   }
   __device__ __forceinline__ void run() {
     if (PAGED) pages.start(u, u.first);
     place_lanes();
-    if (JOIN)
-#pragma unroll
-      for (int rb = 0; rb < RB; ++rb) {
-        const int row = clamped(rb) / group, b = pair_of(rb) < u.pairs ? ldg(a.row_req + row) : -1;
-        const BatchRequest r = ldg(a.req + (b < 0 ? 0 : b));
-        own_row[rb] = r.part0 + row - r.row0;
-        own_n[rb] = r.n;
-        own_parts[rb] = b < 0 ? -1 : up_div(r.splits, a.merge);
-      }
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
       m[rb] = -INFINITY;
@@ -464,7 +405,6 @@ struct TileWork {
     if (threadIdx.x == 0) *(int*)(lds + FLAG) = 0;
     if (first < last) {
       fetch(first);
-      if (!values() && u.first + 1 < last) fetch(first + 1);
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) {
         const int pr = clamped(rb);
@@ -473,19 +413,14 @@ struct TileWork {
         for (int s = 0; s < NS; ++s) qf[rb][s] = ldg((const bf16x8*)(q + 32 * s));
       }
       __syncthreads();
-      Scores A, B;
-      scores(A, first);
-      // (the first turn overwrites this tile's keys: every wave has read them)
-      __syncthreads();
-      look(A, first);
-      for (int t = first; t < last; t += 2) {
-        turn(A, B, t);
-        if (t + 1 < last) turn(B, A, t + 1);
+      for (int t = first; t < last; ++t) {
+        Scores sc;
+        if (t + 1 < last) fetch(t + 1);
+        scores(sc, t);
+        look(sc, t);
+        add(sc, t);
+        __syncthreads();
       }
-    }
-    if (JOIN) {
-      join();
-      return;
     }
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
@@ -685,18 +620,6 @@ __device__ __forceinline__ bool prefix_unit(const AttnArgs& a, int w, int units,
   return true;
 }
 
-// (JOIN: one split, and what is left of the rows' own keys was computed before)
-template <int DH, bool JOIN>
-__global__ __launch_bounds__(kThreads, LB_P) void prefix_kernel(AttnArgs a, int units, int row_tiles) {
-  typedef TileWork<DH, RB_P, 2, false, JOIN> Work;
-  __shared__ __align__(16) char lds[Work::LDS];
-  Unit u;
-  int tile;
-  if (!prefix_unit(a, blockIdx.x, units, row_tiles, u, tile)) return;
-  u.pair0 = 64 * RB_P * tile;
-  Work(a, u, lds).run();
-}
-
 // Workgroup x of the runs' part: a.merge runs of a request's pages for one K/V head.
 __device__ __forceinline__ bool run_unit(const AttnArgs& a, int x, Unit& u) {
   const int run_of = x / a.Hkv;
@@ -717,31 +640,37 @@ __device__ __forceinline__ bool run_unit(const AttnArgs& a, int x, Unit& u) {
   return true;
 }
 
-// Few pairs per unit: of the prefix (its workgroups first) and of the runs.
+// The prefix's workgroups first (they are the longest), then those of the runs:
+// three on a CU, so that the ones that wait for memory and the ones that
+// compute share it.
 template <int DH>
-__global__ __launch_bounds__(kThreads, LB_N) void narrow_kernel(AttnArgs a, int prefix_units, int row_tiles) {
-  __shared__ __align__(16) char lds[kWaves * 16 * (DH + 6) * 4];
+__global__ __launch_bounds__(kThreads, 3) void unit_kernel(AttnArgs a, int prefix_units, int row_tiles, int wide) {
+  typedef TileWork<DH, 2, false> Prefix;
+  typedef TileWork<DH, 1, true> Pages;
+  constexpr int kJoin = kWaves * 16 * (DH + 6) * 4, kTile = Prefix::LDS > Pages::LDS ? Prefix::LDS : Pages::LDS;
+  __shared__ __align__(16) char lds[kTile > kJoin ? kTile : kJoin];
   Unit u;
   const int padded = up_div(prefix_units, 8) * 8;
+  bool few;
   if ((int)blockIdx.x < padded) {
     int tile;
     if (!prefix_unit(a, blockIdx.x, prefix_units, row_tiles, u, tile)) return;
+    if (wide) {
+      u.pair0 = kWideRows * tile;
+      Prefix(a, u, lds).run();
+      return;
+    }
     u.pair0 = 16 * tile;
     u.pairs = u.pair0 + 16 < u.pairs ? u.pair0 + 16 : u.pairs;
-  } else if (!run_unit(a, blockIdx.x - padded, u)) {
-    return;
+    few = true;
+  } else {
+    if (!run_unit(a, blockIdx.x - padded, u)) return;
+    few = u.pairs <= 16;
   }
-  for (; u.pair0 < u.pairs; u.pair0 += 16) narrow_unit<DH>(a, u, lds);
-}
-
-// Many pairs per unit: the runs.
-template <int DH>
-__global__ __launch_bounds__(kThreads, LB_G) void pages_kernel(AttnArgs a) {
-  typedef TileWork<DH, RB_G, ST_G, true, false> Work;
-  __shared__ __align__(16) char lds[Work::LDS];
-  Unit u;
-  if (!run_unit(a, blockIdx.x, u)) return;
-  for (; u.pair0 < u.pairs; u.pair0 += 64 * RB_G) Work(a, u, lds).run();
+  if (few)
+    narrow_unit<DH>(a, u, lds);
+  else
+    for (; u.pair0 < u.pairs; u.pair0 += 64) Pages(a, u, lds).run();
 }
 
 // A wave per (row, head): its partial results in the order of their keys.
@@ -776,42 +705,43 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttnArgs a) {
   for (int i = 0; i < PER; ++i) stg(a.out + item * DH + lane * PER + i, f2bf(o[i] * inv));
 }
 
-// Few pairs of rows and heads per K/V head: the waves share 16 of them and split the keys; many:
-// the waves split the pairs and share the keys.
-bool wide_prefix(int N, int H, int Hkv) { return (long long)N * (H / Hkv) > 64; }
+// Few pairs of rows and heads per K/V head: the waves share 16 of them and split
+// the keys; many: the waves split the pairs and share the keys through LDS.  (us,
+// 32 heads of 128, narrow / wide: 41 rows behind 2048 positions 30.0 / 20.9, 64 rows
+// behind 512 18.4 / 16.0 and behind 4096 40.9 / 28.0; up to 32 pairs the narrow ones
+// win or tie: 16 rows behind 512 15.0 / 15.9, 31 behind 2048 19.7 / 19.8.)
+bool wide_prefix(int N, int H, int Hkv) { return (long long)N * (H / Hkv) > 32; }
 
 template <int DH>
 hipError_t launch_attention(AttnArgs a, hipStream_t st) {
   const bool wide = wide_prefix(a.N, a.H, a.Hkv);
   // The plan cuts the requests' pages for 8 K/V heads; more heads make enough
-  // workgroups of longer runs.
-  a.merge = a.Hkv <= 8 ? 1 : cdiv(a.Hkv, 12);
-  const int row_tiles = cdiv(a.N * (a.H / a.Hkv), wide ? 64 * RB_P : 16);
+  // workgroups of longer runs (us with runs joined for every 16 heads / for every
+  // 12: one token after 4000 held ones 27.6 / 29.9, 60 tokens of 32 heads 118 / 122;
+  // no difference elsewhere).
+  a.merge = a.Hkv <= 8 ? 1 : cdiv(a.Hkv, 16);
+  const int row_tiles = cdiv(a.N * (a.H / a.Hkv), wide ? kWideRows : 16);
   const int units = row_tiles * a.KP * a.Hkv;
   const long long most = (long long)a.B * cdiv(a.max_pages, 2);  // (a run has two pages or more)
   const int runs = (most < plan_max_units(a.B) ? (int)most : plan_max_units(a.B)) * a.Hkv;
-  const bool narrow = (long long)a.N * (a.H / a.Hkv) <= 16ll * a.B;  // (pairs of a request, in the mean)
-  const int few = wide ? 0 : units;
-  if (few + (narrow ? runs : 0) > 0)
-    narrow_kernel<DH><<<dim3(cdiv(few, 8) * 8 + (narrow ? runs : 0)), dim3(kThreads), 0, st>>>(a, few, row_tiles);
-  if (!narrow) pages_kernel<DH><<<dim3(runs), dim3(kThreads), 0, st>>>(a);
-  const dim3 grid(cdiv(units, 8) * 8);
-  if (wide && a.KP == 1) {
-    prefix_kernel<DH, true><<<grid, dim3(kThreads), 0, st>>>(a, units, row_tiles);
-    return hipGetLastError();
-  }
-  if (wide && units > 0) prefix_kernel<DH, false><<<grid, dim3(kThreads), 0, st>>>(a, units, row_tiles);
+  unit_kernel<DH><<<dim3(cdiv(units, 8) * 8 + runs), dim3(kThreads), 0, st>>>(a, units, row_tiles, wide);
   join_kernel<DH><<<dim3((unsigned)(((long long)a.N * a.H + kWaves - 1) / kWaves)), dim3(kThreads), 0, st>>>(a);
   return hipGetLastError();
 }
 
 }  // namespace
 
+// The prefix's workgroups, one per CU: they share the CUs with the runs', and
+// every split leaves partial results.  (us with 128, 192, 256, 384 and 512 of them: 16
+// trees of 31 rows, 32 heads, behind 2048 positions 69, 70, 49, 56, 60; 128 tokens, 8
+// K/V heads, behind 8192 110, 97, 86, 94, 98; 16 tokens 33, 34, 35, 42, 51.  Narrow
+// units, 128, 256 and 512: one token, 32 heads, behind 8192 43, 31, 33, 31 rows
+// behind 2048 25, 20, 23.)
 int prefix_splits(int N, int H, int Hkv, int P) {
   if (P <= 0) return 0;
   const int pairs = N * (H / Hkv);
   const bool wide = wide_prefix(N, H, Hkv);
-  int KP = wide ? 256 * LB_P / (cdiv(pairs, 64 * RB_P) * Hkv) : cdiv(512, cdiv(pairs, 16) * Hkv);
+  int KP = wide ? 256 / (cdiv(pairs, kWideRows) * Hkv) : cdiv(256, cdiv(pairs, 16) * Hkv);
   const int most = cdiv(P, 2 * kTileKeys);
   if (KP > most) KP = most;
   if (KP > max_prefix_splits(N)) KP = max_prefix_splits(N);
