@@ -23,7 +23,7 @@ constexpr int kPieces = 4;  // 16-byte pieces of a row per thread and tile
 constexpr int kList = 2048;
 constexpr int kGroups = 256;
 constexpr float kLowest = -3.402823466e38f;        // (finite: x - m stays a number for rows of -inf)
-constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 struct ScoreLds {
   float m[16], s[16], t[16];  // by wave
@@ -170,11 +170,61 @@ __device__ __attribute__((noinline)) void best_in_steps(const void* row, int V, 
   keep_best<THREADS>(L, L.count, k);
 }
 
+// A maximum m, S = sum of exp(x - m) and T = sum of exp(x - m) (x - m).
+struct Sums {
+  float m, s, t;
+};
+// The same over the workgroup: lanes, then waves in order.  unit: log2 of the base
+// that the sums are in.  All threads call it.
+template <int THREADS>
+__device__ __forceinline__ void join(ScoreLds& L, Sums& w, float unit) {
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) {
+    const float om = __shfl_xor(w.m, off, kWave), os = __shfl_xor(w.s, off, kWave), ot = __shfl_xor(w.t, off, kWave);
+    const float mm = fmaxf(w.m, om), da = fmaxf(w.m - mm, -1e4f), db = fmaxf(om - mm, -1e4f);
+    const float ea = __builtin_amdgcn_exp2f(da * unit), eb = __builtin_amdgcn_exp2f(db * unit);
+    w.t = ea * (w.t + w.s * da) + eb * (ot + os * db);
+    w.s = ea * w.s + eb * os;
+    w.m = mm;
+  }
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) {
+    L.m[threadIdx.x >> 6] = w.m;
+    L.s[threadIdx.x >> 6] = w.s;
+    L.t[threadIdx.x >> 6] = w.t;
+  }
+  __syncthreads();
+  w.m = L.m[0];
+  for (int i = 1; i < THREADS / kWave; ++i) w.m = fmaxf(w.m, L.m[i]);
+  w.s = w.t = 0.0f;
+  for (int i = 0; i < THREADS / kWave; ++i) {
+    const float d = fmaxf(L.m[i] - w.m, -1e4f), e = __builtin_amdgcn_exp2f(d * unit);
+    w.t += e * (L.t[i] + L.s[i] * d);
+    w.s += e * L.s[i];
+  }
+}
+
+// The sums of a row in natural units, which hold for every finite value.
+template <bool BF16, int THREADS>
+__device__ __attribute__((noinline)) Sums sums_again(const void* row, int V, ScoreLds& L) {
+  Sums w = {kLowest, 0.0f, 0.0f};
+  for (int i = threadIdx.x; i < V; i += THREADS) {
+    const float x = value_at<BF16>(row, i), grown = fmaxf(w.m, x), step = fmaxf(w.m - grown, -1e4f);
+    const float alpha = __builtin_amdgcn_exp2f(step * kLog2e);
+    const float d = x - grown, p = __builtin_amdgcn_exp2f(d * kLog2e);  // (NaN for NaN and +inf)
+    w.t = alpha * (w.t + w.s * step) + p * fmaxf(d, -1e4f);
+    w.s = alpha * w.s + p;
+    w.m = grown;
+  }
+  join<THREADS>(L, w, kLog2e);
+  return w;
+}
+
 template <bool BF16, int THREADS>
 __global__ __launch_bounds__(THREADS) void scores_kernel(ScoresArgs a) {
   typedef Tile<BF16, THREADS> T_;
   __shared__ ScoreLds L;
-  const int r = blockIdx.x, tid = threadIdx.x, wave = tid >> 6, V = a.V, k = a.k;
+  const int r = blockIdx.x, tid = threadIdx.x, V = a.V, k = a.k;
   constexpr int ESIZE = BF16 ? 2 : 4;
   const char* row = (const char*)a.logits + (size_t)r * a.stride * ESIZE;
   // tiles start on the 16-byte boundary at or before the row
@@ -183,28 +233,34 @@ __global__ __launch_bounds__(THREADS) void scores_kernel(ScoresArgs a) {
     L.count = 0;
     L.bound = -INFINITY;
   }
-  float m = kLowest, S = 0.0f, T = 0.0f, bound = -INFINITY;
+  Sums w = {-1e37f, 0.0f, 0.0f};  // (in the log2 domain: one product less per value)
+  float bound = -INFINITY;
   T_ tile, ahead;
   ahead.load(row, -lead, V);
   int done = 0;  // tiles
   for (long base = -lead; base < V; base += T_::SIZE) {
     tile = ahead;
     if (base + T_::SIZE < V) ahead.load(row, base + T_::SIZE, V);
-    float top = tile.value(0);
+    float tops[kPieces], top = -INFINITY;  // largest values of the pieces, of all
 #pragma unroll
-    for (int e = 1; e < T_::PER; ++e) top = fmaxf(top, tile.value(e));
-    const float grown = fmaxf(m, top);
-    const float step = fmaxf(m - grown, -1e4f);  // (0 where the maximum stays)
-    const float alpha = __builtin_amdgcn_exp2f(step * kLog2e);
-    T = alpha * (T + S * step);
-    S = alpha * S;
-    m = grown;
+    for (int v = 0; v < kPieces; ++v) {
+      tops[v] = tile.value(v * T_::N);
+#pragma unroll
+      for (int e = 1; e < T_::N; ++e) tops[v] = fmaxf(tops[v], tile.value(v * T_::N + e));
+      top = fmaxf(top, tops[v]);
+    }
+    const float grown = fmaxf(w.m, top * kLog2e);
+    const float step = fmaxf(w.m - grown, -1e4f);  // (0 where the maximum stays)
+    const float alpha = __builtin_amdgcn_exp2f(step);
+    w.t = alpha * (w.t + w.s * step);
+    w.s = alpha * w.s;
+    w.m = grown;
 #pragma unroll
     for (int e = 0; e < T_::PER; ++e) {
-      const float d = tile.value(e) - m;  // (NaN for NaN and +inf: S tells)
-      const float p = __builtin_amdgcn_exp2f(d * kLog2e);
-      S += p;
-      T += p * fmaxf(d, -1e4f);  // (0 (-inf) is no number)
+      const float d = __builtin_fmaf(tile.value(e), kLog2e, -w.m);
+      const float p = __builtin_amdgcn_exp2f(d);
+      w.s += p;
+      w.t += p * fmaxf(d, -1e4f);  // (0 (-inf) is no number)
     }
     if (k > 0) {
       if (done == 0) {  // the first tile: the bound
@@ -228,9 +284,11 @@ __global__ __launch_bounds__(THREADS) void scores_kernel(ScoresArgs a) {
         __syncthreads();
         bound = fmaxf(L.bound, kLowest);  // (-inf is no alternative)
       }
-      if (__any(top >= bound)) {
 #pragma unroll
-        for (int e = 0; e < T_::PER; ++e) {
+      for (int v = 0; v < kPieces; ++v) {
+        if (!__any(tops[v] >= bound)) continue;
+#pragma unroll
+        for (int e = v * T_::N; e < (v + 1) * T_::N; ++e) {
           const float x = tile.value(e);
           const uint64_t hits = __ballot(x >= bound);
           if (hits == 0) continue;
@@ -248,43 +306,24 @@ __global__ __launch_bounds__(THREADS) void scores_kernel(ScoresArgs a) {
       }
     }
   }
-  // (m, S, T) over the workgroup: lanes, then waves in order
-#pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) {
-    const float om = __shfl_xor(m, off, kWave), os = __shfl_xor(S, off, kWave), ot = __shfl_xor(T, off, kWave);
-    const float mm = fmaxf(m, om), da = fmaxf(m - mm, -1e4f), db = fmaxf(om - mm, -1e4f);
-    const float ea = __builtin_amdgcn_exp2f(da * kLog2e), eb = __builtin_amdgcn_exp2f(db * kLog2e);
-    T = ea * (T + S * da) + eb * (ot + os * db);
-    S = ea * S + eb * os;
-    m = mm;
-  }
-  if ((tid & 63) == 0) {
-    L.m[wave] = m;
-    L.s[wave] = S;
-    L.t[wave] = T;
-  }
-  __syncthreads();
-  m = kLowest;
-  for (int w = 0; w < (THREADS / kWave); ++w) m = fmaxf(m, L.m[w]);
-  S = T = 0.0f;
-  for (int w = 0; w < (THREADS / kWave); ++w) {
-    const float d = fmaxf(L.m[w] - m, -1e4f), e = __builtin_amdgcn_exp2f(d * kLog2e);
-    T += e * (L.t[w] + L.s[w] * d);
-    S += e * L.s[w];
-  }
-  const bool none = S == 0.0f, bad = S != S;
-  const float logS = none ? 0.0f : logf(S);
-  const float lse = bad ? S : none ? -INFINITY : m + logS;
+  join<THREADS>(L, w, 1.0f);
+  // A sum of 0 or NaN: a row of nothing but -inf, with a NaN or +inf -- or with
+  // values so large that their log2 is no fp32 number.
+  const bool plain = w.s > 0.0f;
+  if (!plain) w = sums_again<BF16, THREADS>(row, V, L);
+  const bool none = w.s == 0.0f, bad = w.s != w.s;
+  const float unit = plain ? kLn2 : 1.0f, logS = none ? 0.0f : plain ? log2f(w.s) : logf(w.s);
+  auto log_prob = [&](float x) { return fminf(((plain ? __builtin_fmaf(x, kLog2e, -w.m) : x - w.m) - logS) * unit, 0.0f); };
   if (tid == 0) {
-    stg(a.lse + r, lse);
-    stg(a.entropy + r, bad ? S : none ? 0.0f : logS - T / S);
+    stg(a.lse + r, bad ? w.s : none ? -INFINITY : (w.m + logS) * unit);
+    stg(a.entropy + r, bad ? w.s : none ? 0.0f : (logS - w.t / w.s) * unit);
   }
   // the given tokens under this row
   auto score = [&](int q) {
     const int t = ldg(a.tokens + q);
     float v = 0.0f;
     if (t >= V) v = NAN;
-    else if (t >= 0) v = bad ? S : none ? -INFINITY : (value_at<BF16>(row, t) - m) - logS;
+    else if (t >= 0) v = bad ? w.s : none ? -INFINITY : log_prob(value_at<BF16>(row, t));
     stg(a.logprob + q, v);
   };
   if (a.row_of == nullptr) {
@@ -308,7 +347,7 @@ __global__ __launch_bounds__(THREADS) void scores_kernel(ScoresArgs a) {
   if (tid < k) {
     const uint64_t e = L.keep[tid];
     stg(a.top_token + (size_t)r * k + tid, e ? (int)~(uint32_t)e : -1);
-    stg(a.top_logprob + (size_t)r * k + tid, bad ? S : e ? (unordered((uint32_t)(e >> 32)) - m) - logS : -INFINITY);
+    stg(a.top_logprob + (size_t)r * k + tid, bad ? w.s : e ? log_prob(unordered((uint32_t)(e >> 32))) : -INFINITY);
   }
 }
 
