@@ -440,7 +440,7 @@ size_t llmcad_batch_workspace_bytes(const llmcad_config* cfg, int32_t n_kv_heads
  * that the plan did not place, are left as they were.
  *
  * Errors: as llmcad_batch_store; LLMCAD_ECAPACITY unless 0 <= prefix_len <=
- * capacity and capacity is a positive multiple of 64 (with a prefix);
+ * capacity and capacity is a positive multiple of 64 up to 2^24 (with a prefix);
  * LLMCAD_EWORKSPACE for a plan or workspace that is too small.
  */
 int llmcad_batch_attention(const llmcad_config* cfg, int32_t n_kv_heads, int32_t layer, const void* q, int64_t q_stride,

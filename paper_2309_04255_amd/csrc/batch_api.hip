@@ -166,7 +166,8 @@ int llmcad_batch_attention(const llmcad_config* cfg, int32_t n_kv_heads, int32_t
   if (prefix_len < 0) return LLMCAD_ECAPACITY;
   if (prefix_len > 0) {
     if (!k_cache || !v_cache || !aligned16(k_cache) || !aligned16(v_cache)) return LLMCAD_EARG;
-    if (capacity < 64 || capacity % 64 != 0 || prefix_len > capacity) return LLMCAD_ECAPACITY;
+    // (the offset of a value within a head's V^T is 32 bits)
+    if (capacity < 64 || capacity % 64 != 0 || capacity > (1 << 24) || prefix_len > capacity) return LLMCAD_ECAPACITY;
   }
   const int64_t H = cfg->n_heads, Dh = cfg->head_dim;
   if (q_stride < H * Dh) return LLMCAD_ESHAPE;

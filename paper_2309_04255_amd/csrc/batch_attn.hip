@@ -185,6 +185,7 @@ struct TileWork {
   static constexpr int NS = Frags<DH>::NS, NB = Frags<DH>::NB;
   static constexpr int STEPS = 1;
   static constexpr int KEYS = 32 * STEPS;       // of a tile: half a page
+  static_assert(STEPS == 1, "a wave fetches one key block, or half of the dims");
   static constexpr int PARTS = kTileKeys / KEYS;
   static constexpr int HALF = KEYS * DH * 2;    // bytes of a tile's keys, or of its values
   static constexpr int FLAG = 4 * HALF;         // (a flag behind the buffers)
@@ -203,7 +204,8 @@ struct TileWork {
   Strays strays[RB];
   bool there;
   PageIds pages;
-  uint32_t lane_at[4];  // byte offset of the lane's part of a fetched KiB, by the KiB's index
+  const char* src;          // where this wave's part of the next tile to fetch begins
+  uint32_t lane_at[PER];    // byte offsets from there of the lane's pieces, by KiB
 
   __device__ __forceinline__ TileWork(const AttnArgs& a_, const Unit& u_, char* lds_) : a(a_), u(u_), lds(lds_) {
     lane = threadIdx.x & 63;
@@ -239,34 +241,29 @@ struct TileWork {
   // waves 0 and 1 fetch a step's keys each, 2 and 3 half of the values' dims each
   __device__ __forceinline__ bool values() const { return wave >= 2; }
   __device__ __forceinline__ void place_lanes() {
+    const int part = wave & 1;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (values()) {
-        const int dim = lane / (VROW / 16), piece = lane % (VROW / 16);
-        lane_at[i] = ((uint32_t)dim * (PAGED ? kPage : a.cap) + 8 * (piece ^ swap(VROW, i * DIMS + dim))) * 2;
-      } else {
-        const int row = lane / (ROW / 16), piece = lane % (ROW / 16);
-        lane_at[i] = (8 * (row >> 2) + (row & 3)) * ROW + (piece ^ swap(ROW, i % NS * ROWS + row)) * 16;
+    for (int e = 0; e < PER; ++e)
+      if (values()) {  // dims DIMS (PER part + e) ..
+        const int dim = DIMS * (PER * part + e) + lane / (VROW / 16), piece = lane % (VROW / 16);
+        lane_at[e] = ((uint32_t)dim * (PAGED ? kPage : a.cap) + 8 * (piece ^ swap(VROW, dim & 15))) * 2;
+      } else {  // key block `part`, rows ROWS e .. of it (key 8 (row / 4) + 4 part + row % 4)
+        const int row = ROWS * e + lane / (ROW / 16), piece = lane % (ROW / 16);
+        lane_at[e] = (8 * (row >> 2) + 4 * part + (row & 3)) * ROW + (piece ^ swap(ROW, row)) * 16;
       }
+    if (!PAGED) set_src(prefix_tile(a, u, first / PARTS), first);
   }
-  // copies this wave's part of tile t straight to LDS
+  __device__ __forceinline__ void set_src(const TileAt& at, int t) {
+    const int key = t % PARTS * KEYS;
+    src = values() ? (const char*)(at.v + key) : (const char*)(at.k + key * DH);
+  }
+  // copies this wave's part of tile t straight to LDS (called for one tile after the other)
   __device__ __forceinline__ void fetch(int t) {
-    const TileAt at = PAGED ? page_tile(a, u, pages.get(u, t / PARTS)) : prefix_tile(a, u, t / PARTS);
-    const int key = t % PARTS * KEYS, part = wave & 1;
-    if (values()) {
-      char* to = lds + (2 + (t & 1)) * HALF + part * PER * 1024;
-      const bf16* v = at.v + key + (size_t)(DIMS * PER * part) * at.vs;
+    if (PAGED && (t % PARTS == 0 || t == first)) set_src(page_tile(a, u, pages.get(u, t / PARTS)), t);
+    char* to = lds + ((values() ? 2 : 0) + (t & 1)) * HALF + (wave & 1) * PER * 1024;
 #pragma unroll
-      for (int e = 0; e < PER; ++e) dma16((const char*)(v + (size_t)(DIMS * e) * at.vs) + lane_at[e & 3], to + e * 1024);
-    } else {  // (a part: a step's keys, or with tiles of one step a key block's)
-      char* to = lds + (t & 1) * HALF + part * PER * 1024;
-      const char* k = (const char*)(at.k + (key + (STEPS == 2 ? 32 : 4) * part) * DH);
-#pragma unroll
-      for (int e = 0; e < PER; ++e) {  // key block e / NS, rows ROWS (e % NS) .. of it: keys 2 ROWS (e % NS) + 4 (e / NS) ..
-        const int i = e % NS;
-        dma16(k + (2 * ROWS * i + 4 * (e / NS)) * ROW + lane_at[i], to + e * 1024);
-      }
-    }
+    for (int e = 0; e < PER; ++e) dma16(src + lane_at[e], to + e * 1024);
+    src += values() ? VROW : KEYS * ROW;
   }
 
   // scores of tile t (its keys in LDS)

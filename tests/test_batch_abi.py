@@ -107,7 +107,7 @@ def _attention(binding, cfg, **kw):
 
 @pytest.mark.parametrize("kw,status", [
     (dict(Hkv=3), "ESHAPE"), (dict(layer=32), "EARG"), (dict(q=None), "EARG"), (dict(qs=4088), "ESHAPE"), (dict(qs=4100), "EARG"),
-    (dict(kc=None), "EARG"), (dict(vc=FAKE + 2), "EARG"), (dict(cap=100), "ECAPACITY"), (dict(cap=64), "ECAPACITY"),
+    (dict(kc=None), "EARG"), (dict(vc=FAKE + 2), "EARG"), (dict(cap=100), "ECAPACITY"), (dict(cap=64), "ECAPACITY"), (dict(cap=(1 << 24) + 64), "ECAPACITY"),
     (dict(prefix=-1), "ECAPACITY"), (dict(prefix=129), "ECAPACITY"), (dict(kp=None), "EARG"), (dict(table=None), "EARG"),
     (dict(max_pages=0), "EARG"), (dict(out=FAKE + 4), "EARG"), (dict(ws=None), "EARG"), (dict(ws_bytes=1000), "EWORKSPACE"),
     (dict(bytes=1000), "EWORKSPACE"), (dict(B=2000), "EARG"), (dict(N=-1), "EARG"),
