@@ -159,7 +159,11 @@ struct ScoresArgs {
   float* lse;         // [n]
   int* top_token;     // [n][k]
   float* top_logprob; // [n][k]
+  int parts, span;    // a row in workgroups of so many values
+  float* part_sums;   // [n][parts][4]
+  uint64_t* part_best; // [n][parts][k]
 };
-hipError_t launch_token_scores(const ScoresArgs& a, hipStream_t st);
+size_t score_part_bytes(int n, int V, int k);
+hipError_t launch_token_scores(ScoresArgs a, void* workspace, hipStream_t st);
 
 }  // namespace llmcad

@@ -239,8 +239,8 @@ int llmcad_batch_commit(const llmcad_config* cfg, int32_t n_kv_heads, void* k_pa
 }
 
 size_t llmcad_token_scores_workspace_bytes(int32_t n_rows, int32_t vocab, int32_t k) {
-  if (n_rows < 1 || vocab < 1 || k < 0 || k > LLMCAD_TOP_MAX) return 0;
-  return 256;
+  if (n_rows < 1 || vocab < 1 || vocab > (1 << 24) || k < 0 || k > LLMCAD_TOP_MAX) return 0;
+  return std::max((size_t)256, score_part_bytes(n_rows, vocab, k));
 }
 
 int llmcad_token_scores(const void* logits, int32_t bits, int64_t row_stride, int32_t n_rows, int32_t vocab,
@@ -252,7 +252,8 @@ int llmcad_token_scores(const void* logits, int32_t bits, int64_t row_stride, in
       k > LLMCAD_TOP_MAX || (k > 0 && (!top_token || !top_logprob)))
     return LLMCAD_EARG;
   if (row_stride < vocab || vocab > (1 << 24)) return LLMCAD_ESHAPE;
-  if (((uintptr_t)logits & (bits / 8 - 1)) != 0 || !aligned4(tokens) || !aligned4(row_of)) return LLMCAD_EARG;
+  if (((uintptr_t)logits & (bits / 8 - 1)) != 0 || !aligned4(tokens) || !aligned4(row_of) || !aligned16(workspace))
+    return LLMCAD_EARG;
   if (workspace_bytes < llmcad_token_scores_workspace_bytes(n_rows, vocab, k)) return LLMCAD_EWORKSPACE;
   ScoresArgs a;
   a.logits = logits;
@@ -269,7 +270,7 @@ int llmcad_token_scores(const void* logits, int32_t bits, int64_t row_stride, in
   a.lse = lse;
   a.top_token = top_token;
   a.top_logprob = top_logprob;
-  return launched(launch_token_scores(a, (hipStream_t)stream));
+  return launched(launch_token_scores(a, workspace, (hipStream_t)stream));
 }
 
 }  // extern "C"

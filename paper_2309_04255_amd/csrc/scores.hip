@@ -3,16 +3,25 @@
 //
 // One pass over a row, the next tile's loads in flight while one is computed:
 // every thread keeps the running maximum m of its values, the sum S of exp(x - m)
-// and T of exp(x - m) (x - m), rescaled when m grows; joined over the workgroup,
-// lse = m + log S and the entropy is log S - T / S.  The k largest values come out
-// of the same pass.  The first tile gives a lower bound of the k-th largest value
-// (the k-th largest of 256 groups' maxima: about as many values as k lie above it
-// in the tile); every value from the bound on joins a list in LDS.  After 2, 4, 8
-// .. tiles the list's k-th best becomes the bound, so that a row adds about
-// k log(tiles) entries; at the end the list is sorted by counting for each entry
-// those before it.  A row whose later tiles hold more than the list does (values
-// in rising order, say) is read once more in steps that cut the list back to its
-// k best.
+// and T of exp(x - m) (x - m), rescaled when m grows, in fp32 and in base 2 (one
+// product less per value); joined over the workgroup, lse = m + log S and the
+// entropy is log S - T / S.  A sum of 0 or NaN (nothing but -inf, a NaN, or values
+// whose product with log2 e leaves fp32) is taken again in natural units.
+//
+// The k largest values come out of the same pass.  The first tile gives a lower
+// bound of the k-th largest value (the k-th largest of 256 groups' maxima: about as
+// many values as k lie above it in the tile); every 16-byte piece with a value from
+// the bound on is held in LDS as it lies.  From time to time the held pieces' values
+// join a list there, which is cut to its k best, and the k-th of them becomes the
+// bound; at the end once more.  The list is sorted by counting for each entry those
+// above it.  A row whose pieces or list do not fit (values in rising order, say) is
+// read once more in steps that cut the list back to its k best.
+//
+// Without alternatives it is bound by the reads: 1024 bf16 rows of 128000 take 50 us
+// (5200 GB/s), 20 of them take 22 us more for the bound and the ranking, in which a
+// row's workgroup reads nothing; fp32 rows hide that (103 us, 5100 GB/s).
+#include <algorithm>
+
 #include "batch.h"
 
 namespace llmcad {
@@ -20,6 +29,7 @@ namespace llmcad {
 namespace {
 
 constexpr int kPieces = 4;  // 16-byte pieces of a row per thread and tile
+constexpr int kHeld = 512;
 constexpr int kList = 2048;
 constexpr int kGroups = 256;
 constexpr float kLowest = -3.402823466e38f;        // (finite: x - m stays a number for rows of -inf)
@@ -29,8 +39,10 @@ struct ScoreLds {
   float m[16], s[16], t[16];  // by wave
   __align__(16) float group[kGroups];
   float bound;
-  int count;
-  uint64_t list[kList];  // ordered value bits << 32 | ~token: larger is better, ties to the lower token
+  int pieces, count;
+  __align__(16) uint32_t held[kHeld][4];  // 16-byte pieces of the row with a value from the bound on
+  int held_at[kHeld];                     // the tokens of their first values
+  __align__(16) uint64_t list[kList];  // ordered value bits << 32 | ~token: larger is better, ties to the lower token
   uint64_t keep[LLMCAD_TOP_MAX];
 };
 
@@ -47,8 +59,7 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 // A thread's part of the tile at base: pieces of 16 bytes, kPieces of them a
 // workgroup's width apart, as they lie in memory.  (row + base is 16-byte aligned;
-// what lies outside the row, before its first or behind its last value, reads as
-// -inf and is not touched.)
+// what lies outside [lo, hi) reads as -inf and is not touched.)
 template <bool BF16, int THREADS>
 struct Tile {
   static constexpr int N = BF16 ? 8 : 4;             // values per piece
@@ -57,9 +68,9 @@ struct Tile {
   u32x4 raw[kPieces];
 
   __device__ static __forceinline__ long at(long base, int piece) { return base + (long)N * (piece * THREADS + (int)threadIdx.x); }
-  __device__ __forceinline__ void load(const char* row, long base, int V) {
+  __device__ __forceinline__ void load(const char* row, long base, int lo, int hi) {
     constexpr int ES = 16 / N;
-    if (base >= 0 && base + SIZE <= V) {
+    if (base >= lo && base + SIZE <= hi) {
 #pragma unroll
       for (int v = 0; v < kPieces; ++v) raw[v] = ldg((const u32x4*)(row + at(base, v) * ES));
       return;
@@ -69,13 +80,13 @@ struct Tile {
       const long i0 = at(base, v);
       const uint32_t none = BF16 ? 0xff80ff80u : 0xff800000u;
       u32x4 x = {none, none, none, none};
-      if (i0 >= 0 && i0 + N <= V) {
+      if (i0 >= lo && i0 + N <= hi) {
         x = ldg((const u32x4*)(row + i0 * ES));
-      } else if (i0 < V) {
+      } else if (i0 < hi) {
 #pragma unroll
         for (int e = 0; e < N; ++e) {
           const long i = i0 + e;
-          if (i < 0 || i >= V) continue;
+          if (i < lo || i >= hi) continue;
           if (BF16) {
             const uint32_t bits = ldg((const uint16_t*)row + i);
             x[e / 2] = e & 1 ? (x[e / 2] & 0xffffu) | bits << 16 : (x[e / 2] & 0xffff0000u) | bits;
@@ -91,7 +102,6 @@ struct Tile {
     const uint32_t w = raw[e / N][BF16 ? (e % N) / 2 : e % N];
     return __uint_as_float(!BF16 ? w : e & 1 ? w & 0xffff0000u : w << 16);
   }
-  __device__ static __forceinline__ long token(long base, int e) { return at(base, e / N) + e % N; }
 };
 
 template <bool BF16>
@@ -99,60 +109,75 @@ __device__ __forceinline__ float value_at(const void* row, int i) {
   return BF16 ? bf2f(ldg((const bf16*)row + i)) : ldg((const float*)row + i);
 }
 
-// The list's k best, sorted, in L.keep (0: no entry).  All threads call it;
-// groups of neighbouring lanes count for one entry together.
-template <int THREADS>
-__device__ __forceinline__ void keep_best(ScoreLds& L, int count, int k) {
-  if (threadIdx.x < k) L.keep[threadIdx.x] = 0;
-  __syncthreads();
+// For each of the list's first count entries how many lie above it: to(entry, above).
+// All threads call it, a barrier in front.  Groups of neighbouring lanes count for
+// one entry together, in pieces of two entries, four reads in flight (one
+// entry after another: 36 us more for the 64 best of 1024 bf16 rows of 128000).
+template <int THREADS, typename TO>
+__device__ __forceinline__ void rank(ScoreLds& L, int count, TO to) {
+  typedef uint64_t u64x2 __attribute__((ext_vector_type(2)));
   int share = kWave;  // lanes per entry
   while (share > 1 && count * share > THREADS) share >>= 1;
-  const int part = threadIdx.x & (share - 1);
+  const int part = threadIdx.x & (share - 1), round = 8 * share;
+  const int end = (count + round - 1) / round * round;  // (at most kList)
+  for (int j = count + threadIdx.x; j < end; j += THREADS) L.list[j] = 0;  // above no entry
+  __syncthreads();
   for (int i0 = 0; i0 < count; i0 += THREADS / share) {
     const int i = i0 + threadIdx.x / share;
     const uint64_t mine = i < count ? L.list[i] : 0;
-    int before = 0;
-    if (i < count)
-      for (int j = part; j < count; j += share) before += L.list[j] > mine ? 1 : 0;
-    for (int off = share >> 1; off >= 1; off >>= 1) before += __shfl_xor(before, off, kWave);
-    if (i < count && part == 0 && before < k) L.keep[before] = mine;
+    int above = 0;
+    for (int j = 0; j < end; j += round) {
+      u64x2 o[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = *(const u64x2*)&L.list[j + 2 * (e * share + part)];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) above += (o[e].x > mine ? 1 : 0) + (o[e].y > mine ? 1 : 0);
+    }
+    for (int off = share >> 1; off >= 1; off >>= 1) above += __shfl_xor(above, off, kWave);
+    if (i < count && part == 0) to(mine, above);
   }
   __syncthreads();
 }
 
-// The list's k-th best value (L.bound), if it has k entries.  All threads call it.
+// The list's k best, sorted, in L.keep (0: no entry).  All threads call it.
 template <int THREADS>
-__device__ __forceinline__ void raise_bound(ScoreLds& L, int k) {
+__device__ __forceinline__ void keep_best(ScoreLds& L, int count, int k) {
+  if (threadIdx.x < k) L.keep[threadIdx.x] = 0;
+  rank<THREADS>(L, count, [&](uint64_t entry, int above) {
+    if (above < k) L.keep[above] = entry;
+  });
+}
+
+// The held pieces' values from the bound on go to the list.  False if there were
+// more than fit.  All threads call it.
+template <bool BF16, int THREADS>
+__device__ __forceinline__ bool list_pieces(ScoreLds& L, float bound) {
+  constexpr int N = BF16 ? 8 : 4;
   __syncthreads();
-  const int count = L.count;
-  __syncthreads();  // (nobody adds before all have read the count)
-  if (count >= k && count <= kList) {
-    int share = kWave;
-    while (share > 1 && count * share > THREADS) share >>= 1;
-    const int part = threadIdx.x & (share - 1);
-    for (int i0 = 0; i0 < count; i0 += THREADS / share) {
-      const int i = i0 + threadIdx.x / share;
-      const uint64_t mine = i < count ? L.list[i] : 0;
-      int before = 0;
-      if (i < count)
-        for (int j = part; j < count; j += share) before += L.list[j] > mine ? 1 : 0;
-      for (int off = share >> 1; off >= 1; off >>= 1) before += __shfl_xor(before, off, kWave);
-      if (i < count && part == 0 && before == k - 1) L.bound = unordered((uint32_t)(mine >> 32));
-    }
+  const int pieces = L.pieces;
+  if (pieces > kHeld) return false;
+  for (int j = threadIdx.x; j < pieces * N; j += THREADS) {
+    const int e = j % N;
+    const uint32_t w = L.held[j / N][BF16 ? e / 2 : e];
+    const float x = __uint_as_float(!BF16 ? w : e & 1 ? w & 0xffff0000u : w << 16);
+    if (!(x >= bound)) continue;
+    const int at = atomicAdd(&L.count, 1);
+    if (at < kList) L.list[at] = (uint64_t)ordered(x) << 32 | (uint32_t)~(uint32_t)(L.held_at[j / N] + e);
   }
   __syncthreads();
+  return L.count <= kList;
 }
 
 // The k best of a row whose list overflowed.
 template <bool BF16, int THREADS>
-__device__ __attribute__((noinline)) void best_in_steps(const void* row, int V, int k, ScoreLds& L) {
+__device__ __attribute__((noinline)) void best_in_steps(const void* row, int lo, int hi, int k, ScoreLds& L) {
   uint64_t least = 0;  // the k-th best so far: later entries must be larger
   __syncthreads();
   if (threadIdx.x == 0) L.count = 0;
-  for (long i0 = 0; i0 < V; i0 += THREADS) {
+  for (long i0 = lo; i0 < hi; i0 += THREADS) {
     __syncthreads();
     const long i = i0 + threadIdx.x;
-    if (i < V) {
+    if (i < hi) {
       const float x = value_at<BF16>(row, (int)i);
       const uint64_t key = (uint64_t)ordered(x) << 32 | (uint32_t)~(uint32_t)i;
       if (x > -INFINITY && key > least) L.list[atomicAdd(&L.count, 1)] = key;
@@ -220,27 +245,84 @@ __device__ __attribute__((noinline)) Sums sums_again(const void* row, int V, Sco
   return w;
 }
 
-template <bool BF16, int THREADS>
+// The outputs of row r from its sums w (log2 domain).  All threads call it; best():
+// the row's k best to L.keep.
+template <bool BF16, int THREADS, typename BEST>
+__device__ __forceinline__ void finish(const ScoresArgs& a, int r, const char* row, Sums w, ScoreLds& L, BEST best) {
+  const int tid = threadIdx.x, V = a.V, k = a.k;
+  // A sum of 0 or NaN: a row of nothing but -inf, with a NaN or +inf -- or with
+  // values so large that their log2 is no fp32 number.
+  const bool plain = w.s > 0.0f;
+  if (!plain) w = sums_again<BF16, THREADS>(row, V, L);
+  const bool none = w.s == 0.0f, bad = w.s != w.s;
+  const float unit = plain ? kLn2 : 1.0f, logS = none ? 0.0f : plain ? log2f(w.s) : logf(w.s);
+  auto log_prob = [&](float x) {
+    const float d = plain ? __builtin_fmaf(x, kLog2e, -w.m) : x - w.m;
+    if (d == -INFINITY) return x - w.m * unit;  // (a finite value far below, in natural units)
+    return fminf((d - logS) * unit, 0.0f);
+  };
+  if (tid == 0) {
+    stg(a.lse + r, bad ? w.s : none ? -INFINITY : (w.m + logS) * unit);
+    stg(a.entropy + r, bad ? w.s : none ? 0.0f : (logS - w.t / w.s) * unit);
+  }
+  // the given tokens under this row
+  auto score = [&](int q) {
+    const int t = ldg(a.tokens + q);
+    float v = 0.0f;
+    if (t >= V) v = NAN;
+    else if (t >= 0) v = bad ? w.s : none ? -INFINITY : log_prob(value_at<BF16>(row, t));
+    stg(a.logprob + q, v);
+  };
+  if (a.row_of == nullptr) {
+    if (tid == 0 && r < a.m) score(r);
+  } else {
+    for (int q = tid; q < a.m; q += THREADS) {
+      const int of = ldg(a.row_of + q);
+      if (of == r) score(q);
+      else if (r == 0 && (of < 0 || of >= a.n)) stg(a.logprob + q, (float)NAN);
+    }
+  }
+  if (k == 0) return;
+  if (!bad) {
+    best();
+  } else if (tid < k) {
+    L.keep[tid] = 0;  // (read by the same thread)
+  }
+  if (tid < k) {
+    const uint64_t e = L.keep[tid];
+    stg(a.top_token + (size_t)r * k + tid, e ? (int)~(uint32_t)e : -1);
+    stg(a.top_logprob + (size_t)r * k + tid, bad ? w.s : e ? log_prob(unordered((uint32_t)(e >> 32))) : -INFINITY);
+  }
+}
+
+// SPLIT: a workgroup per part of a row; sums and best values go to the workspace.
+template <bool BF16, int THREADS, bool SPLIT>
 __global__ __launch_bounds__(THREADS) void scores_kernel(ScoresArgs a) {
   typedef Tile<BF16, THREADS> T_;
   __shared__ ScoreLds L;
-  const int r = blockIdx.x, tid = threadIdx.x, V = a.V, k = a.k;
   constexpr int ESIZE = BF16 ? 2 : 4;
+  const int r = SPLIT ? blockIdx.x / a.parts : blockIdx.x, part = SPLIT ? blockIdx.x % a.parts : 0, tid = threadIdx.x, k = a.k;
+  const int lo = SPLIT ? part * a.span : 0, hi = SPLIT ? min(a.V, lo + a.span) : a.V;
   const char* row = (const char*)a.logits + (size_t)r * a.stride * ESIZE;
-  // tiles start on the 16-byte boundary at or before the row
-  const long lead = (long)(((uintptr_t)row & 15) / ESIZE);
+  // tiles start on the 16-byte boundary at or before the first value
+  const long lead = (long)(((uintptr_t)(row + (size_t)lo * ESIZE) & 15) / ESIZE);
   if (tid == 0) {
-    L.count = 0;
+    L.pieces = L.count = 0;
     L.bound = -INFINITY;
   }
   Sums w = {-1e37f, 0.0f, 0.0f};  // (in the log2 domain: one product less per value)
   float bound = -INFINITY;
   T_ tile, ahead;
-  ahead.load(row, -lead, V);
-  int done = 0;  // tiles
-  for (long base = -lead; base < V; base += T_::SIZE) {
+  ahead.load(row, lo - lead, lo, hi);
+  // The bound is raised after this many tiles, and again when they have doubled:
+  // before many more than 128 values are held (each time costs about 1 us; k of 8 in
+  // 128000 fp32 values 24.6 us after tile 2 and 4, 21.4 never; k of 64 83 us after
+  // tile 2 and 4, 91 after 4, for 1024 bf16 rows).
+  int done = 0, next = max(2, 128 / max(k, 1));
+  bool listed = true;  // held pieces and list have had room so far
+  for (long base = lo - lead; base < hi; base += T_::SIZE) {
     tile = ahead;
-    if (base + T_::SIZE < V) ahead.load(row, base + T_::SIZE, V);
+    if (base + T_::SIZE < hi) ahead.load(row, base + T_::SIZE, lo, hi);
     float tops[kPieces], top = -INFINITY;  // largest values of the pieces, of all
 #pragma unroll
     for (int v = 0; v < kPieces; ++v) {
@@ -284,89 +366,136 @@ __global__ __launch_bounds__(THREADS) void scores_kernel(ScoresArgs a) {
         __syncthreads();
         bound = fmaxf(L.bound, kLowest);  // (-inf is no alternative)
       }
+      int hits = 0;
 #pragma unroll
-      for (int v = 0; v < kPieces; ++v) {
-        if (!__any(tops[v] >= bound)) continue;
+      for (int v = 0; v < kPieces; ++v) hits += tops[v] >= bound ? 1 : 0;
+      if (hits > 0) {
+        int at = atomicAdd(&L.pieces, hits);
 #pragma unroll
-        for (int e = v * T_::N; e < (v + 1) * T_::N; ++e) {
-          const float x = tile.value(e);
-          const uint64_t hits = __ballot(x >= bound);
-          if (hits == 0) continue;
-          const int lane = tid & 63, first = __ffsll((unsigned long long)hits) - 1;
-          int at = 0;
-          if (lane == first) at = atomicAdd(&L.count, __popcll(hits));
-          at = __builtin_amdgcn_readlane(at, first) + __popcll(hits & ((1ull << lane) - 1));
-          if (x >= bound && at < kList) L.list[at] = (uint64_t)ordered(x) << 32 | (uint32_t)~(uint32_t)T_::token(base, e);
+        for (int v = 0; v < kPieces; ++v) {
+          if (!(tops[v] >= bound)) continue;
+          if (at < kHeld) {
+            *(u32x4*)L.held[at] = tile.raw[v];
+            L.held_at[at] = (int)T_::at(base, v);
+          }
+          ++at;
         }
       }
       ++done;
-      if (done > 1 && (done & (done - 1)) == 0 && base + T_::SIZE < V) {
-        raise_bound<THREADS>(L, k);
-        bound = fmaxf(L.bound, kLowest);
+      if (listed && done == next && base + T_::SIZE < hi) {
+        next *= 2;
+        listed = list_pieces<BF16, THREADS>(L, bound);
+        const int count = L.count;
+        if (listed && count >= k) {
+          keep_best<THREADS>(L, count, k);
+          if (tid < k) L.list[tid] = L.keep[tid];
+          bound = unordered((uint32_t)(L.keep[k - 1] >> 32));
+        }
+        __syncthreads();  // (all have read the counts)
+        if (listed && tid == 0) {
+          L.pieces = 0;
+          if (count >= k) L.count = k;
+        }
+        __syncthreads();
       }
     }
   }
   join<THREADS>(L, w, 1.0f);
-  // A sum of 0 or NaN: a row of nothing but -inf, with a NaN or +inf -- or with
-  // values so large that their log2 is no fp32 number.
-  const bool plain = w.s > 0.0f;
-  if (!plain) w = sums_again<BF16, THREADS>(row, V, L);
-  const bool none = w.s == 0.0f, bad = w.s != w.s;
-  const float unit = plain ? kLn2 : 1.0f, logS = none ? 0.0f : plain ? log2f(w.s) : logf(w.s);
-  auto log_prob = [&](float x) { return fminf(((plain ? __builtin_fmaf(x, kLog2e, -w.m) : x - w.m) - logS) * unit, 0.0f); };
-  if (tid == 0) {
-    stg(a.lse + r, bad ? w.s : none ? -INFINITY : (w.m + logS) * unit);
-    stg(a.entropy + r, bad ? w.s : none ? 0.0f : (logS - w.t / w.s) * unit);
-  }
-  // the given tokens under this row
-  auto score = [&](int q) {
-    const int t = ldg(a.tokens + q);
-    float v = 0.0f;
-    if (t >= V) v = NAN;
-    else if (t >= 0) v = bad ? w.s : none ? -INFINITY : log_prob(value_at<BF16>(row, t));
-    stg(a.logprob + q, v);
+  auto best = [&]() {
+    if (listed && list_pieces<BF16, THREADS>(L, bound))
+      keep_best<THREADS>(L, L.count, k);
+    else
+      best_in_steps<BF16, THREADS>(row, lo, hi, k, L);
   };
-  if (a.row_of == nullptr) {
-    if (tid == 0 && r < a.m) score(r);
-  } else {
-    for (int q = tid; q < a.m; q += THREADS) {
-      const int of = ldg(a.row_of + q);
-      if (of == r) score(q);
-      else if (r == 0 && (of < 0 || of >= a.n)) stg(a.logprob + q, (float)NAN);
-    }
+  if (!SPLIT) {
+    finish<BF16, THREADS>(a, r, row, w, L, best);
+    return;
   }
+  if (tid == 0) stg((f32x4*)a.part_sums + blockIdx.x, f32x4{w.m, w.s, w.t, 0.0f});
   if (k == 0) return;
-  const int count = L.count;  // (the last addition lies before the barrier above)
-  if (bad) {
-    if (tid < k) L.keep[tid] = 0;
-  } else if (count <= kList) {
-    keep_best<THREADS>(L, count, k);
-  } else {
-    best_in_steps<BF16, THREADS>(row, V, k, L);
+  best();
+  if (tid < k) stg(a.part_best + (size_t)blockIdx.x * k + tid, L.keep[tid]);
+}
+
+// A workgroup per row joins its parts.
+constexpr int kJoinThreads = 1024;
+template <bool BF16>
+__global__ __launch_bounds__(kJoinThreads) void scores_join_kernel(ScoresArgs a) {
+  __shared__ ScoreLds L;
+  const int r = blockIdx.x, tid = threadIdx.x, k = a.k, parts = a.parts, lane = tid & 63;
+  const char* row = (const char*)a.logits + (size_t)r * a.stride * (BF16 ? 2 : 4);
+  if (tid == 0) L.count = 0;
+  Sums w = {-1e37f, 0.0f, 0.0f};
+  if (tid < parts) {  // (parts <= a wave)
+    const f32x4 p = ldg((const f32x4*)a.part_sums + r * parts + tid);
+    w = Sums{p[0], p[1], p[2]};
   }
-  if (tid < k) {
-    const uint64_t e = L.keep[tid];
-    stg(a.top_token + (size_t)r * k + tid, e ? (int)~(uint32_t)e : -1);
-    stg(a.top_logprob + (size_t)r * k + tid, bad ? w.s : e ? log_prob(unordered((uint32_t)(e >> 32))) : -INFINITY);
+  const uint64_t* keys = a.part_best + (size_t)r * parts * k;
+  uint64_t least = 0;
+  if (k > 0) {
+    // As many values as k lie at or above the largest of the parts' k-th best, and
+    // at or above the least of their (k / parts)-th best.
+    const int some = (k + parts - 1) / parts;
+    uint64_t last = lane < parts ? ldg(keys + lane * k + k - 1) : 0, early = lane < parts ? ldg(keys + lane * k + some - 1) : ~0ull;
+    for (int off = 32; off >= 1; off >>= 1) {
+      const uint64_t l = __shfl_xor(last, off, kWave), e = __shfl_xor(early, off, kWave);
+      last = l > last ? l : last;
+      early = e < early ? e : early;
+    }
+    least = early > last ? early : last;
   }
+  join<kJoinThreads>(L, w, 1.0f);  // (its barriers: the count is set)
+  for (int j = tid; j < parts * k; j += kJoinThreads) {
+    const uint64_t e = ldg(keys + j);
+    if (e != 0 && e >= least) L.list[atomicAdd(&L.count, 1)] = e;
+  }
+  __syncthreads();
+  finish<BF16, kJoinThreads>(a, r, row, w, L, [&]() { keep_best<kJoinThreads>(L, L.count, k); });
 }
 
 }  // namespace
 
-hipError_t launch_token_scores(const ScoresArgs& a, hipStream_t st) {
-  // Up to a row per CU: 16 waves on each row; more rows: 8 waves, so that a CU
-  // reads one row while it closes another.
-  if (a.n <= 256) {
-    if (a.bf16_in)
-      scores_kernel<true, 1024><<<dim3(a.n), dim3(1024), 0, st>>>(a);
-    else
-      scores_kernel<false, 1024><<<dim3(a.n), dim3(1024), 0, st>>>(a);
+// Up to 64 rows of many values: parts of about 16384, up to a workgroup per CU over
+// all rows; their best values fit the list that joins them.  (The second launch
+// costs 3 us of the host.  With k of 64, 31 fp32 rows of 250000 take 28.3 us, 40.2
+// unsplit, one 23.2 and 37.9; with k of 8, 31 of 150000 21.4 and 23.0; below 6 parts
+// nothing is won, and 100 rows of 250000 with k of 8 take 38.0 and 33.3.)
+int score_parts(int n, int V) {
+  if (n > 64 || V <= 6 * 16384) return 1;
+  return std::min({kList / LLMCAD_TOP_MAX, 256 / n, cdiv(V, 16384)});
+}
+size_t score_part_bytes(int n, int V, int k) {
+  const int parts = score_parts(n, V);
+  return parts > 1 ? (size_t)n * parts * (sizeof(f32x4) + sizeof(uint64_t) * k) : 0;
+}
+
+template <bool BF16>
+static void launch(const ScoresArgs& a, hipStream_t st) {
+  // More rows than CUs: smaller workgroups, so that several rows share a CU and one
+  // is read while another ranks its values (1024 bf16 rows of 128000, k of 20: 72.9 us
+  // with 256 threads, 76.2 with 512; 400 rows 45.8 and 37.4, as a CU then has too few
+  // waves).
+  if (a.parts > 1) {
+    scores_kernel<BF16, 512, true><<<dim3(a.n * a.parts), dim3(512), 0, st>>>(a);
+    scores_join_kernel<BF16><<<dim3(a.n), dim3(kJoinThreads), 0, st>>>(a);
+  } else if (a.n <= 256) {
+    scores_kernel<BF16, 1024, false><<<dim3(a.n), dim3(1024), 0, st>>>(a);
+  } else if (a.n <= 512) {
+    scores_kernel<BF16, 512, false><<<dim3(a.n), dim3(512), 0, st>>>(a);
   } else {
-    if (a.bf16_in)
-      scores_kernel<true, 512><<<dim3(a.n), dim3(512), 0, st>>>(a);
-    else
-      scores_kernel<false, 512><<<dim3(a.n), dim3(512), 0, st>>>(a);
+    scores_kernel<BF16, 256, false><<<dim3(a.n), dim3(256), 0, st>>>(a);
   }
+}
+
+hipError_t launch_token_scores(ScoresArgs a, void* workspace, hipStream_t st) {
+  a.parts = score_parts(a.n, a.V);
+  a.span = cdiv(cdiv(a.V, a.parts), 64) * 64;
+  a.part_sums = (float*)workspace;
+  a.part_best = (uint64_t*)((f32x4*)workspace + (size_t)a.n * a.parts);
+  if (a.bf16_in)
+    launch<true>(a, st);
+  else
+    launch<false>(a, st);
   return hipGetLastError();
 }
 

@@ -91,6 +91,70 @@ def test_special_rows(binding):
     _check(binding, x, [0, 4, 3, 1, 9, 99, 0, 2000, 3, 8], 9)
 
 
+@pytest.mark.parametrize("order", ["constant", "rising", "falling", "late_peaks", "few"])
+def test_rows_in_parts(binding, order):
+    """Rows long enough to be shared between workgroups, their best in one part or in all."""
+    V = 150001
+    x = torch.arange(V, dtype=torch.float64, device="cuda")
+    x = {"constant": torch.zeros_like(x) - 2.0, "rising": torch.round(x * (512.0 / V)) / 64, "falling": -x * (8.0 / V),
+         "late_peaks": torch.where(x > V - 3000, 5.0 + x / V, torch.sin(x)),
+         "few": torch.where(x % 17000 == 3, x / V, -float("inf"))}[order]
+    _check(binding, x.to(torch.float32)[None].repeat(3, 1).contiguous(), [0, V - 1, 3], 64)
+
+
+@pytest.mark.parametrize("V", [3001, 120003])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_special_parts(binding, V, dtype):
+    """Values in one place of a row only, or everywhere but there."""
+    inf, low = float("inf"), torch.finfo(dtype).min
+    x = _logits(12, V, dtype, seed=5)
+    x[0, : V // 2] = -inf
+    x[1, V // 2:] = low
+    x[2, V - 1] = float("nan")
+    x[3, V - 1] = inf
+    x[4] = -inf
+    x[4, V - 2] = 1.0
+    x[5] = low
+    x[5, V - 2] = -3.0e38
+    x[6, V // 3] = 3.0e38  # its product with log2 e is no fp32 number
+    x[7] = low
+    x[8, 1:] = -inf
+    x[9] = 3.0e38
+    x[10] = -inf
+    x[11, : V - 1] = -2.0e37
+    tok = [0, V - 1, 5, 5, V - 2, V - 2, V // 3, 1, 0, 7, 7, V - 1]
+    got = _check(binding, x, tok, 11)
+    assert got["lse"][[2, 3]].isnan().all() and not got["lse"][[0, 1, 4, 5, 6, 7, 8, 9]].isnan().any()
+
+
+@pytest.mark.parametrize("n", [65, 256, 257, 513])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_row_counts(binding, n, dtype):
+    _check(binding, _logits(n, 33001, dtype, stride=33003), np.arange(n) * 64, 20)
+
+
+def test_parts_in_graphs_that_share_a_workspace(binding):
+    V, k = 140000, 9
+    x = [_logits(5, V, seed=i) for i in range(2)]
+    tok = torch.arange(5, dtype=torch.int32, device="cuda") * 1000
+    ws = torch.zeros(binding.token_scores_workspace_bytes(5, V, k), dtype=torch.uint8, device="cuda")
+    graphs, got = [], []
+    for i in range(2):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            got.append(binding.token_scores(x[i], tok, k, workspace=ws))
+    for turn in range(3):
+        for i in range(2):
+            x[i].copy_(_logits(5, V, seed=10 * turn + i + 7))
+        for i in (0, 1, 0):
+            graphs[i].replay()
+        for i in range(2):
+            want = binding.token_scores(x[i], tok, k)
+            torch.cuda.synchronize()
+            for name in want:
+                assert torch.equal(got[i][name], want[name]), (turn, i, name)
+
+
 def test_given_tokens_of_a_tree(binding):
     x = _logits(7, 997)
     _check(binding, x, [5, 996, -1, 0, 3, 900, 997, 5, 5, 1 << 30], 3, row_of=[0, 0, 1, 6, 6, 2, 3, -1, 7, 0])
