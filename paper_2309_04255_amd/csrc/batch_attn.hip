@@ -23,7 +23,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWaves = 4;
 constexpr int kWideRows = 128;  // pairs per workgroup of the prefix, where there are many
-constexpr int kTileKeys = kPage;  // keys of a tile: two 32-key steps, one page
+constexpr int kTileKeys = kPage;  // keys that units are cut by: a page
 constexpr float kSlack = 8.0f;
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -183,15 +183,13 @@ __device__ __forceinline__ bf16x8 finite(const bf16x8& v) {
 template <int DH, int RB, bool PAGED>
 struct TileWork {
   static constexpr int NS = Frags<DH>::NS, NB = Frags<DH>::NB;
-  static constexpr int STEPS = 1;
-  static constexpr int KEYS = 32 * STEPS;       // of a tile: half a page
-  static_assert(STEPS == 1, "a wave fetches one key block, or half of the dims");
+  static constexpr int KEYS = 32;               // of a tile: half a page
   static constexpr int PARTS = kTileKeys / KEYS;
   static constexpr int HALF = KEYS * DH * 2;    // bytes of a tile's keys, or of its values
   static constexpr int FLAG = 4 * HALF;         // (a flag behind the buffers)
   static constexpr int LDS = FLAG + 16;
   static constexpr int PER = HALF / 2048;       // KiB that a wave fetches: half of the keys, or of the values
-  typedef f32x4 Scores[RB][2 * STEPS];          // [row block][step, key block]
+  typedef f32x4 Scores[RB][2];                  // [row block][key block]
 
   const AttnArgs& a;
   const Unit& u;
@@ -220,7 +218,7 @@ struct TileWork {
   __device__ __forceinline__ int pair_of(int rb) const { return u.pair0 + (wave * RB + rb) * 16 + li; }
   __device__ __forceinline__ int clamped(int rb) const { return pair_of(rb) < u.pairs ? pair_of(rb) : u.pairs - 1; }
 
-  // LDS holds a tile's keys as [step][key block][16 rows][DH] and its values as
+  // LDS holds a tile's keys as [key block][16 rows][DH] and its values as
   // [DH][KEYS], so that a KiB copied to it is whole rows: 64 lanes read 4 to 16
   // rows of 64 to 256 contiguous bytes.  (In fragment order each lane's 16 bytes
   // are another row than its neighbours', and the vector cache takes them one by
@@ -235,10 +233,10 @@ struct TileWork {
   __device__ __forceinline__ const char* key_at(int t, int sb, int s) const {
     return lds + (t & 1) * HALF + sb * 16 * ROW + li * ROW + (((4 * s + g) ^ swap(ROW, li)) * 16);
   }
-  __device__ __forceinline__ char* value_at(int t, int st, int db) const {
-    return lds + (2 + (t & 1)) * HALF + (16 * db + li) * VROW + (((4 * st + g) ^ swap(VROW, li)) * 16);
+  __device__ __forceinline__ char* value_at(int t, int db) const {
+    return lds + (2 + (t & 1)) * HALF + (16 * db + li) * VROW + ((g ^ swap(VROW, li)) * 16);
   }
-  // waves 0 and 1 fetch a step's keys each, 2 and 3 half of the values' dims each
+  // waves 0 and 1 fetch a key block each, 2 and 3 half of the values' dims each
   __device__ __forceinline__ bool values() const { return wave >= 2; }
   __device__ __forceinline__ void place_lanes() {
     const int part = wave & 1;
@@ -269,7 +267,7 @@ struct TileWork {
   // scores of tile t (its keys in LDS)
   __device__ __forceinline__ void scores(Scores& sc, int t) {
 #pragma unroll
-    for (int sb = 0; sb < 2 * STEPS; ++sb) {
+    for (int sb = 0; sb < 2; ++sb) {
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) sc[rb][sb] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -283,13 +281,13 @@ struct TileWork {
   // Clears, where they lie, tile t's values of keys that are not there, and takes
   // out the Inf and NaN of those that some rows see and others do not.  A wave does
   // a quarter; all waves of the workgroup come here for the same tiles.
-  __device__ __forceinline__ void clean(int t, const uint32_t (&vis)[RB][STEPS]) {
+  __device__ __forceinline__ void clean(int t, const uint32_t (&vis)[RB]) {
     int* flag = (int*)(lds + FLAG);
     u16x8 most = (uint16_t)0;
 #pragma unroll 1
-    for (int f = wave; f < STEPS * NB; f += kWaves) {
-      char* at = value_at(t, f / NB, f % NB);
-      const int left = u.lim - (t * KEYS + 32 * (f / NB) + 8 * g);
+    for (int db = wave; db < NB; db += kWaves) {
+      char* at = value_at(t, db);
+      const int left = u.lim - (t * KEYS + 8 * g);
       const bf16x8 v = keep(lds_ld<bf16x8>(at), kept_words(!there || left <= 0 ? 0u : left >= 8 ? 0xffu : (1u << left) - 1u));
       if (PAGED) largest(most, v);
       lds_st<bf16x8>(at, v);
@@ -297,19 +295,17 @@ struct TileWork {
     if (PAGED && __any(nonfinite(most)) && lane == 0) *flag = 1;
     __syncthreads();
     if (PAGED && *flag != 0) {
-#pragma unroll
-      for (int st = 0; st < STEPS; ++st)
 #pragma unroll 1
-        for (int db = 0; db < NB; ++db) {
-          const bf16x8 v = lds_ld<bf16x8>(value_at(t, st, db));
+      for (int db = 0; db < NB; ++db) {
+        const bf16x8 v = lds_ld<bf16x8>(value_at(t, db));
 #pragma unroll
-          for (int rb = 0; rb < RB; ++rb) strays[rb].note(v, vis[rb][st], db);
-        }
+        for (int rb = 0; rb < RB; ++rb) strays[rb].note(v, vis[rb], db);
+      }
       __syncthreads();
       if (threadIdx.x == 0) *flag = 0;
 #pragma unroll 1
-      for (int f = wave; f < STEPS * NB; f += kWaves) {
-        char* at = value_at(t, f / NB, f % NB);
+      for (int db = wave; db < NB; db += kWaves) {
+        char* at = value_at(t, db);
         lds_st<bf16x8>(at, finite(lds_ld<bf16x8>(at)));
       }
       __syncthreads();
@@ -323,7 +319,7 @@ struct TileWork {
       there = id >= 0 && id < a.n_pages;
     }
     if ((t + 1) * KEYS > u.held || !there) {  // (not every row sees every key)
-      uint32_t vis[RB][STEPS];
+      uint32_t vis[RB];
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) {
         uint32_t anc[4] = {0, 0, 0, 0};
@@ -332,13 +328,10 @@ struct TileWork {
 #pragma unroll
           for (int j = 0; j < 4; ++j) anc[j] = ldg(a.mask + row * 4 + j);
         }
+        vis[rb] = there ? seen8(anc, t * KEYS + 8 * g, u.held, u.lim) : 0u;
 #pragma unroll
-        for (int st = 0; st < STEPS; ++st) {
-          vis[rb][st] = there ? seen8(anc, t * KEYS + 32 * st + 8 * g, u.held, u.lim) : 0u;
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (!((vis[rb][st] >> e) & 1u)) sc[rb][2 * st + (e >> 2)][e & 3] = -INFINITY;
-        }
+        for (int e = 0; e < 8; ++e)
+          if (!((vis[rb] >> e) & 1u)) sc[rb][e >> 2][e & 3] = -INFINITY;
       }
       clean(t, vis);
     }
@@ -348,7 +341,7 @@ struct TileWork {
     for (int rb = 0; rb < RB; ++rb) {
       mx[rb] = sc[rb][0][0];
 #pragma unroll
-      for (int e = 1; e < 8 * STEPS; ++e) mx[rb] = fmaxf(mx[rb], sc[rb][e >> 2][e & 3]);
+      for (int e = 1; e < 8; ++e) mx[rb] = fmaxf(mx[rb], sc[rb][e >> 2][e & 3]);
       mx[rb] *= a.scale_log2;
       grow |= mx[rb] > m[rb] + kSlack;
     }
@@ -368,25 +361,21 @@ struct TileWork {
   }
   // Tile t's probabilities and its part of the output.
   __device__ __forceinline__ void add(Scores& sc, int t) {
-    bf16x8 p[RB][STEPS];
+    bf16x8 p[RB];
 #pragma unroll
-    for (int st = 0; st < STEPS; ++st)
+    for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
-      for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float v = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[rb][2 * st + (e >> 2)][e & 3], a.scale_log2, neg_m[rb]));
-          l[rb] += v;
-          p[rb][st][e] = f2bf(v);
-        }
-#pragma unroll
-    for (int st = 0; st < STEPS; ++st)
-#pragma unroll
-      for (int db = 0; db < NB; ++db) {
-        const bf16x8 v = lds_ld<bf16x8>(value_at(t, st, db));
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) o[rb][db] = mfma16x16x32(v, p[rb][st], o[rb][db]);
+      for (int e = 0; e < 8; ++e) {
+        const float v = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[rb][e >> 2][e & 3], a.scale_log2, neg_m[rb]));
+        l[rb] += v;
+        p[rb][e] = f2bf(v);
       }
+#pragma unroll
+    for (int db = 0; db < NB; ++db) {
+      const bf16x8 v = lds_ld<bf16x8>(value_at(t, db));
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) o[rb][db] = mfma16x16x32(v, p[rb], o[rb][db]);
+    }
   }
   __device__ __forceinline__ void run() {
     if (PAGED) pages.start(u, u.first);
@@ -670,36 +659,59 @@ __global__ __launch_bounds__(kThreads, 3) void unit_kernel(AttnArgs a, int prefi
     for (; u.pair0 < u.pairs; u.pair0 += 64) Pages(a, u, lds).run();
 }
 
-// A wave per (row, head): its partial results in the order of their keys.
+// A row's partial results of a head, in the order of their keys: DH / 4 lanes with
+// four dims each.  Each lane first takes one part's maximum and sum, so that the
+// reads of the outputs wait for nothing but each other.
 template <int DH>
 __global__ __launch_bounds__(kThreads) void join_kernel(AttnArgs a) {
-  const size_t item = (size_t)blockIdx.x * kWaves + wave_index();
-  const int lane = threadIdx.x & 63;
+  constexpr int LANES = DH / 4;
+  const size_t item = ((size_t)blockIdx.x * kThreads + threadIdx.x) / LANES;
+  const int lane = threadIdx.x % LANES;
   if (item >= (size_t)a.N * a.H) return;
   const int row = (int)(item / a.H), h = (int)(item % a.H);
   const int b = ldg(a.row_req + row);
   if (b < 0) return;  // (no request's row: left as it was)
   const BatchRequest r = ldg(a.req + b);
   const int parts = a.KP + up_div(r.splits, a.merge);
-  constexpr int PER = DH / 64;
-  float m = -INFINITY, l = 0.0f, o[PER];
-#pragma unroll
-  for (int i = 0; i < PER; ++i) o[i] = 0.0f;
-  for (int p = 0; p < parts; ++p) {
+  auto place = [&](int p) {
     const size_t pr = p < a.KP ? (size_t)p * a.N + row
                                : (size_t)a.KP * a.N + r.part0 + (size_t)(p - a.KP) * r.n + (row - r.row0);
-    const size_t at = pr * a.H + h;
-    const float pm = ldg(a.part_ml + at * 2), pl = ldg(a.part_ml + at * 2 + 1);
-    const float mm = fmaxf(m, pm), mu = mm == -INFINITY ? 0.0f : mm;
-    const float fa = __builtin_amdgcn_exp2f(m - mu), fb = __builtin_amdgcn_exp2f(pm - mu);
+    return pr * a.H + h;
+  };
+  float m = -INFINITY, l = 0.0f;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  for (int p0 = 0; p0 < parts; p0 += LANES) {
+    float pm = -INFINITY, pl = 0.0f;
+    if (p0 + lane < parts) {
+      const float2 ml = ldg((const float2*)a.part_ml + place(p0 + lane));
+      pm = ml.x;
+      pl = ml.y;
+    }
+    float mm = pm;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) o[i] = fa * o[i] + fb * ldg(a.part_o + at * DH + lane * PER + i);
-    l = fa * l + fb * pl;
+    for (int off = LANES / 2; off >= 1; off >>= 1) mm = fmaxf(mm, __shfl_xor(mm, off, LANES));
+    mm = fmaxf(mm, m);
+    const float mu = mm == -INFINITY ? 0.0f : mm, fa = __builtin_amdgcn_exp2f(m - mu), f = __builtin_amdgcn_exp2f(pm - mu);
+    pl *= f;
+#pragma unroll
+    for (int off = LANES / 2; off >= 1; off >>= 1) pl += __shfl_xor(pl, off, LANES);
+    l = fa * l + pl;
+    o = o * fa;
     m = mm;
+    const int n = parts - p0 < LANES ? parts - p0 : LANES;
+    for (int q = 0; q < n; q += 4) {
+      f32x4 x[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = q + i < n ? ldg((const f32x4*)(a.part_o + place(p0 + q + i) * DH) + lane) : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o += x[i] * __shfl(f, q + i, LANES);  // (f is 0 past the last part)
+    }
   }
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+  bf16x4 out;
 #pragma unroll
-  for (int i = 0; i < PER; ++i) stg(a.out + item * DH + lane * PER + i, f2bf(o[i] * inv));
+  for (int i = 0; i < 4; ++i) out[i] = f2bf(o[i] * inv);
+  stg((bf16x4*)(a.out + item * DH) + lane, out);
 }
 
 // Few pairs of rows and heads per K/V head: the waves share 16 of them and split
@@ -722,7 +734,7 @@ hipError_t launch_attention(AttnArgs a, hipStream_t st) {
   const long long most = (long long)a.B * cdiv(a.max_pages, 2);  // (a run has two pages or more)
   const int runs = (most < plan_max_units(a.B) ? (int)most : plan_max_units(a.B)) * a.Hkv;
   unit_kernel<DH><<<dim3(cdiv(units, 8) * 8 + runs), dim3(kThreads), 0, st>>>(a, units, row_tiles, wide);
-  join_kernel<DH><<<dim3((unsigned)(((long long)a.N * a.H + kWaves - 1) / kWaves)), dim3(kThreads), 0, st>>>(a);
+  join_kernel<DH><<<dim3((unsigned)(((long long)a.N * a.H * (DH / 4) + kThreads - 1) / kThreads)), dim3(kThreads), 0, st>>>(a);
   return hipGetLastError();
 }
 

@@ -413,6 +413,70 @@ def test_attention_layers_and_streams(binding):
     assert torch.equal(out, want[1])
 
 
+@pytest.mark.parametrize("n,held,P", [
+    (128, 83210, 1),    # tiles: runs of 82 pages
+    (16, 614401, 100),  # few rows: runs of 76 pages
+])
+def test_attention_of_long_runs(binding, n, held, P):
+    """A request whose pages are cut into runs of more than 64 pages."""
+    c = Case(binding, [n], [held], P=P, H=1, Dh=64, tree=True)
+    c.plan()
+    kp, vp = c.pages()
+    kc, vc = _prefix(c)
+    q = _queries(c)
+    out = _attend(c, None, q, kc, vc, kp, vp)
+    ids = c.d_table[0, :-(-(held + n) // PAGE)].long()
+    k = torch.cat([kc[0, 0, :P], kp[0, ids, 0].reshape(-1, c.Dh)[:held + n]]).double()
+    v = torch.cat([vc[0, 0, :, :P].t(), vp[0, ids, 0].transpose(1, 2).reshape(-1, c.Dh)[:held + n]]).double()
+    see = torch.ones(n, P + held + n, dtype=torch.bool)
+    see[:, P + held:] = False
+    for r, a in enumerate(c.want()["ancestors"]):
+        see[r, [P + held + j for j in a]] = True
+    z = (q[:n, 0].double() @ k.t()) / 8.0
+    w = torch.softmax(z.masked_fill(~see.cuda(), -float("inf")), 1)
+    want, size = _np((w @ v).cpu().double()), _np((w @ v.abs()).cpu().double())
+    got = _np(out)[:n, 0]
+    assert np.all(np.abs(got - want) <= 2.0 ** -8 * np.abs(want) + (2.0 ** -8 + 2.0 ** -11) * size)
+
+
+@pytest.mark.parametrize("n,held,P,kw", [
+    ([1, 2, 3, 4] * 256, [(7 * i) % 130 for i in range(1024)], 70, {"H": 2, "Hkv": 1}),      # more rows than kSplitRows
+    ([128, 127, 120], [0, 1, 64], 129, {"H": 64}),                                      # one split of the prefix
+    ([40, 1, 16, 17, 2], [700, 900, 0, 64, 3], 1000, {"H": 16, "Hkv": 16, "Dh": 128}),      # tiles and few rows side by side
+    ([3, 1], [5000, 1], 0, {"H": 48, "Hkv": 48}),                                           # runs joined for many K/V heads
+])
+def test_attention_of_many(binding, n, held, P, kw):
+    c = Case(binding, n, held, P=P, **kw)
+    c.plan()
+    kp, vp = c.pages()
+    kc, vc = _prefix(c)
+    q = _queries(c)
+    _check_attention(c, q, kc, vc, kp, vp, _attend(c, None, q, kc, vc, kp, vp))
+
+
+def test_two_steps_at_once(binding):
+    """Two steps on two streams, each with its own plan and workspace, over one prefix."""
+    cases = [Case(binding, [31, 2, 9], [700, 5, 64], P=700, H=8, Hkv=4, Dh=128, seed=i) for i in range(2)]
+    kc, vc = _prefix(cases[0])
+    state, want = [], []
+    for c in cases:
+        c.plan()
+        kp, vp = c.pages()
+        state.append((c, kp, vp, _queries(c)))
+        want.append(_attend(c, None, state[-1][3], kc, vc, kp, vp))
+    streams = [torch.cuda.Stream() for _ in cases]
+    outs = [torch.empty_like(w) for w in want]
+    spaces = [torch.zeros(binding.batch_workspace_bytes(c.cfg, c.Hkv, c.B, c.N), dtype=torch.uint8, device="cuda") for c in cases]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for i, (c, kp, vp, q) in enumerate(state):
+            binding.batch_attention(c.cfg, c.Hkv, 0, q, kc, vc, c.P, kp, vp, c.d_table, c.d_plan, outs[i], spaces[i],
+                                    stream=streams[i])
+    torch.cuda.synchronize()
+    for i, c in enumerate(cases):
+        assert torch.equal(outs[i][:c.total], want[i][:c.total])
+
+
 def test_attention_beyond_32_bit_offsets(binding):
     # a pool of more than 2^32 bytes (and 2^31 elements): the request's pages at its two ends
     c = Case(binding, [3], [100], H=32, Dh=128, P=10)
