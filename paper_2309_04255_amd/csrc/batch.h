@@ -115,6 +115,7 @@ struct CommitArgs {
   const BatchRequest* req;
   const int* slot;
   int B, N, L, Hkv, Dh, n_pages;
+  int heads_per;  // K/V heads per workgroup
 };
 hipError_t launch_batch_commit(const CommitArgs& a, hipStream_t st);
 

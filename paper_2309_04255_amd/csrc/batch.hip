@@ -10,6 +10,8 @@ namespace {
 
 constexpr int kThreads = 256;
 
+__device__ __forceinline__ int up_div(int x, int a) { return (x + a - 1) / a; }
+
 // Sum of a pair of 64-bit values over the workgroup, in every thread.
 __device__ __forceinline__ void block_sum(long long (&v)[4], long long* lds) {
 #pragma unroll
@@ -373,60 +375,100 @@ __global__ __launch_bounds__(kThreads) void store_kernel(StoreArgs a, int turn_b
 // ---------------------------------------------------------------- rollback
 //
 // As llmcad_commit_path, in pages.  Accepted row path[k] moves to row k, and
-// path[k] > k: a row that a move writes is never the source of a later one, so
-// a thread that moves its piece of the rows in the order of k needs no other
-// thread's and no copy in between (in batches: eight loads, then their eight
-// stores).  A thread's piece is 16 bytes of a K row or one dim of V^T.
+// path[k] > k: a row may be written only after the moves of smaller k have read it.
+// A K row's 16-byte piece is one thread's, which makes the moves in the order of k
+// (in batches: eight loads, then their eight stores).  A dim of V^T is a line of
+// its page with an entry per move: as many lanes of one wave as there are moves
+// read theirs in one instruction, and write them after it, several dims in flight.
+//
+// Chains are in place: a workgroup that finds no move ends (32 requests, 32 layers,
+// 32 heads of 128: 8 us, the launch).  49 moves of 22 such requests' trees take 178 us:
+// an entry per dim costs a 128-byte line's read and a 32-byte write (430 MB and 110
+// MB, 3 TB/s with such writes), which is the price of V^T's layout; K's rows are 26
+// MB each way.
 constexpr int kCommitBatch = 8;
 
-template <class T>
-__device__ __forceinline__ void move_rows(T* base, size_t page_step, int slot_step, const int* src, const int* dst, int len) {
-  for (int k0 = 0; k0 < len; k0 += kCommitBatch) {
-    T v[kCommitBatch];
+__device__ __forceinline__ void move_keys(bf16x8* base, size_t page_step, int slot_step, const int* src, const int* dst, int moves) {
+  for (int k0 = 0; k0 < moves; k0 += kCommitBatch) {
+    bf16x8 v[kCommitBatch];
 #pragma unroll
-    for (int u = 0; u < kCommitBatch; ++u) {
-      const int s = k0 + u < len ? src[k0 + u] : -1;
-      if (s >= 0) v[u] = ldg(base + (size_t)(s / kPage) * page_step + (s % kPage) * slot_step);
-    }
+    for (int u = 0; u < kCommitBatch; ++u)
+      if (k0 + u < moves) v[u] = ldg(base + (size_t)(src[k0 + u] / kPage) * page_step + (src[k0 + u] % kPage) * slot_step);
 #pragma unroll
-    for (int u = 0; u < kCommitBatch; ++u) {
-      const int s = k0 + u < len ? src[k0 + u] : -1;
-      if (s >= 0) {
-        const int d = dst[k0 + u];
-        stg(base + (size_t)(d / kPage) * page_step + (d % kPage) * slot_step, v[u]);
-      }
-    }
+    for (int u = 0; u < kCommitBatch; ++u)
+      if (k0 + u < moves) stg(base + (size_t)(dst[k0 + u] / kPage) * page_step + (dst[k0 + u] % kPage) * slot_step, v[u]);
   }
 }
 
+// V^T entries of `dims` dims from base on (lines of kPage entries), `moves` entries
+// of each: REACH per lane.
+template <int REACH>
+__device__ __forceinline__ void move_values(uint16_t* base, size_t page_step, const int* src, const int* dst, int moves, int dims) {
+  constexpr int AHEAD = 8 / REACH;
+  int lanes = 1;  // per dim
+  while (lanes * REACH < moves) lanes *= 2;
+  const int k = threadIdx.x % lanes, step = kThreads / lanes;
+  size_t from[REACH], to[REACH];
+#pragma unroll
+  for (int i = 0; i < REACH; ++i) {
+    const int m = k + i * lanes < moves ? k + i * lanes : 0;
+    from[i] = (size_t)(src[m] / kPage) * page_step + src[m] % kPage;
+    to[i] = (size_t)(dst[m] / kPage) * page_step + dst[m] % kPage;
+  }
+  for (int d0 = threadIdx.x / lanes; d0 < dims; d0 += AHEAD * step) {
+    uint16_t v[AHEAD][REACH];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u)
+#pragma unroll
+      for (int i = 0; i < REACH; ++i)
+        if (d0 + u * step < dims && k + i * lanes < moves) v[u][i] = ldg(base + (size_t)(d0 + u * step) * kPage + from[i]);
+    __builtin_amdgcn_wave_barrier();  // (no store moves before a load: another lane may read what it overwrites)
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u)
+#pragma unroll
+      for (int i = 0; i < REACH; ++i)
+        if (d0 + u * step < dims && k + i * lanes < moves) stg(base + (size_t)(d0 + u * step) * kPage + to[i], v[u][i]);
+  }
+}
+
+// A workgroup per request and a.heads_per neighbouring K/V heads of a layer.
 __global__ __launch_bounds__(kThreads) void commit_kernel(CommitArgs a) {
-  __shared__ int src_s[128], dst_s[128];  // slots of the moves k = 1 .. len
-  const int b = blockIdx.y, tid = threadIdx.x, dh = a.Dh;
+  __shared__ int src_s[128], dst_s[128], moves_s[2];  // slots of the moves, in the order of k
+  const int b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, dh = a.Dh;
   const BatchRequest r = ldg(a.req + b);
   const int len = ldg(a.accept_len + b);
   if (len < 1 || len >= r.n) return;  // (nothing moves, or not the outcome of a tree of n rows)
   const int limit = a.n_pages * kPage;
+  int src = -1, dst = -1;
   if (tid < len) {
     const int k = tid + 1, p = ldg(a.path + r.row0 + k);
-    const int dst = ldg(a.slot + r.row0 + k);
-    int src = p > k && p < r.n ? ldg(a.slot + r.row0 + p) : -1;  // (in place already, or no row of the tree)
-    if (dst < 0 || dst >= limit || src >= limit) src = -1;
-    src_s[tid] = src;
-    dst_s[tid] = dst;
+    dst = ldg(a.slot + r.row0 + k);
+    src = p > k && p < r.n ? ldg(a.slot + r.row0 + p) : -1;  // (in place already, or no row of the tree)
+  }
+  const bool moves_here = src >= 0 && src < limit && dst >= 0 && dst < limit;
+  const uint64_t all = __ballot(moves_here);
+  if (lane == 0 && wave < 2) moves_s[wave] = __popcll(all);
+  __syncthreads();
+  const int moves = moves_s[0] + moves_s[1];
+  if (moves == 0) return;
+  if (moves_here) {
+    const int at = __popcll(all & ((1ull << lane) - 1)) + (wave == 1 ? moves_s[0] : 0);
+    src_s[at] = src;
+    dst_s[at] = dst;
   }
   __syncthreads();
-  const int kp = dh / 8, per = kp + dh;  // pieces of a (layer, K/V head): V^T's, K's
   const size_t page = (size_t)a.Hkv * kPage * dh;  // elements of a page
-  const long long pieces = (long long)a.L * a.Hkv * per;
-  for (long long e = (long long)blockIdx.x * kThreads + tid; e < pieces; e += (long long)gridDim.x * kThreads) {
-    const long long lh = e / per;
-    const int c = (int)(e % per);
-    const size_t at = (size_t)(lh / a.Hkv) * a.n_pages * page + (size_t)(lh % a.Hkv) * kPage * dh;
-    if (c < dh)
-      move_rows(a.v_pages + at + (size_t)c * kPage, page, 1, src_s, dst_s, len);
-    else
-      move_rows((bf16x8*)(a.k_pages + at) + (c - dh), page / 8, kp, src_s, dst_s, len);
-  }
+  const int groups = up_div(a.Hkv, a.heads_per), layer = blockIdx.x / groups, kh0 = blockIdx.x % groups * a.heads_per;
+  const int heads = a.Hkv - kh0 < a.heads_per ? a.Hkv - kh0 : a.heads_per;
+  const size_t at = (size_t)layer * a.n_pages * page + (size_t)kh0 * kPage * dh;
+  const int kp = dh / 8;  // pieces of a K row
+  for (int e = tid; e < heads * kp; e += kThreads)
+    move_keys((bf16x8*)(a.k_pages + at + (size_t)(e / kp) * kPage * dh) + e % kp, page / 8, kp, src_s, dst_s, moves);
+  uint16_t* values = (uint16_t*)(a.v_pages + at);
+  if (moves <= 64)
+    move_values<1>(values, page, src_s, dst_s, moves, heads * dh);
+  else
+    move_values<2>(values, page, src_s, dst_s, moves, heads * dh);
 }
 
 }  // namespace
@@ -447,10 +489,12 @@ hipError_t launch_batch_store(const StoreArgs& args, hipStream_t st) {
   return hipGetLastError();
 }
 
-hipError_t launch_batch_commit(const CommitArgs& a, hipStream_t st) {
-  const long long pieces = (long long)a.L * a.Hkv * (a.Dh + a.Dh / 8);
-  const int all = (int)((pieces + kThreads - 1) / kThreads);
-  commit_kernel<<<dim3(all, a.B), dim3(kThreads), 0, st>>>(a);
+hipError_t launch_batch_commit(const CommitArgs& args, hipStream_t st) {
+  CommitArgs a = args;
+  // heads per workgroup: up to eight, if about 2048 workgroups are left
+  const long long heads = (long long)a.B * a.L * a.Hkv;
+  a.heads_per = (int)(heads / 2048 < 1 ? 1 : heads / 2048 > 8 ? 8 : heads / 2048);
+  commit_kernel<<<dim3(a.L * cdiv(a.Hkv, a.heads_per), a.B), dim3(kThreads), 0, st>>>(a);
   return hipGetLastError();
 }
 

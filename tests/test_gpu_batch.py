@@ -506,6 +506,8 @@ def test_attention_beyond_32_bit_offsets(binding):
     ([4], [0], {}),
     ([31, 1, 41, 0, 7], [60, 5, 3, 2, 128], {"Dh": 128, "L": 3, "H": 2}),
     ([128, 128], [1, 63], {"H": 4, "Hkv": 2, "L": 2, "tree": False}),
+    ([9] * 200, [(11 * i) % 140 for i in range(200)], {"H": 7, "L": 5}),  # several heads per workgroup, not all of them full
+    ([128, 80], [7, 64], {"H": 2, "Dh": 128}),                            # more moves than lanes
 ])
 @pytest.mark.parametrize("kind", ["branch", "shift", "bad", "none"])
 def test_commit(binding, n, held, kw, kind):
