@@ -14,6 +14,13 @@
 // cores with K and V^T taken from memory in fragment order: K block b of a
 // 32-key step puts key 8 (r / 4) + 4 b + r % 4 in its row r, so that the lane
 // that holds a score also holds the value operand's slot for that key.
+//
+// One token per request: bound by the reads of the pages and the prefix (128 tokens,
+// 32 query heads on 8 K/V heads of 128, behind 8192 positions and up to 1024 tokens of
+// their own: 82 us, 305 MB read, 3.6 TB/s; the narrow units' loads are 16 rows of
+// 64 bytes).  Trees: bound by the instructions beside the matrix products (32 trees of 41, 40
+// heads of 128, behind 4099: 192 us, 680 TFLOP/s in the first launch, the matrix
+// cores busy 42% of it, 491 MB read where each byte once is 463).
 #include "batch.h"
 
 namespace llmcad {
@@ -174,6 +181,11 @@ __device__ __forceinline__ bf16x8 finite(const bf16x8& v) {
 //
 // 64 RB pairs per workgroup, 16 RB per wave.  Tiles of 32 keys are shared
 // through LDS, in two buffers: while one is computed the next is copied.
+//
+// Two row blocks per wave for the prefix: each fragment read from LDS feeds two
+// products, in 168 registers, three waves per SIMD (three or four blocks leave one
+// wave, and nothing runs beside it: slower).  64-key tiles with two waves per SIMD
+// read the prefix 7% faster and the mix of prefix and pages slower.
 //
 // The running maximum is only a reference point: any value near it serves, so
 // the output is rescaled only when some score exceeds it by 2^kSlack, and
@@ -661,7 +673,9 @@ __global__ __launch_bounds__(kThreads, 3) void unit_kernel(AttnArgs a, int prefi
 
 // A row's partial results of a head, in the order of their keys: DH / 4 lanes with
 // four dims each.  Each lane first takes one part's maximum and sum, so that the
-// reads of the outputs wait for nothing but each other.
+// reads of the outputs wait for nothing but each other.  Bound by the parts' bytes
+// (32 trees of 41 rows, 40 heads: 19 us, 55 MB of parts, 13 MB of results; 22.6 a
+// wave per head with one part after the other).
 template <int DH>
 __global__ __launch_bounds__(kThreads) void join_kernel(AttnArgs a) {
   constexpr int LANES = DH / 4;
