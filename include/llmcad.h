@@ -348,7 +348,9 @@ int llmcad_commit_path(const llmcad_config* cfg, void* k_cache, void* v_cache, i
  * A step is llmcad_batch_plan once, llmcad_batch_store and
  * llmcad_batch_attention in every layer, and llmcad_batch_commit after the
  * target has answered.  Lengths, tables and trees are device arrays, so that a
- * step can be captured and replayed while requests grow.
+ * step can be captured and replayed while requests grow.  They take the plan's
+ * n_requests and n_rows; with others (or a buffer that holds no plan) they leave
+ * everything as it was.
  *
  * The configuration gives L, H, Dh and theta; n_kv_heads (Hkv) divides H, and
  * query head h reads K/V head h / (H / Hkv).  Pointers to bf16 data, plans and
@@ -385,7 +387,10 @@ int llmcad_batch_plan_region(const llmcad_config* cfg, int32_t n_requests, int32
  * free_pages int32 [n_free] (device arrays).  Requests take the pages that
  * their rows need beyond those they hold from free_pages in the order of the
  * requests; block_table receives them, and "pages taken" their number: the
- * caller's free list begins behind them in the next step.  Where the free list
+ * caller's free list begins behind them in the next step.  A request holds
+ * ceil(held / LLMCAD_PAGE) pages; entries of its table row past them (pages of
+ * rows that a rollback dropped) are not used again but overwritten: they belong
+ * back on the free list.  Where the free list
  * is too short, the requests whose share lies within it are placed and the
  * others are not (status LLMCAD_PLAN_NO_PAGES, their shares stay counted in
  * "pages taken", which then exceeds n_free).  A request that is not placed has

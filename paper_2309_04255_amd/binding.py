@@ -582,7 +582,7 @@ def token_scores(logits, tokens, k: int = 0, row_of=None, workspace=None, stream
         with torch.cuda.device(dev), torch.cuda.stream(stream):
             return token_scores(logits, tokens, k, row_of, workspace)
     if workspace is None:
-        workspace = torch.zeros(token_scores_workspace_bytes(n, V, k), dtype=torch.uint8, device=logits.device)
+        workspace = torch.empty(token_scores_workspace_bytes(n, V, k), dtype=torch.uint8, device=logits.device)
     else:
         _want(what, "workspace", workspace, torch.uint8, None)
     out = torch.empty(m + 2 * n + 2 * n * k, dtype=torch.float32, device=logits.device)
@@ -718,6 +718,8 @@ class Session:
         """Takes tokens in as prefill does and scores every position: {"logprob" [n] of the next token of
         `tokens` (the last entry is 0), "entropy", "lse" [n], "top_token", "top_logprob" [n, k]}."""
         tokens = np.asarray(tokens, dtype=np.int32)
+        if len(tokens) == 0:
+            raise ValueError("score: no tokens")
         following = torch.from_numpy(np.append(tokens[1:], np.int32(-1))).to(self.device)
         parts = []
         for off in range(0, len(tokens), self.max_n):
@@ -778,10 +780,11 @@ class Batch:
     workspace for a model of `shape` (device buffers owned here), with the prefix in k_cache / v_cache
     (a Session's, or any of that layout with n_kv_heads heads; None: no prefix).
 
-    A step: plan(row_start, held, parent), then per layer store and attention, then commit with the
-    verified paths.  Lengths are the caller's: after a step request b holds held[b] + its accepted rows.
-    Pages go out in the order of `free_pages`; advance(pages taken) drops the ones a plan handed out,
-    release(b) takes back a finished request's."""
+    A step: plan(row_start, held, parent), advance(), per layer store and attention, then commit with the
+    verified paths and trim(held) with the lengths after it.  Lengths are the caller's: after a step request b
+    holds held[b] + its accepted rows.  Pages go out in the order of `free_pages`; advance drops the ones a
+    plan handed out, trim takes back those of rejected rows, release(b) a finished request's.  (They replace
+    `free_pages`: a captured step takes batch_plan with a free list of its own.)"""
 
     def __init__(self, shape, n_requests: int, n_rows: int, n_pages: int, max_pages: int, prefix_len: int = 0,
                  k_cache=None, v_cache=None, n_kv_heads=None, device="cuda"):
@@ -825,11 +828,23 @@ class Batch:
 
     def advance(self, taken=None):
         """Drops the pages that the last plan handed out from the free list (taken: their number if the
-        caller has it; read from the device otherwise).  Raises if a request was not placed."""
-        taken = int(self.taken.item()) if taken is None else int(taken)
+        caller has it and every request was placed; both are read from the device otherwise, and a request
+        that was not placed raises)."""
+        if taken is None:
+            taken, bad = torch.cat([self.taken, self.status.max()[None]]).tolist()
+            if bad != PLAN_OK:
+                raise RuntimeError(f"requests {self.status.nonzero()[:, 0].tolist()} were not placed (plan status {bad})")
+        taken = int(taken)
         if taken > self.free_pages.shape[0]:
             raise RuntimeError(f"the step needs {taken} pages and {self.free_pages.shape[0]} are free")
         self.free_pages = self.free_pages[taken:].clone()
+
+    def trim(self, held):
+        """Takes back the pages past the requests' held tokens (int32 [n_requests], the lengths after a
+        rollback; reads how many from the device).  Without it the next plan overwrites their entries."""
+        past = torch.arange(self.block_table.shape[1], device=held.device) * PAGE >= held[:, None]
+        self.free_pages = torch.cat([self.block_table[past & (self.block_table >= 0)], self.free_pages])
+        self.block_table.masked_fill_(past, -1)
 
     def release(self, request: int):
         """Takes back the pages of a finished request."""

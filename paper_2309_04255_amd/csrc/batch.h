@@ -45,7 +45,11 @@ struct BatchUnit {
 };
 
 // Head of a plan (int32 words).
-enum PlanWord { PLAN_UNITS = 0, PLAN_TAKEN = 1, PLAN_WORDS = 64 };
+enum PlanWord { PLAN_UNITS = 0, PLAN_TAKEN = 1, PLAN_REQUESTS = 2, PLAN_ROWS = 3, PLAN_WORDS = 64 };
+// A plan for other sizes lies elsewhere in its buffer: the operators leave it unused.
+__device__ __forceinline__ bool plan_is_for(const int* head, int B, int N) {
+  return ldg(head + PLAN_REQUESTS) == B && ldg(head + PLAN_ROWS) == N;
+}
 
 inline int plan_max_units(int B) { return B + kSplitRuns; }
 inline size_t plan_part_rows(int n_rows) { return (size_t)n_rows + (n_rows > kSplitRows ? n_rows : kSplitRows); }
@@ -100,9 +104,10 @@ struct StoreArgs {
   bf16* q_out;                             // [N][H][Dh]
   bf16* k_pages;                           // the layer's pages [n_pages][Hkv][64][Dh]
   bf16* v_pages;                           // [n_pages][Hkv][Dh][64]
+  const int* head;
   const int* slot;
   const float* rope;
-  int N, H, Hkv, Dh, n_pages;
+  int B, N, H, Hkv, Dh, n_pages;
   int heads_per;  // heads that a workgroup turns (the launch sets it)
 };
 hipError_t launch_batch_store(const StoreArgs& a, hipStream_t st);
@@ -112,6 +117,7 @@ struct CommitArgs {
   bf16* v_pages;
   const int* path;        // [N]
   const int* accept_len;  // [B]
+  const int* head;
   const BatchRequest* req;
   const int* slot;
   int B, N, L, Hkv, Dh, n_pages;

@@ -238,6 +238,8 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(PlanArgs a) {
     if (b == 0) {
       stg(a.head + PLAN_UNITS, (int)(invalid ? 0 : w[1]));
       stg(a.head + PLAN_TAKEN, (int)(invalid ? 0 : taken));
+      stg(a.head + PLAN_REQUESTS, B);
+      stg(a.head + PLAN_ROWS, a.N);
     }
   }
   if (!invalid)
@@ -374,6 +376,7 @@ __device__ __forceinline__ void write_values(const StoreArgs& a, int block, int 
 
 template <int DH>
 __global__ __launch_bounds__(kThreads) void store_kernel(StoreArgs a, int turn_blocks, int head_blocks) {
+  if (!plan_is_for(a.head, a.B, a.N)) return;
   const int x = blockIdx.x, turns = turn_blocks * head_blocks;
   if (x < turns)
     turn_rows<DH>(a, x % turn_blocks, x / turn_blocks * a.heads_per);
@@ -446,6 +449,7 @@ __global__ __launch_bounds__(kThreads) void commit_kernel(CommitArgs a) {
   const int b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, dh = a.Dh;
   const BatchRequest r = ldg(a.req + b);
   const int len = ldg(a.accept_len + b);
+  if (!plan_is_for(a.head, a.B, a.N)) return;
   if (len < 1 || len >= r.n) return;  // (nothing moves, or not the outcome of a tree of n rows)
   const int limit = a.n_pages * kPage;
   int src = -1, dst = -1;

@@ -136,8 +136,10 @@ int llmcad_batch_store(const llmcad_config* cfg, int32_t n_kv_heads, int32_t lay
   a.q_out = (bf16*)q_out;
   a.k_pages = (bf16*)k_pages + layer_at;
   a.v_pages = (bf16*)v_pages + layer_at;
+  a.head = (const int*)((const char*)plan + P.head);
   a.slot = (const int*)((const char*)plan + P.slot);
   a.rope = (const float*)((const char*)plan + P.rope);
+  a.B = n_requests;
   a.N = n_rows;
   a.H = cfg->n_heads;
   a.Hkv = n_kv_heads;
@@ -227,6 +229,7 @@ int llmcad_batch_commit(const llmcad_config* cfg, int32_t n_kv_heads, void* k_pa
   a.v_pages = (bf16*)v_pages;
   a.path = path;
   a.accept_len = accept_len;
+  a.head = (const int*)((const char*)plan + P.head);
   a.req = (const BatchRequest*)((const char*)plan + P.req);
   a.slot = (const int*)((const char*)plan + P.slot);
   a.B = n_requests;

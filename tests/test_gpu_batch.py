@@ -596,6 +596,58 @@ def test_step_in_a_graph(binding):
         free.copy_(torch.roll(free, -taken))
 
 
+def test_plan_of_other_sizes_is_not_used(binding):
+    """Operators called with other counts than the plan's, or with a buffer that holds none, write nothing."""
+    c = Case(binding, [5, 20, 3], [70, 10, 64], P=40, H=4, Hkv=2, Dh=64)
+    c.plan()
+    kp, vp = c.pages()
+    kc, vc = _prefix(c)
+    q = _queries(c)
+    k0, v0 = kp.clone(), vp.clone()
+    path = _dev([0] + list(range(2, c.N + 1)))
+    x = torch.randn(c.N, 2, 64, device="cuda").to(torch.bfloat16)
+    qo = torch.full_like(q, 5.0)
+    good = c.d_plan
+    for plan, B in ((good, 2), (torch.zeros_like(good), 3), (torch.full_like(good, 0x5A), 3)):
+        c.d_plan = plan
+        out = _attend(c, None, q, kc, vc, kp, vp, table=c.d_table[:B].contiguous())
+        assert bool((out == 77.0).all())
+        binding.batch_store(c.cfg, 2, 0, q, x, x, qo, kp, vp, plan, B)
+        binding.batch_commit(c.cfg, 2, kp, vp, plan, B, path, _dev([2] * B))
+        torch.cuda.synchronize()
+        assert bool((qo == 5.0).all()) and torch.equal(kp, k0) and torch.equal(vp, v0)
+
+
+def test_batch_keeps_its_pages(binding):
+    """Many steps whose trees are mostly rejected: trimmed, the pool loses no page; a request that
+    cannot be placed is reported."""
+    import workloads
+
+    shape = workloads.MODELS["tiny"]
+    b = binding.Batch(shape, 3, 96, n_pages=9, max_pages=6)
+    held = torch.tensor([0, 60, 100], dtype=torch.int32, device="cuda")
+    b.plan(_dev([0, 0, 60, 96]), _dev([0, 0, 65]))
+    assert b.status.tolist() == [0, 0, binding.PLAN_NO_PAGES]  # (the page of its 65th token is not in its table)
+    with pytest.raises(RuntimeError):
+        b.advance()
+    b.block_table.fill_(-1)
+    b.block_table[1, 0], b.block_table[2, 0], b.block_table[2, 1] = 0, 1, 2
+    b.free_pages = _dev(range(3, 9))
+    for step in range(12):
+        b.plan(_dev([0, 30, 60, 90]), held)
+        assert not b.status.any()
+        b.advance()
+        used = b.block_table[b.block_table >= 0].tolist()
+        assert sorted(used + b.free_pages.tolist()) == list(range(9)), step
+        held += _dev([1, 2, 3])
+        b.trim(held)
+        used = b.block_table[b.block_table >= 0].tolist()
+        assert sorted(used + b.free_pages.tolist()) == list(range(9)), step
+        assert len(used) == sum(-(-int(h) // PAGE) for h in held)
+    b.release(2)
+    assert len(b.free_pages) == 9 - 1 - 2  # (12 and 84 tokens are held by the others)
+
+
 def test_refusals_of_the_binding(binding):
     c = Case(binding, [2, 1], [5, 0], P=10, H=2, Dh=128)
     c.plan()
