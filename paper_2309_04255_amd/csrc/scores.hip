@@ -18,8 +18,9 @@
 // read once more in steps that cut the list back to its k best.
 //
 // Without alternatives it is bound by the reads: 1024 bf16 rows of 128000 take 50 us
-// (5200 GB/s), 20 of them take 22 us more for the bound and the ranking, in which a
-// row's workgroup reads nothing; fp32 rows hide that (103 us, 5100 GB/s).
+// (5200 GB/s); the best 8 of them take 14 us more, 20 about 20, for the bound and the
+// ranking, in which a row's workgroup reads nothing.  fp32 rows hide most of that
+// (103 us, 5100 GB/s).
 #include <algorithm>
 
 #include "batch.h"
@@ -315,10 +316,12 @@ __global__ __launch_bounds__(THREADS) void scores_kernel(ScoresArgs a) {
   T_ tile, ahead;
   ahead.load(row, lo - lead, lo, hi);
   // The bound is raised after this many tiles, and again when they have doubled:
-  // before many more than 128 values are held (each time costs about 1 us; k of 8 in
-  // 128000 fp32 values 24.6 us after tile 2 and 4, 21.4 never; k of 64 83 us after
-  // tile 2 and 4, 91 after 4, for 1024 bf16 rows).
-  int done = 0, next = max(2, 128 / max(k, 1));
+  // before many more than kHits values are held.  Each time costs about 1 us, which
+  // a row alone on its CU waits for (31 fp32 rows of 90000, k of 8: 18.8 us with 128,
+  // 20.1 with 32) and other rows' workgroups fill (1024 bf16 rows of 128000, k of 8:
+  // 72.1 and 64.0; k of 20 the same, 70 to 73).
+  constexpr int kHits = THREADS == 1024 ? 128 : 32;
+  int done = 0, next = max(2, kHits / max(k, 1));
   bool listed = true;  // held pieces and list have had room so far
   for (long base = lo - lead; base < hi; base += T_::SIZE) {
     tile = ahead;
@@ -472,9 +475,9 @@ size_t score_part_bytes(int n, int V, int k) {
 template <bool BF16>
 static void launch(const ScoresArgs& a, hipStream_t st) {
   // More rows than CUs: smaller workgroups, so that several rows share a CU and one
-  // is read while another ranks its values (1024 bf16 rows of 128000, k of 20: 72.9 us
-  // with 256 threads, 76.2 with 512; 400 rows 45.8 and 37.4, as a CU then has too few
-  // waves).
+  // is read while another ranks its values (1024 bf16 rows of 128000, k of 20: 73 us
+  // with 256 threads, 76 with 512; k of 8 64 and 69; 400 rows 45.8 and 37.4, as a CU
+  // then has too few waves).
   if (a.parts > 1) {
     scores_kernel<BF16, 512, true><<<dim3(a.n * a.parts), dim3(512), 0, st>>>(a);
     scores_join_kernel<BF16><<<dim3(a.n), dim3(kJoinThreads), 0, st>>>(a);
