@@ -276,7 +276,7 @@ namespace {
 // together, 16 bytes per dim if there are eight of them.
 //
 // Bound by bytes, of which V^T's are pieces of lines: 64 trees of up to 31 rows, 32 heads of
-// 128 and as many of K/V, take 14.5 us where the 49 MB stay in the caches and 20 to 26 where they
+// 128 and as many of K/V, take 15 us where the 49 MB stay in the caches and 20 to 26 where they
 // do not (2400 to 1900 GB/s); one row each of 512 requests takes 73 to 101 us, two
 // bytes of a line per dim and head.  (The values' workgroups first: the same.)
 constexpr int kStoreRows = 64;

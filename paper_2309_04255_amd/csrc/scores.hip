@@ -9,18 +9,19 @@
 // whose product with log2 e leaves fp32) is taken again in natural units.
 //
 // The k largest values come out of the same pass.  The first tile gives a lower
-// bound of the k-th largest value (the k-th largest of 256 groups' maxima: about as
-// many values as k lie above it in the tile); every 16-byte piece with a value from
-// the bound on is held in LDS as it lies.  From time to time the held pieces' values
-// join a list there, which is cut to its k best, and the k-th of them becomes the
-// bound; at the end once more.  The list is sorted by counting for each entry those
-// above it.  A row whose pieces or list do not fit (values in rising order, say) is
-// read once more in steps that cut the list back to its k best.
+// bound of the k-th largest value: the k-th largest of 64 groups' maxima, of 256 for
+// k above 32 (about as many values as k lie above it in the tile; always 256: 64.3 us
+// for the 52.8 below).  Every 16-byte piece with a value from the bound on is held in
+// LDS as it lies.  From time to time the held pieces' values join a list there, which
+// is cut to its k best, and the k-th of them becomes the bound; at the end once more.
+// The list is sorted by counting for each entry those above it.  A row whose pieces
+// or list do not fit (values in rising order, say) is read once more in steps that
+// cut the list back to its k best.
 //
-// Without alternatives it is bound by the reads: 1024 bf16 rows of 128000 take 50 us
-// (5200 GB/s); the best 8 of them take 14 us more, 20 about 20, for the bound and the
-// ranking, in which a row's workgroup reads nothing.  fp32 rows hide most of that
-// (103 us, 5100 GB/s).
+// Bound by the reads up to k of 32: 1024 bf16 rows of 128000 take 50.3 us without
+// alternatives (5200 GB/s), 52.8 with 8 or 16, 56.3 with 32; 81 with 64, where the
+// bound and the ranking, in which a row's workgroup reads nothing, are not hidden.
+// fp32 rows with 20 take 94 us (5600 GB/s).
 #include <algorithm>
 
 #include "batch.h"
@@ -147,6 +148,27 @@ __device__ __forceinline__ void keep_best(ScoreLds& L, int count, int k) {
   rank<THREADS>(L, count, [&](uint64_t entry, int above) {
     if (above < k) L.keep[above] = entry;
   });
+}
+
+// L.bound: the k-th largest of groups' maxima, groups of neighbouring threads (64
+// of them for k up to 32: at most about 44 values of a tile lie above it then).
+template <int THREADS>
+__device__ __forceinline__ void first_bound(ScoreLds& L, float top, int k) {
+  const int groups = k <= 32 ? 64 : kGroups, lanes = THREADS / groups, share = groups / lanes;
+  float gm = top;
+  for (int off = 1; off < lanes; off <<= 1) gm = fmaxf(gm, __shfl_xor(gm, off, kWave));
+  const int group = threadIdx.x / lanes, part = threadIdx.x % lanes;
+  if (part == 0) L.group[group] = gm;
+  __syncthreads();
+  int before = 0;  // the groups before this one, a share of them per lane
+  for (int j = part * share; j < (part + 1) * share; j += 4) {
+    const f32x4 o = *(const f32x4*)&L.group[j];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) before += o[e] > gm || (o[e] == gm && j + e < group) ? 1 : 0;
+  }
+  for (int off = 1; off < lanes; off <<= 1) before += __shfl_xor(before, off, kWave);
+  if (part == 0 && before == k - 1) L.bound = gm;
+  __syncthreads();
 }
 
 // The held pieces' values from the bound on go to the list.  False if there were
@@ -298,7 +320,7 @@ __device__ __forceinline__ void finish(const ScoresArgs& a, int r, const char* r
 
 // SPLIT: a workgroup per part of a row; sums and best values go to the workspace.
 template <bool BF16, int THREADS, bool SPLIT>
-__global__ __launch_bounds__(THREADS) void scores_kernel(ScoresArgs a) {
+__global__ __launch_bounds__(THREADS, SPLIT ? 2 : 4) void scores_kernel(ScoresArgs a) {
   typedef Tile<BF16, THREADS> T_;
   __shared__ ScoreLds L;
   constexpr int ESIZE = BF16 ? 2 : 4;
@@ -319,7 +341,7 @@ __global__ __launch_bounds__(THREADS) void scores_kernel(ScoresArgs a) {
   // before many more than kHits values are held.  Each time costs about 1 us, which
   // a row alone on its CU waits for (31 fp32 rows of 90000, k of 8: 18.8 us with 128,
   // 20.1 with 32) and other rows' workgroups fill (1024 bf16 rows of 128000, k of 8:
-  // 72.1 and 64.0; k of 20 the same, 70 to 73).
+  // 63.5 and 52.9; k of 32 59.7 and 56.4).
   constexpr int kHits = THREADS == 1024 ? 128 : 32;
   int done = 0, next = max(2, kHits / max(k, 1));
   bool listed = true;  // held pieces and list have had room so far
@@ -349,24 +371,7 @@ __global__ __launch_bounds__(THREADS) void scores_kernel(ScoresArgs a) {
     }
     if (k > 0) {
       if (done == 0) {  // the first tile: the bound
-        constexpr int PER_GROUP = THREADS / kGroups;
-        float gm = top;
-#pragma unroll
-        for (int off = 1; off < PER_GROUP; off <<= 1) gm = fmaxf(gm, __shfl_xor(gm, off, kWave));
-        const int group = tid / PER_GROUP, part = tid % PER_GROUP;
-        if (part == 0) L.group[group] = gm;
-        __syncthreads();
-        int before = 0;  // the groups before this one, a share of them per lane
-#pragma unroll 4
-        for (int j = part * (kGroups / PER_GROUP); j < (part + 1) * (kGroups / PER_GROUP); j += 4) {
-          const f32x4 o = *(const f32x4*)&L.group[j];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) before += o[e] > gm || (o[e] == gm && j + e < group) ? 1 : 0;
-        }
-#pragma unroll
-        for (int off = 1; off < PER_GROUP; off <<= 1) before += __shfl_xor(before, off, kWave);
-        if (part == 0 && before == k - 1) L.bound = gm;
-        __syncthreads();
+        first_bound<THREADS>(L, top, k);
         bound = fmaxf(L.bound, kLowest);  // (-inf is no alternative)
       }
       int hits = 0;
@@ -475,9 +480,9 @@ size_t score_part_bytes(int n, int V, int k) {
 template <bool BF16>
 static void launch(const ScoresArgs& a, hipStream_t st) {
   // More rows than CUs: smaller workgroups, so that several rows share a CU and one
-  // is read while another ranks its values (1024 bf16 rows of 128000, k of 20: 73 us
-  // with 256 threads, 76 with 512; k of 8 64 and 69; 400 rows 45.8 and 37.4, as a CU
-  // then has too few waves).
+  // is read while another ranks its values (1024 bf16 rows of 128000, k of 8: 52.9 us
+  // with 256 threads, 57.8 with 512; 2000 of 32000 44 and 49; 400 rows 45.8 and 37.4,
+  // as a CU then has too few waves).
   if (a.parts > 1) {
     scores_kernel<BF16, 512, true><<<dim3(a.n * a.parts), dim3(512), 0, st>>>(a);
     scores_join_kernel<BF16><<<dim3(a.n), dim3(kJoinThreads), 0, st>>>(a);

@@ -1,9 +1,10 @@
 """Token scores (llmcad_token_scores) against their float64 statement (oracle/batch.py).
 
 Tolerances: a logit enters exactly; lse and log probabilities are m + log S (in base 2, where a
-product with log2 e takes another half step of the value) with S a sum of fp32 exponentials (each within 2^-22, the sum of up to 2^18 of them in chains of at most 2^9 additions and
-14 joins: 2^-14 at the worst, 2^-20 in the mean of random roundings), the difference x - m rounded
-once: 2^-18 absolute and 2^-22 of the value.  The entropy adds products p (x - m) of size up to about
+product with log2 e takes another half step of the value) with S a sum of fp32 exponentials (each
+within 2^-22, the sum of up to 2^18 of them in chains of at most 2^9 additions and 14 joins: 2^-14 at
+the worst, 2^-20 in the mean of random roundings), the difference x - m rounded once: 2^-18 absolute
+and 2^-22 of the value.  The entropy adds products p (x - m) of size up to about
 100: 2^-15."""
 
 import numpy as np
