@@ -784,7 +784,12 @@ class Batch:
     verified paths and trim(held) with the lengths after it.  Lengths are the caller's: after a step request b
     holds held[b] + its accepted rows.  Pages go out in the order of `free_pages`; advance drops the ones a
     plan handed out, trim takes back those of rejected rows, release(b) a finished request's.  (They replace
-    `free_pages`: a captured step takes batch_plan with a free list of its own.)"""
+    `free_pages`: a captured step takes batch_plan with a free list of its own.)
+
+    Until advance, a plan's new pages are in the block tables and on the free list both.  Where it did not
+    place every request, advance (which raises), release and trim take them out of the tables, and the step can
+    be planned anew; so does another plan, which replaces one that was not advanced.  release and trim after a
+    good plan give back the requests' own pages alone, and advance drops those that the tables still hold."""
 
     def __init__(self, shape, n_requests: int, n_rows: int, n_pages: int, max_pages: int, prefix_len: int = 0,
                  k_cache=None, v_cache=None, n_kv_heads=None, device="cuda"):
@@ -809,8 +814,43 @@ class Batch:
         self.workspace = torch.zeros(work, dtype=torch.uint8, device=dev)
         for name, view in batch_plan_views(self.cfg, self.n_requests, self.n_rows, self.plan_buffer).items():
             setattr(self, name, view)  # slot, position, mask, rope, status, taken
+        self._planned = False  # the last plan's pages are on the free list still
+        self._changed = False  # ... and some of them have left the tables
+
+    def _among(self, ids, others):
+        """Which of ids are pages that others hold too (what is no page is not)."""
+        index = lambda p: torch.where((p >= 0) & (p < self.n_pages), p, self.n_pages).long()  # noqa: E731
+        held = torch.zeros(self.n_pages + 1, dtype=torch.bool, device=ids.device)
+        held[index(others)] = True
+        held[self.n_pages] = False
+        return held[index(ids)]
+
+    def _new_pages(self):
+        """Which table entries are pages that are on the free list still (those of a plan before advance)."""
+        return self._among(self.block_table, self.free_pages)
+
+    def _undo(self):
+        """Takes the pages of a plan that was not advanced out of the tables."""
+        self.block_table.masked_fill_(self._new_pages(), -1)
+        self._planned = self._changed = False
+
+    def _give_back(self, entries):
+        """Takes the table entries marked in `entries` out and those of them that are owned onto the free list
+        (returned)."""
+        if self._planned and bool(self.status.any()):
+            self._undo()
+        owned = entries & (self.block_table >= 0)
+        if self._planned:
+            owned &= ~self._new_pages()
+            self._changed = True
+        pages = self.block_table[owned]
+        self.block_table.masked_fill_(entries, -1)
+        return pages
 
     def plan(self, row_start, held, parent=None):
+        if self._planned:
+            self._undo()
+        self._planned = True
         batch_plan(self.cfg, row_start, held, parent, self.prefix_len, self.block_table, self.free_pages,
                    self.n_pages, self.plan_buffer, self.n_rows)
 
@@ -829,25 +869,30 @@ class Batch:
     def advance(self, taken=None):
         """Drops the pages that the last plan handed out from the free list (taken: their number if the
         caller has it and every request was placed; both are read from the device otherwise, and a request
-        that was not placed raises)."""
+        that was not placed raises, with the tables and the free list as they were before the plan)."""
         if taken is None:
             taken, bad = torch.cat([self.taken, self.status.max()[None]]).tolist()
             if bad != PLAN_OK:
+                if self._planned:
+                    self._undo()
                 raise RuntimeError(f"requests {self.status.nonzero()[:, 0].tolist()} were not placed (plan status {bad})")
         taken = int(taken)
         if taken > self.free_pages.shape[0]:
             raise RuntimeError(f"the step needs {taken} pages and {self.free_pages.shape[0]} are free")
-        self.free_pages = self.free_pages[taken:].clone()
+        if self._changed:  # (a request of the plan was released or trimmed: what the tables hold is taken)
+            self.free_pages = self.free_pages[~self._among(self.free_pages, self.block_table)]
+        else:
+            self.free_pages = self.free_pages[taken:].clone()
+        self._planned = self._changed = False
 
     def trim(self, held):
         """Takes back the pages past the requests' held tokens (int32 [n_requests], the lengths after a
         rollback; reads how many from the device).  Without it the next plan overwrites their entries."""
-        past = torch.arange(self.block_table.shape[1], device=held.device) * PAGE >= held[:, None]
-        self.free_pages = torch.cat([self.block_table[past & (self.block_table >= 0)], self.free_pages])
-        self.block_table.masked_fill_(past, -1)
+        pages = self._give_back(torch.arange(self.block_table.shape[1], device=held.device) * PAGE >= held[:, None])
+        self.free_pages = torch.cat([pages, self.free_pages])
 
     def release(self, request: int):
         """Takes back the pages of a finished request."""
-        row = self.block_table[request]
-        self.free_pages = torch.cat([self.free_pages, row[row >= 0]])
-        row.fill_(-1)
+        entries = torch.zeros_like(self.block_table, dtype=torch.bool)
+        entries[request] = True
+        self.free_pages = torch.cat([self.free_pages, self._give_back(entries)])
