@@ -562,6 +562,34 @@ __device__ __forceinline__ void narrow_unit(const AttnArgs& a, const Unit& u, ch
     }
     if (more) fetch_values(at, j + kWaves);
   }
+  // A probability's second half may be 0 or negative, so that its product with an
+  // Inf that every row sees is not that Inf: such outputs are set from the values.
+  bool bad = false;
+#pragma unroll
+  for (int db = 0; db < NB; ++db)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) bad |= !__builtin_isfinite(o[db][i]);
+  if (__any(bad)) {
+    Strays seen;
+    if (u.table) pages.start(u, u.first);
+#pragma unroll 1
+    for (int j = j0; j < j1; j += kWaves) {
+      at = where(j);
+      if (32 * (j + 1) > u.held || !at.there) continue;  // (taken care of above)
+#pragma unroll 1
+      for (int db = 0; db < NB; ++db) {
+        const bf16* src = at.v + 32 * (j & 1) + (size_t)(16 * db) * at.vs;
+        seen.note(ldg((const bf16x8*)((const char*)src + lane_v)), 0xffu, db);
+      }
+    }
+#pragma unroll
+    for (int db = 0; db < NB; ++db)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (((seen.up | seen.down) >> (4 * db + i)) & 1u) o[db][i] = 0.0f;
+    strays.up |= seen.up;
+    strays.down |= seen.down;
+  }
   // the four waves' states, joined in wave order
   l = col4_sum(l);
   strays.give(o);
