@@ -343,7 +343,8 @@ int llmcad_commit_path(const llmcad_config* cfg, void* k_cache, void* v_cache, i
  * Row i of a request is its token held + i, at position prefix_len + held +
  * depth(i), and sees the prefix, the request's held tokens, its ancestors and
  * itself.  Rows [row_start[B], n_rows) are padding (a step captured in a graph
- * has a fixed n_rows): no operator reads or writes theirs.
+ * has a fixed n_rows): no operator writes theirs, and what they hold changes
+ * no other row's results.
  *
  * A step is llmcad_batch_plan once, llmcad_batch_store and
  * llmcad_batch_attention in every layer, and llmcad_batch_commit after the

@@ -88,6 +88,11 @@ struct PageIds {
   }
 };
 
+// A row of the prefix's units that belongs to no placed request.  Its scores are all 0 around a
+// reference point of 0: whatever lies in its query, it moves no other row's reference
+// point (a wave moves those of its rows together).
+__device__ __forceinline__ bool no_request(const AttnArgs& a, int row) { return ldg(a.row_req + row) < 0; }
+
 // Direct global -> LDS copy of 16 bytes per lane: lane l's land at lds + 16 l
 // (lds the same in every lane).
 __device__ __forceinline__ void dma16(const void* src, char* lds) {
@@ -406,9 +411,15 @@ struct TileWork {
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) {
         const int pr = clamped(rb);
+        const bool nobody = !PAGED && no_request(a, u.row0 + pr / group);
         const bf16* q = a.q + (size_t)(u.row0 + pr / group) * a.q_stride + (size_t)(u.kh * group + pr % group) * DH + 8 * g;
 #pragma unroll
         for (int s = 0; s < NS; ++s) qf[rb][s] = ldg((const bf16x8*)(q + 32 * s));
+        if (nobody) {
+          m[rb] = 0.0f;
+#pragma unroll
+          for (int s = 0; s < NS; ++s) qf[rb][s] = (bf16)0.0f;
+        }
       }
       __syncthreads();
       for (int t = first; t < last; ++t) {
@@ -453,6 +464,7 @@ __device__ __forceinline__ void narrow_unit(const AttnArgs& a, const Unit& u, ch
   const int group = a.H / a.Hkv, pair0 = u.pair0;
   const int pr = pair0 + li < u.pairs ? pair0 + li : u.pairs - 1;
   const size_t row = (size_t)u.row0 + pr / group;
+  const bool nobody = !u.table && no_request(a, (int)row);
   const int j0 = 2 * u.first + wave, j1 = u.last * kTileKeys <= u.lim ? 2 * u.last : (u.lim + 31) / 32;
   PageIds pages;
   if (u.table) pages.start(u, u.first);
@@ -480,7 +492,10 @@ __device__ __forceinline__ void narrow_unit(const AttnArgs& a, const Unit& u, ch
 #pragma unroll
   for (int s = 0; s < NS; ++s)
     qf[s] = ldg((const bf16x8*)(a.q + row * a.q_stride + (size_t)(u.kh * group + pr % group) * DH + 32 * s + 8 * g));
-  float m = -INFINITY, l = 0.0f;
+  float m = nobody ? 0.0f : -INFINITY, l = 0.0f;
+  if (nobody)
+#pragma unroll
+    for (int s = 0; s < NS; ++s) qf[s] = (bf16)0.0f;
   Strays strays;
   f32x4 o[NB];
 #pragma unroll
