@@ -540,8 +540,8 @@ def batch_attention(cfg, n_kv_heads: int, layer: int, q, k_cache, v_cache, prefi
 
 
 def batch_commit(cfg, n_kv_heads: int, k_pages, v_pages, plan, n_requests: int, path, accept_len, stream=None):
-    """Rollback of every request to its verified sequence (see llmcad_batch_commit): path int32 [n_rows],
-    accept_len int32 [n_requests], on the device."""
+    """Rollback of every request to its verified sequence (see llmcad_batch_commit): path int32 [n_rows] (the
+    plan's, padding included: with another length nothing moves), accept_len int32 [n_requests], on the device."""
     what = "batch_commit"
     dev = _on_device(what, k_pages, v_pages, plan, path, accept_len)
     _want(what, "path", path, torch.int32, None)
@@ -854,15 +854,24 @@ class Batch:
         batch_plan(self.cfg, row_start, held, parent, self.prefix_len, self.block_table, self.free_pages,
                    self.n_pages, self.plan_buffer, self.n_rows)
 
+    def _rows(self, what, **tensors):
+        """Every tensor has the plan's n_rows rows (with another number the kernels would leave all as it was)."""
+        for name, t in tensors.items():
+            if t.dim() == 0 or t.shape[0] != self.n_rows:
+                raise ValueError(f"Batch.{what}: {name} must have {self.n_rows} rows, padding included, got {tuple(t.shape)}")
+
     def store(self, layer, q, k, v, q_out):
+        self._rows("store", q=q, k=k, v=v, q_out=q_out)
         batch_store(self.cfg, self.n_kv_heads, layer, q, k, v, q_out, self.k_pages, self.v_pages, self.plan_buffer,
                     self.n_requests)
 
     def attention(self, layer, q, out):
+        self._rows("attention", q=q, out=out)
         batch_attention(self.cfg, self.n_kv_heads, layer, q, self.k_cache, self.v_cache, self.prefix_len, self.k_pages,
                         self.v_pages, self.block_table, self.plan_buffer, out, self.workspace)
 
     def commit(self, path, accept_len):
+        self._rows("commit", path=path)
         batch_commit(self.cfg, self.n_kv_heads, self.k_pages, self.v_pages, self.plan_buffer, self.n_requests, path,
                      accept_len)
 

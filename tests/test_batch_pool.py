@@ -1,6 +1,6 @@
 """Batch's page accounting on the CPU, its plans made by the oracle: whatever a program does after a step that
 could not be placed, or between a plan and advance, every page is in one table entry or once on the
-free list, and no two requests share one."""
+free list, and no two requests share one; and its refusals."""
 
 import numpy as np
 import pytest
@@ -148,6 +148,23 @@ def test_entries_that_are_no_pages(pool, entry):
     b.release(1)
     b.advance()
     assert b.block_table[0].tolist() == [0, 1, -1] and b.free_pages.tolist() == [2, entry, 4, 5, 6, 7, 8]
+
+
+@pytest.mark.parametrize("rows", [0, 7, 9])
+def test_tensors_of_other_row_counts_are_refused(pool, rows):
+    # (the kernels would take them for those of another plan and do nothing)
+    b = pool(2, 8, 9, 3)
+    H, Dh = b.cfg.n_heads, b.cfg.head_dim
+    good, bad = torch.zeros(8, H, Dh, dtype=torch.bfloat16), torch.zeros(rows, H, Dh, dtype=torch.bfloat16)
+    for i in range(4):
+        with pytest.raises(ValueError, match="must have 8 rows"):
+            b.store(0, *[bad if j == i else good for j in range(4)])
+    for args in ((bad, good), (good, bad)):
+        with pytest.raises(ValueError, match="must have 8 rows"):
+            b.attention(0, *args)
+    for path in (torch.zeros(rows, dtype=torch.int32), torch.tensor(0, dtype=torch.int32)):
+        with pytest.raises(ValueError, match="must have 8 rows"):
+            b.commit(path, _i([0, 0]))
 
 
 def _walk(b, seed):
