@@ -394,8 +394,15 @@ def _on_device(what, first, *others):
     return dev
 
 
+def _same_device(dev, stream):
+    """A stream's kernels run on its own GPU: it must be the tensors'."""
+    if stream is not None and stream.device.index != dev:
+        raise ValueError(f"the stream is on {stream.device}, the tensors on cuda:{dev}")
+
+
 def _enqueue(fn, dev, stream, args):
     """fn(*args, stream) with dev the current device (a launch goes to the current device's kernels)."""
+    _same_device(dev, stream)
     if dev == torch.cuda.current_device():
         return fn(*args, _current_stream(dev) if stream is None else stream.cuda_stream)
     with torch.cuda.device(dev):
@@ -579,6 +586,7 @@ def token_scores(logits, tokens, k: int = 0, row_of=None, workspace=None, stream
         if row_of is not None:
             _want(what, "row_of", row_of, torch.int32, m)
     if stream is not None or dev != torch.cuda.current_device():
+        _same_device(dev, stream)
         with torch.cuda.device(dev), torch.cuda.stream(stream):
             return token_scores(logits, tokens, k, row_of, workspace)
     if workspace is None:

@@ -171,3 +171,18 @@ def test_wrappers_refuse_host_tensors(binding, cfg):
         binding.batch_plan(cfg, t, t[:3], None, 0, t[None], t, 9, t, 3)
     with pytest.raises(ValueError):
         binding.token_scores(torch.zeros(2, 5), t[:2])
+
+
+def test_streams_of_another_gpu_are_refused(binding, monkeypatch):
+    import types
+
+    import torch
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    ran = []
+    stream = lambda i: types.SimpleNamespace(device=torch.device("cuda", i), cuda_stream=77 + i)  # noqa: E731
+    with pytest.raises(ValueError, match="stream"):
+        binding._enqueue(lambda *a: ran.append(a), 0, stream(1), (1, 2))
+    assert not ran
+    binding._enqueue(lambda *a: ran.append(a), 0, stream(0), (1, 2))
+    assert ran == [(1, 2, 77)]

@@ -208,3 +208,11 @@ def test_refusals(binding):
             binding.token_scores(x, tok, k)
     with pytest.raises(binding.LlmcadError):
         binding.token_scores(x, tok, 3, workspace=torch.zeros(8, dtype=torch.uint8, device="cuda"))
+
+
+def test_a_stream_of_another_gpu_is_refused(binding):
+    import types
+
+    x = _logits(2, 100)
+    with pytest.raises(ValueError, match="stream"):
+        binding.token_scores(x, None, stream=types.SimpleNamespace(device=torch.device("cuda", 1)))
