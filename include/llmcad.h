@@ -364,8 +364,9 @@ int llmcad_commit_path(const llmcad_config* cfg, void* k_cache, void* v_cache, i
 #define LLMCAD_PLAN_OK 0
 #define LLMCAD_PLAN_BAD_LENGTHS 1 /* row_start does not rise from 0 to at most n_rows in steps of at most
                                      LLMCAD_MAX_NODES, or a length is negative: no request is placed */
-#define LLMCAD_PLAN_NO_PAGES 2    /* the request's rows need pages past its table or the free list, or an
-                                     entry of either is not in [0, n_pages): the request is not placed */
+#define LLMCAD_PLAN_NO_PAGES 2    /* the request's rows need pages past its table or the free list, an entry
+                                     of either is not in [0, n_pages), or prefix_len + held + rows passes
+                                     2^31: the request is not placed */
 #define LLMCAD_PLAN_BAD_TREE 3    /* its parents are not a tree (-1 for the first row, then earlier rows) */
 
 /* Bytes of a plan (0 if the configuration or a size is invalid: 1 <= n_requests

@@ -35,7 +35,7 @@ def plan(row_start, held, parent, prefix_len, block_table, free_pages, n_pages, 
             taken += want - have
             if count[b] == 0:
                 continue
-            if want > table.shape[1] or taken > len(free_pages):
+            if want > table.shape[1] or taken > len(free_pages) or prefix_len + end > 2**31:
                 status[b] = NO_PAGES
                 continue
             pages = list(table[b, :have]) + [free_pages[i] for i in mine]

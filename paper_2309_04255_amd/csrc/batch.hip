@@ -119,7 +119,8 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(PlanArgs a) {
   __syncthreads();
   int st = LLMCAD_PLAN_OK;
   if (invalid) st = LLMCAD_PLAN_BAD_LENGTHS;
-  else if (nb > 0 && (end > (long long)a.max_pages * kPage || need_before + need > a.n_free)) st = LLMCAD_PLAN_NO_PAGES;
+  else if (nb > 0 && (end > (long long)a.max_pages * kPage || need_before + need > a.n_free || a.prefix_len + end > 1ll << 31))
+    st = LLMCAD_PLAN_NO_PAGES;  // (the last: a position that is no int32)
   const int col0 = hb / kPage;  // table column of the first new row
   if (st == LLMCAD_PLAN_OK && nb > 0 && tid < 4) {
     const int col = col0 + tid;

@@ -179,6 +179,24 @@ def test_plan_that_cannot_be(binding, what):
     _check_plan(c.plan(**kw), want, c.d_table)
 
 
+@pytest.mark.parametrize("P,n,placed", [((1 << 30) - 1, 1, True), ((1 << 30) - 1, 2, False), (1 << 30, 1, False), ((1 << 30) - 2, 2, True)])
+def test_plan_at_the_last_position(binding, P, n, placed):
+    """Positions up to 2^31 - 1, those behind them refused."""
+    held, columns = 1 << 30, (1 << 24) + 1
+    cfg = _cfg(binding, 2, 64)
+    table = torch.full((1, columns), -1, dtype=torch.int32, device="cuda")
+    plan = torch.full((binding.batch_plan_bytes(cfg, 1, n),), 0x5A, dtype=torch.uint8, device="cuda")
+    binding.batch_plan(cfg, _dev([0, n]), _dev([held]), None, P, table, _dev([3]), 4, plan, n)
+    got = binding.batch_plan_views(cfg, 1, n, plan)
+    assert got["status"].tolist() == [binding.PLAN_OK if placed else binding.PLAN_NO_PAGES]
+    assert got["position"].tolist() == ([P + held + i for i in range(n)] if placed else [0] * n)
+    assert got["slot"].tolist() == ([3 * PAGE + i for i in range(n)] if placed else [-1] * n)
+    assert int(table[0, -1]) == (3 if placed else -1)
+    if placed:
+        ang = np.array(got["position"].tolist(), dtype=np.float64)[:, None] * THETA ** (-2.0 * np.arange(32) / 64)
+        np.testing.assert_allclose(got["rope"].cpu().numpy(), np.stack([np.cos(ang), np.sin(ang)], -1), atol=2.0 ** -20, rtol=0)
+
+
 def _strided(t, gap):
     """A copy of t [N, heads, Dh] whose rows lie `gap` elements further apart."""
     N, h, d = t.shape
