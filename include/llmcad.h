@@ -485,7 +485,8 @@ size_t llmcad_token_scores_workspace_bytes(int32_t n_rows, int32_t vocab, int32_
  * they are, and what else they hold likely.
  *
  * logits [n_rows][vocab], rows row_stride elements apart, fp32 (bits 32; what
- * the passes return) or bf16 (bits 16), 1 <= vocab <= 2^24.
+ * the passes return) or bf16 (bits 16), 1 <= n_rows < 2^24, 1 <= vocab <= 2^24,
+ * n_tokens <= 2^30.
  *   lse fp32 [n_rows]      log sum_t exp(logit_t)
  *   entropy fp32 [n_rows]  -sum_t p_t log p_t, p = exp(logit - lse)
  *   logprob fp32 [n_tokens] log p of tokens[i] under row row_of[i] (NULL: row i,

@@ -585,6 +585,8 @@ def token_scores(logits, tokens, k: int = 0, row_of=None, workspace=None, stream
         _want(what, "tokens", tokens, torch.int32, n if row_of is None else m)
         if row_of is not None:
             _want(what, "row_of", row_of, torch.int32, m)
+    if max(n, m) >= 1 << 31:  # (ctypes would cut the count)
+        raise ValueError(f"token_scores: {n} rows and {m} tokens are too many")
     if stream is not None or dev != torch.cuda.current_device():
         _same_device(dev, stream)
         with torch.cuda.device(dev), torch.cuda.stream(stream):

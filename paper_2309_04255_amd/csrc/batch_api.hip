@@ -242,7 +242,7 @@ int llmcad_batch_commit(const llmcad_config* cfg, int32_t n_kv_heads, void* k_pa
 }
 
 size_t llmcad_token_scores_workspace_bytes(int32_t n_rows, int32_t vocab, int32_t k) {
-  if (n_rows < 1 || vocab < 1 || vocab > (1 << 24) || k < 0 || k > LLMCAD_TOP_MAX) return 0;
+  if (n_rows < 1 || n_rows >= (1 << 24) || vocab < 1 || vocab > (1 << 24) || k < 0 || k > LLMCAD_TOP_MAX) return 0;
   return std::max((size_t)256, score_part_bytes(n_rows, vocab, k));
 }
 
@@ -254,6 +254,8 @@ int llmcad_token_scores(const void* logits, int32_t bits, int64_t row_stride, in
       (n_tokens > 0 && (!tokens || !logprob)) || (n_tokens > 0 && !row_of && n_tokens != n_rows) || k < 0 ||
       k > LLMCAD_TOP_MAX || (k > 0 && (!top_token || !top_logprob)))
     return LLMCAD_EARG;
+  // (more rows than a launch takes workgroups of 256 threads; a workgroup counts the tokens in 32 bits, past the last)
+  if (n_rows >= (1 << 24) || n_tokens > (1 << 30)) return LLMCAD_EARG;
   if (row_stride < vocab || vocab > (1 << 24)) return LLMCAD_ESHAPE;
   if (((uintptr_t)logits & (bits / 8 - 1)) != 0 || !aligned4(tokens) || !aligned4(row_of) || !aligned16(workspace))
     return LLMCAD_EARG;

@@ -154,6 +154,13 @@ def test_scores_refusals(binding, kw, status):
     assert _scores(binding, **kw) == getattr(binding, status)
 
 
+@pytest.mark.parametrize("kw", [dict(n=1 << 24, m=1 << 24), dict(m=(1 << 30) + 1, row_of=FAKE), dict(m=(1 << 31) - 1, row_of=FAKE)])
+def test_scores_of_too_many(binding, kw):
+    # (2^31 - 1 tokens: the count of the last step past them would turn negative, and an index with it)
+    assert _scores(binding, **kw) == binding.EARG
+    assert binding.token_scores_workspace_bytes((1 << 24) - 1, 5, 1) > 0 and binding.token_scores_workspace_bytes(1 << 24, 5, 1) == 0
+
+
 def test_bad_configurations(binding):
     bad = binding.make_config(workloads.MODELS["llama7b"])
     bad.head_dim = 96
