@@ -355,7 +355,8 @@ int llmcad_commit_path(const llmcad_config* cfg, void* k_cache, void* v_cache, i
  *
  * The configuration gives L, H, Dh and theta; n_kv_heads (Hkv) divides H, and
  * query head h reads K/V head h / (H / Hkv).  Pointers to bf16 data, plans and
- * workspaces are 16-byte aligned, row strides multiples of 8 elements.
+ * workspaces are 16-byte aligned, those to int32 arrays 4-byte, row strides
+ * multiples of 8 elements.
  */
 #define LLMCAD_PAGE 64
 #define LLMCAD_MAX_REQUESTS 1024

@@ -11,7 +11,10 @@ using namespace llmcad;
 namespace {
 
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
-bool aligned4(const void* p) { return ((uintptr_t)p & 3) == 0; }
+template <typename... P>
+bool aligned4(P... p) {
+  return ((... | (uintptr_t)p) & 3) == 0;
+}
 
 // (Limits that keep every product below in 64 bits and every slot in 32.)
 constexpr int kMaxRows = kMaxRequests * LLMCAD_MAX_NODES * 2;
@@ -75,7 +78,8 @@ int llmcad_batch_plan(const llmcad_config* cfg, int32_t n_requests, int32_t n_ro
   const int rc = check_batch(cfg, n_requests, n_rows);
   if (rc != LLMCAD_OK) return rc;
   if (!row_start || !held || !block_table || !plan || !aligned16(plan) || max_pages < 1 || max_pages > kMaxPages ||
-      n_pages < 1 || n_pages > kMaxPages || n_free < 0 || (n_free > 0 && !free_pages))
+      n_pages < 1 || n_pages > kMaxPages || n_free < 0 || (n_free > 0 && !free_pages) ||
+      !aligned4(row_start, held, parent, block_table, free_pages))
     return LLMCAD_EARG;
   if (prefix_len < 0 || prefix_len > (1 << 30)) return LLMCAD_ECAPACITY;
   const PlanLayout P(n_requests, n_rows, cfg->head_dim);
@@ -174,7 +178,7 @@ int llmcad_batch_attention(const llmcad_config* cfg, int32_t n_kv_heads, int32_t
   const int64_t H = cfg->n_heads, Dh = cfg->head_dim;
   if (q_stride < H * Dh) return LLMCAD_ESHAPE;
   if (q_stride % 8 || !aligned16(q) || !aligned16(out) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(plan) ||
-      !aligned16(workspace))
+      !aligned16(workspace) || !aligned4(block_table))
     return LLMCAD_EARG;
   const PlanLayout P(n_requests, n_rows, cfg->head_dim);
   if (plan_bytes < P.total || workspace_bytes < llmcad_batch_workspace_bytes(cfg, n_kv_heads, n_requests, n_rows))
@@ -220,7 +224,7 @@ int llmcad_batch_commit(const llmcad_config* cfg, int32_t n_kv_heads, void* k_pa
   rc = check_kv_heads(cfg, n_kv_heads);
   if (rc != LLMCAD_OK) return rc;
   if (!k_pages || !v_pages || !plan || !path || !accept_len || n_pages < 1 || n_pages > kMaxPages || !aligned16(k_pages) ||
-      !aligned16(v_pages) || !aligned16(plan))
+      !aligned16(v_pages) || !aligned16(plan) || !aligned4(path, accept_len))
     return LLMCAD_EARG;
   const PlanLayout P(n_requests, n_rows, cfg->head_dim);
   if (plan_bytes < P.total) return LLMCAD_EWORKSPACE;
@@ -257,7 +261,8 @@ int llmcad_token_scores(const void* logits, int32_t bits, int64_t row_stride, in
   // (more rows than a launch takes workgroups of 256 threads; a workgroup counts the tokens in 32 bits, past the last)
   if (n_rows >= (1 << 24) || n_tokens > (1 << 30)) return LLMCAD_EARG;
   if (row_stride < vocab || vocab > (1 << 24)) return LLMCAD_ESHAPE;
-  if (((uintptr_t)logits & (bits / 8 - 1)) != 0 || !aligned4(tokens) || !aligned4(row_of) || !aligned16(workspace))
+  if (((uintptr_t)logits & (bits / 8 - 1)) != 0 || !aligned16(workspace) ||
+      !aligned4(tokens, row_of, logprob, entropy, lse, top_token, top_logprob))
     return LLMCAD_EARG;
   if (workspace_bytes < llmcad_token_scores_workspace_bytes(n_rows, vocab, k)) return LLMCAD_EWORKSPACE;
   ScoresArgs a;

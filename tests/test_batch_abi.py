@@ -161,6 +161,15 @@ def test_scores_of_too_many(binding, kw):
     assert binding.token_scores_workspace_bytes((1 << 24) - 1, 5, 1) > 0 and binding.token_scores_workspace_bytes(1 << 24, 5, 1) == 0
 
 
+@pytest.mark.parametrize("call,names", [(_plan, ("row_start", "held", "parent", "table", "free")), (_attention, ("table",)),
+                                        (_commit, ("path", "acc")), (_scores, ("row_of", "lp", "ent", "lse", "tt", "tl"))])
+def test_unaligned_words(binding, cfg, call, names):
+    for name in names:
+        for off in (1, 2, 3):
+            args = (binding,) if call is _scores else (binding, cfg)
+            assert call(*args, **{name: FAKE + off}) == binding.EARG, (name, off)
+
+
 def test_bad_configurations(binding):
     bad = binding.make_config(workloads.MODELS["llama7b"])
     bad.head_dim = 96
