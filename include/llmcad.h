@@ -350,8 +350,8 @@ int llmcad_commit_path(const llmcad_config* cfg, void* k_cache, void* v_cache, i
  * llmcad_batch_attention in every layer, and llmcad_batch_commit after the
  * target has answered.  Lengths, tables and trees are device arrays, so that a
  * step can be captured and replayed while requests grow.  They take the plan's
- * n_requests and n_rows; with others (or a buffer that holds no plan) they leave
- * everything as it was.
+ * n_requests and n_rows, the attention a table of its max_pages columns or more;
+ * with others (or a buffer that holds no plan) they leave everything as it was.
  *
  * The configuration gives L, H, Dh and theta; n_kv_heads (Hkv) divides H, and
  * query head h reads K/V head h / (H / Hkv).  Pointers to bf16 data, plans and

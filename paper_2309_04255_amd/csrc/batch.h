@@ -45,7 +45,7 @@ struct BatchUnit {
 };
 
 // Head of a plan (int32 words).
-enum PlanWord { PLAN_UNITS = 0, PLAN_TAKEN = 1, PLAN_REQUESTS = 2, PLAN_ROWS = 3, PLAN_WORDS = 64 };
+enum PlanWord { PLAN_UNITS = 0, PLAN_TAKEN = 1, PLAN_REQUESTS = 2, PLAN_ROWS = 3, PLAN_MAX_PAGES = 4, PLAN_WORDS = 64 };
 // A plan for other sizes lies elsewhere in its buffer: the operators leave it unused.
 __device__ __forceinline__ bool plan_is_for(const int* head, int B, int N) {
   return ldg(head + PLAN_REQUESTS) == B && ldg(head + PLAN_ROWS) == N;

@@ -241,6 +241,7 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(PlanArgs a) {
       stg(a.head + PLAN_TAKEN, (int)(invalid ? 0 : taken));
       stg(a.head + PLAN_REQUESTS, B);
       stg(a.head + PLAN_ROWS, a.N);
+      stg(a.head + PLAN_MAX_PAGES, a.max_pages);
     }
   }
   if (!invalid)

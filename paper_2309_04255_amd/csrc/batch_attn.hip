@@ -661,12 +661,18 @@ __device__ __forceinline__ bool prefix_unit(const AttnArgs& a, int w, int units,
   return true;
 }
 
+// The plan is for this call.  (A narrower table than the plan's gives fewer
+// workgroups than the plan has runs.)
+__device__ __forceinline__ bool plan_fits(const AttnArgs& a) {
+  return plan_is_for(a.head, a.B, a.N) && ldg(a.head + PLAN_MAX_PAGES) <= a.max_pages;
+}
+
 // Workgroup x of the runs' part: a.merge runs of a request's pages for one K/V head.
 __device__ __forceinline__ bool run_unit(const AttnArgs& a, int x, Unit& u) {
   const int run_of = x / a.Hkv;
   u.kh = x % a.Hkv;
   const BatchUnit r = ldg(a.units + run_of);  // (what lies behind the last one is not used)
-  if (run_of >= ldg(a.head + PLAN_UNITS) || !plan_is_for(a.head, a.B, a.N) || r.n == 0 || r.run % a.merge != 0) return false;
+  if (run_of >= ldg(a.head + PLAN_UNITS) || !plan_fits(a) || r.n == 0 || r.run % a.merge != 0) return false;
   u.row0 = r.row0;
   u.pairs = r.n * (a.H / a.Hkv);
   u.held = r.held;
@@ -727,7 +733,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttnArgs a) {
   if (item >= (size_t)a.N * a.H) return;
   const int row = (int)(item / a.H), h = (int)(item % a.H);
   const int b = ldg(a.row_req + row);
-  if (!plan_is_for(a.head, a.B, a.N) || b < 0) return;  // (no request's row: left as it was)
+  if (!plan_fits(a) || b < 0) return;  // (no request's row: left as it was)
   const BatchRequest r = ldg(a.req + b);
   const int parts = a.KP + up_div(r.splits, a.merge);
   auto place = [&](int p) {

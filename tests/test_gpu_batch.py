@@ -636,6 +636,20 @@ def test_plan_of_other_sizes_is_not_used(binding):
         assert bool((qo == 5.0).all()) and torch.equal(kp, k0) and torch.equal(vp, v0)
 
 
+def test_attention_with_a_narrower_table_than_the_plans(binding):
+    """The plan's runs of pages past the table would have no workgroup: all is left as it was.  A wider table serves."""
+    c = Case(binding, [5, 3], [700, 10], P=40, H=4, Hkv=2, Dh=64)
+    c.plan()
+    kp, vp = c.pages()
+    kc, vc = _prefix(c)
+    q = _queries(c)
+    want = _attend(c, None, q, kc, vc, kp, vp)
+    out = _attend(c, None, q, kc, vc, kp, vp, table=c.d_table[:, :4].contiguous())
+    assert bool((out == 77.0).all())
+    wider = torch.cat([c.d_table, torch.full_like(c.d_table, 1 << 30)], 1)
+    assert torch.equal(_attend(c, None, q, kc, vc, kp, vp, table=wider), want)
+
+
 def test_batch_keeps_its_pages(binding):
     """Many steps whose trees are mostly rejected: trimmed, the pool loses no page; a request that
     cannot be placed is reported."""
