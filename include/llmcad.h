@@ -477,8 +477,8 @@ int llmcad_batch_commit(const llmcad_config* cfg, int32_t n_kv_heads, void* k_pa
 #define LLMCAD_TOP_MAX 64
 
 /* Bytes of llmcad_token_scores' workspace (0 if an argument is invalid; 16-byte
- * aligned): up to 64 long rows are shared between workgroups through it.  It need
- * not be cleared; calls that share one must not overlap. */
+ * aligned): up to 64 long rows are shared between workgroups through it, and the
+ * rows' sums handed to a launch over many tokens with row_of.  It need not be cleared; calls that share one must not overlap. */
 size_t llmcad_token_scores_workspace_bytes(int32_t n_rows, int32_t vocab, int32_t k);
 
 /*

@@ -169,8 +169,9 @@ struct ScoresArgs {
   int parts, span;    // a row in workgroups of so many values
   float* part_sums;   // [n][parts][4]
   uint64_t* part_best; // [n][parts][k]
+  float* row_scores;   // [n][4] where a second launch takes the tokens, else null
 };
-size_t score_part_bytes(int n, int V, int k);
+size_t score_work_bytes(int n, int V, int k);
 hipError_t launch_token_scores(ScoresArgs a, void* workspace, hipStream_t st);
 
 }  // namespace llmcad

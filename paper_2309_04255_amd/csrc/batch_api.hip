@@ -247,7 +247,7 @@ int llmcad_batch_commit(const llmcad_config* cfg, int32_t n_kv_heads, void* k_pa
 
 size_t llmcad_token_scores_workspace_bytes(int32_t n_rows, int32_t vocab, int32_t k) {
   if (n_rows < 1 || n_rows >= (1 << 24) || vocab < 1 || vocab > (1 << 24) || k < 0 || k > LLMCAD_TOP_MAX) return 0;
-  return std::max((size_t)256, score_part_bytes(n_rows, vocab, k));
+  return std::max((size_t)256, score_work_bytes(n_rows, vocab, k));
 }
 
 int llmcad_token_scores(const void* logits, int32_t bits, int64_t row_stride, int32_t n_rows, int32_t vocab,

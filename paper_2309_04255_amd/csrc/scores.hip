@@ -268,6 +268,27 @@ __device__ __attribute__((noinline)) Sums sums_again(const void* row, int V, Sco
   return w;
 }
 
+// What a row's log probabilities need: its maximum and the logarithm of its sum, in
+// base 2 or natural units.
+typedef f32x4 RowScore;  // (maximum, logarithm, kind)
+enum { ROW_LOG2 = 0, ROW_NATURAL = 1, ROW_NONE = 2, ROW_BAD = 3 };
+__device__ __forceinline__ float log_prob(const RowScore& s, float x) {
+  const bool plain = s[2] == ROW_LOG2;
+  const float unit = plain ? kLn2 : 1.0f;
+  const float d = plain ? __builtin_fmaf(x, kLog2e, -s[0]) : x - s[0];
+  if (d == -INFINITY) return x - s[0] * unit;  // (a finite value far below, in natural units)
+  return fminf((d - s[1]) * unit, 0.0f);
+}
+// Given token q under its row.
+template <bool BF16>
+__device__ __forceinline__ void score_token(const ScoresArgs& a, int q, const char* row, const RowScore& s) {
+  const int t = ldg(a.tokens + q);
+  float v = 0.0f;
+  if (t >= a.V) v = NAN;
+  else if (t >= 0) v = s[2] == ROW_BAD ? NAN : s[2] == ROW_NONE ? -INFINITY : log_prob(s, value_at<BF16>(row, t));
+  stg(a.logprob + q, v);
+}
+
 // The outputs of row r from its sums w (log2 domain).  All threads call it; best():
 // the row's k best to L.keep.
 template <bool BF16, int THREADS, typename BEST>
@@ -279,29 +300,20 @@ __device__ __forceinline__ void finish(const ScoresArgs& a, int r, const char* r
   if (!plain) w = sums_again<BF16, THREADS>(row, V, L);
   const bool none = w.s == 0.0f, bad = w.s != w.s;
   const float unit = plain ? kLn2 : 1.0f, logS = none ? 0.0f : plain ? log2f(w.s) : logf(w.s);
-  auto log_prob = [&](float x) {
-    const float d = plain ? __builtin_fmaf(x, kLog2e, -w.m) : x - w.m;
-    if (d == -INFINITY) return x - w.m * unit;  // (a finite value far below, in natural units)
-    return fminf((d - logS) * unit, 0.0f);
-  };
+  const RowScore row_score = {w.m, logS, (float)(bad ? ROW_BAD : none ? ROW_NONE : plain ? ROW_LOG2 : ROW_NATURAL), 0.0f};
   if (tid == 0) {
     stg(a.lse + r, bad ? w.s : none ? -INFINITY : (w.m + logS) * unit);
     stg(a.entropy + r, bad ? w.s : none ? 0.0f : (logS - w.t / w.s) * unit);
   }
   // the given tokens under this row
-  auto score = [&](int q) {
-    const int t = ldg(a.tokens + q);
-    float v = 0.0f;
-    if (t >= V) v = NAN;
-    else if (t >= 0) v = bad ? w.s : none ? -INFINITY : log_prob(value_at<BF16>(row, t));
-    stg(a.logprob + q, v);
-  };
   if (a.row_of == nullptr) {
-    if (tid == 0 && r < a.m) score(r);
+    if (tid == 0 && r < a.m) score_token<BF16>(a, r, row, row_score);
+  } else if (a.row_scores != nullptr) {
+    if (tid == 0) stg((RowScore*)a.row_scores + r, row_score);
   } else {
     for (int q = tid; q < a.m; q += THREADS) {
       const int of = ldg(a.row_of + q);
-      if (of == r) score(q);
+      if (of == r) score_token<BF16>(a, q, row, row_score);
       else if (r == 0 && (of < 0 || of >= a.n)) stg(a.logprob + q, (float)NAN);
     }
   }
@@ -314,7 +326,7 @@ __device__ __forceinline__ void finish(const ScoresArgs& a, int r, const char* r
   if (tid < k) {
     const uint64_t e = L.keep[tid];
     stg(a.top_token + (size_t)r * k + tid, e ? (int)~(uint32_t)e : -1);
-    stg(a.top_logprob + (size_t)r * k + tid, bad ? w.s : e ? log_prob(unordered((uint32_t)(e >> 32))) : -INFINITY);
+    stg(a.top_logprob + (size_t)r * k + tid, bad ? w.s : e ? log_prob(row_score, unordered((uint32_t)(e >> 32))) : -INFINITY);
   }
 }
 
@@ -427,6 +439,18 @@ __global__ __launch_bounds__(THREADS, SPLIT ? 2 : 4) void scores_kernel(ScoresAr
   if (tid < k) stg(a.part_best + (size_t)blockIdx.x * k + tid, L.keep[tid]);
 }
 
+// Many given tokens, each under its row: a thread per token.
+template <bool BF16>
+__global__ __launch_bounds__(256) void tokens_kernel(ScoresArgs a) {
+  const int q = blockIdx.x * 256 + threadIdx.x;
+  if (q >= a.m) return;
+  const int r = ldg(a.row_of + q);
+  if (r < 0 || r >= a.n)
+    stg(a.logprob + q, (float)NAN);
+  else
+    score_token<BF16>(a, q, (const char*)a.logits + (size_t)r * a.stride * (BF16 ? 2 : 4), ldg((const RowScore*)a.row_scores + r));
+}
+
 // A workgroup per row joins its parts.
 constexpr int kJoinThreads = 1024;
 template <bool BF16>
@@ -474,10 +498,18 @@ int score_parts(int n, int V) {
   if (n > 64 || V <= 6 * 16384) return 1;
   return std::min({kList / LLMCAD_TOP_MAX, 256 / n, cdiv(V, 16384)});
 }
-size_t score_part_bytes(int n, int V, int k) {
-  const int parts = score_parts(n, V);
-  return parts > 1 ? (size_t)n * parts * (sizeof(f32x4) + sizeof(uint64_t) * k) : 0;
+static size_t part_bytes(int n, int parts, int k) {
+  return parts > 1 ? align_up((size_t)n * parts * (sizeof(f32x4) + sizeof(uint64_t) * k), 16) : 0;
 }
+size_t score_work_bytes(int n, int V, int k) { return part_bytes(n, score_parts(n, V), k) + (size_t)n * sizeof(RowScore); }
+
+// Tokens under rows of their own (row_of): up to this many, every row's workgroup
+// looks through all of them; above, a second launch takes them.  The look grows
+// with rows times tokens, the launch costs 2 to 3 us.  (us, looking / launching, bf16 rows and as
+// many tokens: 31 of 32000 13.8 / 16.0, 1000 of 32000 16.5 / 18.6, 2000 of 32000 29.2 / 29.0, 4000 of
+// 32000 54.6 / 47.7, of 2000 25.0 / 17.9, 20000 of 32000 594 / 231, 60000 of 8000 2749 / 222; 4000
+// tokens under 31 rows 14.2 / 16.1.)
+constexpr int kScanTokens = 2048;
 
 template <bool BF16>
 static void launch(const ScoresArgs& a, hipStream_t st) {
@@ -495,6 +527,7 @@ static void launch(const ScoresArgs& a, hipStream_t st) {
   } else {
     scores_kernel<BF16, 256, false><<<dim3(a.n), dim3(256), 0, st>>>(a);
   }
+  if (a.row_scores != nullptr) tokens_kernel<BF16><<<dim3(cdiv(a.m, 256)), dim3(256), 0, st>>>(a);
 }
 
 hipError_t launch_token_scores(ScoresArgs a, void* workspace, hipStream_t st) {
@@ -502,6 +535,7 @@ hipError_t launch_token_scores(ScoresArgs a, void* workspace, hipStream_t st) {
   a.span = cdiv(cdiv(a.V, a.parts), 64) * 64;
   a.part_sums = (float*)workspace;
   a.part_best = (uint64_t*)((f32x4*)workspace + (size_t)a.n * a.parts);
+  a.row_scores = a.row_of != nullptr && a.m > kScanTokens ? (float*)((char*)workspace + part_bytes(a.n, a.parts, a.k)) : nullptr;
   if (a.bf16_in)
     launch<true>(a, st);
   else

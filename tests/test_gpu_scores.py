@@ -164,6 +164,49 @@ def test_given_tokens_of_a_tree(binding):
     _check(binding, x, [1, 2, 3, 4, 5, 6, -3], 0)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n,V,m", [(6000, 300, 2048), (6000, 300, 2049), (3, 150001, 5000), (9, 3000, 40000)])
+def test_many_tokens_under_rows_of_their_own(binding, dtype, n, V, m):
+    """The same bits as a few at a time, whatever the rows hold."""
+    x = _logits(n, V, dtype, stride=V + 5)
+    x[0] = -float("inf")
+    x[1, 7] = float("nan")
+    x[2] = torch.finfo(dtype).max  # (whose product with log2 e is no number of these)
+    g = torch.Generator(device="cuda").manual_seed(m)
+    tok = torch.randint(-2, V + 2, (m,), device="cuda", generator=g, dtype=torch.int32)
+    row = torch.randint(-1, n + 1, (m,), device="cuda", generator=g, dtype=torch.int32)
+    row[:40] = torch.arange(40, device="cuda", dtype=torch.int32) % 3
+    got = binding.token_scores(x, tok, 3, row_of=row)
+    parts = [binding.token_scores(x, tok[i:i + 1000].contiguous(), 3, row_of=row[i:i + 1000].contiguous()) for i in range(0, m, 1000)]
+    want = torch.cat([p["logprob"] for p in parts])
+    assert torch.equal(got["logprob"].isnan(), want.isnan())
+    assert torch.equal(got["logprob"].nan_to_num(nan=7.0), want.nan_to_num(nan=7.0))
+    for name in ("lse", "entropy", "top_token", "top_logprob"):
+        assert torch.equal(got[name].nan_to_num(nan=7.0), parts[0][name].nan_to_num(nan=7.0))
+
+
+def test_time_of_many_tokens_grows_with_their_number(binding):
+    """300000 rows and tokens: within five times the call without row_of (looking through all
+    tokens for every row would take a hundred times it)."""
+    n, V = 300000, 64
+    x = _logits(n, V, torch.bfloat16)
+    tok = torch.arange(n, device="cuda", dtype=torch.int32) % V
+    row = torch.arange(n, device="cuda", dtype=torch.int32)
+
+    def ms(row_of):
+        ev = [torch.cuda.Event(enable_timing=True) for _ in range(2)]
+        for i in range(2):  # (the second one counts)
+            ev[0].record()
+            got = binding.token_scores(x, tok, row_of=row_of)
+            ev[1].record()
+        torch.cuda.synchronize()
+        return ev[0].elapsed_time(ev[1]), got
+
+    (plain, a), (under, b) = ms(None), ms(row)
+    assert torch.equal(a["logprob"], b["logprob"])
+    assert under <= 5 * plain, (plain, under)
+
+
 def test_near_certain_row(binding):
     x = torch.full((1, 32000), -30.0, device="cuda")
     x[0, 123] = 10.0
