@@ -17,10 +17,11 @@
 //
 // One token per request: bound by the reads of the pages and the prefix (128 tokens,
 // 32 query heads on 8 K/V heads of 128, behind 8192 positions and up to 1024 tokens of
-// their own: 82 us, 305 MB read, 3.6 TB/s; the narrow units' loads are 16 rows of
-// 64 bytes).  Trees: bound by the instructions beside the matrix products (32 trees of 41, 40
-// heads of 128, behind 4099: 192 us, 680 TFLOP/s in the first launch, the matrix
-// cores busy 42% of it, 491 MB read where each byte once is 463).
+// their own: 83 us, 305 MB read, 3.6 TB/s; the narrow units' loads are 16 rows of
+// 64 bytes, and a wave waits for all it has in flight twice a step).  Trees: bound by
+// the instructions beside the matrix products (32 trees of 41, 40 heads of 128, behind
+// 4099: 194 to 200 us, 650 to 700 TFLOP/s in the first launch, the matrix cores busy 41% of
+// it, 491 MB read where each byte once is 463).
 #include "batch.h"
 
 namespace llmcad {
@@ -185,7 +186,10 @@ __device__ __forceinline__ bf16x8 finite(const bf16x8& v) {
 // ---------------------------------------------------------------- many rows
 //
 // 64 RB pairs per workgroup, 16 RB per wave.  Tiles of 32 keys are shared
-// through LDS, in two buffers: while one is computed the next is copied.
+// through LDS, in two buffers: while one is computed the next is copied.  (So in
+// the prefix.  In pages look() asks for the tile's page again, a lane of a register
+// that may have just been loaded, and waits there for the next tile's copy too: it
+// overlaps the score products alone.)
 //
 // Two row blocks per wave for the prefix: each fragment read from LDS feeds two
 // products, in 168 registers, three waves per SIMD (three or four blocks leave one
@@ -196,7 +200,9 @@ __device__ __forceinline__ bf16x8 finite(const bf16x8& v) {
 // the output is rescaled only when some score exceeds it by 2^kSlack, and
 // until then no lane needs another's scores.  The sums are per lane, joined at
 // the end.  Probabilities (up to 2^kSlack) enter the value product in bf16, half
-// a step of 2^-8 each.
+// a step of 2^-8 each: 0.0023 of the outputs against 64 bits, where their own rounding
+// is 0.0017.  (Two bf16 parts, as with few rows, were measured: 16 trees of 31 rows 46 us
+// and 55, 32 of 41 194 and 244, 128 tokens 84 and 86; the matrix products are the price.)
 template <int DH, int RB, bool PAGED>
 struct TileWork {
   static constexpr int NS = Frags<DH>::NS, NB = Frags<DH>::NB;
@@ -451,10 +457,13 @@ struct TileWork {
 // ---------------------------------------------------------------- few rows
 //
 // 16 pairs at a time: the waves take every fourth 32-key step each and meet in
-// LDS.  What such a unit takes is the time of its loads, so a wave fetches the
-// next step's keys as soon as the scores have taken this one's, and its values
-// behind the value product; and the probabilities enter that product as two bf16
-// halves (about 16 bits): the matrix cores have the time.
+// LDS.  What such a unit takes is the time of its loads.  A wave issues the next
+// step's keys as soon as the scores have taken this one's, and its values behind
+// the value product, but does not overlap them with its own work: the score products wait
+// for everything (the queries are the youngest loads in front of the loop), and so
+// does the next step's page, whose lane may have just been loaded; other
+// workgroups fill the time.  The probabilities enter the value product as two
+// bf16 halves (about 16 bits): the matrix cores have the time.
 template <int DH>
 __device__ __forceinline__ void narrow_unit(const AttnArgs& a, const Unit& u, char* lds) {
   constexpr int NS = Frags<DH>::NS, NB = Frags<DH>::NB;

@@ -492,8 +492,11 @@ __global__ __launch_bounds__(kJoinThreads) void scores_join_kernel(ScoresArgs a)
 // Up to 64 rows of many values: parts of about 16384, up to a workgroup per CU over
 // all rows; their best values fit the list that joins them.  (The second launch
 // costs 3 us of the host.  With k of 64, 31 fp32 rows of 250000 take 28.3 us, 40.2
-// unsplit, one 23.2 and 37.9; with k of 8, 31 of 150000 21.4 and 23.0; below 6 parts
-// nothing is won, and 100 rows of 250000 with k of 8 take 38.0 and 33.3.)
+// unsplit, one 23.2 and 37.9; with k of 8, 31 of 150000 21.4 and 23.0.  Rows of up to six
+// such parts win nothing.  From 43 rows on the CUs allow five or four parts of longer
+// rows, which pay all the same: with k of 8 on the GPU alone, 44 fp32 rows of 250000 20.9
+// and 29.9, 64 of them 23.1 and 30.1, 44 and 64 of 100000 15.6 and 16.8, 17.1 and 17.0;
+// 100 rows of 250000 take 38.0 and 33.3.)
 int score_parts(int n, int V) {
   if (n > 64 || V <= 6 * 16384) return 1;
   return std::min({kList / LLMCAD_TOP_MAX, 256 / n, cdiv(V, 16384)});
