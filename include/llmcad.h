@@ -430,6 +430,25 @@ int llmcad_batch_store(const llmcad_config* cfg, int32_t n_kv_heads, int32_t lay
                        void* v_pages, int32_t n_pages, const void* plan, size_t plan_bytes, int32_t n_requests,
                        int32_t n_rows, void* stream);
 
+/*
+ * llmcad_batch_store for models that norm the queries and keys of each head: a
+ * head x becomes x / sqrt(mean(x^2) + cfg->rms_eps) times its gain, is turned, and
+ * is rounded to bf16 once; squares, their sum and the rotation are in fp32.
+ *
+ * q_gain and k_gain are bf16: [Dh] with a gain stride of 0 (one gain for all
+ * heads), or one gain per head, q_gain_stride and k_gain_stride elements apart; NULL
+ * is a gain of ones.  Everything else is as in llmcad_batch_store.
+ *
+ * Errors: as llmcad_batch_store; LLMCAD_EARG for a gain that is not 16-byte aligned or
+ * a gain stride that is no multiple of 8, LLMCAD_ESHAPE for one that is neither 0 nor
+ * at least Dh.
+ */
+int llmcad_batch_norm_store(const llmcad_config* cfg, int32_t n_kv_heads, int32_t layer, const void* q, int64_t q_stride,
+                            const void* k, int64_t k_stride, const void* v, int64_t v_stride, const void* q_gain,
+                            int64_t q_gain_stride, const void* k_gain, int64_t k_gain_stride, void* q_out, void* k_pages,
+                            void* v_pages, int32_t n_pages, const void* plan, size_t plan_bytes, int32_t n_requests,
+                            int32_t n_rows, void* stream);
+
 /* Bytes of llmcad_batch_attention's workspace (0 if an argument is invalid).  It
  * need not be cleared; calls that share one must not overlap. */
 size_t llmcad_batch_workspace_bytes(const llmcad_config* cfg, int32_t n_kv_heads, int32_t n_requests, int32_t n_rows);
@@ -472,6 +491,140 @@ int llmcad_batch_attention(const llmcad_config* cfg, int32_t n_kv_heads, int32_t
 int llmcad_batch_commit(const llmcad_config* cfg, int32_t n_kv_heads, void* k_pages, void* v_pages, int32_t n_pages,
                         const void* plan, size_t plan_bytes, int32_t n_requests, int32_t n_rows, const int32_t* path,
                         const int32_t* accept_len, void* stream);
+
+/* What llmcad_batch_adjust applies to a step's logits (device arrays; NULL: none of it).
+ * A row's text is its request's tokens behind the prefix, as many as the plan says it
+ * holds, then the tokens of the row's ancestors and its own.  Entries that are no token
+ * of the vocabulary count as absent. */
+typedef struct llmcad_adjustments {
+  const int32_t* tokens;     /* [n_rows] the rows' tokens (required with penalties)          */
+  const int32_t* history;    /* [n_requests][history_stride]: token t of request b; tokens
+                                from history_stride on count as absent                       */
+  int64_t history_stride;
+  const int32_t* prompt_len; /* [n_requests] the first tokens of the text that are a prompt
+                                (NULL: 0)                                                    */
+  const uint32_t* seen;      /* [W] tokens that every text holds besides (the prefix's): bit
+                                t % 32 of word t / 32, W = ceil(vocab / 32)                  */
+  const float* penalties;    /* [n_requests][3] repetition, presence, frequency              */
+  const int32_t* bias_start; /* [n_requests + 1] request b's biases are entries bias_start[b]
+                                .. bias_start[b + 1] - 1 of the next two, those in [0, n_bias) */
+  const int32_t* bias_token; /* [n_bias]; of a token's entries in one list the last counts   */
+  const float* bias_value;   /* [n_bias]                                                     */
+  int32_t n_bias;
+  const uint32_t* allow;     /* [n_masks][W] allowed tokens, bits as in seen                 */
+  int32_t n_masks;
+  const int32_t* mask_of;    /* [n_rows] the row's mask; negative: every token is allowed;
+                                from n_masks on: none is                                     */
+} llmcad_adjustments;
+
+/* Bytes of llmcad_batch_adjust's workspace (0 if an argument is invalid).  It need not
+ * be cleared; calls that share one must not overlap. */
+size_t llmcad_batch_adjust_workspace_bytes(const llmcad_config* cfg, int32_t n_rows);
+
+/*
+ * Adjusted logits of a step's rows, and every row's greedy token under them.
+ *
+ * logits [n_rows][vocab], rows row_stride elements apart, fp32 (bits 32) or bf16
+ * (bits 16).  With c the times that token t occurs in the row's text from prompt_len
+ * on, its logit x becomes, in fp32 and in this order:
+ *   t in the text, or in `seen`:  x / repetition if x > 0, x repetition otherwise
+ *   then                          x - frequency c, and x - presence if c > 0
+ *   then                          x + bias
+ *   t not allowed:                -inf
+ * and is rounded to the logits' type once.  Repetition 1 with presence and frequency 0
+ * changes nothing.
+ *   out     [n_rows][vocab], of the logits' type, rows out_stride elements apart; it
+ *           may be the logits (with their stride); NULL: not wanted
+ *   greedy  int32 [n_rows] the token of the largest adjusted (and rounded) logit, the
+ *           lowest among equals; -1 if all are -inf or an allowed one is NaN; NULL: not
+ *           wanted
+ * Rows of no request, or of one that the plan did not place, are left as they were.
+ *
+ * Errors (checked on the host, nothing enqueued): LLMCAD_EARG (a NULL or unaligned
+ * pointer, bits or a count out of range, neither out nor greedy; penalties without
+ * tokens, a negative history_stride, bias_start without its lists, n_masks < 1 with
+ * allow, allow or mask_of without the other, an out that overlaps the logits otherwise), LLMCAD_ESHAPE (a stride
+ * below vocab), LLMCAD_EWORKSPACE.
+ */
+int llmcad_batch_adjust(const llmcad_config* cfg, const void* plan, size_t plan_bytes, int32_t n_requests, int32_t n_rows,
+                        const void* logits, int32_t bits, int64_t row_stride, const llmcad_adjustments* by, void* out,
+                        int64_t out_stride, int32_t* greedy, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The accept walk of every request's tree (§3.2; llmcad_verify_tree's, for a batch): the
+ * longest root path whose draft tokens are the greedy tokens of their parents, the
+ * lowest node among equally deep ends.
+ *
+ * tokens int32 [n_rows] the rows' tokens, greedy int32 [n_rows] the target's token after
+ * each row.  path int32 [n_rows] receives each request's path, counted within the request,
+ * from entry row_start[b] on, and -1 behind it; accept_len int32 [n_requests] the accepted
+ * draft tokens (both as llmcad_batch_commit takes them); next_token int32 [n_requests] the
+ * greedy token after the path.  history int32 [n_requests][history_stride] (NULL: none)
+ * receives the path's tokens behind the held ones, entries held .. held + accept_len, those
+ * below history_stride.  A negative greedy token ends its branch.  A request without rows, or
+ * that the plan did not place, gets accept_len -1 (so held + accept_len + 1 is its length
+ * too); the rest of its outputs, and padding rows', are left as they were.
+ *
+ * Errors: LLMCAD_EARG (a NULL or unaligned pointer, a size out of range, a negative
+ * history_stride), LLMCAD_EWORKSPACE (plan_bytes).
+ */
+int llmcad_batch_accept(const llmcad_config* cfg, const void* plan, size_t plan_bytes, int32_t n_requests, int32_t n_rows,
+                        const int32_t* tokens, const int32_t* greedy, int32_t* path, int32_t* accept_len,
+                        int32_t* next_token, int32_t* history, int64_t history_stride, void* stream);
+
+/* Most pages of a pool, and most columns of its tables, that llmcad_batch_fork and
+ * llmcad_batch_compact take. */
+#define LLMCAD_MAX_POOL (1 << 18)
+
+/* Bytes of their workspace (0 if an argument is invalid).  It need not be cleared; calls
+ * that share one must not overlap. */
+size_t llmcad_batch_pages_workspace_bytes(int32_t n_requests, int32_t n_pages);
+
+/*
+ * Requests that continue from others, between two steps: request b continues from what
+ * request source[b] holds (itself: nothing changes; negative: it ends and holds nothing).
+ * Several answers to one prompt, beams that change places, requests that end.
+ *
+ * block_table int32 [n_requests][max_pages], held int32 [n_requests], source int32
+ * [n_requests] (device arrays).  table_out and held_out receive the new tables and lengths;
+ * entries past a request's pages are -1.  Full pages are shared: no step writes into them.  A last
+ * page that is not full goes on with its own request, or, where that continues from another or
+ * ends, with the first request that continues from it; the others get a copy (of the tokens it
+ * holds, in every layer and K/V head; the rest of the new page stays) in a page that no request
+ * held, the lowest pages first.
+ * free_pages int32 [n_pages] receives the pages that no table holds now, in order, then -1;
+ * n_free int32 [1] their number.  A request's last page that is not full must be in no other
+ * table before the call.
+ *
+ * status int32 [1]: LLMCAD_PLAN_OK; LLMCAD_PLAN_BAD_LENGTHS (a length is negative or past
+ * its table row, a source is not below n_requests); LLMCAD_PLAN_NO_PAGES (fewer pages are
+ * free than copies needed).  If it is not OK no page is written, table_out and held_out are
+ * the old ones, and n_free is 0.
+ *
+ * Errors (checked on the host, nothing enqueued): as llmcad_batch_commit; LLMCAD_EARG too for
+ * n_pages or max_pages above LLMCAD_MAX_POOL and for table_out or held_out that overlaps an
+ * input; LLMCAD_EWORKSPACE.
+ */
+int llmcad_batch_fork(const llmcad_config* cfg, int32_t n_kv_heads, void* k_pages, void* v_pages, int32_t n_pages,
+                      int32_t n_requests, const int32_t* block_table, int32_t max_pages, const int32_t* held,
+                      const int32_t* source, int32_t* table_out, int32_t* held_out, int32_t* free_pages, int32_t* n_free,
+                      int32_t* status, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Moves the pages that requests hold to the front of the pool, between two steps: the k-th
+ * page in use from n_used on is copied (every layer and K/V head) to the k-th unused one below,
+ * so that pages [0, n_used) are in use and the others are free.
+ *
+ * table_out int32 [n_requests][max_pages] receives the tables with the new pages, entries
+ * past a request's pages and those that are no page -1; n_used int32 [1] the number of pages
+ * in use.  Pages in several tables stay shared.  A length below 0 counts as 0, one past its
+ * table row as the row.
+ *
+ * Errors: as llmcad_batch_fork.
+ */
+int llmcad_batch_compact(const llmcad_config* cfg, int32_t n_kv_heads, void* k_pages, void* v_pages, int32_t n_pages,
+                         int32_t n_requests, const int32_t* block_table, int32_t max_pages, const int32_t* held,
+                         int32_t* table_out, int32_t* n_used, void* workspace, size_t workspace_bytes, void* stream);
 
 /* Most alternatives llmcad_token_scores returns per row. */
 #define LLMCAD_TOP_MAX 64

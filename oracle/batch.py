@@ -158,3 +158,123 @@ def token_scores(logits, tokens, row_of, k):
         elif t >= 0:
             logprob[i] = -np.inf if lse[r] == -np.inf else (logits[r, t] - shift[r, 0]) - shift[r, 1]
     return {"logprob": logprob, "entropy": entropy, "lse": lse, "top_token": top, "top_logprob": top_lp}
+
+
+def norm(x, gain, eps):
+    """RMSNorm of every head of x [N, heads, Dh] with gain [Dh] or [heads, Dh] (None: ones)."""
+    y = x / np.sqrt((x * x).mean(-1, keepdims=True) + eps)
+    return y if gain is None else y * gain
+
+
+def adjust(logits, row_start, held, ancestors, tokens, history=None, prompt_len=None, seen=(), penalties=None, bias=None,
+           allow=None, mask_of=None):
+    """Adjusted logits of every placed row, one token after the other, each step rounded to fp32 as the operator
+    states it: logits float32 [N, V], history a list of token lists, seen a collection of tokens, penalties float32
+    [B, 3], bias a list of (token, value) lists, allow a list of sets.  Rows of no placed request are as they were."""
+    N, V = logits.shape
+    out = logits.astype(np.float32).copy()
+    f = np.float32
+    for b in range(len(held)):
+        for r in range(row_start[b], row_start[b + 1]):
+            if not ancestors[r]:
+                continue
+            text = list(history[b][:held[b]]) if history is not None else []
+            text += [None] * (held[b] - len(text))  # (tokens past the history count as absent)
+            text += [tokens[row_start[b] + j] for j in ancestors[r]] if tokens is not None else []
+            x = out[r]
+            if penalties is not None:
+                rho, presence, frequency = (f(v) for v in penalties[b])
+                answer = {}
+                for t in text[prompt_len[b] if prompt_len is not None else 0:]:
+                    answer[t] = answer.get(t, 0) + 1
+                for t in set(text) | set(seen):
+                    if t is None or not 0 <= t < V:
+                        continue
+                    c = answer.get(t, 0)
+                    with np.errstate(all="ignore"):
+                        x[t] = f(x[t] / rho) if x[t] > 0 else f(x[t] * rho)
+                        x[t] = f(x[t] - f(frequency * f(c)))
+                        if c:
+                            x[t] = f(x[t] - presence)
+            if bias is not None:
+                for t, v in dict(bias[b]).items():  # (the last of a token's entries)
+                    if 0 <= t < V:
+                        with np.errstate(all="ignore"):
+                            x[t] = f(x[t] + f(v))
+            if allow is not None and mask_of[r] >= 0:
+                ok = allow[mask_of[r]] if mask_of[r] < len(allow) else ()
+                for t in range(V):
+                    if t not in ok:
+                        x[t] = -np.inf
+    return out
+
+
+def greedy(row):
+    """The token of the largest value, the lowest among equals; -1 if there is none or a NaN."""
+    if np.isnan(row).any() or row.max() == -np.inf:
+        return -1
+    return int(np.flatnonzero(row == row.max())[0])
+
+
+def accept(tokens, parent, best):
+    """One request's walk: (path, token after it).  tokens, parent and best are its rows'."""
+    reached = [0]
+    depth = [0] * len(tokens)
+    for i in range(1, len(tokens)):
+        depth[i] = depth[parent[i]] + 1
+        if parent[i] in reached and best[parent[i]] >= 0 and tokens[i] == best[parent[i]]:
+            reached.append(i)
+    end = max(reached, key=lambda i: (depth[i], -i))
+    path = []
+    i = end
+    while i >= 0:
+        path.append(i)
+        i = parent[i]
+    return path[::-1], int(best[end])
+
+
+def fork(table, held, source, n_pages):
+    """What requests that continue from others hold: dict with block_table, held, free, status, and copies, a list of
+    (page, new page, tokens).  Requests' pages are lists; who shares a page with whom follows from the order."""
+    B, width = table.shape
+    old = dict(block_table=table.copy(), held=list(held), free=[], copies=[])
+    if any(h < 0 or -(-h // PAGE) > width for h in held) or any(s >= B for s in source):
+        return dict(old, status=BAD_LENGTHS)
+    mine = [list(table[b, :-(-held[b] // PAGE)]) for b in range(B)]
+    taken = {p for pages in mine for p in pages}
+    free = [p for p in range(n_pages) if p not in taken]
+    owner = {}  # who goes on with a request's last page
+    for b, s in enumerate(source):
+        if s >= 0 and (s == b or s not in owner):
+            owner[s] = b
+    pages, copies = [], []
+    for b, s in enumerate(source):
+        now = list(mine[s]) if s >= 0 else []
+        if s >= 0 and owner[s] != b and held[s] % PAGE and 0 <= now[-1] < n_pages:
+            copies.append([now[-1], None, held[s] % PAGE])
+            now[-1] = copies[-1]
+        pages.append(now)
+    if len(copies) > len(free):
+        return dict(old, status=NO_PAGES)
+    for c, p in zip(copies, free):
+        c[1] = p
+    out = np.full((B, width), -1)
+    for b, now in enumerate(pages):
+        out[b, :len(now)] = [p[1] if isinstance(p, list) else p for p in now]
+    left = set(out.reshape(-1).tolist())
+    return dict(block_table=out, held=[held[s] if s >= 0 else 0 for s in source], status=OK,
+                free=[p for p in range(n_pages) if p not in left], copies=[tuple(c) for c in copies])
+
+
+def compact(table, held, n_pages):
+    """(new table, pages in use, moves as (page, new page))."""
+    B, width = table.shape
+    mine = [[p for p in table[b, :min(-(-max(held[b], 0) // PAGE), width)]] for b in range(B)]
+    used = sorted({p for pages in mine for p in pages if 0 <= p < n_pages})
+    holes = [p for p in range(len(used)) if p not in set(used)]
+    moves = list(zip([p for p in used if p >= len(used)], holes))
+    to = dict(moves)
+    out = np.full((B, width), -1)
+    for b, pages in enumerate(mine):
+        out[b, :len(pages)] = [to.get(p, p) if 0 <= p < n_pages else -1 for p in pages]
+    return out, len(used), moves

@@ -42,9 +42,16 @@ SYMBOLS = (
     "llmcad_batch_plan_region",
     "llmcad_batch_plan",
     "llmcad_batch_store",
+    "llmcad_batch_norm_store",
     "llmcad_batch_workspace_bytes",
     "llmcad_batch_attention",
     "llmcad_batch_commit",
+    "llmcad_batch_adjust_workspace_bytes",
+    "llmcad_batch_adjust",
+    "llmcad_batch_accept",
+    "llmcad_batch_pages_workspace_bytes",
+    "llmcad_batch_fork",
+    "llmcad_batch_compact",
     "llmcad_token_scores_workspace_bytes",
     "llmcad_token_scores",
     "llmcad_status_string",
@@ -83,6 +90,14 @@ class LlmcadQ4Matrix(ctypes.Structure):
 class LlmcadQ4LayerWeights(ctypes.Structure):
     _fields_ = [("attn_norm", ctypes.c_void_p), ("w_qkv", LlmcadQ4Matrix), ("w_o", LlmcadQ4Matrix),
                 ("ffn_norm", ctypes.c_void_p), ("w_gate_up", LlmcadQ4Matrix), ("w_down", LlmcadQ4Matrix)]
+
+
+class LlmcadAdjustments(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_void_p), ("history", ctypes.c_void_p), ("history_stride", ctypes.c_int64),
+                ("prompt_len", ctypes.c_void_p), ("seen", ctypes.c_void_p), ("penalties", ctypes.c_void_p),
+                ("bias_start", ctypes.c_void_p), ("bias_token", ctypes.c_void_p), ("bias_value", ctypes.c_void_p),
+                ("n_bias", ctypes.c_int32), ("allow", ctypes.c_void_p), ("n_masks", ctypes.c_int32),
+                ("mask_of", ctypes.c_void_p)]
 
 
 Q4_GROUP = 128  # inputs per scale group of a 4-bit matrix
@@ -144,6 +159,15 @@ def _load():
         "llmcad_batch_attention": (ctypes.c_int, [CFG, I32, I32, P, I64, P, P, I32, I32, P, P, I32, P, I32, P, SZ, I32,
                                                   I32, P, P, SZ, P]),
         "llmcad_batch_commit": (ctypes.c_int, [CFG, I32, P, P, I32, P, SZ, I32, I32, P, P, P]),
+        "llmcad_batch_norm_store": (ctypes.c_int, [CFG, I32, I32, P, I64, P, I64, P, I64, P, I64, P, I64, P, P, P, I32, P,
+                                                   SZ, I32, I32, P]),
+        "llmcad_batch_adjust_workspace_bytes": (SZ, [CFG, I32]),
+        "llmcad_batch_adjust": (ctypes.c_int, [CFG, P, SZ, I32, I32, P, I32, I64, ctypes.POINTER(LlmcadAdjustments), P,
+                                               I64, P, P, SZ, P]),
+        "llmcad_batch_accept": (ctypes.c_int, [CFG, P, SZ, I32, I32, P, P, P, P, P, P, I64, P]),
+        "llmcad_batch_pages_workspace_bytes": (SZ, [I32, I32]),
+        "llmcad_batch_fork": (ctypes.c_int, [CFG, I32, P, P, I32, I32, P, I32, P, P, P, P, P, P, P, P, SZ, P]),
+        "llmcad_batch_compact": (ctypes.c_int, [CFG, I32, P, P, I32, I32, P, I32, P, P, P, P, SZ, P]),
         "llmcad_token_scores_workspace_bytes": (SZ, [I32, I32, I32]),
         "llmcad_token_scores": (ctypes.c_int, [P, I32, I64, I32, I32, P, P, I32, P, P, P, I32, P, P, P, SZ, P]),
         "llmcad_status_string": (ctypes.c_char_p, [ctypes.c_int]),
@@ -369,6 +393,7 @@ def commit_path(cfg, k_cache, v_cache, prefix_len: int, path, accept_len, n: int
 
 PAGE = 64  # LLMCAD_PAGE, slots of a page
 MAX_REQUESTS = 1024
+MAX_POOL = 1 << 18  # LLMCAD_MAX_POOL
 TOP_MAX = 64  # LLMCAD_TOP_MAX
 PLAN_OK = 0
 PLAN_BAD_LENGTHS = 1
@@ -495,6 +520,17 @@ def _want_pages(what, cfg, n_kv_heads, k_pages, v_pages):
     return n_pages
 
 
+def _store_args(what, cfg, n_kv_heads, q, k, v, q_out, k_pages, v_pages, plan):
+    """The distances between the rows of q, k and v, and the number of pages."""
+    N, H, Dh = q.shape[0], cfg.n_heads, cfg.head_dim
+    qs = _want_rows(what, "q", q, N, H, Dh)
+    ks = _want_rows(what, "k", k, N, n_kv_heads, Dh)
+    vs = _want_rows(what, "v", v, N, n_kv_heads, Dh)
+    _want(what, "q_out", q_out, torch.bfloat16, N, H, Dh)
+    _want(what, "plan", plan, torch.uint8, None)
+    return qs, ks, vs, _want_pages(what, cfg, n_kv_heads, k_pages, v_pages)
+
+
 def batch_store(cfg, n_kv_heads: int, layer: int, q, k, v, q_out, k_pages, v_pages, plan, n_requests: int,
                 stream=None):
     """Rotary embedding of q [N, H, Dh] (to q_out) and k [N, Hkv, Dh], and the write of k and v into the
@@ -502,17 +538,37 @@ def batch_store(cfg, n_kv_heads: int, layer: int, q, k, v, q_out, k_pages, v_pag
     projection; q_out may be q."""
     what = "batch_store"
     dev = _on_device(what, q, k, v, q_out, k_pages, v_pages, plan)
-    N, H, Dh = q.shape[0], cfg.n_heads, cfg.head_dim
-    qs = _want_rows(what, "q", q, N, H, Dh)
-    ks = _want_rows(what, "k", k, N, n_kv_heads, Dh)
-    vs = _want_rows(what, "v", v, N, n_kv_heads, Dh)
-    _want(what, "q_out", q_out, torch.bfloat16, N, H, Dh)
-    _want(what, "plan", plan, torch.uint8, None)
-    n_pages = _want_pages(what, cfg, n_kv_heads, k_pages, v_pages)
+    qs, ks, vs, n_pages = _store_args(what, cfg, n_kv_heads, q, k, v, q_out, k_pages, v_pages, plan)
     _check(_enqueue(_lib.llmcad_batch_store, dev, stream,
                     (ctypes.byref(cfg), int(n_kv_heads), int(layer), q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs,
                      q_out.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), n_pages, plan.data_ptr(), plan.shape[0],
-                     int(n_requests), N)), "llmcad_batch_store")
+                     int(n_requests), q.shape[0])), "llmcad_batch_store")
+
+
+def _want_gain(what, name, t, heads, dh):
+    """t is None, bf16 [dh] (one gain for all heads) or [heads, dh]; returns the distance between heads' gains."""
+    if t is None:
+        return 0
+    if t.dtype != torch.bfloat16 or tuple(t.shape) not in ((dh,), (heads, dh)) or t.stride(-1) != 1:
+        raise ValueError(f"{what}: {name} must be bfloat16 [{dh}] or [{heads}, {dh}] with contiguous rows, "
+                         f"got {t.dtype} {tuple(t.shape)}")
+    return t.stride(0) if t.dim() == 2 and heads > 1 else 0
+
+
+def batch_norm_store(cfg, n_kv_heads: int, layer: int, q, k, v, q_gain, k_gain, q_out, k_pages, v_pages, plan,
+                     n_requests: int, stream=None):
+    """batch_store with each head's queries and keys normed first (RMSNorm with cfg.rms_eps, see
+    llmcad_batch_norm_store): q_gain bf16 [Dh] for all heads or [H, Dh], k_gain [Dh] or [Hkv, Dh]; None: ones."""
+    what = "batch_norm_store"
+    dev = _on_device(what, q, k, v, q_gain, k_gain, q_out, k_pages, v_pages, plan)
+    qs, ks, vs, n_pages = _store_args(what, cfg, n_kv_heads, q, k, v, q_out, k_pages, v_pages, plan)
+    qg = _want_gain(what, "q_gain", q_gain, cfg.n_heads, cfg.head_dim)
+    kg = _want_gain(what, "k_gain", k_gain, n_kv_heads, cfg.head_dim)
+    _check(_enqueue(_lib.llmcad_batch_norm_store, dev, stream,
+                    (ctypes.byref(cfg), int(n_kv_heads), int(layer), q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs,
+                     None if q_gain is None else q_gain.data_ptr(), qg, None if k_gain is None else k_gain.data_ptr(), kg,
+                     q_out.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), n_pages, plan.data_ptr(), plan.shape[0],
+                     int(n_requests), q.shape[0])), "llmcad_batch_norm_store")
 
 
 def batch_workspace_bytes(cfg, n_kv_heads: int, n_requests: int, n_rows: int) -> int:
@@ -559,6 +615,139 @@ def batch_commit(cfg, n_kv_heads: int, k_pages, v_pages, plan, n_requests: int, 
                     (ctypes.byref(cfg), int(n_kv_heads), k_pages.data_ptr(), v_pages.data_ptr(), n_pages, plan.data_ptr(),
                      plan.shape[0], int(n_requests), path.shape[0], path.data_ptr(), accept_len.data_ptr())),
            "llmcad_batch_commit")
+
+
+def batch_adjust_workspace_bytes(cfg, n_rows: int) -> int:
+    return _lib.llmcad_batch_adjust_workspace_bytes(ctypes.byref(cfg), int(n_rows))
+
+
+def token_mask(tokens, vocab: int):
+    """Tokens (an int tensor, any shape) as a mask of one bit per token, as batch_adjust takes them: int32
+    [ceil(vocab / 32)], bit t % 32 of word t / 32.  What is no token of the vocabulary is left out."""
+    flags = torch.zeros((vocab + 31) // 32 * 32 + 1, dtype=torch.int64, device=tokens.device)
+    t = tokens.reshape(-1).long()
+    flags[torch.where((t >= 0) & (t < vocab), t, flags.shape[0] - 1)] = 1
+    words = (flags[:-1].view(-1, 32) << torch.arange(32, device=tokens.device)).sum(-1)
+    return torch.where(words >= 1 << 31, words - (1 << 32), words).to(torch.int32)
+
+
+def batch_adjust(cfg, plan, n_requests: int, logits, tokens=None, history=None, prompt_len=None, seen=None,
+                 penalties=None, bias=None, allow=None, mask_of=None, out=None, greedy=None, workspace=None, stream=None):
+    """Adjusted logits of a step's rows, logits [N, V] float32 or bfloat16 (any distance between rows), to `out`
+    (which may be logits), and each row's greedy token to `greedy` int32 [N]; either may be None (see
+    llmcad_batch_adjust).  tokens int32 [N]; history int32 [B, any], prompt_len int32 [B]; penalties float32
+    [B, 3]: repetition, presence, frequency; bias (start int32 [B + 1], token int32 [n], value float32 [n]);
+    seen int32 [W], allow int32 [n_masks, W] with mask_of int32 [N], W = ceil(V / 32) (see token_mask).
+    workspace: batch_adjust_workspace_bytes."""
+    what = "batch_adjust"
+    start, token, value = bias if bias is not None else (None, None, None)
+    if workspace is None:
+        raise ValueError("batch_adjust: a workspace of batch_adjust_workspace_bytes is needed")
+    dev = _on_device(what, logits, plan, tokens, history, prompt_len, seen, penalties, start, token, value, allow, mask_of,
+                     out, greedy, workspace)
+    V, B = cfg.vocab, int(n_requests)
+    fp32 = logits.dtype is torch.float32
+    for name, t in (("logits", logits), ("out", out)):
+        if t is not None and (t.dtype is not logits.dtype or not (fp32 or t.dtype is torch.bfloat16) or t.dim() != 2 or
+                              t.shape != (logits.shape[0], V) or (V > 1 and t.stride(1) != 1)):
+            raise ValueError(f"batch_adjust: {name} must be float32 or bfloat16 [n, {V}] with contiguous rows, the "
+                             f"logits' type and shape, got {t.dtype} {tuple(t.shape)}")
+    N, W = logits.shape[0], (V + 31) // 32
+    for name, t, dtype, shape in (
+            ("plan", plan, torch.uint8, (None,)), ("tokens", tokens, torch.int32, (N,)),
+            ("history", history, torch.int32, (B, None)), ("prompt_len", prompt_len, torch.int32, (B,)),
+            ("seen", seen, torch.int32, (W,)), ("penalties", penalties, torch.float32, (B, 3)),
+            ("bias[0]", start, torch.int32, (B + 1,)), ("bias[1]", token, torch.int32, (None,)),
+            ("bias[2]", value, torch.float32, (None,)), ("allow", allow, torch.int32, (None, W)),
+            ("mask_of", mask_of, torch.int32, (N,)), ("greedy", greedy, torch.int32, (N,)),
+            ("workspace", workspace, torch.uint8, (None,))):
+        if t is not None:
+            _want(what, name, t, dtype, *shape)
+    if bias is not None and token.shape != value.shape:
+        raise ValueError("batch_adjust: a bias needs a value for each token")
+    at = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+    by = LlmcadAdjustments(at(tokens), at(history), history.shape[1] if history is not None else 0, at(prompt_len), at(seen),
+                           at(penalties), at(start), at(token), at(value), token.shape[0] if token is not None else 0,
+                           at(allow), allow.shape[0] if allow is not None else 0, at(mask_of))
+    _check(_enqueue(_lib.llmcad_batch_adjust, dev, stream,
+                    (ctypes.byref(cfg), plan.data_ptr(), plan.shape[0], B, N, logits.data_ptr(), 32 if fp32 else 16,
+                     logits.stride(0) if N > 1 else V, ctypes.byref(by), at(out),
+                     0 if out is None else out.stride(0) if N > 1 else V, at(greedy), workspace.data_ptr(),
+                     workspace.shape[0])), "llmcad_batch_adjust")
+
+
+def batch_accept(cfg, plan, n_requests: int, tokens, greedy, path, accept_len, next_token, history=None, stream=None):
+    """The accept walk of every request's tree along the rows' greedy tokens (see llmcad_batch_accept): tokens,
+    greedy, path int32 [N]; accept_len, next_token int32 [B]; history int32 [B, any] receives the accepted tokens."""
+    what = "batch_accept"
+    dev = _on_device(what, plan, tokens, greedy, path, accept_len, next_token, history)
+    N, B = tokens.shape[0], int(n_requests)
+    _want(what, "plan", plan, torch.uint8, None)
+    _want(what, "tokens", tokens, torch.int32, N)
+    _want(what, "greedy", greedy, torch.int32, N)
+    _want(what, "path", path, torch.int32, N)
+    _want(what, "accept_len", accept_len, torch.int32, B)
+    _want(what, "next_token", next_token, torch.int32, B)
+    if history is not None:
+        _want(what, "history", history, torch.int32, B, None)
+    _check(_enqueue(_lib.llmcad_batch_accept, dev, stream,
+                    (ctypes.byref(cfg), plan.data_ptr(), plan.shape[0], B, N, tokens.data_ptr(), greedy.data_ptr(),
+                     path.data_ptr(), accept_len.data_ptr(), next_token.data_ptr(),
+                     None if history is None else history.data_ptr(), 0 if history is None else history.shape[1])),
+           "llmcad_batch_accept")
+
+
+def batch_pages_workspace_bytes(n_requests: int, n_pages: int) -> int:
+    return _lib.llmcad_batch_pages_workspace_bytes(int(n_requests), int(n_pages))
+
+
+def batch_fork(cfg, n_kv_heads: int, k_pages, v_pages, block_table, held, source, table_out, held_out, free_pages, workspace,
+               stream=None):
+    """Requests that continue from others (see llmcad_batch_fork): block_table int32 [B, max_pages], held and source
+    int32 [B]; table_out, held_out and free_pages int32 [n_pages] are written.  Returns (n_free, status), int32 [1] each,
+    new tensors of `stream`.  workspace: batch_pages_workspace_bytes."""
+    what = "batch_fork"
+    dev = _on_device(what, k_pages, v_pages, block_table, held, source, table_out, held_out, free_pages, workspace)
+    n_pages = _want_pages(what, cfg, n_kv_heads, k_pages, v_pages)
+    _want(what, "block_table", block_table, torch.int32, None, None)
+    B, width = block_table.shape
+    for name, t, shape in (("held", held, (B,)), ("source", source, (B,)), ("table_out", table_out, (B, width)),
+                           ("held_out", held_out, (B,)), ("free_pages", free_pages, (n_pages,))):
+        _want(what, name, t, torch.int32, *shape)
+    _want(what, "workspace", workspace, torch.uint8, None)
+    if stream is not None or dev != torch.cuda.current_device():
+        _same_device(dev, stream)
+        with torch.cuda.device(dev), torch.cuda.stream(stream):
+            return batch_fork(cfg, n_kv_heads, k_pages, v_pages, block_table, held, source, table_out, held_out, free_pages,
+                              workspace)
+    said = torch.empty(2, dtype=torch.int32, device=held.device)
+    _check(_lib.llmcad_batch_fork(ctypes.byref(cfg), int(n_kv_heads), k_pages.data_ptr(), v_pages.data_ptr(), n_pages, B,
+                                  block_table.data_ptr(), width, held.data_ptr(), source.data_ptr(), table_out.data_ptr(),
+                                  held_out.data_ptr(), free_pages.data_ptr(), said.data_ptr(), said.data_ptr() + 4,
+                                  workspace.data_ptr(), workspace.shape[0], _current_stream(dev)), "llmcad_batch_fork")
+    return said[:1], said[1:]
+
+
+def batch_compact(cfg, n_kv_heads: int, k_pages, v_pages, block_table, held, table_out, workspace, stream=None):
+    """Moves the pages in use to the front of the pool (see llmcad_batch_compact): block_table int32 [B, max_pages],
+    held int32 [B]; table_out is written.  Returns the number of pages in use, int32 [1], a new tensor of `stream`."""
+    what = "batch_compact"
+    dev = _on_device(what, k_pages, v_pages, block_table, held, table_out, workspace)
+    n_pages = _want_pages(what, cfg, n_kv_heads, k_pages, v_pages)
+    _want(what, "block_table", block_table, torch.int32, None, None)
+    B, width = block_table.shape
+    _want(what, "held", held, torch.int32, B)
+    _want(what, "table_out", table_out, torch.int32, B, width)
+    _want(what, "workspace", workspace, torch.uint8, None)
+    if stream is not None or dev != torch.cuda.current_device():
+        _same_device(dev, stream)
+        with torch.cuda.device(dev), torch.cuda.stream(stream):
+            return batch_compact(cfg, n_kv_heads, k_pages, v_pages, block_table, held, table_out, workspace)
+    n_used = torch.empty(1, dtype=torch.int32, device=held.device)
+    _check(_lib.llmcad_batch_compact(ctypes.byref(cfg), int(n_kv_heads), k_pages.data_ptr(), v_pages.data_ptr(), n_pages, B,
+                                     block_table.data_ptr(), width, held.data_ptr(), table_out.data_ptr(), n_used.data_ptr(),
+                                     workspace.data_ptr(), workspace.shape[0], _current_stream(dev)), "llmcad_batch_compact")
+    return n_used
 
 
 def token_scores_workspace_bytes(n_rows: int, vocab: int, k: int) -> int:
@@ -824,7 +1013,9 @@ class Batch:
         self.workspace = torch.zeros(work, dtype=torch.uint8, device=dev)
         for name, view in batch_plan_views(self.cfg, self.n_requests, self.n_rows, self.plan_buffer).items():
             setattr(self, name, view)  # slot, position, mask, rope, status, taken
+        self.adjust_workspace = torch.zeros(batch_adjust_workspace_bytes(self.cfg, self.n_rows), dtype=torch.uint8, device=dev)
         self._planned = False  # the last plan's pages are on the free list still
+        self._shared = False   # some pages may be in several tables (fork)
         self._changed = False  # ... and some of them have left the tables
 
     def _among(self, ids, others):
@@ -855,6 +1046,11 @@ class Batch:
             self._changed = True
         pages = self.block_table[owned]
         self.block_table.masked_fill_(entries, -1)
+        if self._shared:  # (what another request holds stays, what two gave back is one page)
+            pages = pages[~self._among(pages, self.block_table)]
+            at = torch.arange(len(pages), device=pages.device)
+            first = torch.full((self.n_pages,), len(pages), device=pages.device).scatter_reduce_(0, pages.long(), at, "amin")
+            pages = pages[first[pages.long()] == at]
         return pages
 
     def plan(self, row_start, held, parent=None):
@@ -875,10 +1071,26 @@ class Batch:
         batch_store(self.cfg, self.n_kv_heads, layer, q, k, v, q_out, self.k_pages, self.v_pages, self.plan_buffer,
                     self.n_requests)
 
+    def norm_store(self, layer, q, k, v, q_gain, k_gain, q_out):
+        self._rows("norm_store", q=q, k=k, v=v, q_out=q_out)
+        batch_norm_store(self.cfg, self.n_kv_heads, layer, q, k, v, q_gain, k_gain, q_out, self.k_pages, self.v_pages,
+                         self.plan_buffer, self.n_requests)
+
     def attention(self, layer, q, out):
         self._rows("attention", q=q, out=out)
         batch_attention(self.cfg, self.n_kv_heads, layer, q, self.k_cache, self.v_cache, self.prefix_len, self.k_pages,
                         self.v_pages, self.block_table, self.plan_buffer, out, self.workspace)
+
+    def adjust(self, logits, tokens=None, out=None, greedy=None, **by):
+        """batch_adjust of the step's rows (by: history, prompt_len, seen, penalties, bias, allow, mask_of)."""
+        self._rows("adjust", logits=logits)
+        batch_adjust(self.cfg, self.plan_buffer, self.n_requests, logits, tokens=tokens, out=out, greedy=greedy,
+                     workspace=self.adjust_workspace, **by)
+
+    def accept(self, tokens, greedy, path, accept_len, next_token, history=None):
+        """The accept walk of every request's tree: what commit takes, and the tokens after it."""
+        self._rows("accept", tokens=tokens)
+        batch_accept(self.cfg, self.plan_buffer, self.n_requests, tokens, greedy, path, accept_len, next_token, history)
 
     def commit(self, path, accept_len):
         self._rows("commit", path=path)
@@ -906,7 +1118,17 @@ class Batch:
 
     def trim(self, held):
         """Takes back the pages past the requests' held tokens (int32 [n_requests], the lengths after a
-        rollback; reads how many from the device).  Without it the next plan overwrites their entries."""
+        rollback; reads how many from the device).  Without it the next plan overwrites their entries.  A length
+        that ends inside a page which another request holds too is refused: the next step would write there."""
+        if self._shared:
+            cols = torch.arange(self.block_table.shape[1], device=held.device)
+            cut = (cols == (held // PAGE)[:, None]) & (held % PAGE > 0)[:, None] & (self.block_table >= 0)
+            kept = torch.where(cols * PAGE < held[:, None], self.block_table, -1)
+            index = torch.where((kept >= 0) & (kept < self.n_pages), kept, self.n_pages).long()
+            holders = torch.zeros(self.n_pages + 1, dtype=torch.int32, device=held.device)
+            holders.scatter_add_(0, index.view(-1), torch.ones_like(index.view(-1), dtype=torch.int32))
+            if bool((cut & (holders[index] > 1) & (index < self.n_pages)).any()):
+                raise ValueError("trim: a request would end inside a page that another one holds")
         pages = self._give_back(torch.arange(self.block_table.shape[1], device=held.device) * PAGE >= held[:, None])
         self.free_pages = torch.cat([pages, self.free_pages])
 
@@ -915,3 +1137,42 @@ class Batch:
         entries = torch.zeros_like(self.block_table, dtype=torch.bool)
         entries[request] = True
         self.free_pages = torch.cat([self.free_pages, self._give_back(entries)])
+
+    def _between_steps(self, what):
+        if self._planned:
+            raise RuntimeError(f"Batch.{what}: a plan was not advanced")
+
+    def _pages_workspace(self):
+        if not hasattr(self, "_pages_work"):
+            size = batch_pages_workspace_bytes(self.n_requests, self.n_pages)
+            self._pages_work = torch.empty(size, dtype=torch.uint8, device=self.block_table.device)
+        return self._pages_work
+
+    def fork(self, source, held):
+        """Request b continues from request source[b], which holds held[source[b]] tokens (itself: it stays; negative:
+        it ends; int32 [n_requests] both; see llmcad_batch_fork).  Between steps: after advance (and commit).  Full pages
+        are shared from then on, and pages past the held tokens come back as with trim.  Returns the new lengths; reads
+        the free list's from the device.  Raises, with everything as it was, if pages run out or a length is none."""
+        self._between_steps("fork")
+        table, lengths = torch.empty_like(self.block_table), torch.empty_like(held)
+        free = torch.empty(self.n_pages, dtype=torch.int32, device=held.device)
+        n_free, status = batch_fork(self.cfg, self.n_kv_heads, self.k_pages, self.v_pages, self.block_table, held, source,
+                                    table, lengths, free, self._pages_workspace())
+        n_free, status = torch.cat([n_free, status]).tolist()
+        if status != PLAN_OK:
+            raise RuntimeError(f"the requests were not forked (plan status {status})")
+        self.block_table.copy_(table)
+        self.free_pages = free[:n_free].clone()
+        self._shared = True
+        return lengths
+
+    def compact(self, held):
+        """Moves the pages that requests hold (held int32 [n_requests]) to the front of the pool, between steps; pages
+        past the held tokens come back as with trim.  Returns their number, read from the device."""
+        self._between_steps("compact")
+        table = torch.empty_like(self.block_table)
+        n_used = int(batch_compact(self.cfg, self.n_kv_heads, self.k_pages, self.v_pages, self.block_table, held, table,
+                                   self._pages_workspace()))
+        self.block_table.copy_(table)
+        self.free_pages = torch.arange(n_used, self.n_pages, dtype=torch.int32, device=held.device)
+        return n_used

@@ -109,8 +109,14 @@ struct StoreArgs {
   const float* rope;
   int B, N, H, Hkv, Dh, n_pages;
   int heads_per;  // heads that a workgroup turns (the launch sets it)
+  // llmcad_batch_norm_store alone
+  const bf16* q_gain;  // null: ones
+  const bf16* k_gain;
+  long long q_gain_stride, k_gain_stride;  // elements between heads (0: one gain for all)
+  float eps;
 };
 hipError_t launch_batch_store(const StoreArgs& a, hipStream_t st);
+hipError_t launch_batch_norm_store(const StoreArgs& a, hipStream_t st);
 
 struct CommitArgs {
   bf16* k_pages;  // [L][n_pages][Hkv][64][Dh]
@@ -173,5 +179,67 @@ struct ScoresArgs {
 };
 size_t score_work_bytes(int n, int V, int k);
 hipError_t launch_token_scores(ScoresArgs a, void* workspace, hipStream_t st);
+
+// Tokens of the vocabulary that a workgroup of the logits' adjustment takes.
+constexpr int kAdjustChunk = 4096;
+
+struct AdjustArgs {
+  const void* logits;
+  int bf16_in;
+  long long stride, out_stride;  // elements between rows
+  void* out;                     // null: not wanted
+  int* greedy;                   // [N], null: not wanted
+  llmcad_adjustments by;
+  const int* head;
+  const BatchRequest* req;
+  const int* row_req;
+  const uint32_t* mask;
+  int B, N, V;
+  int chunks, rows_per;  // pieces of a row; rows of a workgroup (the launch sets it)
+  uint64_t* part;        // [N][chunks]: the best of each piece
+};
+hipError_t launch_batch_adjust(const AdjustArgs& a, hipStream_t st);
+
+struct AcceptArgs {
+  const int* head;
+  const BatchRequest* req;
+  const uint32_t* mask;
+  const int* tokens;  // [N]
+  const int* greedy;  // [N]
+  int* path;          // [N]
+  int* accept_len;    // [B]
+  int* next_token;    // [B]
+  int* history;       // [B][history_stride] or null
+  long long history_stride;
+  int B, N;
+};
+hipError_t launch_batch_accept(const AcceptArgs& a, hipStream_t st);
+
+// A page, or its first rows, that fork or compact copies to another.
+struct PageCopy {
+  int src, dst, rows;
+};
+struct PagesArgs {
+  bf16* k_pages;  // [L][n_pages][Hkv][64][Dh]
+  bf16* v_pages;
+  int L, Hkv, Dh, n_pages;
+  int B, max_pages;
+  const int* table;   // [B][max_pages]
+  const int* held;    // [B]
+  const int* source;  // [B], fork alone
+  int* table_out;     // [B][max_pages]
+  int* held_out;      // [B], fork alone
+  int* free_pages;    // [n_pages], fork alone
+  int* n_free;        // fork alone
+  int* status;        // fork alone
+  int* n_used;        // compact alone
+  int* n_copies;      // in the workspace, before the copies
+  PageCopy* copies;
+};
+inline size_t pages_work_bytes(int B, int n_pages) {
+  return 256 + align_up(sizeof(PageCopy) * (size_t)(B > n_pages / 2 ? B : n_pages / 2), 256);
+}
+hipError_t launch_batch_fork(const PagesArgs& a, hipStream_t st);
+hipError_t launch_batch_compact(const PagesArgs& a, hipStream_t st);
 
 }  // namespace llmcad

@@ -288,7 +288,32 @@ __device__ __forceinline__ int slot_of(const StoreArgs& a, int row) {
   return s < a.n_pages * kPage ? s : -1;
 }
 
-template <int DH>
+// x / sqrt(mean x^2 + eps) times the gain, for a head whose dims lie in groups of
+// LANES neighbouring lanes, 8 and their partners in each.
+template <int LANES>
+__device__ __forceinline__ void norm_head(float (&u)[8], float (&v)[8], const bf16* gain, int c, float eps) {
+  float sum = 0.0f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) sum += u[e] * u[e] + v[e] * v[e];
+  sum += dpp_f<kDppQuadXor1>(sum);
+  sum += dpp_f<kDppQuadXor2>(sum);
+  if (LANES == 8) sum += dpp_f<kDppRowHalfMirror>(sum);
+  const float scale = 1.0f / sqrtf(sum * (1.0f / (16 * LANES)) + eps);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    u[e] *= scale;
+    v[e] *= scale;
+  }
+  if (!gain) return;
+  const bf16x8 g = ldg((const bf16x8*)(gain + c)), h = ldg((const bf16x8*)(gain + c + 8 * LANES));
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    u[e] *= bf2f(g[e]);
+    v[e] *= bf2f(h[e]);
+  }
+}
+
+template <int DH, bool NORM>
 __device__ __forceinline__ void turn_rows(const StoreArgs& a, int block, int heads0) {
   constexpr int HALF = DH / 2, LANES = HALF / 8, ROWS = kThreads / LANES;
   const int row = block * ROWS + threadIdx.x / LANES, c = 8 * (threadIdx.x % LANES);
@@ -306,11 +331,28 @@ __device__ __forceinline__ void turn_rows(const StoreArgs& a, int block, int hea
                        : a.k_pages + (((size_t)(s / kPage) * a.Hkv + kh) * kPage + s % kPage) * DH;
     const bf16x8 p = ldg((const bf16x8*)(src + c)), q = ldg((const bf16x8*)(src + c + HALF));
     bf16x8 x, y;
+    if (NORM) {
+      float u[8], v[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float u = bf2f(p[e]), v = bf2f(q[e]), co = cs[e >> 1][2 * (e & 1)], si = cs[e >> 1][2 * (e & 1) + 1];
-      x[e] = f2bf(u * co - v * si);
-      y[e] = f2bf(v * co + u * si);
+      for (int e = 0; e < 8; ++e) {
+        u[e] = bf2f(p[e]);
+        v[e] = bf2f(q[e]);
+      }
+      const bf16* gain = kh < 0 ? a.q_gain : a.k_gain;
+      norm_head<LANES>(u, v, gain ? gain + (kh < 0 ? h * a.q_gain_stride : kh * a.k_gain_stride) : nullptr, c, a.eps);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float co = cs[e >> 1][2 * (e & 1)], si = cs[e >> 1][2 * (e & 1) + 1];
+        x[e] = f2bf(u[e] * co - v[e] * si);
+        y[e] = f2bf(v[e] * co + u[e] * si);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float u = bf2f(p[e]), v = bf2f(q[e]), co = cs[e >> 1][2 * (e & 1)], si = cs[e >> 1][2 * (e & 1) + 1];
+        x[e] = f2bf(u * co - v * si);
+        y[e] = f2bf(v * co + u * si);
+      }
     }
     stg((bf16x8*)(dst + c), x);
     stg((bf16x8*)(dst + c + HALF), y);
@@ -376,12 +418,12 @@ __device__ __forceinline__ void write_values(const StoreArgs& a, int block, int 
   }
 }
 
-template <int DH>
+template <int DH, bool NORM>
 __global__ __launch_bounds__(kThreads) void store_kernel(StoreArgs a, int turn_blocks, int head_blocks) {
   if (!plan_is_for(a.head, a.B, a.N)) return;
   const int x = blockIdx.x, turns = turn_blocks * head_blocks;
   if (x < turns)
-    turn_rows<DH>(a, x % turn_blocks, x / turn_blocks * a.heads_per);
+    turn_rows<DH, NORM>(a, x % turn_blocks, x / turn_blocks * a.heads_per);
   else
     write_values<DH>(a, (x - turns) / a.Hkv, (x - turns) % a.Hkv);
 }
@@ -488,7 +530,10 @@ __global__ __launch_bounds__(kThreads) void commit_kernel(CommitArgs a) {
 
 }  // namespace
 
-hipError_t launch_batch_store(const StoreArgs& args, hipStream_t st) {
+namespace {
+
+template <bool NORM>
+hipError_t launch_store(const StoreArgs& args, hipStream_t st) {
   StoreArgs a = args;
   const int turn_blocks = cdiv(a.N, kThreads / (a.Dh / 16)), heads = a.H + a.Hkv;
   // heads per workgroup: a table row for up to eight, if about 128 workgroups are left (64
@@ -498,11 +543,16 @@ hipError_t launch_batch_store(const StoreArgs& args, hipStream_t st) {
   const int head_blocks = cdiv(heads, a.heads_per);
   const dim3 grid(turn_blocks * head_blocks + cdiv(a.N, kStoreRows) * a.Hkv);
   if (a.Dh == 128)
-    store_kernel<128><<<grid, dim3(kThreads), 0, st>>>(a, turn_blocks, head_blocks);
+    store_kernel<128, NORM><<<grid, dim3(kThreads), 0, st>>>(a, turn_blocks, head_blocks);
   else
-    store_kernel<64><<<grid, dim3(kThreads), 0, st>>>(a, turn_blocks, head_blocks);
+    store_kernel<64, NORM><<<grid, dim3(kThreads), 0, st>>>(a, turn_blocks, head_blocks);
   return hipGetLastError();
 }
+
+}  // namespace
+
+hipError_t launch_batch_store(const StoreArgs& a, hipStream_t st) { return launch_store<false>(a, st); }
+hipError_t launch_batch_norm_store(const StoreArgs& a, hipStream_t st) { return launch_store<true>(a, st); }
 
 hipError_t launch_batch_commit(const CommitArgs& args, hipStream_t st) {
   CommitArgs a = args;

@@ -43,6 +43,88 @@ size_t attn_ml_bytes(const llmcad_config* cfg, int n_rows) {
   return align_up(attn_part_rows(n_rows) * cfg->n_heads * 8, 256);
 }
 
+// The checks and arguments of a store.
+int store_args(const llmcad_config* cfg, int32_t n_kv_heads, int32_t layer, const void* q, int64_t q_stride, const void* k,
+               int64_t k_stride, const void* v, int64_t v_stride, void* q_out, void* k_pages, void* v_pages,
+               int32_t n_pages, const void* plan, size_t plan_bytes, int32_t n_requests, int32_t n_rows, StoreArgs& a) {
+  int rc = check_batch(cfg, n_requests, n_rows);
+  if (rc != LLMCAD_OK) return rc;
+  rc = check_kv_heads(cfg, n_kv_heads);
+  if (rc != LLMCAD_OK) return rc;
+  if (!q || !k || !v || !q_out || !k_pages || !v_pages || !plan || layer < 0 || layer >= cfg->n_layers || n_pages < 1 ||
+      n_pages > kMaxPages)
+    return LLMCAD_EARG;
+  const int64_t H = cfg->n_heads, Hkv = n_kv_heads, Dh = cfg->head_dim;
+  if (q_stride < H * Dh || k_stride < Hkv * Dh || v_stride < Hkv * Dh) return LLMCAD_ESHAPE;
+  if (q_stride % 8 || k_stride % 8 || v_stride % 8 || !aligned16(q) || !aligned16(k) || !aligned16(v) ||
+      !aligned16(q_out) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(plan))
+    return LLMCAD_EARG;
+  const PlanLayout P(n_requests, n_rows, cfg->head_dim);
+  if (plan_bytes < P.total) return LLMCAD_EWORKSPACE;
+  const size_t layer_at = (size_t)layer * n_pages * Hkv * kPage * Dh;
+  a.q = (const bf16*)q;
+  a.k = (const bf16*)k;
+  a.v = (const bf16*)v;
+  a.q_stride = q_stride;
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  a.q_out = (bf16*)q_out;
+  a.k_pages = (bf16*)k_pages + layer_at;
+  a.v_pages = (bf16*)v_pages + layer_at;
+  a.head = (const int*)((const char*)plan + P.head);
+  a.slot = (const int*)((const char*)plan + P.slot);
+  a.rope = (const float*)((const char*)plan + P.rope);
+  a.B = n_requests;
+  a.N = n_rows;
+  a.H = cfg->n_heads;
+  a.Hkv = n_kv_heads;
+  a.Dh = cfg->head_dim;
+  a.n_pages = n_pages;
+  a.heads_per = 0;
+  a.q_gain = a.k_gain = nullptr;
+  a.q_gain_stride = a.k_gain_stride = 0;
+  a.eps = 0.0f;
+  return LLMCAD_OK;
+}
+
+// Whether n bytes from a on and m bytes from b on have one in common.
+bool overlap(const void* a, size_t n, const void* b, size_t m) {
+  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+  return x < y + m && y < x + n;
+}
+
+// The checks and arguments that fork and compact have in common.
+int pages_args(const llmcad_config* cfg, int32_t n_kv_heads, void* k_pages, void* v_pages, int32_t n_pages,
+               int32_t n_requests, const int32_t* block_table, int32_t max_pages, const int32_t* held, int32_t* table_out,
+               void* workspace, size_t workspace_bytes, PagesArgs& a) {
+  int rc = check_batch(cfg, n_requests, 1);
+  if (rc != LLMCAD_OK) return rc;
+  rc = check_kv_heads(cfg, n_kv_heads);
+  if (rc != LLMCAD_OK) return rc;
+  if (!k_pages || !v_pages || !block_table || !held || !table_out || !workspace || n_pages < 1 || n_pages > LLMCAD_MAX_POOL ||
+      max_pages < 1 || max_pages > LLMCAD_MAX_POOL || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(workspace) ||
+      !aligned4(block_table, held, table_out))
+    return LLMCAD_EARG;
+  const size_t table = (size_t)n_requests * max_pages * 4, lengths = (size_t)n_requests * 4;
+  if (overlap(table_out, table, block_table, table) || overlap(table_out, table, held, lengths)) return LLMCAD_EARG;
+  if (workspace_bytes < pages_work_bytes(n_requests, n_pages)) return LLMCAD_EWORKSPACE;
+  a = PagesArgs{};
+  a.k_pages = (bf16*)k_pages;
+  a.v_pages = (bf16*)v_pages;
+  a.L = cfg->n_layers;
+  a.Hkv = n_kv_heads;
+  a.Dh = cfg->head_dim;
+  a.n_pages = n_pages;
+  a.B = n_requests;
+  a.max_pages = max_pages;
+  a.table = block_table;
+  a.held = held;
+  a.table_out = table_out;
+  a.n_copies = (int*)workspace;
+  a.copies = (PageCopy*)((char*)workspace + 256);
+  return LLMCAD_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -115,41 +197,30 @@ int llmcad_batch_store(const llmcad_config* cfg, int32_t n_kv_heads, int32_t lay
                        const void* k, int64_t k_stride, const void* v, int64_t v_stride, void* q_out, void* k_pages,
                        void* v_pages, int32_t n_pages, const void* plan, size_t plan_bytes, int32_t n_requests,
                        int32_t n_rows, void* stream) {
-  int rc = check_batch(cfg, n_requests, n_rows);
-  if (rc != LLMCAD_OK) return rc;
-  rc = check_kv_heads(cfg, n_kv_heads);
-  if (rc != LLMCAD_OK) return rc;
-  if (!q || !k || !v || !q_out || !k_pages || !v_pages || !plan || layer < 0 || layer >= cfg->n_layers || n_pages < 1 ||
-      n_pages > kMaxPages)
-    return LLMCAD_EARG;
-  const int64_t H = cfg->n_heads, Hkv = n_kv_heads, Dh = cfg->head_dim;
-  if (q_stride < H * Dh || k_stride < Hkv * Dh || v_stride < Hkv * Dh) return LLMCAD_ESHAPE;
-  if (q_stride % 8 || k_stride % 8 || v_stride % 8 || !aligned16(q) || !aligned16(k) || !aligned16(v) ||
-      !aligned16(q_out) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(plan))
-    return LLMCAD_EARG;
-  const PlanLayout P(n_requests, n_rows, cfg->head_dim);
-  if (plan_bytes < P.total) return LLMCAD_EWORKSPACE;
-  const size_t layer_at = (size_t)layer * n_pages * Hkv * kPage * Dh;
   StoreArgs a;
-  a.q = (const bf16*)q;
-  a.k = (const bf16*)k;
-  a.v = (const bf16*)v;
-  a.q_stride = q_stride;
-  a.k_stride = k_stride;
-  a.v_stride = v_stride;
-  a.q_out = (bf16*)q_out;
-  a.k_pages = (bf16*)k_pages + layer_at;
-  a.v_pages = (bf16*)v_pages + layer_at;
-  a.head = (const int*)((const char*)plan + P.head);
-  a.slot = (const int*)((const char*)plan + P.slot);
-  a.rope = (const float*)((const char*)plan + P.rope);
-  a.B = n_requests;
-  a.N = n_rows;
-  a.H = cfg->n_heads;
-  a.Hkv = n_kv_heads;
-  a.Dh = cfg->head_dim;
-  a.n_pages = n_pages;
-  return launched(launch_batch_store(a, (hipStream_t)stream));
+  const int rc = store_args(cfg, n_kv_heads, layer, q, q_stride, k, k_stride, v, v_stride, q_out, k_pages, v_pages, n_pages,
+                            plan, plan_bytes, n_requests, n_rows, a);
+  return rc != LLMCAD_OK ? rc : launched(launch_batch_store(a, (hipStream_t)stream));
+}
+
+int llmcad_batch_norm_store(const llmcad_config* cfg, int32_t n_kv_heads, int32_t layer, const void* q, int64_t q_stride,
+                            const void* k, int64_t k_stride, const void* v, int64_t v_stride, const void* q_gain,
+                            int64_t q_gain_stride, const void* k_gain, int64_t k_gain_stride, void* q_out, void* k_pages,
+                            void* v_pages, int32_t n_pages, const void* plan, size_t plan_bytes, int32_t n_requests,
+                            int32_t n_rows, void* stream) {
+  StoreArgs a;
+  const int rc = store_args(cfg, n_kv_heads, layer, q, q_stride, k, k_stride, v, v_stride, q_out, k_pages, v_pages, n_pages,
+                            plan, plan_bytes, n_requests, n_rows, a);
+  if (rc != LLMCAD_OK) return rc;
+  const int64_t Dh = cfg->head_dim;
+  if (!aligned16(q_gain) || !aligned16(k_gain) || q_gain_stride % 8 || k_gain_stride % 8) return LLMCAD_EARG;
+  if ((q_gain_stride != 0 && q_gain_stride < Dh) || (k_gain_stride != 0 && k_gain_stride < Dh)) return LLMCAD_ESHAPE;
+  a.q_gain = (const bf16*)q_gain;
+  a.k_gain = (const bf16*)k_gain;
+  a.q_gain_stride = q_gain_stride;
+  a.k_gain_stride = k_gain_stride;
+  a.eps = cfg->rms_eps;
+  return launched(launch_batch_norm_store(a, (hipStream_t)stream));
 }
 
 size_t llmcad_batch_workspace_bytes(const llmcad_config* cfg, int32_t n_kv_heads, int32_t n_requests, int32_t n_rows) {
@@ -243,6 +314,123 @@ int llmcad_batch_commit(const llmcad_config* cfg, int32_t n_kv_heads, void* k_pa
   a.Dh = cfg->head_dim;
   a.n_pages = n_pages;
   return launched(launch_batch_commit(a, (hipStream_t)stream));
+}
+
+size_t llmcad_batch_adjust_workspace_bytes(const llmcad_config* cfg, int32_t n_rows) {
+  if (check_batch(cfg, 1, n_rows) != LLMCAD_OK) return 0;
+  return align_up((size_t)n_rows * cdiv(cfg->vocab, kAdjustChunk) * 8, 256);
+}
+
+int llmcad_batch_adjust(const llmcad_config* cfg, const void* plan, size_t plan_bytes, int32_t n_requests, int32_t n_rows,
+                        const void* logits, int32_t bits, int64_t row_stride, const llmcad_adjustments* by, void* out,
+                        int64_t out_stride, int32_t* greedy, void* workspace, size_t workspace_bytes, void* stream) {
+  const int rc = check_batch(cfg, n_requests, n_rows);
+  if (rc != LLMCAD_OK) return rc;
+  if (!plan || !aligned16(plan) || !logits || (bits != 16 && bits != 32) || !by || (!out && !greedy) || !workspace ||
+      !aligned16(workspace))
+    return LLMCAD_EARG;
+  const uintptr_t element = bits / 8;
+  if ((uintptr_t)logits % element || (uintptr_t)out % element ||
+      !aligned4(greedy, by->tokens, by->history, by->prompt_len, by->seen, by->penalties, by->bias_start, by->bias_token,
+                by->bias_value, by->allow, by->mask_of))
+    return LLMCAD_EARG;
+  if ((by->penalties && !by->tokens) || (by->history && by->history_stride < 0) ||
+      (by->bias_start && (!by->bias_token || !by->bias_value || by->n_bias < 0)) || (by->allow && by->n_masks < 1) ||
+      (!by->allow != !by->mask_of))
+    return LLMCAD_EARG;
+  if (row_stride < cfg->vocab || (out && out_stride < cfg->vocab)) return LLMCAD_ESHAPE;
+  // (in place every element is read by the thread that writes it, if the rows are the same ones)
+  if (out && !(out == logits && (out_stride == row_stride || n_rows == 1))) {
+    const size_t V = (size_t)cfg->vocab, rows = (size_t)n_rows - 1;
+    if (overlap(out, (rows * out_stride + V) * element, logits, (rows * row_stride + V) * element)) return LLMCAD_EARG;
+  }
+  const PlanLayout P(n_requests, n_rows, cfg->head_dim);
+  if (plan_bytes < P.total || workspace_bytes < llmcad_batch_adjust_workspace_bytes(cfg, n_rows)) return LLMCAD_EWORKSPACE;
+  const char* at = (const char*)plan;
+  AdjustArgs a;
+  a.logits = logits;
+  a.bf16_in = bits == 16;
+  a.stride = row_stride;
+  a.out_stride = out_stride;
+  a.out = out;
+  a.greedy = greedy;
+  a.by = *by;
+  a.head = (const int*)(at + P.head);
+  a.req = (const BatchRequest*)(at + P.req);
+  a.row_req = (const int*)(at + P.row_req);
+  a.mask = (const uint32_t*)(at + P.mask);
+  a.B = n_requests;
+  a.N = n_rows;
+  a.V = cfg->vocab;
+  a.chunks = a.rows_per = 0;
+  a.part = (uint64_t*)workspace;
+  return launched(launch_batch_adjust(a, (hipStream_t)stream));
+}
+
+int llmcad_batch_accept(const llmcad_config* cfg, const void* plan, size_t plan_bytes, int32_t n_requests, int32_t n_rows,
+                        const int32_t* tokens, const int32_t* greedy, int32_t* path, int32_t* accept_len,
+                        int32_t* next_token, int32_t* history, int64_t history_stride, void* stream) {
+  const int rc = check_batch(cfg, n_requests, n_rows);
+  if (rc != LLMCAD_OK) return rc;
+  if (!plan || !aligned16(plan) || !tokens || !greedy || !path || !accept_len || !next_token ||
+      (history && history_stride < 0) || !aligned4(tokens, greedy, path, accept_len, next_token, history))
+    return LLMCAD_EARG;
+  const PlanLayout P(n_requests, n_rows, cfg->head_dim);
+  if (plan_bytes < P.total) return LLMCAD_EWORKSPACE;
+  const char* at = (const char*)plan;
+  AcceptArgs a;
+  a.head = (const int*)(at + P.head);
+  a.req = (const BatchRequest*)(at + P.req);
+  a.mask = (const uint32_t*)(at + P.mask);
+  a.tokens = tokens;
+  a.greedy = greedy;
+  a.path = path;
+  a.accept_len = accept_len;
+  a.next_token = next_token;
+  a.history = history;
+  a.history_stride = history_stride;
+  a.B = n_requests;
+  a.N = n_rows;
+  return launched(launch_batch_accept(a, (hipStream_t)stream));
+}
+
+size_t llmcad_batch_pages_workspace_bytes(int32_t n_requests, int32_t n_pages) {
+  if (n_requests < 1 || n_requests > kMaxRequests || n_pages < 1 || n_pages > LLMCAD_MAX_POOL) return 0;
+  return pages_work_bytes(n_requests, n_pages);
+}
+
+int llmcad_batch_fork(const llmcad_config* cfg, int32_t n_kv_heads, void* k_pages, void* v_pages, int32_t n_pages,
+                      int32_t n_requests, const int32_t* block_table, int32_t max_pages, const int32_t* held,
+                      const int32_t* source, int32_t* table_out, int32_t* held_out, int32_t* free_pages, int32_t* n_free,
+                      int32_t* status, void* workspace, size_t workspace_bytes, void* stream) {
+  PagesArgs a;
+  const int rc = pages_args(cfg, n_kv_heads, k_pages, v_pages, n_pages, n_requests, block_table, max_pages, held, table_out,
+                            workspace, workspace_bytes, a);
+  if (rc != LLMCAD_OK) return rc;
+  if (!source || !held_out || !free_pages || !n_free || !status || !aligned4(source, held_out, free_pages, n_free, status))
+    return LLMCAD_EARG;
+  const size_t table = (size_t)n_requests * max_pages * 4, lengths = (size_t)n_requests * 4;
+  if (overlap(table_out, table, source, lengths) || overlap(held_out, lengths, block_table, table) ||
+      overlap(held_out, lengths, held, lengths) || overlap(held_out, lengths, source, lengths))
+    return LLMCAD_EARG;
+  a.source = source;
+  a.held_out = held_out;
+  a.free_pages = free_pages;
+  a.n_free = n_free;
+  a.status = status;
+  return launched(launch_batch_fork(a, (hipStream_t)stream));
+}
+
+int llmcad_batch_compact(const llmcad_config* cfg, int32_t n_kv_heads, void* k_pages, void* v_pages, int32_t n_pages,
+                         int32_t n_requests, const int32_t* block_table, int32_t max_pages, const int32_t* held,
+                         int32_t* table_out, int32_t* n_used, void* workspace, size_t workspace_bytes, void* stream) {
+  PagesArgs a;
+  const int rc = pages_args(cfg, n_kv_heads, k_pages, v_pages, n_pages, n_requests, block_table, max_pages, held, table_out,
+                            workspace, workspace_bytes, a);
+  if (rc != LLMCAD_OK) return rc;
+  if (!n_used || !aligned4(n_used)) return LLMCAD_EARG;
+  a.n_used = n_used;
+  return launched(launch_batch_compact(a, (hipStream_t)stream));
 }
 
 size_t llmcad_token_scores_workspace_bytes(int32_t n_rows, int32_t vocab, int32_t k) {
