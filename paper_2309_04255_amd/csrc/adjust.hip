@@ -7,266 +7,454 @@ namespace llmcad {
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 512;
+constexpr int kWaves = kThreads / kWave;
 constexpr int kWords = kAdjustChunk / 32;
+static_assert(kThreads == kAdjustThreads && kAdjustChunk == 8 * kThreads && LLMCAD_MAX_NODES <= kThreads, "eight tokens of a piece, a row of a request per thread");
 
 // 16 bytes of logits at any element's alignment (one global load or store: they need
 // no more than that on this GPU; a template's argument would lose the types' alignment).
 typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8u __attribute__((ext_vector_type(8), aligned(2)));
 
-__device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
-  const f32x4u a = *(const LLMCAD_GLOBAL f32x4u*)p, b = *((const LLMCAD_GLOBAL f32x4u*)p + 1);
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    x[e] = a[e];
-    x[4 + e] = b[e];
-  }
-}
-__device__ __forceinline__ void load8(const bf16* p, float (&x)[8]) {
-  const bf16x8u a = *(const LLMCAD_GLOBAL bf16x8u*)p;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) x[e] = bf2f(a[e]);
-}
-__device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
+// Eight of a row's logits as they lie.  What is behind the row's end is -inf.
+template <class T>
+struct Eight;
+template <>
+struct Eight<float> {
   f32x4u a, b;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    a[e] = x[e];
-    b[e] = x[4 + e];
+  __device__ __forceinline__ void load(const float* p) {
+    a = *(const LLMCAD_GLOBAL f32x4u*)p;
+    b = *((const LLMCAD_GLOBAL f32x4u*)p + 1);
   }
-  *(LLMCAD_GLOBAL f32x4u*)p = a;
-  *((LLMCAD_GLOBAL f32x4u*)p + 1) = b;
-}
-__device__ __forceinline__ void store8(bf16* p, const float (&x)[8]) {
-  bf16x8u a;
+  __device__ __forceinline__ void load(const float* p, int n) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) a[e] = f2bf(x[e]);
-  *(LLMCAD_GLOBAL bf16x8u*)p = a;
-}
-__device__ __forceinline__ float load1(const float* p) { return ldg(p); }
-__device__ __forceinline__ float load1(const bf16* p) { return bf2f(ldg(p)); }
-__device__ __forceinline__ void store1(float* p, float x) { stg(p, x); }
-__device__ __forceinline__ void store1(bf16* p, float x) { stg(p, f2bf(x)); }
-__device__ __forceinline__ float rounded(float x, const float*) { return x; }
-__device__ __forceinline__ float rounded(float x, const bf16*) { return bf2f(f2bf(x)); }
+    for (int e = 0; e < 4; ++e) {
+      a[e] = e < n ? ldg(p + e) : -INFINITY;
+      b[e] = 4 + e < n ? ldg(p + 4 + e) : -INFINITY;
+    }
+  }
+  __device__ __forceinline__ float get(int e) const { return e < 4 ? a[e] : b[e - 4]; }
+  __device__ __forceinline__ void set(int e, float x) {
+    if (e < 4) a[e] = x;
+    else b[e - 4] = x;
+  }
+  __device__ __forceinline__ void store(float* p) const {
+    *(LLMCAD_GLOBAL f32x4u*)p = a;
+    *((LLMCAD_GLOBAL f32x4u*)p + 1) = b;
+  }
+  __device__ __forceinline__ void store(float* p, int n) const {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < n) stg(p + e, get(e));
+  }
+  static __device__ __forceinline__ float rounded(float x) { return x; }
+};
+template <>
+struct Eight<bf16> {
+  bf16x8u a;
+  __device__ __forceinline__ void load(const bf16* p) { a = *(const LLMCAD_GLOBAL bf16x8u*)p; }
+  __device__ __forceinline__ void load(const bf16* p, int n) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) a[e] = e < n ? ldg(p + e) : (bf16)-INFINITY;
+  }
+  __device__ __forceinline__ float get(int e) const { return bf2f(a[e]); }
+  __device__ __forceinline__ void set(int e, float x) { a[e] = f2bf(x); }
+  __device__ __forceinline__ void store(bf16* p) const { *(LLMCAD_GLOBAL bf16x8u*)p = a; }
+  __device__ __forceinline__ void store(bf16* p, int n) const {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const bf16 x = a[e];
+      if (e < n) stg(p + e, x);
+    }
+  }
+  static __device__ __forceinline__ float rounded(float x) { return bf2f(f2bf(x)); }
+};
 
 // Order of a row's candidates in 64 bits: the value, then the lower token.  NaN is
 // above all; -0 is 0.
 __device__ __forceinline__ uint64_t best_key(float v, int token) {
-  if (v != v) return ~0ull;
   const uint32_t u = __float_as_uint(v + 0.0f);
-  return (uint64_t)(u >> 31 ? ~u : u | 0x80000000u) << 32 | (uint32_t)~token;
+  return v != v ? ~0ull : (uint64_t)(u >> 31 ? ~u : u | 0x80000000u) << 32 | (uint32_t)~token;
 }
 constexpr uint64_t kNone = (uint64_t)(~0xff800000u) << 32 | 0xffffffffu;  // -inf at token 0: nothing is above
-__device__ __forceinline__ int best_token(uint64_t key) {
-  return key == ~0ull || key <= kNone ? -1 : (int)~(uint32_t)key;
+__device__ __forceinline__ int best_token(uint64_t key) { return key == ~0ull || key <= kNone ? -1 : (int)~(uint32_t)key; }
+
+// What a workgroup knows of its piece of the vocabulary: how often a token occurs in
+// the answer so far, which ones occur at all, and which have a bias (the index of its
+// last entry).
+template <bool TEXT, bool BIAS>
+struct Marks {
+  uint32_t count[TEXT ? kAdjustChunk : 4];
+  uint32_t bias[BIAS ? kAdjustChunk : 4];  // entry + 1 of the request's list
+  uint32_t seen[kWords];                   // in the history
+  uint32_t own[2][kWords];                 // in the row's branch (while one row's is cleared the next one's fills)
+  uint32_t biased[kWords];
+};
+
+__device__ __forceinline__ uint32_t byte_of(const uint32_t* words, int piece) { return ((const uint8_t*)words)[piece]; }
+
+// Tokens of the history in a workgroup's pieces, where it has several: those whose
+// occurrence counts have the top bit.
+constexpr int kKept = 4096;
+struct Kept {
+  uint32_t token[kKept];
+  int n;  // more than kKept: the history itself is read for every piece
+};
+
+// What is the same for all rows of a request.
+struct Request {
+  float rho, presence, frequency;
+  bool active, listed;  // has penalties, has biases
+  int row0, n, held, answer0;
+  const int* text;  // its history, `len` tokens
+  int len;
+  int bias0, biases;
+};
+
+template <bool TEXT, bool BIAS>
+__device__ __forceinline__ Request request_of(const AdjustArgs& a, int request) {
+  Request q{};
+  if (TEXT) {
+    const float* p = a.by.penalties + 3 * (size_t)request;
+    q.rho = ldg(p);
+    q.presence = ldg(p + 1);
+    q.frequency = ldg(p + 2);
+    const BatchRequest* b = a.req + request;
+    q.row0 = ldg(&b->row0);
+    q.n = ldg(&b->n);
+    q.held = ldg(&b->held);
+    q.answer0 = a.by.prompt_len ? ldg(a.by.prompt_len + request) : 0;
+    q.active = !(q.rho == 1.0f && q.presence == 0.0f && q.frequency == 0.0f);  // (1 and zeros change no value)
+    q.text = a.by.history + (long long)request * a.by.history_stride;
+    q.len = !q.active || !a.by.history ? 0 : q.held < a.by.history_stride ? q.held : (int)a.by.history_stride;
+  }
+  if (BIAS) {
+    int lo = ldg(a.by.bias_start + request), hi = ldg(a.by.bias_start + request + 1);
+    lo = lo < 0 ? 0 : lo;
+    hi = hi > a.by.n_bias ? a.by.n_bias : hi;
+    q.bias0 = lo;
+    q.biases = hi > lo ? hi - lo : 0;
+    q.listed = hi > lo;
+  }
+  return q;
 }
-__device__ __forceinline__ uint64_t wave_best(uint64_t k) {
+
+// Gathers the tokens of the history in pieces first, first + step, ...
+__device__ __forceinline__ void keep_history(Kept& k, const Request& q, int first, int step) {
+  const int tid = threadIdx.x, lane = tid & 63;
+  if (tid == 0) k.n = 0;
+  lds_barrier();
+  for (int i0 = 0; i0 < q.len; i0 += 4 * kThreads) {
+    int id[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int i = i0 + j * kThreads + tid;
+      id[j] = i < q.len ? ldg(q.text + i) : -1;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const bool in = id[j] >= 0 && (uint32_t)id[j] / kAdjustChunk % (uint32_t)step == (uint32_t)first;
+      const uint64_t all = __ballot(in);
+      if (!all) continue;
+      int at = 0;
+      if (lane == 0) at = atomicAdd(&k.n, __popcll(all));
+      at = __builtin_amdgcn_readfirstlane(at) + __popcll(all & ((1ull << lane) - 1));
+      if (in && at < kKept) k.token[at] = (uint32_t)id[j] | (i0 + j * kThreads + tid >= q.answer0 ? 0x80000000u : 0u);
+    }
+  }
+  lds_barrier();
+}
+
+// Clears the marks and makes those of the history and the biases in a piece.
+template <bool TEXT, bool BIAS>
+__device__ __forceinline__ void mark_piece(const AdjustArgs& a, Marks<TEXT, BIAS>& m, const Request& q, const Kept* kept, int base, int size) {
+  const int tid = threadIdx.x;
+  constexpr int PER = kAdjustChunk / 4 / kThreads;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    if (TEXT && q.active) ((uint4*)m.count)[tid + i * kThreads] = make_uint4(0, 0, 0, 0);
+    if (BIAS && q.listed) ((uint4*)m.bias)[tid + i * kThreads] = make_uint4(0, 0, 0, 0);
+  }
+  if (tid < kWords) m.seen[tid] = m.own[0][tid] = m.own[1][tid] = m.biased[tid] = 0;
+  lds_barrier();
+  if (TEXT && q.active) {
+    const auto mark = [&](uint32_t id, bool counts) {
+      const uint32_t t = id - (uint32_t)base;
+      if (t < (uint32_t)size) {
+        atomicOr(&m.seen[t >> 5], 1u << (t & 31));
+        if (counts) atomicAdd(&m.count[t], 1u);
+      }
+    };
+    if (kept && kept->n <= kKept) {
+      for (int i = tid; i < kept->n; i += kThreads) mark(kept->token[i] & 0x7fffffffu, kept->token[i] >> 31);
+    } else {
+#pragma unroll 4
+      for (int i = tid; i < q.len; i += kThreads) mark((uint32_t)ldg(q.text + i), i >= q.answer0);
+    }
+  }
+  if (BIAS && q.listed)
+    for (int i = tid; i < q.biases; i += kThreads) {
+      const uint32_t t = (uint32_t)ldg(a.by.bias_token + q.bias0 + i) - (uint32_t)base;
+      if (t < (uint32_t)size) {
+        atomicOr(&m.biased[t >> 5], 1u << (t & 31));
+        atomicMax(&m.bias[t], (uint32_t)i + 1);
+      }
+    }
+}
+
+// The thread's token of a row's branch, if there is one in the piece: marks it.
+template <bool TEXT, bool BIAS>
+struct Own {
+  int at = -1;
+  bool counted = false;
+  __device__ __forceinline__ void mark(Marks<TEXT, BIAS>& m, int turn, const Request& q, int token, u32x4 branch, int base, int size) {
+    const int tid = threadIdx.x;
+    const uint32_t word = tid < 64 ? (tid < 32 ? branch.x : branch.y) : (tid < 96 ? branch.z : branch.w);
+    const uint32_t t = (uint32_t)token - (uint32_t)base;
+    at = -1;
+    if (tid < LLMCAD_MAX_NODES && (word >> (tid & 31) & 1) && t < (uint32_t)size) {
+      int depth = __popc(word & ((1u << (tid & 31)) - 1));
+      depth += (tid >= 32 ? __popc(branch.x) : 0) + (tid >= 64 ? __popc(branch.y) : 0) + (tid >= 96 ? __popc(branch.z) : 0);
+      at = (int)t;
+      counted = (long long)q.held + depth >= q.answer0;
+      atomicOr(&m.own[turn][t >> 5], 1u << (t & 31));
+      if (counted) atomicAdd(&m.count[t], 1u);
+    }
+  }
+  __device__ __forceinline__ void unmark(Marks<TEXT, BIAS>& m, int turn) const {
+    if (at < 0) return;
+    m.own[turn][at >> 5] = 0;
+    if (counted) atomicSub(&m.count[at], 1u);
+  }
+};
+
+// A thread's best of a row so far; NaN stays.
+struct Best {
+  float value = -INFINITY;
+  int token = 0;
+  __device__ __forceinline__ void join(const float (&x)[8], int first) {
+    float top = x[0];
+#pragma unroll
+    for (int e = 1; e < 8; ++e) top = __builtin_elementwise_maximum(top, x[e]);
+    if (!(top <= value)) {
+      int e0 = 7;
+#pragma unroll
+      for (int e = 6; e >= 0; --e) e0 = x[e] == top ? e : e0;
+      token = first + e0;
+      value = __builtin_elementwise_maximum(value, top);
+    }
+  }
+  // The wave's best, to lane 0's partial result.
+  __device__ __forceinline__ void write(uint64_t* part) const {
+    float top = value;
+    int at = token;
+    const bool nan = __ballot(value != value) != 0;
+    row16_argmax(top, at);
+    col4_argmax(top, at);
+    if ((threadIdx.x & 63) == 0) stg(part, nan ? (uint64_t)~0ull : best_key(top, at));
+  }
+};
+
+// The eight logits of a thread, adjusted: in x, and rounded in f.
+template <class T, bool TEXT, bool BIAS>
+__device__ __forceinline__ void adjust_eight(const AdjustArgs& a, const Marks<TEXT, BIAS>& m, int turn, const Request& q, Eight<T>& x,
+                                             float (&f)[8], uint32_t allowed, uint32_t prefix) {
+#pragma clang fp contract(off)
+#pragma unroll
+  for (int e = 0; e < 8; ++e) f[e] = x.get(e);
+  uint32_t seen = 0, biased = 0;
+  if (TEXT && q.active) seen = (byte_of(m.seen, threadIdx.x) | byte_of(m.own[turn], threadIdx.x) | prefix) & allowed;
+  if (BIAS && q.listed) biased = byte_of(m.biased, threadIdx.x) & allowed;
+  if (TEXT || BIAS) {
+    // (few of a wave's tokens are touched: one after the other)
+    for (uint32_t touched = seen | biased; touched; touched &= touched - 1) {
+      const int i = __ffs(touched) - 1;
+      float v = f[0];
+#pragma unroll
+      for (int e = 1; e < 8; ++e) v = i == e ? f[e] : v;
+      if (TEXT && (seen >> i & 1)) {
+        const uint32_t n = m.count[8 * threadIdx.x + i];
+        v = v > 0.0f ? v / q.rho : v * q.rho;
+        v = v - q.frequency * (float)n;
+        v = v - (n > 0 ? q.presence : 0.0f);
+      }
+      if (BIAS && (biased >> i & 1)) v = v + ldg(a.by.bias_value + q.bias0 + (m.bias[8 * threadIdx.x + i] - 1));
+      v = Eight<T>::rounded(v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[e] = i == e ? v : f[e];
+    }
+  }
+  const bool masked = allowed != 0xffu;
+  if (__ballot(masked)) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = allowed >> e & 1 ? f[e] : -INFINITY;
+  }
+  if (a.out && __ballot(masked || (seen | biased) != 0)) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x.set(e, f[e]);
+  }
+}
+
+template <class T>
+__device__ __forceinline__ void load_eight(Eight<T>& x, const T* row, int base, int size) {
+  const int at = 8 * threadIdx.x;
+  if (at + 8 <= size)
+    x.load(row + base + at);
+  else
+    x.load(row + base + at, size - at);
+}
+template <class T>
+__device__ __forceinline__ void store_eight(const Eight<T>& x, T* row, int base, int size) {
+  const int at = 8 * threadIdx.x;
+  if (at + 8 <= size)
+    x.store(row + base + at);
+  else
+    x.store(row + base + at, size - at);
+}
+// The thread's byte of a mask (bytes past the vocabulary's words are not read).
+__device__ __forceinline__ uint32_t mask_byte(const uint32_t* words, int base, int size) {
+  return 8 * (int)threadIdx.x < size ? ldg((const uint8_t*)words + base / 8 + threadIdx.x) : 0u;
+}
+__device__ __forceinline__ uint32_t allowed_byte(const AdjustArgs& a, int state, int base, int size) {
+  if (state < 0) return 0xffu;
+  return state < a.by.n_masks ? mask_byte(a.by.allow + (size_t)state * ((a.V + 31) / 32), base, size) : 0u;
+}
+
+// Where requests have several rows: a workgroup takes one piece of rows [r0, r1).  A
+// request's marks are made once; the next row's logits are on their way while one
+// is computed.
+template <class T, bool TEXT, bool BIAS>
+__global__ __launch_bounds__(kThreads, 6) void adjust_rows_kernel(AdjustArgs a) {
+  __shared__ Marks<TEXT, BIAS> m;
+  const int tid = threadIdx.x, lane = tid & 63, c = blockIdx.x % a.chunks, base = c * kAdjustChunk;
+  const int size = a.V - base < kAdjustChunk ? a.V - base : kAdjustChunk;
+  const int r0 = blockIdx.x / a.chunks * a.rows_per, r1 = r0 + a.rows_per < a.N ? r0 + a.rows_per : a.N;
+  // (a lane for each of the workgroup's rows, at most 64)
+  const int mine = r0 + lane < r1 ? r0 + lane : r1 - 1;
+  const int requests = ldg(a.row_req + mine), states = a.by.mask_of ? ldg(a.by.mask_of + mine) : -1;
+  if (!plan_is_for(a.head, a.B, a.N)) return;
+  const T* logits = (const T*)a.logits;
+  uint32_t prefix = 0;
+  if (TEXT && a.by.seen) prefix = mask_byte(a.by.seen, base, size);
+  int turn = 0;
+  for (int r = r0; r < r1;) {
+    // the rows of one request
+    const int request = __builtin_amdgcn_readlane(requests, r - r0), first = r;
+    const uint64_t others = __ballot(requests != request || r0 + lane >= r1) >> (r - r0);
+    r = others ? r + __ffsll((unsigned long long)others) - 1 : r1;
+    if (request < 0) continue;
+    Eight<T> next;
+    load_eight(next, logits + (long long)first * a.stride, base, size);
+    uint32_t next_allowed = allowed_byte(a, __builtin_amdgcn_readlane(states, first - r0), base, size);
+    const Request q = request_of<TEXT, BIAS>(a, request);
+    const bool marked = (TEXT && q.active) || (BIAS && q.listed);
+    int token = -1;
+    u32x4 branch = {0, 0, 0, 0};
+    if (TEXT && q.active) {
+      if (tid < q.n) token = ldg(a.by.tokens + q.row0 + tid);  // (n is at most 128)
+      branch = ldg((const u32x4*)(a.mask + (size_t)first * 4));
+    }
+    if (marked) mark_piece<TEXT, BIAS>(a, m, q, nullptr, base, size);
+    for (int row = first; row < r; ++row) {
+      Own<TEXT, BIAS> own;
+      if (TEXT && q.active) own.mark(m, turn, q, token, branch, base, size);
+      if ((TEXT && q.active) || (marked && row == first)) lds_barrier();
+      Eight<T> x = next;
+      const uint32_t allowed = next_allowed;
+      if (row + 1 < r) {
+        load_eight(next, logits + (long long)(row + 1) * a.stride, base, size);
+        next_allowed = allowed_byte(a, __builtin_amdgcn_readlane(states, row + 1 - r0), base, size);
+        if (TEXT && q.active) branch = ldg((const u32x4*)(a.mask + (size_t)(row + 1) * 4));
+      }
+      float f[8];
+      adjust_eight<T, TEXT, BIAS>(a, m, turn, q, x, f, allowed, prefix);
+      if (a.out) store_eight(x, (T*)a.out + (long long)row * a.out_stride, base, size);
+      if (a.greedy) {
+        Best best;
+        best.join(f, base + 8 * tid);
+        best.write(a.part + ((size_t)row * a.chunks + c) * kWaves + tid / kWave);
+      }
+      if (TEXT && q.active) {
+        lds_barrier();  // (every wave is done with the row's marks)
+        own.unmark(m, turn);
+        turn ^= 1;
+      }
+    }
+    if (marked) lds_barrier();  // (the next request's marks begin with clear ones)
+  }
+}
+
+// Where they have few: a workgroup takes every a.segments-th piece of one row (tokens
+// that a text repeats lie near each other in many vocabularies).  The row's text is read
+// once; the next piece's logits are on their way while one is computed.
+template <class T, bool TEXT, bool BIAS>
+__global__ __launch_bounds__(kThreads, 6) void adjust_row_kernel(AdjustArgs a) {
+  __shared__ Marks<TEXT, BIAS> m;
+  __shared__ Kept kept;
+  const int tid = threadIdx.x, segment = blockIdx.x % a.segments, row = blockIdx.x / a.segments;
+  const int c0 = segment, step = a.segments;
+  const int request = wave_uniform(ldg(a.row_req + row)), state = a.by.mask_of ? wave_uniform(ldg(a.by.mask_of + row)) : -1;
+  const T* logits = (const T*)a.logits + (long long)row * a.stride;
+  auto size_of = [&](int c) { return a.V - c * kAdjustChunk < kAdjustChunk ? a.V - c * kAdjustChunk : kAdjustChunk; };
+  Eight<T> next;
+  load_eight(next, logits, c0 * kAdjustChunk, size_of(c0));
+  if (request < 0 || !plan_is_for(a.head, a.B, a.N)) return;
+  uint32_t next_allowed = allowed_byte(a, state, c0 * kAdjustChunk, size_of(c0)), next_prefix = 0;
+  const bool prefixed = TEXT && a.by.seen;
+  if (prefixed) next_prefix = mask_byte(a.by.seen, c0 * kAdjustChunk, size_of(c0));
+  const Request q = request_of<TEXT, BIAS>(a, request);
+  const bool marked = (TEXT && q.active) || (BIAS && q.listed);
+  int token = -1;
+  u32x4 branch = {0, 0, 0, 0};
+  if (TEXT && q.active) {
+    if (tid < q.n) token = ldg(a.by.tokens + q.row0 + tid);
+    branch = ldg((const u32x4*)(a.mask + (size_t)row * 4));
+    if (step < a.chunks) keep_history(kept, q, c0, step);
+  }
+  Best best;
+  for (int c = c0; c < a.chunks; c += step) {
+    const int base = c * kAdjustChunk, size = size_of(c);
+    if (marked) {
+      mark_piece<TEXT, BIAS>(a, m, q, step < a.chunks ? &kept : nullptr, base, size);
+      Own<TEXT, BIAS> own;
+      if (TEXT && q.active) own.mark(m, 0, q, token, branch, base, size);
+      lds_barrier();
+    }
+    Eight<T> x = next;
+    const uint32_t allowed = next_allowed, prefix = next_prefix;
+    if (c + step < a.chunks) {
+      const int to = (c + step) * kAdjustChunk;
+      load_eight(next, logits, to, size_of(c + step));
+      next_allowed = allowed_byte(a, state, to, size_of(c + step));
+      if (prefixed) next_prefix = mask_byte(a.by.seen, to, size_of(c + step));
+    }
+    float f[8];
+    adjust_eight<T, TEXT, BIAS>(a, m, 0, q, x, f, allowed, prefix);
+    if (a.out) store_eight(x, (T*)a.out + (long long)row * a.out_stride, base, size);
+    if (a.greedy) best.join(f, base + 8 * tid);
+    if (marked) lds_barrier();  // (the next piece's marks begin with clear ones)
+  }
+  if (a.greedy) best.write(a.part + ((size_t)row * a.segments + segment) * kWaves + tid / kWave);
+}
+
+// The best of a row's parts: a wave per row.
+__global__ __launch_bounds__(256) void greedy_kernel(AdjustArgs a) {
+  const int r = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (r >= a.N) return;
+  const int request = ldg(a.row_req + r), parts = a.segments * kWaves;
+  uint64_t k = 0;
+  for (int c = lane; c < parts; c += kWave) {  // (of a row without a request: whatever lies there)
+    const uint64_t o = ldg(a.part + (size_t)r * parts + c);
+    if (o > k) k = o;
+  }
 #pragma unroll
   for (int off = 32; off >= 1; off >>= 1) {
     const uint64_t o = __shfl_xor((unsigned long long)k, off, kWave);
     if (o > k) k = o;
   }
-  return k;
-}
-
-// What a workgroup knows of its piece of the vocabulary: how often a token occurs in
-// the answer so far, which ones occur at all, and which have a bias (the index of its
-// last entry).
-struct Marks {
-  uint32_t count[kAdjustChunk];
-  uint32_t bias[kAdjustChunk];  // entry + 1 of the request's list
-  uint32_t seen[kWords];        // in the history
-  uint32_t own[kWords];         // in the row's branch
-  uint32_t biased[kWords];
-  uint64_t best[kThreads / kWave];
-};
-
-__device__ __forceinline__ uint32_t byte_of(const uint32_t* words, int piece) { return ((const uint8_t*)words)[piece]; }
-
-template <class T>
-__global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs a) {
-#pragma clang fp contract(off)
-  __shared__ Marks m;
-  if (!plan_is_for(a.head, a.B, a.N)) return;
-  const int tid = threadIdx.x, chunk = blockIdx.x % a.chunks, base = chunk * kAdjustChunk;
-  const int r0 = blockIdx.x / a.chunks * a.rows_per, r1 = r0 + a.rows_per < a.N ? r0 + a.rows_per : a.N;
-  const int size = a.V - base < kAdjustChunk ? a.V - base : kAdjustChunk;
-  const int words = (a.V + 31) / 32;
-  int current = -1, answer0 = 0, bias0 = 0;
-  bool active = false, listed = false;
-  float rho = 1.0f, presence = 0.0f, frequency = 0.0f;
-  BatchRequest q{};
-  for (int r = r0; r < r1; ++r) {
-    const int request = wave_uniform(ldg(a.row_req + r));
-    if (request < 0) continue;
-    constexpr int PIECES = kAdjustChunk / kThreads / 8;
-    const T* in = (const T*)a.logits + (long long)r * a.stride + base;
-    float x[PIECES][8];
-#pragma unroll
-    for (int p = 0; p < PIECES; ++p) {
-      const int at = (p * kThreads + tid) * 8;
-      if (at + 8 <= size) {
-        load8(in + at, x[p]);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[p][e] = at + e < size ? load1(in + at + e) : 0.0f;
-      }
-    }
-    if (request != current) {
-      if (current >= 0) lds_barrier();
-      current = request;
-      q = ldg(a.req + request);
-      active = false;
-      if (a.by.penalties) {
-        rho = ldg(a.by.penalties + 3 * (size_t)request);
-        presence = ldg(a.by.penalties + 3 * (size_t)request + 1);
-        frequency = ldg(a.by.penalties + 3 * (size_t)request + 2);
-        active = !(rho == 1.0f && presence == 0.0f && frequency == 0.0f);  // (1 and zeros change no value)
-      }
-      answer0 = a.by.prompt_len ? ldg(a.by.prompt_len + request) : 0;
-      int bias1 = 0;
-      bias0 = 0;
-      if (a.by.bias_start) {
-        bias0 = ldg(a.by.bias_start + request);
-        bias1 = ldg(a.by.bias_start + request + 1);
-        bias0 = bias0 < 0 ? 0 : bias0;
-        bias1 = bias1 > a.by.n_bias ? a.by.n_bias : bias1;
-      }
-      listed = bias0 < bias1;
-      if (active || listed) {
-        for (int e = tid; e < kAdjustChunk / 4; e += kThreads) {
-          ((uint4*)m.count)[e] = make_uint4(0, 0, 0, 0);
-          if (listed) ((uint4*)m.bias)[e] = make_uint4(0, 0, 0, 0);
-        }
-        for (int e = tid; e < kWords; e += kThreads) m.seen[e] = m.own[e] = m.biased[e] = 0;
-        lds_barrier();
-        if (active && a.by.history) {
-          const int* text = a.by.history + (long long)request * a.by.history_stride;
-          const int len = q.held < a.by.history_stride ? q.held : (int)a.by.history_stride;
-#pragma unroll 4
-          for (int i = tid; i < len; i += kThreads) {
-            const uint32_t t = (uint32_t)ldg(text + i) - (uint32_t)base;
-            if (t < (uint32_t)size) {
-              atomicOr(&m.seen[t >> 5], 1u << (t & 31));
-              if (i >= answer0) atomicAdd(&m.count[t], 1u);
-            }
-          }
-        }
-        if (listed)
-          for (int i = bias0 + tid; i < bias1; i += kThreads) {
-            const uint32_t t = (uint32_t)ldg(a.by.bias_token + i) - (uint32_t)base;
-            if (t < (uint32_t)size) {
-              atomicOr(&m.biased[t >> 5], 1u << (t & 31));
-              atomicMax(&m.bias[t], (uint32_t)(i - bias0) + 1);
-            }
-          }
-      }
-    }
-    // the row's branch: its ancestors' tokens and its own
-    int mine = -1;
-    bool counted = false;
-    if (active && tid < LLMCAD_MAX_NODES) {
-      const uint4 w = ldg((const uint4*)(a.mask + (size_t)r * 4));
-      const uint32_t word = tid < 64 ? (tid < 32 ? w.x : w.y) : (tid < 96 ? w.z : w.w);
-      if (word >> (tid & 31) & 1) {
-        const uint32_t t = (uint32_t)ldg(a.by.tokens + q.row0 + tid) - (uint32_t)base;
-        if (t < (uint32_t)size) {
-          int depth = __popc(word & ((1u << (tid & 31)) - 1));
-          depth += (tid >= 32 ? __popc(w.x) : 0) + (tid >= 64 ? __popc(w.y) : 0) + (tid >= 96 ? __popc(w.z) : 0);
-          mine = (int)t;
-          counted = (long long)q.held + depth >= answer0;
-          atomicOr(&m.own[t >> 5], 1u << (t & 31));
-          if (counted) atomicAdd(&m.count[t], 1u);
-        }
-      }
-    }
-    if (active || listed) lds_barrier();
-    const int state = a.by.allow && a.by.mask_of ? ldg(a.by.mask_of + r) : -1;
-    const uint8_t* allow = state >= 0 && state < a.by.n_masks ? (const uint8_t*)(a.by.allow + (size_t)state * words) : nullptr;
-    float best = -INFINITY;
-    int best_at = 0;
-    bool nan = false;
-#pragma unroll
-    for (int p = 0; p < PIECES; ++p) {
-      const int at = (p * kThreads + tid) * 8;
-      if (at >= size) continue;
-      const int piece = at / 8, global = (base + at) / 8;
-      uint32_t seen = 0, biased = 0, allowed = state < 0 ? 0xffu : 0u;
-      if (allow) allowed = ldg(allow + global);
-      if (active) {
-        seen = byte_of(m.seen, piece) | byte_of(m.own, piece);
-        if (a.by.seen) seen |= ldg((const uint8_t*)a.by.seen + global);
-      }
-      if (listed) biased = byte_of(m.biased, piece);
-      if (seen | biased) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          float v = x[p][e];
-          if (seen >> e & 1) {
-            const uint32_t c = m.count[at + e];
-            v = v > 0.0f ? v / rho : v * rho;
-            v = v - frequency * (float)c;
-            v = v - (c > 0 ? presence : 0.0f);
-          }
-          if (biased >> e & 1) v = v + ldg(a.by.bias_value + bias0 + (m.bias[at + e] - 1));
-          x[p][e] = v;
-        }
-      }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        x[p][e] = rounded(allowed >> e & 1 ? x[p][e] : -INFINITY, (const T*)nullptr);
-        if (at + e < size) {
-          nan |= x[p][e] != x[p][e];
-          if (x[p][e] > best) {
-            best = x[p][e];
-            best_at = at + e;
-          }
-        }
-      }
-      if (a.out) {
-        T* out = (T*)a.out + (long long)r * a.out_stride + base + at;
-        if (at + 8 <= size) {
-          store8(out, x[p]);
-        } else {
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (at + e < size) store1(out + e, x[p][e]);
-        }
-      }
-    }
-    if (a.greedy) {
-      const uint64_t k = wave_best(nan ? ~0ull : best_key(best, base + best_at));
-      if ((tid & 63) == 0) m.best[tid >> 6] = k;
-    }
-    if (a.greedy || active) lds_barrier();  // (every wave is done with the row's marks)
-    if (a.greedy && tid == 0) {
-      uint64_t k = m.best[0];
-      for (int w = 1; w < kThreads / kWave; ++w) k = m.best[w] > k ? m.best[w] : k;
-      if (a.chunks > 1)
-        stg(a.part + (size_t)r * a.chunks + chunk, k);
-      else
-        stg(a.greedy + r, best_token(k));
-    }
-    if (mine >= 0) {
-      m.own[mine >> 5] = 0;
-      if (counted) atomicSub(&m.count[mine], 1u);
-    }
-    if (a.greedy || active) lds_barrier();
-  }
-}
-
-// The best of a row's pieces: a wave per row.
-__global__ __launch_bounds__(kThreads) void greedy_kernel(AdjustArgs a) {
-  const int r = blockIdx.x * (kThreads / kWave) + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (!plan_is_for(a.head, a.B, a.N) || r >= a.N || ldg(a.row_req + r) < 0) return;
-  uint64_t k = 0;
-  for (int c = lane; c < a.chunks; c += kWave) {
-    const uint64_t o = ldg(a.part + (size_t)r * a.chunks + c);
-    if (o > k) k = o;
-  }
-  k = wave_best(k);
+  if (request < 0 || !plan_is_for(a.head, a.B, a.N)) return;
   if (lane == 0) stg(a.greedy + r, best_token(k));
 }
 
@@ -343,17 +531,45 @@ __global__ __launch_bounds__(LLMCAD_MAX_NODES) void accept_kernel(AcceptArgs a) 
 
 }  // namespace
 
+namespace {
+
+template <class T, bool TEXT, bool BIAS>
+void launch_adjust(const AdjustArgs& a, hipStream_t st) {
+  const dim3 grid((unsigned)((long long)a.segments * cdiv(a.N, a.rows_per)));
+  if (a.chunks_per == 0)
+    adjust_rows_kernel<T, TEXT, BIAS><<<grid, dim3(kThreads), 0, st>>>(a);
+  else
+    adjust_row_kernel<T, TEXT, BIAS><<<grid, dim3(kThreads), 0, st>>>(a);
+}
+template <class T>
+void launch_adjust(const AdjustArgs& a, hipStream_t st) {
+  if (a.by.penalties)
+    a.by.bias_start ? launch_adjust<T, true, true>(a, st) : launch_adjust<T, true, false>(a, st);
+  else
+    a.by.bias_start ? launch_adjust<T, false, true>(a, st) : launch_adjust<T, false, false>(a, st);
+}
+
+}  // namespace
+
 hipError_t launch_batch_adjust(const AdjustArgs& args, hipStream_t st) {
   AdjustArgs a = args;
   a.chunks = cdiv(a.V, kAdjustChunk);
+  // About as many workgroups as the GPU holds (three on a CU, four without penalties):
+  // of several rows each where requests have several, of several pieces of a row otherwise.
+  const long long tiles = (long long)a.chunks * a.N, want = a.by.penalties ? 768 : 1024;
+  const int per = (int)((tiles + want - 1) / want);
   a.rows_per = 1;
-  while ((size_t)a.chunks * cdiv(a.N, a.rows_per) >= 1u << 24) a.rows_per *= 2;  // (a launch takes 2^32 threads)
-  const dim3 grid((unsigned)((size_t)a.chunks * cdiv(a.N, a.rows_per)));
+  a.chunks_per = 0;
+  if (a.N >= 4ll * a.B && tiles < 1ll << 26)
+    a.rows_per = per < 16 ? per : 16;
+  else  // (a launch takes 2^32 threads)
+    a.chunks_per = per < a.chunks ? per : a.chunks;
+  a.segments = a.chunks_per == 0 ? a.chunks : cdiv(a.chunks, a.chunks_per);
   if (a.bf16_in)
-    adjust_kernel<bf16><<<grid, dim3(kThreads), 0, st>>>(a);
+    launch_adjust<bf16>(a, st);
   else
-    adjust_kernel<float><<<grid, dim3(kThreads), 0, st>>>(a);
-  if (a.greedy && a.chunks > 1) greedy_kernel<<<dim3(cdiv(a.N, kThreads / kWave)), dim3(kThreads), 0, st>>>(a);
+    launch_adjust<float>(a, st);
+  if (a.greedy) greedy_kernel<<<dim3(cdiv(a.N, 4)), dim3(256), 0, st>>>(a);
   return hipGetLastError();
 }
 

@@ -180,8 +180,8 @@ struct ScoresArgs {
 size_t score_work_bytes(int n, int V, int k);
 hipError_t launch_token_scores(ScoresArgs a, void* workspace, hipStream_t st);
 
-// Tokens of the vocabulary that a workgroup of the logits' adjustment takes.
-constexpr int kAdjustChunk = 4096;
+// Tokens of the vocabulary that a workgroup of the logits' adjustment takes at a time, and its threads.
+constexpr int kAdjustChunk = 4096, kAdjustThreads = 512;
 
 struct AdjustArgs {
   const void* logits;
@@ -195,8 +195,10 @@ struct AdjustArgs {
   const int* row_req;
   const uint32_t* mask;
   int B, N, V;
-  int chunks, rows_per;  // pieces of a row; rows of a workgroup (the launch sets it)
-  uint64_t* part;        // [N][chunks]: the best of each piece
+  int chunks;                // pieces of a row
+  int chunks_per, rows_per;  // a workgroup's pieces (0: one, of several rows) and rows (the launch sets them)
+  int segments;              // workgroups that share a row
+  uint64_t* part;            // [N][segments][waves]: the best of each one's pieces
 };
 hipError_t launch_batch_adjust(const AdjustArgs& a, hipStream_t st);
 

@@ -318,7 +318,7 @@ int llmcad_batch_commit(const llmcad_config* cfg, int32_t n_kv_heads, void* k_pa
 
 size_t llmcad_batch_adjust_workspace_bytes(const llmcad_config* cfg, int32_t n_rows) {
   if (check_batch(cfg, 1, n_rows) != LLMCAD_OK) return 0;
-  return align_up((size_t)n_rows * cdiv(cfg->vocab, kAdjustChunk) * 8, 256);
+  return align_up((size_t)n_rows * cdiv(cfg->vocab, kAdjustChunk) * (kAdjustThreads / kWave) * 8, 256);
 }
 
 int llmcad_batch_adjust(const llmcad_config* cfg, const void* plan, size_t plan_bytes, int32_t n_requests, int32_t n_rows,
@@ -362,7 +362,7 @@ int llmcad_batch_adjust(const llmcad_config* cfg, const void* plan, size_t plan_
   a.B = n_requests;
   a.N = n_rows;
   a.V = cfg->vocab;
-  a.chunks = a.rows_per = 0;
+  a.chunks = a.chunks_per = a.rows_per = a.segments = 0;
   a.part = (uint64_t*)workspace;
   return launched(launch_batch_adjust(a, (hipStream_t)stream));
 }

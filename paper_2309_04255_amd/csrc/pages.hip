@@ -172,18 +172,17 @@ __global__ __launch_bounds__(kThreads) void fork_plan_kernel(PagesArgs a) {
   __syncthreads();
   const bool ok = status == LLMCAD_PLAN_OK;
   const int left = ok ? after.count(a.n_pages, lds) : 0;  // (pages nobody holds now)
-  // tables and lengths: a workgroup's share of the requests
-  for (int b = g; b < B; b += G) {
-    const int s = ok ? source_s[b] : b;
+  // tables and lengths: a workgroup's share
+#pragma unroll 4
+  for (int e = g * kThreads + tid; e < B * a.max_pages; e += G * kThreads) {
+    const int b = e / a.max_pages, col = e % a.max_pages, s = ok ? source_s[b] : b;
     const int have = ok ? (s < 0 ? 0 : pages_of(held_s[s])) : a.max_pages;
-    for (int col = tid; col < a.max_pages; col += kThreads) {
-      int p = -1;
-      if (col < have) p = ldg(a.table + (size_t)s * a.max_pages + col);
-      if (ok && page_s[b] >= 0 && col == have - 1) p = page_s[b];
-      stg(a.table_out + (size_t)b * a.max_pages + col, p);
-    }
-    if (tid == 0) stg(a.held_out + b, ok ? (s < 0 ? 0 : held_s[s]) : held_s[b]);
+    int p = -1;
+    if (col < have) p = ldg(a.table + (size_t)s * a.max_pages + col);
+    if (ok && page_s[b] >= 0 && col == have - 1) p = page_s[b];
+    stg(a.table_out + e, p);
   }
+  if (g == 0 && tid < B) stg(a.held_out + tid, !ok ? held : source < 0 ? 0 : held_s[source]);
   // the free list: pages in order, then -1
   if (ok) {
     const int pairs = (a.n_pages + 63) / 64, wave = g * (kThreads / kWave) + (tid >> 6), lane = tid & 63;
@@ -240,17 +239,15 @@ __global__ __launch_bounds__(kThreads) void compact_plan_kernel(PagesArgs a) {
       stg(&c->rows, kPage);
     }
   }
-  for (int b = g; b < B; b += G) {
-    const int have = pages_of(held_s[b]);
-    for (int col = tid; col < a.max_pages; col += kThreads) {
-      int p = -1;
-      if (col < have) {
-        p = ldg(a.table + (size_t)b * a.max_pages + col);
-        if (p < 0 || p >= a.n_pages) p = -1;
-        else if (p >= n_used) p = used.nth_zero((p - n_used) - (used.zeros_before(p) - moves), a.n_pages);
-      }
-      stg(a.table_out + (size_t)b * a.max_pages + col, p);
+  for (int e = g * kThreads + tid; e < B * a.max_pages; e += G * kThreads) {
+    const int b = e / a.max_pages, col = e % a.max_pages;
+    int p = -1;
+    if (col < pages_of(held_s[b])) {
+      p = ldg(a.table + e);
+      if (p < 0 || p >= a.n_pages) p = -1;
+      else if (p >= n_used) p = used.nth_zero((p - n_used) - (used.zeros_before(p) - moves), a.n_pages);
     }
+    stg(a.table_out + e, p);
   }
   if (g == 0 && tid == 0) {
     stg(a.n_used, n_used);
@@ -261,41 +258,42 @@ __global__ __launch_bounds__(kThreads) void compact_plan_kernel(PagesArgs a) {
 // ---------------------------------------------------------------- copies
 constexpr int kCopyThreads = 256;
 
-// A head's first `rows` keys: one run of memory.
+// A head's first `rows` keys (one run of memory) and the first `rows` entries of each
+// dim's line of values, in 16-byte pieces, all loads before the first store.  The piece
+// of a line that they end in is written entry by entry, so that what lies behind stays.
 template <int DH>
-__device__ __forceinline__ void copy_keys(const bf16x8* src, bf16x8* dst, int rows) {
+__device__ __forceinline__ void copy_head(const bf16x8* ks, bf16x8* kd, const bf16x8* vs, bf16x8* vd, int rows) {
   constexpr int PER = kPage * DH / 8 / kCopyThreads;
-  const int n = rows * (DH / 8);
-  bf16x8 v[PER];
-#pragma unroll
-  for (int i = 0; i < PER; ++i)
-    if ((int)threadIdx.x + i * kCopyThreads < n) v[i] = ldg(src + threadIdx.x + i * kCopyThreads);
-#pragma unroll
-  for (int i = 0; i < PER; ++i)
-    if ((int)threadIdx.x + i * kCopyThreads < n) stg(dst + threadIdx.x + i * kCopyThreads, v[i]);
-}
-
-// A head's values: the first `rows` entries of each dim's line.  The piece that they end
-// in is written entry by entry, so that what lies behind them stays.
-template <int DH>
-__device__ __forceinline__ void copy_values(const bf16x8* src, bf16x8* dst, int rows) {
-  constexpr int PER = kPage * DH / 8 / kCopyThreads;
-  bf16x8 v[PER];
+  const int n = rows * (DH / 8), line = (rows + 7) / 8, m = DH * line;  // pieces of the keys, of a line, of the values
+  bf16x8 k[PER], v[PER];
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
     const int e = threadIdx.x + i * kCopyThreads;
-    if (8 * (e % 8) < rows) v[i] = ldg(src + e);
+    if (e < n) k[i] = ldg(ks + e);
   }
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
-    const int e = threadIdx.x + i * kCopyThreads, n = rows - 8 * (e % 8);
-    if (n >= 8) {
-      stg(dst + e, v[i]);
-    } else if (n > 0) {
+    const int e = threadIdx.x + i * kCopyThreads;
+    if (e < m) v[i] = ldg(vs + e / line * 8 + e % line);
+  }
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int e = threadIdx.x + i * kCopyThreads;
+    if (e < n) stg(kd + e, k[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int e = threadIdx.x + i * kCopyThreads;
+    if (e >= m) continue;
+    bf16x8* to = vd + e / line * 8 + e % line;
+    const int left = rows - 8 * (e % line);
+    if (left >= 8) {
+      stg(to, v[i]);
+    } else {
 #pragma unroll
       for (int u = 0; u < 7; ++u) {
         const bf16 x = v[i][u];
-        if (u < n) stg((bf16*)(dst + e) + u, x);
+        if (u < left) stg((bf16*)to + u, x);
       }
     }
   }
@@ -310,8 +308,8 @@ __global__ __launch_bounds__(kCopyThreads) void copy_kernel(PagesArgs a) {
     const int at = (int)(unit % heads), layer = at / a.Hkv, kh = at % a.Hkv;
     const size_t src = (((size_t)layer * a.n_pages + c.src) * a.Hkv + kh) * head;
     const size_t dst = (((size_t)layer * a.n_pages + c.dst) * a.Hkv + kh) * head;
-    copy_keys<DH>((const bf16x8*)a.k_pages + src, (bf16x8*)a.k_pages + dst, c.rows);
-    copy_values<DH>((const bf16x8*)a.v_pages + src, (bf16x8*)a.v_pages + dst, c.rows);
+    copy_head<DH>((const bf16x8*)a.k_pages + src, (bf16x8*)a.k_pages + dst, (const bf16x8*)a.v_pages + src,
+                  (bf16x8*)a.v_pages + dst, c.rows);
   }
 }
 
