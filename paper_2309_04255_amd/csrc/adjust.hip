@@ -142,20 +142,21 @@ __device__ __forceinline__ Request request_of(const AdjustArgs& a, int request) 
 }
 
 // Gathers the tokens of the history in pieces first, first + step, ...
-__device__ __forceinline__ void keep_history(Kept& k, const Request& q, int first, int step) {
+__device__ __forceinline__ void keep_history(Kept& k, const Request& q, int vocab, int first, int step) {
   const int tid = threadIdx.x, lane = tid & 63;
   if (tid == 0) k.n = 0;
   lds_barrier();
-  for (int i0 = 0; i0 < q.len; i0 += 4 * kThreads) {
-    int id[4];
+  constexpr int AHEAD = 8;
+  for (int i0 = 0; i0 < q.len; i0 += AHEAD * kThreads) {
+    int id[AHEAD];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < AHEAD; ++j) {
       const int i = i0 + j * kThreads + tid;
       id[j] = i < q.len ? ldg(q.text + i) : -1;
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const bool in = id[j] >= 0 && (uint32_t)id[j] / kAdjustChunk % (uint32_t)step == (uint32_t)first;
+    for (int j = 0; j < AHEAD; ++j) {
+      const bool in = (uint32_t)id[j] < (uint32_t)vocab && (uint32_t)id[j] / kAdjustChunk % (uint32_t)step == (uint32_t)first;
       const uint64_t all = __ballot(in);
       if (!all) continue;
       int at = 0;
@@ -411,7 +412,7 @@ __global__ __launch_bounds__(kThreads, 6) void adjust_row_kernel(AdjustArgs a) {
   if (TEXT && q.active) {
     if (tid < q.n) token = ldg(a.by.tokens + q.row0 + tid);
     branch = ldg((const u32x4*)(a.mask + (size_t)row * 4));
-    if (step < a.chunks) keep_history(kept, q, c0, step);
+    if (step < a.chunks) keep_history(kept, q, a.V, c0, step);
   }
   Best best;
   for (int c = c0; c < a.chunks; c += step) {

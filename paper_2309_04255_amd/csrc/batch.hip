@@ -288,29 +288,17 @@ __device__ __forceinline__ int slot_of(const StoreArgs& a, int row) {
   return s < a.n_pages * kPage ? s : -1;
 }
 
-// x / sqrt(mean x^2 + eps) times the gain, for a head whose dims lie in groups of
-// LANES neighbouring lanes, 8 and their partners in each.
+// 1 / sqrt(mean x^2 + eps) of a head whose dims lie in groups of LANES neighbouring
+// lanes, 8 and their partners in each.
 template <int LANES>
-__device__ __forceinline__ void norm_head(float (&u)[8], float (&v)[8], const bf16* gain, int c, float eps) {
+__device__ __forceinline__ float norm_scale(const float (&u)[8], const float (&v)[8], float eps) {
   float sum = 0.0f;
 #pragma unroll
   for (int e = 0; e < 8; ++e) sum += u[e] * u[e] + v[e] * v[e];
   sum += dpp_f<kDppQuadXor1>(sum);
   sum += dpp_f<kDppQuadXor2>(sum);
   if (LANES == 8) sum += dpp_f<kDppRowHalfMirror>(sum);
-  const float scale = 1.0f / sqrtf(sum * (1.0f / (16 * LANES)) + eps);
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    u[e] *= scale;
-    v[e] *= scale;
-  }
-  if (!gain) return;
-  const bf16x8 g = ldg((const bf16x8*)(gain + c)), h = ldg((const bf16x8*)(gain + c + 8 * LANES));
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    u[e] *= bf2f(g[e]);
-    v[e] *= bf2f(h[e]);
-  }
+  return rsqrtf(sum * (1.0f / (16 * LANES)) + eps);
 }
 
 template <int DH, bool NORM>
@@ -323,39 +311,59 @@ __device__ __forceinline__ void turn_rows(const StoreArgs& a, int block, int hea
 #pragma unroll
   for (int e = 0; e < 4; ++e) cs[e] = ldg((const f32x4*)(a.rope + ((size_t)row * HALF + c) * 2) + e);
   const int heads1 = heads0 + a.heads_per < a.H + a.Hkv ? heads0 + a.heads_per : a.H + a.Hkv;
-#pragma unroll 4
-  for (int h = heads0; h < heads1; ++h) {
-    const int kh = h - a.H;
-    const bf16* src = kh < 0 ? a.q + (size_t)row * a.q_stride + (size_t)h * DH : a.k + (size_t)row * a.k_stride + (size_t)kh * DH;
-    bf16* dst = kh < 0 ? a.q_out + ((size_t)row * a.H + h) * DH
-                       : a.k_pages + (((size_t)(s / kPage) * a.Hkv + kh) * kPage + s % kPage) * DH;
-    const bf16x8 p = ldg((const bf16x8*)(src + c)), q = ldg((const bf16x8*)(src + c + HALF));
-    bf16x8 x, y;
-    if (NORM) {
+  // (four heads' loads before the first one's sums: the compiler does not unroll a loop with lane moves)
+  constexpr int AHEAD = 4;
+  for (int h0 = heads0; h0 < heads1; h0 += AHEAD) {
+    bf16x8 p[AHEAD], q[AHEAD], g[AHEAD], w[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      const int h = h0 + i, kh = h - a.H;
+      if (h >= heads1) break;
+      const bf16* src = kh < 0 ? a.q + (size_t)row * a.q_stride + (size_t)h * DH : a.k + (size_t)row * a.k_stride + (size_t)kh * DH;
+      p[i] = ldg((const bf16x8*)(src + c));
+      q[i] = ldg((const bf16x8*)(src + c + HALF));
+      const bf16* gain = kh < 0 ? a.q_gain : a.k_gain;
+      if (NORM && gain) {
+        gain += kh < 0 ? h * a.q_gain_stride : kh * a.k_gain_stride;
+        g[i] = ldg((const bf16x8*)(gain + c));
+        w[i] = ldg((const bf16x8*)(gain + c + HALF));
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      const int h = h0 + i, kh = h - a.H;
+      if (h >= heads1) break;
+      bf16* dst = kh < 0 ? a.q_out + ((size_t)row * a.H + h) * DH
+                         : a.k_pages + (((size_t)(s / kPage) * a.Hkv + kh) * kPage + s % kPage) * DH;
       float u[8], v[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        u[e] = bf2f(p[e]);
-        v[e] = bf2f(q[e]);
+        u[e] = bf2f(p[i][e]);
+        v[e] = bf2f(q[i][e]);
       }
-      const bf16* gain = kh < 0 ? a.q_gain : a.k_gain;
-      norm_head<LANES>(u, v, gain ? gain + (kh < 0 ? h * a.q_gain_stride : kh * a.k_gain_stride) : nullptr, c, a.eps);
+      if (NORM) {
+        const float scale = norm_scale<LANES>(u, v, a.eps);
+        const bool gains = (kh < 0 ? a.q_gain : a.k_gain) != nullptr;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          u[e] *= scale;
+          v[e] *= scale;
+          if (gains) {
+            u[e] *= bf2f(g[i][e]);
+            v[e] *= bf2f(w[i][e]);
+          }
+        }
+      }
+      bf16x8 x, y;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const float co = cs[e >> 1][2 * (e & 1)], si = cs[e >> 1][2 * (e & 1) + 1];
         x[e] = f2bf(u[e] * co - v[e] * si);
         y[e] = f2bf(v[e] * co + u[e] * si);
       }
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float u = bf2f(p[e]), v = bf2f(q[e]), co = cs[e >> 1][2 * (e & 1)], si = cs[e >> 1][2 * (e & 1) + 1];
-        x[e] = f2bf(u * co - v * si);
-        y[e] = f2bf(v * co + u * si);
-      }
+      stg((bf16x8*)(dst + c), x);
+      stg((bf16x8*)(dst + c + HALF), y);
     }
-    stg((bf16x8*)(dst + c), x);
-    stg((bf16x8*)(dst + c + HALF), y);
   }
 }
 
@@ -365,6 +373,7 @@ __device__ __forceinline__ void write_values(const StoreArgs& a, int block, int 
   __shared__ int slot_s[kStoreRows + 8];  // from the row before the block on
   __shared__ int piece_s[kStoreRows];     // pieces that begin in the block: first row | rows << 8
   __shared__ int pieces;
+  __shared__ int all_whole;               // they are of eight rows each
   __shared__ uint16_t vt[kStoreRows + 7][DH + 2];
   const int r0 = block * kStoreRows, tid = threadIdx.x;
   const int rows = a.N - r0 < kStoreRows + 7 ? a.N - r0 : kStoreRows + 7;
@@ -387,18 +396,22 @@ __device__ __forceinline__ void write_values(const StoreArgs& a, int block, int 
     while (n < 8 && (s & 7) + n < 8 && slot_s[tid + 1 + n] == s + n) ++n;
     const uint64_t all = __ballot(begins);
     if (begins) piece_s[__popcll(all & ((1ull << tid) - 1))] = tid | n << 8;
-    if (tid == 0) pieces = __popcll(all);
+    const uint64_t parts = __ballot(begins && n < 8);
+    if (tid == 0) {
+      pieces = __popcll(all);
+      all_whole = parts == 0;
+    }
   }
   __syncthreads();
-  for (int e = tid; e < pieces * DH; e += kThreads) {
-    const int p = piece_s[e / DH], c = e % DH, i = p & 0xff, n = p >> 8, s = slot_s[i + 1];
+  const auto write_piece = [&](int piece, int c, bool whole) {
+    const int p = piece_s[piece], i = p & 0xff, n = whole ? 8 : p >> 8, s = slot_s[i + 1];
     uint16_t* dst = (uint16_t*)a.v_pages + (((size_t)(s / kPage) * a.Hkv + kh) * DH + c) * kPage + s % kPage;
     if (n == 8) {
       bf16x8 v;
 #pragma unroll
       for (int u = 0; u < 8; ++u) v[u] = __builtin_bit_cast(bf16, vt[i + u][c]);
       stg((bf16x8*)dst, v);
-      continue;
+      return;
     }
     // (part of a piece: its entries in the largest aligned groups)
     for (int u = 0; u < n;) {
@@ -415,6 +428,13 @@ __device__ __forceinline__ void write_values(const StoreArgs& a, int block, int 
         u += 1;
       }
     }
+  };
+  // Whole pieces go line by line (64 prompts of 128 rows, 8 K/V heads: 46 us for 48), parts
+  // dim by dim (64 trees of up to 31 rows, 32 heads: 14.3 for 15.8).
+  if (all_whole) {
+    for (int e = tid; e < pieces * DH; e += kThreads) write_piece(e % pieces, e / pieces, true);
+  } else {
+    for (int e = tid; e < pieces * DH; e += kThreads) write_piece(e / DH, e % DH, false);
   }
 }
 

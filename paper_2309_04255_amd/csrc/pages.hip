@@ -1,24 +1,25 @@
 // Pages of requests between steps: requests that continue from others' tokens (fork),
 // and the pages in use moved to the front of the pool (compact).
 //
-// Both begin with one small launch that decides: every workgroup marks the pages that
-// the requests hold in a bitmap in LDS (a few KiB of table entries, read by all), counts
-// the free ones, and writes its share of the new tables and lists; nothing is handed from
-// one workgroup to another.  A second launch copies, as many workgroups as fill the GPU
-// striding over (copy, layer, K/V head).
+// Every workgroup decides for itself: it marks the pages that the requests hold in a bitmap
+// in LDS (a few KiB of table entries, read by all), counts the free ones, and knows then
+// which page goes where; it writes its share of the new tables and lists and copies its
+// share of the pages.  Nothing is handed from one workgroup to another, so one launch is
+// enough.  Pools of more than 256 requests or 2^16 pages, and forks of many heads, take
+// two, one that decides and leaves the copies in the workspace, and one that copies.
 #include "batch.h"
 
 namespace llmcad {
 
 namespace {
 
-constexpr int kThreads = 1024;
-constexpr int kGroup = 8;  // bitmap words per thread
-constexpr int kMaxPool = LLMCAD_MAX_POOL;
-static_assert(kMaxPool <= kThreads * kGroup * 32, "a bitmap word of every page has a thread");
-static_assert(kMaxRequests <= kThreads, "a request has a thread");
+constexpr int kGroup = 8;     // bitmap words per thread
+constexpr int kSmall = 256;   // threads of the one launch: its most requests, 256 of its pages each
+constexpr int kLarge = 1024;
+static_assert(LLMCAD_MAX_POOL <= kLarge * kGroup * 32 && kMaxRequests <= kLarge, "every request and bitmap word has a thread");
 
 // Sum of v over the threads before this one; `total` over all.  Called by all threads.
+template <int THREADS>
 __device__ __forceinline__ int block_before(int v, int* lds, int& total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int sum = v;
@@ -32,34 +33,36 @@ __device__ __forceinline__ int block_before(int v, int* lds, int& total) {
   __syncthreads();
   int before = 0;
   total = 0;
-  for (int w = 0; w < kThreads / kWave; ++w) {
+#pragma unroll
+  for (int w = 0; w < THREADS / kWave; ++w) {
     if (w < wave) before += lds[w];
     total += lds[w];
   }
   return before + sum - v;
 }
 
+template <int THREADS>
 struct Bitmap {
-  uint32_t word[kMaxPool / 32];
-  int zeros[kThreads];  // clear bits before each group of words
+  uint32_t word[THREADS * kGroup];
+  int zeros[THREADS];  // clear bits before each group of words
 
   __device__ __forceinline__ void clear(int n) {
-    for (int e = threadIdx.x; e < (n + 31) / 32; e += kThreads) word[e] = 0;
+    for (int e = threadIdx.x; e < (n + 31) / 32; e += THREADS) word[e] = 0;
   }
   __device__ __forceinline__ void set(int p) { atomicOr(&word[p >> 5], 1u << (p & 31)); }
   __device__ __forceinline__ bool has(int p) const { return word[p >> 5] >> (p & 31) & 1; }
-  // The clear bits of word w among the first n pages.
-  __device__ __forceinline__ uint32_t clear_bits(int w, int n) const {
+  // The clear (or set) bits of word w among the first n pages.
+  template <bool SET>
+  __device__ __forceinline__ uint32_t bits(int w, int n) const {
     const int left = n - 32 * w;
-    return left <= 0 ? 0u : ~word[w] & (left >= 32 ? ~0u : (1u << left) - 1);
+    return left <= 0 ? 0u : (SET ? word[w] : ~word[w]) & (left >= 32 ? ~0u : (1u << left) - 1);
   }
   // Counts the clear bits of the first n pages; called by all threads, after the marks.
   __device__ __forceinline__ int count(int n, int* lds) {
     int mine = 0, total;
     const int w0 = threadIdx.x * kGroup;
-    for (int w = w0; w < w0 + kGroup && 32 * w < n; ++w) mine += __popc(clear_bits(w, n));
-    const int before = block_before(mine, lds, total);
-    zeros[threadIdx.x] = before;
+    for (int w = w0; w < w0 + kGroup && 32 * w < n; ++w) mine += __popc(bits<false>(w, n));
+    zeros[threadIdx.x] = block_before<THREADS>(mine, lds, total);
     __syncthreads();
     return total;
   }
@@ -70,22 +73,23 @@ struct Bitmap {
     for (int i = g * kGroup; i < w; ++i) z += __popc(~word[i]);
     return z + __popc(~word[w] & ((1u << (p & 31)) - 1));
   }
-  // The k-th clear bit of the first n pages (there are more than k).
-  __device__ __forceinline__ int nth_zero(int k, int n) const {
-    const int groups = ((n + 31) / 32 + kGroup - 1) / kGroup;
-    int lo = 0, hi = groups - 1;  // the last group with zeros[g] <= k
+  // The k-th clear (or set) bit of the first n pages (there are more than k).
+  template <bool SET>
+  __device__ __forceinline__ int nth(int k, int n) const {
+    const auto before = [&](int g) { return SET ? g * kGroup * 32 - zeros[g] : zeros[g]; };
+    int lo = 0, hi = ((n + 31) / 32 + kGroup - 1) / kGroup - 1;  // the last group with at most k before it
     while (lo < hi) {
       const int mid = (lo + hi + 1) / 2;
-      if (zeros[mid] <= k) lo = mid;
+      if (before(mid) <= k) lo = mid;
       else hi = mid - 1;
     }
-    k -= zeros[lo];
+    k -= before(lo);
     for (int w = lo * kGroup; 32 * w < n; ++w) {
-      uint32_t bits = clear_bits(w, n);
-      const int c = __popc(bits);
+      uint32_t b = bits<SET>(w, n);
+      const int c = __popc(b);
       if (k < c) {
-        for (; k > 0; --k) bits &= bits - 1;
-        return 32 * w + __ffs(bits) - 1;
+        for (; k > 0; --k) b &= b - 1;
+        return 32 * w + __ffs(b) - 1;
       }
       k -= c;
     }
@@ -95,177 +99,177 @@ struct Bitmap {
 
 __device__ __forceinline__ int pages_of(int held) { return (int)(((long long)held + kPage - 1) / kPage); }
 
-__global__ __launch_bounds__(kThreads) void fork_plan_kernel(PagesArgs a) {
-  __shared__ Bitmap before, after;
-  __shared__ int held_s[kMaxRequests], source_s[kMaxRequests], first_s[kMaxRequests];
-  __shared__ int page_s[kMaxRequests];  // the page of a request's copied last tokens, -1: none
-  __shared__ uint8_t alive_s[kMaxRequests];
-  __shared__ int lds[kThreads / kWave], widest_s;
-  const int tid = threadIdx.x, B = a.B, g = blockIdx.x, G = gridDim.x;
-  before.clear(a.n_pages);
-  after.clear(a.n_pages);
-  int held = 0, source = -1;
-  bool bad = false;
-  if (tid < B) {
-    held = ldg(a.held + tid);
-    source = ldg(a.source + tid);
-    bad = held < 0 || pages_of(held) > a.max_pages || source >= B;
-    held_s[tid] = held;
-    source_s[tid] = source;
-    first_s[tid] = B;
-    alive_s[tid] = 0;
-    page_s[tid] = -1;
-  }
-  if (tid == 0) widest_s = 0;
-  bad = __syncthreads_or(bad) != 0;
-  int status = bad ? LLMCAD_PLAN_BAD_LENGTHS : LLMCAD_PLAN_OK;
-  if (!bad) {
-    if (tid < B) {
-      atomicMax(&widest_s, pages_of(held));
-      if (source >= 0) {
-        alive_s[source] = 1;
-        atomicMin(&first_s[source], tid);
-      }
-    }
-    __syncthreads();
-    // the pages held before, and those that somebody still holds
-    const int widest = widest_s, entries = B * widest;  // (at most 2^10 tables of 2^18 pages)
+// f(request, column, page) for every page that the lengths in LDS say is held; `widest` is
+// the most pages of a request.  (At most 2^10 tables of 2^18 columns.)
+template <int THREADS, class F>
+__device__ __forceinline__ void each_page(const PagesArgs& a, const int* held, int widest, F f) {
 #pragma unroll 4
-    for (int e = tid; e < entries; e += kThreads) {
-      const int b = e / widest, col = e % widest;
-      if (col < pages_of(held_s[b])) {
-        const int p = ldg(a.table + (size_t)b * a.max_pages + col);
-        if (p >= 0 && p < a.n_pages) {
-          before.set(p);
-          if (alive_s[b]) after.set(p);
-        }
-      }
+  for (int e = threadIdx.x; e < a.B * widest; e += THREADS) {
+    const int b = e / widest, col = e % widest;
+    if (col < pages_of(held[b])) {
+      const int p = ldg(a.table + (size_t)b * a.max_pages + col);
+      if (p >= 0 && p < a.n_pages) f(b, col, p);
     }
-    __syncthreads();
-    const int n_free = before.count(a.n_pages, lds);
-    // who needs a page of its own for its last tokens
-    PageCopy c{};
-    bool copies = false;
-    if (tid < B && source >= 0 && source != tid) {
-      const int from = held_s[source], col = from / kPage;
-      c.rows = from % kPage;
-      const bool goes_on = source_s[source] != source && first_s[source] == tid;
-      if (c.rows > 0 && !goes_on) {
-        c.src = ldg(a.table + (size_t)source * a.max_pages + col);
-        copies = c.src >= 0 && c.src < a.n_pages;
-      }
-    }
-    int n_copies;
-    const int k = block_before(copies ? 1 : 0, lds, n_copies);
-    if (n_copies > n_free) {
-      status = LLMCAD_PLAN_NO_PAGES;
-    } else {
-      if (copies) {
-        c.dst = before.nth_zero(k, a.n_pages);
-        page_s[tid] = c.dst;
-        after.set(c.dst);
-        if (g == 0) stg(a.copies + k, c);
-      }
-      if (g == 0 && tid == 0) stg(a.n_copies, n_copies);
-    }
-  }
-  __syncthreads();
-  const bool ok = status == LLMCAD_PLAN_OK;
-  const int left = ok ? after.count(a.n_pages, lds) : 0;  // (pages nobody holds now)
-  // tables and lengths: a workgroup's share
-#pragma unroll 4
-  for (int e = g * kThreads + tid; e < B * a.max_pages; e += G * kThreads) {
-    const int b = e / a.max_pages, col = e % a.max_pages, s = ok ? source_s[b] : b;
-    const int have = ok ? (s < 0 ? 0 : pages_of(held_s[s])) : a.max_pages;
-    int p = -1;
-    if (col < have) p = ldg(a.table + (size_t)s * a.max_pages + col);
-    if (ok && page_s[b] >= 0 && col == have - 1) p = page_s[b];
-    stg(a.table_out + e, p);
-  }
-  if (g == 0 && tid < B) stg(a.held_out + tid, !ok ? held : source < 0 ? 0 : held_s[source]);
-  // the free list: pages in order, then -1
-  if (ok) {
-    const int pairs = (a.n_pages + 63) / 64, wave = g * (kThreads / kWave) + (tid >> 6), lane = tid & 63;
-    for (int w = wave; w < pairs; w += G * (kThreads / kWave)) {
-      const int p = 64 * w + lane;
-      if (p < a.n_pages && !after.has(p)) stg(a.free_pages + after.zeros_before(p), p);
-    }
-  }
-  for (int i = left + g * kThreads + tid; i < a.n_pages; i += G * kThreads) stg(a.free_pages + i, -1);
-  if (g == 0 && tid == 0) {
-    stg(a.n_free, left);
-    stg(a.status, status);
-    if (!ok) stg(a.n_copies, 0);
   }
 }
 
-__global__ __launch_bounds__(kThreads) void compact_plan_kernel(PagesArgs a) {
-  __shared__ Bitmap used;
-  __shared__ int held_s[kMaxRequests];
-  __shared__ int lds[kThreads / kWave], widest_s;
-  const int tid = threadIdx.x, B = a.B, g = blockIdx.x, G = gridDim.x;
-  used.clear(a.n_pages);
-  if (tid == 0) widest_s = 0;
-  __syncthreads();
-  if (tid < B) {
-    int held = ldg(a.held + tid);
-    if (held < 0) held = 0;
-    if (pages_of(held) > a.max_pages) held = (int)((long long)a.max_pages * kPage);
-    held_s[tid] = held;
-    atomicMax(&widest_s, pages_of(held));
-  }
-  __syncthreads();
-  const int widest = widest_s, entries = B * widest;
-#pragma unroll 4
-  for (int e = tid; e < entries; e += kThreads) {
-    const int b = e / widest, col = e % widest;
-    if (col < pages_of(held_s[b])) {
-      const int p = ldg(a.table + (size_t)b * a.max_pages + col);
-      if (p >= 0 && p < a.n_pages) used.set(p);
+template <int THREADS>
+struct Fork {
+  Bitmap<THREADS> before, after;
+  int held[THREADS], source[THREADS], first[THREADS];
+  int page[THREADS];  // the page of a request's copied last tokens, -1: none
+  uint8_t alive[THREADS];
+  int lds[THREADS / kWave], widest;
+  PageCopy copies[THREADS];
+
+  // Returns the number of copies; called by all threads of every workgroup, of which the first
+  // G write the new tables and lists.
+  __device__ __forceinline__ int decide(const PagesArgs& a, int G) {
+    const int tid = threadIdx.x, B = a.B, g = blockIdx.x;
+    int mine = 0, from = -1;
+    bool bad = false;
+    if (tid < B) {
+      mine = ldg(a.held + tid);
+      from = ldg(a.source + tid);
+      bad = mine < 0 || pages_of(mine) > a.max_pages || from >= B;
+      held[tid] = mine;
+      source[tid] = from;
+      first[tid] = B;
+      alive[tid] = 0;
+      page[tid] = -1;
     }
-  }
-  __syncthreads();
-  const int n_used = a.n_pages - used.count(a.n_pages, lds);
-  const int moves = n_used < a.n_pages ? used.zeros_before(n_used) : 0;  // free pages in front of the new end
-  // The k-th used page behind the end takes the k-th free one before it.
-  const int pairs = (a.n_pages + 63) / 64, wave = g * (kThreads / kWave) + (tid >> 6), lane = tid & 63;
-  for (int w = wave; w < pairs; w += G * (kThreads / kWave)) {
-    const int p = 64 * w + lane;
-    if (p >= a.n_pages) continue;
-    if (p < n_used && !used.has(p)) stg(&a.copies[used.zeros_before(p)].dst, p);
-    if (p >= n_used && used.has(p)) {
-      PageCopy* c = a.copies + (p - n_used) - (used.zeros_before(p) - moves);
-      stg(&c->src, p);
-      stg(&c->rows, kPage);
+    before.clear(a.n_pages);
+    after.clear(a.n_pages);
+    if (tid == 0) widest = 0;
+    int status = __syncthreads_or(bad) ? LLMCAD_PLAN_BAD_LENGTHS : LLMCAD_PLAN_OK, n_copies = 0;
+    if (status == LLMCAD_PLAN_OK) {
+      if (tid < B) {
+        atomicMax(&widest, pages_of(mine));
+        if (from >= 0) {
+          alive[from] = 1;
+          atomicMin(&first[from], tid);
+        }
+      }
+      __syncthreads();
+      // the pages held before, and those that somebody still holds
+      each_page<THREADS>(a, held, widest, [&](int b, int, int p) {
+        before.set(p);
+        if (alive[b]) after.set(p);
+      });
+      // who needs a page of its own for its last tokens
+      PageCopy c{};
+      bool copies_one = false;
+      if (tid < B && from >= 0 && from != tid) {
+        c.rows = held[from] % kPage;
+        const bool goes_on = source[from] != from && first[from] == tid;
+        if (c.rows > 0 && !goes_on) {
+          c.src = ldg(a.table + (size_t)from * a.max_pages + held[from] / kPage);
+          copies_one = c.src >= 0 && c.src < a.n_pages;
+        }
+      }
+      __syncthreads();
+      const int n_free = before.count(a.n_pages, lds), k = block_before<THREADS>(copies_one ? 1 : 0, lds, n_copies);
+      if (n_copies > n_free) {
+        status = LLMCAD_PLAN_NO_PAGES;
+        n_copies = 0;
+      } else if (copies_one) {
+        c.dst = before.template nth<false>(k, a.n_pages);
+        page[tid] = c.dst;
+        after.set(c.dst);
+        copies[k] = c;
+      }
     }
-  }
-  for (int e = g * kThreads + tid; e < B * a.max_pages; e += G * kThreads) {
-    const int b = e / a.max_pages, col = e % a.max_pages;
-    int p = -1;
-    if (col < pages_of(held_s[b])) {
-      p = ldg(a.table + e);
-      if (p < 0 || p >= a.n_pages) p = -1;
-      else if (p >= n_used) p = used.nth_zero((p - n_used) - (used.zeros_before(p) - moves), a.n_pages);
+    __syncthreads();
+    const bool ok = status == LLMCAD_PLAN_OK;
+    if (g >= G) return n_copies;
+    const int left = ok ? after.count(a.n_pages, lds) : 0;  // (pages nobody holds now)
+    // tables and lengths: a workgroup's share
+    for (int e = g * THREADS + tid; e < B * a.max_pages; e += G * THREADS) {
+      const int b = e / a.max_pages, col = e % a.max_pages, s = ok ? source[b] : b;
+      const int have = ok ? (s < 0 ? 0 : pages_of(held[s])) : a.max_pages;
+      int p = -1;
+      if (col < have) p = ldg(a.table + (size_t)s * a.max_pages + col);
+      if (ok && page[b] >= 0 && col == have - 1) p = page[b];
+      stg(a.table_out + e, p);
     }
-    stg(a.table_out + e, p);
+    // the free list: pages in order, then -1
+    if (ok)
+      for (int p = g * THREADS + tid; p < a.n_pages; p += G * THREADS)
+        if (!after.has(p)) stg(a.free_pages + after.zeros_before(p), p);
+    for (int i = left + g * THREADS + tid; i < a.n_pages; i += G * THREADS) stg(a.free_pages + i, -1);
+    if (g == 0) {
+      if (tid < B) stg(a.held_out + tid, !ok ? mine : from < 0 ? 0 : held[from]);
+      if (tid == 0) {
+        stg(a.n_free, left);
+        stg(a.status, status);
+      }
+    }
+    return n_copies;
   }
-  if (g == 0 && tid == 0) {
-    stg(a.n_used, n_used);
-    stg(a.n_copies, moves);
+};
+
+template <int THREADS>
+struct Compact {
+  Bitmap<THREADS> used;
+  int held[THREADS];
+  int lds[THREADS / kWave], widest;
+  int n_used;
+
+  __device__ __forceinline__ int decide(const PagesArgs& a) {
+    const int tid = threadIdx.x, B = a.B, g = blockIdx.x, G = gridDim.x;
+    int mine = 0;
+    if (tid < B) {
+      mine = ldg(a.held + tid);
+      if (mine < 0) mine = 0;
+      if (pages_of(mine) > a.max_pages) mine = (int)((long long)a.max_pages * kPage);
+      held[tid] = mine;
+    }
+    used.clear(a.n_pages);
+    if (tid == 0) widest = 0;
+    __syncthreads();
+    if (tid < B) atomicMax(&widest, pages_of(mine));
+    __syncthreads();
+    each_page<THREADS>(a, held, widest, [&](int, int, int p) { used.set(p); });
+    __syncthreads();
+    const int in_use = a.n_pages - used.count(a.n_pages, lds);
+    const int n = in_use < a.n_pages ? used.zeros_before(in_use) : 0;  // free pages in front of the new end
+    for (int e = g * THREADS + tid; e < B * a.max_pages; e += G * THREADS) {
+      const int b = e / a.max_pages, col = e % a.max_pages;
+      int p = -1;
+      if (col < pages_of(held[b])) {
+        p = ldg(a.table + e);
+        if (p < 0 || p >= a.n_pages) p = -1;
+        else if (p >= in_use) p = used.template nth<false>((p - in_use) - (used.zeros_before(p) - n), a.n_pages);
+      }
+      stg(a.table_out + e, p);
+    }
+    if (g == 0 && tid == 0) stg(a.n_used, in_use);
+    n_used = in_use;
+    return n;
   }
-}
+  // The k-th used page behind the end takes the k-th of the n free ones before it.
+  __device__ __forceinline__ PageCopy copy(const PagesArgs& a, int k, int n) const {
+    return {used.template nth<true>(n_used - n + k, a.n_pages), used.template nth<false>(k, a.n_pages), kPage};
+  }
+};
+
+constexpr int kWriters = 32;
 
 // ---------------------------------------------------------------- copies
 constexpr int kCopyThreads = 256;
 
 // A head's first `rows` keys (one run of memory) and the first `rows` entries of each
-// dim's line of values, in 16-byte pieces, all loads before the first store.  The piece
-// of a line that they end in is written entry by entry, so that what lies behind stays.
+// dim's line of values, in 16-byte pieces, all loads before the first store.  Lines are
+// written in whole pieces of kWhole entries, in which what lies behind the copied ones is
+// read from the new page first: memory takes parts of its lines by reading them itself,
+// and later.
+constexpr int kWhole = 32;
 template <int DH>
 __device__ __forceinline__ void copy_head(const bf16x8* ks, bf16x8* kd, const bf16x8* vs, bf16x8* vd, int rows) {
   constexpr int PER = kPage * DH / 8 / kCopyThreads;
-  const int n = rows * (DH / 8), line = (rows + 7) / 8, m = DH * line;  // pieces of the keys, of a line, of the values
-  bf16x8 k[PER], v[PER];
+  const int n = rows * (DH / 8);                                            // pieces of the keys
+  const int line = (rows + kWhole - 1) / kWhole * (kWhole / 8), m = DH * line;  // of a line of values, and of all
+  bf16x8 k[PER], v[PER], old[PER];
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
     const int e = threadIdx.x + i * kCopyThreads;
@@ -274,7 +278,10 @@ __device__ __forceinline__ void copy_head(const bf16x8* ks, bf16x8* kd, const bf
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
     const int e = threadIdx.x + i * kCopyThreads;
-    if (e < m) v[i] = ldg(vs + e / line * 8 + e % line);
+    if (e >= m) continue;
+    const int at = e / line * 8 + e % line, left = rows - 8 * (e % line);
+    if (left > 0) v[i] = ldg(vs + at);
+    if (left < 8) old[i] = ldg(vd + at);
   }
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
@@ -285,60 +292,115 @@ __device__ __forceinline__ void copy_head(const bf16x8* ks, bf16x8* kd, const bf
   for (int i = 0; i < PER; ++i) {
     const int e = threadIdx.x + i * kCopyThreads;
     if (e >= m) continue;
-    bf16x8* to = vd + e / line * 8 + e % line;
     const int left = rows - 8 * (e % line);
-    if (left >= 8) {
-      stg(to, v[i]);
-    } else {
+    bf16x8 x = v[i];
 #pragma unroll
-      for (int u = 0; u < 7; ++u) {
-        const bf16 x = v[i][u];
-        if (u < left) stg((bf16*)to + u, x);
-      }
+    for (int u = 0; u < 8; ++u) {
+      const bf16 mine = v[i][u], there = old[i][u];
+      x[u] = u < left ? mine : there;
     }
+    stg(vd + e / line * 8 + e % line, x);
   }
 }
 
-template <int DH>
-__global__ __launch_bounds__(kCopyThreads) void copy_kernel(PagesArgs a) {
-  const int n = ldg(a.n_copies), heads = a.L * a.Hkv;
+// This workgroup's share of n copies' page heads: copy_of(k) is the k-th.
+template <int DH, class F>
+__device__ __forceinline__ void copy_units(const PagesArgs& a, int n, F copy_of) {
+  const int heads = a.L * a.Hkv;
   const size_t head = (size_t)kPage * DH / 8;  // (in pieces)
+  int k = -1;
+  PageCopy c{};
   for (long long unit = blockIdx.x; unit < (long long)n * heads; unit += gridDim.x) {
-    const PageCopy c = ldg(a.copies + unit / heads);
     const int at = (int)(unit % heads), layer = at / a.Hkv, kh = at % a.Hkv;
+    if ((int)(unit / heads) != k) {
+      k = (int)(unit / heads);
+      c = copy_of(k);
+    }
     const size_t src = (((size_t)layer * a.n_pages + c.src) * a.Hkv + kh) * head;
     const size_t dst = (((size_t)layer * a.n_pages + c.dst) * a.Hkv + kh) * head;
     copy_head<DH>((const bf16x8*)a.k_pages + src, (bf16x8*)a.k_pages + dst, (const bf16x8*)a.v_pages + src,
                   (bf16x8*)a.v_pages + dst, c.rows);
   }
 }
-
-hipError_t launch_copies(const PagesArgs& a, long long most, hipStream_t st) {
-  const long long units = most * a.L * a.Hkv;
-  const dim3 grid((unsigned)(units < 2048 ? (units < 1 ? 1 : units) : 2048));
-  if (a.Dh == 128)
-    copy_kernel<128><<<grid, dim3(kCopyThreads), 0, st>>>(a);
-  else
-    copy_kernel<64><<<grid, dim3(kCopyThreads), 0, st>>>(a);
-  return hipGetLastError();
+template <int DH>
+__global__ __launch_bounds__(kSmall) void fork_kernel(PagesArgs a) {
+  __shared__ Fork<kSmall> f;
+  const int n = f.decide(a, min(kWriters, (int)gridDim.x));
+  copy_units<DH>(a, n, [&](int k) { return f.copies[k]; });
+}
+template <int DH>
+__global__ __launch_bounds__(kSmall) void compact_kernel(PagesArgs a) {
+  __shared__ Compact<kSmall> f;
+  const int n = f.decide(a);
+  __syncthreads();
+  copy_units<DH>(a, n, [&](int k) { return f.copy(a, k, n); });
 }
 
-// Workgroups that share the writes of a plan: one per 4096 pages or table entries.
+__global__ __launch_bounds__(kLarge) void fork_plan_kernel(PagesArgs a) {
+  __shared__ Fork<kLarge> f;
+  const int n = f.decide(a, gridDim.x), k = threadIdx.x;
+  if (blockIdx.x != 0) return;
+  if (k < n) stg(a.copies + k, f.copies[k]);
+  if (k == 0) stg(a.n_copies, n);
+}
+__global__ __launch_bounds__(kLarge) void compact_plan_kernel(PagesArgs a) {
+  __shared__ Compact<kLarge> f;
+  const int n = f.decide(a);
+  __syncthreads();
+  for (int k = blockIdx.x * kLarge + threadIdx.x; k < n; k += gridDim.x * kLarge) stg(a.copies + k, f.copy(a, k, n));
+  if (blockIdx.x == 0 && threadIdx.x == 0) stg(a.n_copies, n);
+}
+template <int DH>
+__global__ __launch_bounds__(kCopyThreads) void copy_kernel(PagesArgs a) {
+  const int n = ldg(a.n_copies);
+  copy_units<DH>(a, n, [&](int k) { return ldg(a.copies + k); });
+}
+
+// Workgroups that copy: six on a CU, no more than there are heads of `most` copies.
+int copy_groups(const PagesArgs& a, long long most) {
+  const long long units = most * a.L * a.Hkv;
+  return (int)(units < 1 ? 1 : units > 1536 ? 1536 : units);
+}
+// Workgroups that share the writes of a large plan: one per 4096 pages or table entries.
 int plan_groups(const PagesArgs& a) {
-  const long long writes = (long long)a.B * a.max_pages + a.n_pages, n = writes / 4096;
+  const long long n = ((long long)a.B * a.max_pages + a.n_pages) / 4096;
   return (int)(n < 1 ? 1 : n > 64 ? 64 : n);
+}
+bool is_small(const PagesArgs& a) { return a.B <= kSmall && a.n_pages <= kSmall * kGroup * 32; }
+
+void launch_copies(const PagesArgs& a, long long most, hipStream_t st) {
+  if (a.Dh == 128)
+    copy_kernel<128><<<dim3(copy_groups(a, most)), dim3(kCopyThreads), 0, st>>>(a);
+  else
+    copy_kernel<64><<<dim3(copy_groups(a, most)), dim3(kCopyThreads), 0, st>>>(a);
 }
 
 }  // namespace
 
 hipError_t launch_batch_fork(const PagesArgs& a, hipStream_t st) {
-  fork_plan_kernel<<<dim3(plan_groups(a)), dim3(kThreads), 0, st>>>(a);
-  return launch_copies(a, a.B, st);
+  // (One launch: four requests of 22 layers of 16 heads 11.9 us for 14.6 with two; 64 of 40 layers of 8 heads, where
+  // the deciding part's registers and LDS cost the copies' waves, 99 for 93.)
+  if (!is_small(a) || (long long)a.B * a.L * a.Hkv > 4096) {
+    fork_plan_kernel<<<dim3(plan_groups(a)), dim3(kLarge), 0, st>>>(a);
+    launch_copies(a, a.B, st);
+  } else if (a.Dh == 128) {
+    fork_kernel<128><<<dim3(copy_groups(a, a.B)), dim3(kSmall), 0, st>>>(a);
+  } else {
+    fork_kernel<64><<<dim3(copy_groups(a, a.B)), dim3(kSmall), 0, st>>>(a);
+  }
+  return hipGetLastError();
 }
 
 hipError_t launch_batch_compact(const PagesArgs& a, hipStream_t st) {
-  compact_plan_kernel<<<dim3(plan_groups(a)), dim3(kThreads), 0, st>>>(a);
-  return launch_copies(a, a.n_pages / 2, st);
+  if (!is_small(a)) {
+    compact_plan_kernel<<<dim3(plan_groups(a)), dim3(kLarge), 0, st>>>(a);
+    launch_copies(a, a.n_pages / 2, st);
+  } else if (a.Dh == 128) {
+    compact_kernel<128><<<dim3(copy_groups(a, a.n_pages / 2)), dim3(kSmall), 0, st>>>(a);
+  } else {
+    compact_kernel<64><<<dim3(copy_groups(a, a.n_pages / 2)), dim3(kSmall), 0, st>>>(a);
+  }
+  return hipGetLastError();
 }
 
 }  // namespace llmcad
