@@ -437,9 +437,15 @@ def _enqueue(fn, dev, stream, args):
 def _want(what, name, t, dtype, *shape):
     """t is a contiguous tensor of dtype and shape (None: any size)."""
     got = t.shape
-    if t.dtype is dtype and t.is_contiguous() and \
-            (got == shape or (len(got) == len(shape) and all(w is None or w == s for w, s in zip(shape, got)))):
-        return
+    if t.dtype is dtype and t.is_contiguous():
+        if got == shape:
+            return
+        if len(got) == len(shape):
+            for w, s in zip(shape, got):
+                if w is not None and w != s:
+                    break
+            else:
+                return
     raise ValueError(f"{what}: {name} must be a contiguous {dtype} tensor of shape "
                      f"{tuple('any' if w is None else w for w in shape)}, got {t.dtype} {tuple(got)}")
 
@@ -646,34 +652,54 @@ def batch_adjust(cfg, plan, n_requests: int, logits, tokens=None, history=None, 
     dev = _on_device(what, logits, plan, tokens, history, prompt_len, seen, penalties, start, token, value, allow, mask_of,
                      out, greedy, workspace)
     V, B = cfg.vocab, int(n_requests)
-    fp32 = logits.dtype is torch.float32
-    for name, t in (("logits", logits), ("out", out)):
-        if t is not None and (t.dtype is not logits.dtype or not (fp32 or t.dtype is torch.bfloat16) or t.dim() != 2 or
-                              t.shape != (logits.shape[0], V) or (V > 1 and t.stride(1) != 1)):
-            raise ValueError(f"batch_adjust: {name} must be float32 or bfloat16 [n, {V}] with contiguous rows, the "
-                             f"logits' type and shape, got {t.dtype} {tuple(t.shape)}")
-    N, W = logits.shape[0], (V + 31) // 32
-    for name, t, dtype, shape in (
-            ("plan", plan, torch.uint8, (None,)), ("tokens", tokens, torch.int32, (N,)),
-            ("history", history, torch.int32, (B, None)), ("prompt_len", prompt_len, torch.int32, (B,)),
-            ("seen", seen, torch.int32, (W,)), ("penalties", penalties, torch.float32, (B, 3)),
-            ("bias[0]", start, torch.int32, (B + 1,)), ("bias[1]", token, torch.int32, (None,)),
-            ("bias[2]", value, torch.float32, (None,)), ("allow", allow, torch.int32, (None, W)),
-            ("mask_of", mask_of, torch.int32, (N,)), ("greedy", greedy, torch.int32, (N,)),
-            ("workspace", workspace, torch.uint8, (None,))):
-        if t is not None:
-            _want(what, name, t, dtype, *shape)
-    if bias is not None and token.shape != value.shape:
-        raise ValueError("batch_adjust: a bias needs a value for each token")
-    at = lambda t: None if t is None else t.data_ptr()  # noqa: E731
-    by = LlmcadAdjustments(at(tokens), at(history), history.shape[1] if history is not None else 0, at(prompt_len), at(seen),
-                           at(penalties), at(start), at(token), at(value), token.shape[0] if token is not None else 0,
-                           at(allow), allow.shape[0] if allow is not None else 0, at(mask_of))
+    dtype, shape = logits.dtype, logits.shape
+    fp32 = dtype is torch.float32
+    if not (fp32 or dtype is torch.bfloat16) or len(shape) != 2 or shape[1] != V or (V > 1 and logits.stride(1) != 1):
+        raise ValueError(f"batch_adjust: logits must be float32 or bfloat16 [n, {V}] with contiguous rows, "
+                         f"got {dtype} {tuple(shape)}")
+    if out is not None and (out.dtype is not dtype or out.shape != shape or (V > 1 and out.stride(1) != 1)):
+        raise ValueError(f"batch_adjust: out must have the logits' type and shape and contiguous rows, "
+                         f"got {out.dtype} {tuple(out.shape)}")
+    N, W = shape[0], (V + 31) // 32
+    i32 = torch.int32
+    _want(what, "plan", plan, torch.uint8, None)
+    _want(what, "workspace", workspace, torch.uint8, None)
+    by = LlmcadAdjustments()
+    if greedy is not None:
+        _want(what, "greedy", greedy, i32, N)
+    if tokens is not None:
+        _want(what, "tokens", tokens, i32, N)
+        by.tokens = tokens.data_ptr()
+    if history is not None:
+        _want(what, "history", history, i32, B, None)
+        by.history, by.history_stride = history.data_ptr(), history.shape[1]
+    if prompt_len is not None:
+        _want(what, "prompt_len", prompt_len, i32, B)
+        by.prompt_len = prompt_len.data_ptr()
+    if seen is not None:
+        _want(what, "seen", seen, i32, W)
+        by.seen = seen.data_ptr()
+    if penalties is not None:
+        _want(what, "penalties", penalties, torch.float32, B, 3)
+        by.penalties = penalties.data_ptr()
+    if bias is not None:
+        _want(what, "bias[0]", start, i32, B + 1)
+        _want(what, "bias[1]", token, i32, None)
+        _want(what, "bias[2]", value, torch.float32, None)
+        if token.shape != value.shape:
+            raise ValueError("batch_adjust: a bias needs a value for each token")
+        by.bias_start, by.bias_token, by.bias_value, by.n_bias = start.data_ptr(), token.data_ptr(), value.data_ptr(), token.shape[0]
+    if allow is not None:
+        _want(what, "allow", allow, i32, None, W)
+        by.allow, by.n_masks = allow.data_ptr(), allow.shape[0]
+    if mask_of is not None:
+        _want(what, "mask_of", mask_of, i32, N)
+        by.mask_of = mask_of.data_ptr()
     _check(_enqueue(_lib.llmcad_batch_adjust, dev, stream,
                     (ctypes.byref(cfg), plan.data_ptr(), plan.shape[0], B, N, logits.data_ptr(), 32 if fp32 else 16,
-                     logits.stride(0) if N > 1 else V, ctypes.byref(by), at(out),
-                     0 if out is None else out.stride(0) if N > 1 else V, at(greedy), workspace.data_ptr(),
-                     workspace.shape[0])), "llmcad_batch_adjust")
+                     logits.stride(0) if N > 1 else V, ctypes.byref(by), None if out is None else out.data_ptr(),
+                     0 if out is None else out.stride(0) if N > 1 else V, None if greedy is None else greedy.data_ptr(),
+                     workspace.data_ptr(), workspace.shape[0])), "llmcad_batch_adjust")
 
 
 def batch_accept(cfg, plan, n_requests: int, tokens, greedy, path, accept_len, next_token, history=None, stream=None):
