@@ -95,12 +95,13 @@ struct Marks {
 
 __device__ __forceinline__ uint32_t byte_of(const uint32_t* words, int piece) { return ((const uint8_t*)words)[piece]; }
 
-// Tokens of the history in a workgroup's pieces, where it has several: those whose
-// occurrence counts have the top bit.
-constexpr int kKept = 4096;
+// Tokens of the history in a workgroup's pieces, where it has several, piece by piece;
+// those whose occurrence counts have the top bit.
+constexpr int kKept = 4096, kKeptPieces = 64;
 struct Kept {
   uint32_t token[kKept];
-  int n;  // more than kKept: the history itself is read for every piece
+  int start[kKeptPieces + 1];  // of each piece's; the last: of all (more than kKept: the history itself is read for every piece)
+  int at[kKeptPieces];
 };
 
 // What is the same for all rows of a request.
@@ -141,36 +142,70 @@ __device__ __forceinline__ Request request_of(const AdjustArgs& a, int request) 
   return q;
 }
 
-// Gathers the tokens of the history in pieces first, first + step, ...
+// Sorts the tokens of the history in pieces first, first + step, ... by their piece (at
+// most kKeptPieces): counted once, placed in a second pass.
 __device__ __forceinline__ void keep_history(Kept& k, const Request& q, int vocab, int first, int step) {
-  const int tid = threadIdx.x, lane = tid & 63;
-  if (tid == 0) k.n = 0;
-  lds_barrier();
-  constexpr int AHEAD = 8;
-  for (int i0 = 0; i0 < q.len; i0 += AHEAD * kThreads) {
-    int id[AHEAD];
+  const int tid = threadIdx.x;
+  constexpr int AHEAD = 8;  // loads in flight; so many are not read again for the second pass
+  const float inverse = 1.0f / (float)step;
+  const auto load = [&](int (&id)[AHEAD], int i0) {
 #pragma unroll
     for (int j = 0; j < AHEAD; ++j) {
       const int i = i0 + j * kThreads + tid;
       id[j] = i < q.len ? ldg(q.text + i) : -1;
     }
+  };
+  // f(which of the workgroup's pieces, j) for those of the ids that lie in one
+  const auto each = [&](const int (&id)[AHEAD], auto f) {
 #pragma unroll
     for (int j = 0; j < AHEAD; ++j) {
-      const bool in = (uint32_t)id[j] < (uint32_t)vocab && (uint32_t)id[j] / kAdjustChunk % (uint32_t)step == (uint32_t)first;
-      const uint64_t all = __ballot(in);
-      if (!all) continue;
-      int at = 0;
-      if (lane == 0) at = atomicAdd(&k.n, __popcll(all));
-      at = __builtin_amdgcn_readfirstlane(at) + __popcll(all & ((1ull << lane) - 1));
-      if (in && at < kKept) k.token[at] = (uint32_t)id[j] | (i0 + j * kThreads + tid >= q.answer0 ? 0x80000000u : 0u);
+      if ((uint32_t)id[j] >= (uint32_t)vocab) continue;
+      const int c = id[j] / kAdjustChunk - first, piece = (int)(((float)c + 0.5f) * inverse);  // (at most 2^12: exact)
+      if (c >= 0 && piece * step == c) f(piece, j);
     }
+  };
+  int head[AHEAD], more[AHEAD];
+  load(head, 0);
+  if (tid < kKeptPieces) k.at[tid] = 0;
+  lds_barrier();
+  const auto count = [&](int piece, int) { atomicAdd(&k.at[piece], 1); };
+  each(head, count);
+  for (int i0 = AHEAD * kThreads; i0 < q.len; i0 += AHEAD * kThreads) {
+    load(more, i0);
+    each(more, count);
   }
   lds_barrier();
+  if (tid < kKeptPieces) {  // (one wave)
+    const int mine = k.at[tid];
+    int sum = mine;
+#pragma unroll
+    for (int off = 1; off < kWave; off <<= 1) {
+      const int o = __shfl_up(sum, off, kWave);
+      if (tid >= off) sum += o;
+    }
+    k.start[tid + 1] = sum;
+    k.at[tid] = sum - mine;
+    if (tid == 0) k.start[0] = 0;
+  }
+  lds_barrier();
+  if (k.start[kKeptPieces] > kKept) return;
+  const auto place = [&](const int (&id)[AHEAD], int i0) {
+    each(id, [&](int piece, int j) {
+      k.token[atomicAdd(&k.at[piece], 1)] = (uint32_t)id[j] | (i0 + j * kThreads + tid >= q.answer0 ? 0x80000000u : 0u);
+    });
+  };
+  place(head, 0);
+  for (int i0 = AHEAD * kThreads; i0 < q.len; i0 += AHEAD * kThreads) {
+    load(more, i0);
+    place(more, i0);
+  }
 }
+static_assert(kKeptPieces == kWave, "a lane per piece");
 
-// Clears the marks and makes those of the history and the biases in a piece.
+// Clears the marks and makes those of the history and the biases in a piece; entry: the
+// thread's of the bias list.
 template <bool TEXT, bool BIAS>
-__device__ __forceinline__ void mark_piece(const AdjustArgs& a, Marks<TEXT, BIAS>& m, const Request& q, const Kept* kept, int base, int size) {
+__device__ __forceinline__ void mark_piece(const AdjustArgs& a, Marks<TEXT, BIAS>& m, const Request& q, const Kept* kept, int piece, int entry, int base, int size) {
   const int tid = threadIdx.x;
   constexpr int PER = kAdjustChunk / 4 / kThreads;
 #pragma unroll
@@ -188,21 +223,30 @@ __device__ __forceinline__ void mark_piece(const AdjustArgs& a, Marks<TEXT, BIAS
         if (counts) atomicAdd(&m.count[t], 1u);
       }
     };
-    if (kept && kept->n <= kKept) {
-      for (int i = tid; i < kept->n; i += kThreads) mark(kept->token[i] & 0x7fffffffu, kept->token[i] >> 31);
+    if (kept && kept->start[kKeptPieces] <= kKept) {
+      for (int i = kept->start[piece] + tid; i < kept->start[piece + 1]; i += kThreads) mark(kept->token[i] & 0x7fffffffu, kept->token[i] >> 31);
     } else {
 #pragma unroll 4
       for (int i = tid; i < q.len; i += kThreads) mark((uint32_t)ldg(q.text + i), i >= q.answer0);
     }
   }
-  if (BIAS && q.listed)
-    for (int i = tid; i < q.biases; i += kThreads) {
-      const uint32_t t = (uint32_t)ldg(a.by.bias_token + q.bias0 + i) - (uint32_t)base;
+  if (BIAS && q.listed) {
+    const auto mark = [&](int id, int i) {
+      const uint32_t t = (uint32_t)id - (uint32_t)base;
       if (t < (uint32_t)size) {
         atomicOr(&m.biased[t >> 5], 1u << (t & 31));
         atomicMax(&m.bias[t], (uint32_t)i + 1);
       }
-    }
+    };
+    mark(entry, tid);
+    for (int i = tid + kThreads; i < q.biases; i += kThreads) mark(ldg(a.by.bias_token + q.bias0 + i), i);
+  }
+}
+
+// The thread's entry of the request's bias list: its token.
+template <bool BIAS>
+__device__ __forceinline__ int entry_of(const AdjustArgs& a, const Request& q) {
+  return BIAS && (int)threadIdx.x < q.biases ? ldg(a.by.bias_token + q.bias0 + threadIdx.x) : -1;
 }
 
 // The thread's token of a row's branch, if there is one in the piece: marks it.
@@ -357,7 +401,7 @@ __global__ __launch_bounds__(kThreads, 6) void adjust_rows_kernel(AdjustArgs a) 
       if (tid < q.n) token = ldg(a.by.tokens + q.row0 + tid);  // (n is at most 128)
       branch = ldg((const u32x4*)(a.mask + (size_t)first * 4));
     }
-    if (marked) mark_piece<TEXT, BIAS>(a, m, q, nullptr, base, size);
+    if (marked) mark_piece<TEXT, BIAS>(a, m, q, nullptr, 0, entry_of<BIAS>(a, q), base, size);
     for (int row = first; row < r; ++row) {
       Own<TEXT, BIAS> own;
       if (TEXT && q.active) own.mark(m, turn, q, token, branch, base, size);
@@ -407,18 +451,20 @@ __global__ __launch_bounds__(kThreads, 6) void adjust_row_kernel(AdjustArgs a) {
   if (prefixed) next_prefix = mask_byte(a.by.seen, c0 * kAdjustChunk, size_of(c0));
   const Request q = request_of<TEXT, BIAS>(a, request);
   const bool marked = (TEXT && q.active) || (BIAS && q.listed);
+  const bool sorted = q.len > 0 && step < a.chunks && a.chunks_per <= kKeptPieces;
+  const int entry = entry_of<BIAS>(a, q);
   int token = -1;
   u32x4 branch = {0, 0, 0, 0};
   if (TEXT && q.active) {
     if (tid < q.n) token = ldg(a.by.tokens + q.row0 + tid);
     branch = ldg((const u32x4*)(a.mask + (size_t)row * 4));
-    if (step < a.chunks) keep_history(kept, q, a.V, c0, step);
+    if (sorted) keep_history(kept, q, a.V, c0, step);
   }
   Best best;
-  for (int c = c0; c < a.chunks; c += step) {
+  for (int c = c0, piece = 0; c < a.chunks; c += step, ++piece) {
     const int base = c * kAdjustChunk, size = size_of(c);
     if (marked) {
-      mark_piece<TEXT, BIAS>(a, m, q, step < a.chunks ? &kept : nullptr, base, size);
+      mark_piece<TEXT, BIAS>(a, m, q, sorted ? &kept : nullptr, piece, entry, base, size);
       Own<TEXT, BIAS> own;
       if (TEXT && q.active) own.mark(m, 0, q, token, branch, base, size);
       lds_barrier();
