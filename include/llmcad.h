@@ -542,9 +542,9 @@ size_t llmcad_batch_adjust_workspace_bytes(const llmcad_config* cfg, int32_t n_r
  *
  * Errors (checked on the host, nothing enqueued): LLMCAD_EARG (a NULL or unaligned
  * pointer, bits or a count out of range, neither out nor greedy; penalties without
- * tokens, a negative history_stride, bias_start without its lists, n_masks < 1 with
- * allow, allow or mask_of without the other, an out that overlaps the logits otherwise), LLMCAD_ESHAPE (a stride
- * below vocab), LLMCAD_EWORKSPACE.
+ * tokens, a negative history_stride or n_bias, entries without their lists, n_masks < 1
+ * with allow, allow or mask_of without the other, an out that overlaps the logits
+ * otherwise), LLMCAD_ESHAPE (a stride below vocab), LLMCAD_EWORKSPACE.
  */
 int llmcad_batch_adjust(const llmcad_config* cfg, const void* plan, size_t plan_bytes, int32_t n_requests, int32_t n_rows,
                         const void* logits, int32_t bits, int64_t row_stride, const llmcad_adjustments* by, void* out,
@@ -602,8 +602,8 @@ size_t llmcad_batch_pages_workspace_bytes(int32_t n_requests, int32_t n_pages);
  * the old ones, and n_free is 0.
  *
  * Errors (checked on the host, nothing enqueued): as llmcad_batch_commit; LLMCAD_EARG too for
- * n_pages or max_pages above LLMCAD_MAX_POOL and for table_out or held_out that overlaps an
- * input; LLMCAD_EWORKSPACE.
+ * n_pages or max_pages above LLMCAD_MAX_POOL and for an output that overlaps an input;
+ * LLMCAD_EWORKSPACE.
  */
 int llmcad_batch_fork(const llmcad_config* cfg, int32_t n_kv_heads, void* k_pages, void* v_pages, int32_t n_pages,
                       int32_t n_requests, const int32_t* block_table, int32_t max_pages, const int32_t* held,

@@ -452,11 +452,11 @@ def _want(what, name, t, dtype, *shape):
 
 def _want_rows(what, name, t, n, heads, dh):
     """t is bf16 [n, heads, dh] whose rows are contiguous (any distance between them); returns that distance."""
-    if t.dtype != torch.bfloat16 or t.shape != (n, heads, dh) or t.stride(2) != 1 or \
-            (heads > 1 and t.stride(1) != dh):
+    stride = t.stride()
+    if t.dtype is not torch.bfloat16 or t.shape != (n, heads, dh) or stride[2] != 1 or (heads > 1 and stride[1] != dh):
         raise ValueError(f"{what}: {name} must be bfloat16 [{n}, {heads}, {dh}] with contiguous rows, "
                          f"got {t.dtype} {tuple(t.shape)}")
-    return t.stride(0) if n > 1 else heads * dh
+    return stride[0] if n > 1 else heads * dh
 
 
 def batch_plan_bytes(cfg, n_requests: int, n_rows: int) -> int:
@@ -555,10 +555,11 @@ def _want_gain(what, name, t, heads, dh):
     """t is None, bf16 [dh] (one gain for all heads) or [heads, dh]; returns the distance between heads' gains."""
     if t is None:
         return 0
-    if t.dtype != torch.bfloat16 or tuple(t.shape) not in ((dh,), (heads, dh)) or t.stride(-1) != 1:
+    one = t.dim() == 1
+    if t.dtype is not torch.bfloat16 or t.shape != ((dh,) if one else (heads, dh)) or t.stride(-1) != 1:
         raise ValueError(f"{what}: {name} must be bfloat16 [{dh}] or [{heads}, {dh}] with contiguous rows, "
                          f"got {t.dtype} {tuple(t.shape)}")
-    return t.stride(0) if t.dim() == 2 and heads > 1 else 0
+    return t.stride(0) if not one and heads > 1 else 0
 
 
 def batch_norm_store(cfg, n_kv_heads: int, layer: int, q, k, v, q_gain, k_gain, q_out, k_pages, v_pages, plan,
@@ -1039,9 +1040,9 @@ class Batch:
         self.workspace = torch.zeros(work, dtype=torch.uint8, device=dev)
         for name, view in batch_plan_views(self.cfg, self.n_requests, self.n_rows, self.plan_buffer).items():
             setattr(self, name, view)  # slot, position, mask, rope, status, taken
-        self.adjust_workspace = torch.zeros(batch_adjust_workspace_bytes(self.cfg, self.n_rows), dtype=torch.uint8, device=dev)
         self._planned = False  # the last plan's pages are on the free list still
         self._shared = False   # some pages may be in several tables (fork)
+        self._more_workspaces = {}  # of adjust, fork and compact, made when first used
         self._changed = False  # ... and some of them have left the tables
 
     def _among(self, ids, others):
@@ -1111,7 +1112,7 @@ class Batch:
         """batch_adjust of the step's rows (by: history, prompt_len, seen, penalties, bias, allow, mask_of)."""
         self._rows("adjust", logits=logits)
         batch_adjust(self.cfg, self.plan_buffer, self.n_requests, logits, tokens=tokens, out=out, greedy=greedy,
-                     workspace=self.adjust_workspace, **by)
+                     workspace=self._workspace("adjust", batch_adjust_workspace_bytes(self.cfg, self.n_rows)), **by)
 
     def accept(self, tokens, greedy, path, accept_len, next_token, history=None):
         """The accept walk of every request's tree: what commit takes, and the tokens after it."""
@@ -1168,17 +1169,19 @@ class Batch:
         if self._planned:
             raise RuntimeError(f"Batch.{what}: a plan was not advanced")
 
+    def _workspace(self, what, size):
+        if what not in self._more_workspaces:
+            self._more_workspaces[what] = torch.empty(size, dtype=torch.uint8, device=self.block_table.device)
+        return self._more_workspaces[what]
+
     def _pages_workspace(self):
-        if not hasattr(self, "_pages_work"):
-            size = batch_pages_workspace_bytes(self.n_requests, self.n_pages)
-            self._pages_work = torch.empty(size, dtype=torch.uint8, device=self.block_table.device)
-        return self._pages_work
+        return self._workspace("pages", batch_pages_workspace_bytes(self.n_requests, self.n_pages))
 
     def fork(self, source, held):
         """Request b continues from request source[b], which holds held[source[b]] tokens (itself: it stays; negative:
         it ends; int32 [n_requests] both; see llmcad_batch_fork).  Between steps: after advance (and commit).  Full pages
-        are shared from then on, and pages past the held tokens come back as with trim.  Returns the new lengths; reads
-        the free list's from the device.  Raises, with everything as it was, if pages run out or a length is none."""
+        are shared from then on (a length must not fall below one's end again: trim refuses it), and pages past the held
+        tokens come back as with trim.  Returns the new lengths; reads the free list's from the device.  Raises, with everything as it was, if pages run out or a length is none."""
         self._between_steps("fork")
         table, lengths = torch.empty_like(self.block_table), torch.empty_like(held)
         free = torch.empty(self.n_pages, dtype=torch.int32, device=held.device)

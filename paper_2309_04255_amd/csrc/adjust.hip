@@ -110,8 +110,9 @@ struct Request {
   bool active, listed;  // has penalties, has biases
   int row0, n, held, answer0;
   const int* text;  // its history, `len` tokens
-  int len;
-  int bias0, biases;
+  uint32_t len;     // (loops of a workgroup's steps past 2^31 - 1 stay in range unsigned)
+  int bias0;
+  uint32_t biases;
 };
 
 template <bool TEXT, bool BIAS>
@@ -129,14 +130,14 @@ __device__ __forceinline__ Request request_of(const AdjustArgs& a, int request) 
     q.answer0 = a.by.prompt_len ? ldg(a.by.prompt_len + request) : 0;
     q.active = !(q.rho == 1.0f && q.presence == 0.0f && q.frequency == 0.0f);  // (1 and zeros change no value)
     q.text = a.by.history + (long long)request * a.by.history_stride;
-    q.len = !q.active || !a.by.history ? 0 : q.held < a.by.history_stride ? q.held : (int)a.by.history_stride;
+    q.len = !q.active || !a.by.history ? 0 : (uint32_t)(q.held < a.by.history_stride ? q.held : a.by.history_stride);
   }
   if (BIAS) {
     int lo = ldg(a.by.bias_start + request), hi = ldg(a.by.bias_start + request + 1);
     lo = lo < 0 ? 0 : lo;
     hi = hi > a.by.n_bias ? a.by.n_bias : hi;
     q.bias0 = lo;
-    q.biases = hi > lo ? hi - lo : 0;
+    q.biases = hi > lo ? (uint32_t)(hi - lo) : 0;
     q.listed = hi > lo;
   }
   return q;
@@ -148,10 +149,10 @@ __device__ __forceinline__ void keep_history(Kept& k, const Request& q, int voca
   const int tid = threadIdx.x;
   constexpr int AHEAD = 8;  // loads in flight; so many are not read again for the second pass
   const float inverse = 1.0f / (float)step;
-  const auto load = [&](int (&id)[AHEAD], int i0) {
+  const auto load = [&](int (&id)[AHEAD], uint32_t i0) {
 #pragma unroll
     for (int j = 0; j < AHEAD; ++j) {
-      const int i = i0 + j * kThreads + tid;
+      const uint32_t i = i0 + j * kThreads + tid;
       id[j] = i < q.len ? ldg(q.text + i) : -1;
     }
   };
@@ -170,7 +171,7 @@ __device__ __forceinline__ void keep_history(Kept& k, const Request& q, int voca
   lds_barrier();
   const auto count = [&](int piece, int) { atomicAdd(&k.at[piece], 1); };
   each(head, count);
-  for (int i0 = AHEAD * kThreads; i0 < q.len; i0 += AHEAD * kThreads) {
+  for (uint32_t i0 = AHEAD * kThreads; i0 < q.len; i0 += AHEAD * kThreads) {
     load(more, i0);
     each(more, count);
   }
@@ -189,13 +190,13 @@ __device__ __forceinline__ void keep_history(Kept& k, const Request& q, int voca
   }
   lds_barrier();
   if (k.start[kKeptPieces] > kKept) return;
-  const auto place = [&](const int (&id)[AHEAD], int i0) {
+  const auto place = [&](const int (&id)[AHEAD], uint32_t i0) {
     each(id, [&](int piece, int j) {
-      k.token[atomicAdd(&k.at[piece], 1)] = (uint32_t)id[j] | (i0 + j * kThreads + tid >= q.answer0 ? 0x80000000u : 0u);
+      k.token[atomicAdd(&k.at[piece], 1)] = (uint32_t)id[j] | ((int)(i0 + j * kThreads + tid) >= q.answer0 ? 0x80000000u : 0u);
     });
   };
   place(head, 0);
-  for (int i0 = AHEAD * kThreads; i0 < q.len; i0 += AHEAD * kThreads) {
+  for (uint32_t i0 = AHEAD * kThreads; i0 < q.len; i0 += AHEAD * kThreads) {
     load(more, i0);
     place(more, i0);
   }
@@ -227,26 +228,26 @@ __device__ __forceinline__ void mark_piece(const AdjustArgs& a, Marks<TEXT, BIAS
       for (int i = kept->start[piece] + tid; i < kept->start[piece + 1]; i += kThreads) mark(kept->token[i] & 0x7fffffffu, kept->token[i] >> 31);
     } else {
 #pragma unroll 4
-      for (int i = tid; i < q.len; i += kThreads) mark((uint32_t)ldg(q.text + i), i >= q.answer0);
+      for (uint32_t i = tid; i < q.len; i += kThreads) mark((uint32_t)ldg(q.text + i), (int)i >= q.answer0);
     }
   }
   if (BIAS && q.listed) {
-    const auto mark = [&](int id, int i) {
+    const auto mark = [&](int id, uint32_t i) {
       const uint32_t t = (uint32_t)id - (uint32_t)base;
       if (t < (uint32_t)size) {
         atomicOr(&m.biased[t >> 5], 1u << (t & 31));
-        atomicMax(&m.bias[t], (uint32_t)i + 1);
+        atomicMax(&m.bias[t], i + 1);
       }
     };
     mark(entry, tid);
-    for (int i = tid + kThreads; i < q.biases; i += kThreads) mark(ldg(a.by.bias_token + q.bias0 + i), i);
+    for (uint32_t i = tid + kThreads; i < q.biases; i += kThreads) mark(ldg(a.by.bias_token + q.bias0 + i), i);
   }
 }
 
 // The thread's entry of the request's bias list: its token.
 template <bool BIAS>
 __device__ __forceinline__ int entry_of(const AdjustArgs& a, const Request& q) {
-  return BIAS && (int)threadIdx.x < q.biases ? ldg(a.by.bias_token + q.bias0 + threadIdx.x) : -1;
+  return BIAS && threadIdx.x < q.biases ? ldg(a.by.bias_token + q.bias0 + threadIdx.x) : -1;
 }
 
 // The thread's token of a row's branch, if there is one in the piece: marks it.
@@ -398,7 +399,7 @@ __global__ __launch_bounds__(kThreads, 6) void adjust_rows_kernel(AdjustArgs a) 
     int token = -1;
     u32x4 branch = {0, 0, 0, 0};
     if (TEXT && q.active) {
-      if (tid < q.n) token = ldg(a.by.tokens + q.row0 + tid);  // (n is at most 128)
+      if (tid < q.n) token = ldg(a.by.tokens + q.row0 + tid);  // (at most 128)
       branch = ldg((const u32x4*)(a.mask + (size_t)first * 4));
     }
     if (marked) mark_piece<TEXT, BIAS>(a, m, q, nullptr, 0, entry_of<BIAS>(a, q), base, size);

@@ -335,7 +335,8 @@ int llmcad_batch_adjust(const llmcad_config* cfg, const void* plan, size_t plan_
                 by->bias_value, by->allow, by->mask_of))
     return LLMCAD_EARG;
   if ((by->penalties && !by->tokens) || (by->history && by->history_stride < 0) ||
-      (by->bias_start && (!by->bias_token || !by->bias_value || by->n_bias < 0)) || (by->allow && by->n_masks < 1) ||
+      (by->bias_start && (by->n_bias < 0 || (by->n_bias > 0 && (!by->bias_token || !by->bias_value)))) ||
+      (by->allow && by->n_masks < 1) ||
       (!by->allow != !by->mask_of))
     return LLMCAD_EARG;
   if (row_stride < cfg->vocab || (out && out_stride < cfg->vocab)) return LLMCAD_ESHAPE;
@@ -410,9 +411,14 @@ int llmcad_batch_fork(const llmcad_config* cfg, int32_t n_kv_heads, void* k_page
   if (!source || !held_out || !free_pages || !n_free || !status || !aligned4(source, held_out, free_pages, n_free, status))
     return LLMCAD_EARG;
   const size_t table = (size_t)n_requests * max_pages * 4, lengths = (size_t)n_requests * 4;
-  if (overlap(table_out, table, source, lengths) || overlap(held_out, lengths, block_table, table) ||
-      overlap(held_out, lengths, held, lengths) || overlap(held_out, lengths, source, lengths))
-    return LLMCAD_EARG;
+  const struct {
+    const void* at;
+    size_t bytes;
+  } outs[] = {{table_out, table}, {held_out, lengths}, {free_pages, (size_t)n_pages * 4}, {n_free, 4}, {status, 4}};
+  for (const auto& o : outs)
+    if (overlap(o.at, o.bytes, block_table, table) || overlap(o.at, o.bytes, held, lengths) ||
+        overlap(o.at, o.bytes, source, lengths))
+      return LLMCAD_EARG;
   a.source = source;
   a.held_out = held_out;
   a.free_pages = free_pages;
@@ -428,7 +434,9 @@ int llmcad_batch_compact(const llmcad_config* cfg, int32_t n_kv_heads, void* k_p
   const int rc = pages_args(cfg, n_kv_heads, k_pages, v_pages, n_pages, n_requests, block_table, max_pages, held, table_out,
                             workspace, workspace_bytes, a);
   if (rc != LLMCAD_OK) return rc;
-  if (!n_used || !aligned4(n_used)) return LLMCAD_EARG;
+  const size_t table = (size_t)n_requests * max_pages * 4;
+  if (!n_used || !aligned4(n_used) || overlap(n_used, 4, block_table, table) || overlap(n_used, 4, held, (size_t)n_requests * 4))
+    return LLMCAD_EARG;
   a.n_used = n_used;
   return launched(launch_batch_compact(a, (hipStream_t)stream));
 }

@@ -207,6 +207,28 @@ def test_bias_lists(binding):
     out2, _ = s.run(bias=(start, token, value))
     s.biases = [s.biases[0], s.biases[1] + s.biases[2], []]
     s.check(out2, None, s.oracle("bias"))
+    out3, _ = s.run(bias=(_dev([0] * 4), token[:0], value[:0]))  # (no entries at all)
+    assert torch.equal(out3, s.logits)
+
+
+def test_a_long_bias_list(binding):
+    """More entries than a workgroup has threads, one for most tokens of the vocabulary, some of them twice."""
+    s = Step(binding, [2, 1], [3, 0], 6001)
+    rng = np.random.default_rng(0)
+    s.biases = [[(int(t), np.float32(v)) for t, v in zip(rng.integers(0, 6001, 9000), rng.normal(size=9000))], []]
+    out, best = s.run(**s.kw("bias"))
+    s.check(out, best, s.oracle("bias"))
+
+
+def test_long_histories(binding):
+    """More tokens than a workgroup sorts (all in one piece, or spread), over several pieces a workgroup."""
+    for where, V in (("one", 200003), ("spread", 200003), ("few", 9000)):
+        s = Step(binding, [1] * 40, [9000] * 20 + [5000] * 19 + [1], V, torch.bfloat16, seed=4, masks=0, tree=False)
+        rng = np.random.default_rng(1)
+        s.history[:] = {"one": rng.integers(4096 * 7, 4096 * 7 + 50, s.history.shape), "spread": rng.integers(0, V, s.history.shape),
+                        "few": rng.integers(0, 3, s.history.shape)}[where]
+        out, best = s.run(**s.kw())
+        s.check(out, best, s.oracle())
 
 
 def test_rows_that_are_not_placed(binding):

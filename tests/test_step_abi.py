@@ -93,7 +93,7 @@ FORK = dict(Hkv=32, kp=FAKE, vp=FAKE, n_pages=9, B=4, table=FAKE, max_pages=3, h
     (dict(held_out=None), "EARG"), (dict(free=None), "EARG"), (dict(n_free=None), "EARG"), (dict(status=None), "EARG"), (dict(ws=None), "EARG"),
     (dict(ws=FAKE + 4), "EARG"), (dict(ws_bytes=256), "EWORKSPACE"), (dict(table=FAKE + 2), "EARG"), (dict(status=FAKE + 1), "EARG"),
     (dict(table_out=FAKE), "EARG"), (dict(table_out=FAKE + 44), "EARG"), (dict(held_out=FAKE), "EARG"), (dict(held_out=FAKE + 12), "EARG"),
-    (dict(table=FAR + 4100), "EARG"),
+    (dict(table=FAR + 4100), "EARG"), (dict(free=FAKE + 40), "EARG"), (dict(n_free=FAKE), "EARG"), (dict(status=FAKE + 8), "EARG"),
 ])
 def test_fork(binding, cfg, kw, status):
     assert _call(binding, "llmcad_batch_fork", cfg, FORK, FORK, kw) == getattr(binding, status)
@@ -104,7 +104,7 @@ COMPACT = dict(Hkv=32, kp=FAKE, vp=FAKE, n_pages=9, B=4, table=FAKE, max_pages=3
 
 @pytest.mark.parametrize("kw,status", [
     (dict(cfg=None), "EARG"), (dict(Hkv=5), "ESHAPE"), (dict(kp=FAKE + 2), "EARG"), (dict(n_pages=(1 << 18) + 1), "EARG"), (dict(n_used=None), "EARG"),
-    (dict(n_used=FAR + 2), "EARG"), (dict(table_out=FAKE + 4), "EARG"), (dict(ws_bytes=100), "EWORKSPACE"), (dict(held=None), "EARG"),
+    (dict(n_used=FAR + 2), "EARG"), (dict(n_used=FAKE + 44), "EARG"), (dict(table_out=FAKE + 4), "EARG"), (dict(ws_bytes=100), "EWORKSPACE"), (dict(held=None), "EARG"),
 ])
 def test_compact(binding, cfg, kw, status):
     assert _call(binding, "llmcad_batch_compact", cfg, COMPACT, COMPACT, kw) == getattr(binding, status)
