@@ -605,7 +605,7 @@ hipError_t launch_batch_adjust(const AdjustArgs& args, hipStream_t st) {
   // About as many workgroups as the GPU holds (three on a CU, four without penalties):
   // of several rows each where requests have several, of several pieces of a row otherwise.
   const long long tiles = (long long)a.chunks * a.N, want = a.by.penalties ? 768 : 1024;
-  const int per = (int)((tiles + want - 1) / want);
+  const int per = tiles < want ? 1 : (int)((tiles + want / 2) / want);
   a.rows_per = 1;
   a.chunks_per = 0;
   if (a.N >= 4ll * a.B && tiles < 1ll << 26)

@@ -109,6 +109,7 @@ struct StoreArgs {
   const float* rope;
   int B, N, H, Hkv, Dh, n_pages;
   int heads_per;  // heads that a workgroup turns (the launch sets it)
+  int dim_parts;  // workgroups that share a head's values (the launch sets it)
   // llmcad_batch_norm_store alone
   const bf16* q_gain;  // null: ones
   const bf16* k_gain;

@@ -368,7 +368,7 @@ __device__ __forceinline__ void turn_rows(const StoreArgs& a, int block, int hea
 }
 
 template <int DH>
-__device__ __forceinline__ void write_values(const StoreArgs& a, int block, int kh) {
+__device__ __forceinline__ void write_values(const StoreArgs& a, int block, int kh, int part) {
   // (up to seven rows behind the block's own finish its last piece)
   __shared__ int slot_s[kStoreRows + 8];  // from the row before the block on
   __shared__ int piece_s[kStoreRows];     // pieces that begin in the block: first row | rows << 8
@@ -377,10 +377,11 @@ __device__ __forceinline__ void write_values(const StoreArgs& a, int block, int 
   __shared__ uint16_t vt[kStoreRows + 7][DH + 2];
   const int r0 = block * kStoreRows, tid = threadIdx.x;
   const int rows = a.N - r0 < kStoreRows + 7 ? a.N - r0 : kStoreRows + 7;
+  const int dims = DH / a.dim_parts, d0 = part * dims;  // the workgroup's
   if (tid < kStoreRows + 8) slot_s[tid] = r0 + tid > 0 ? slot_of(a, r0 + tid - 1) : -1;
 #pragma unroll 4
-  for (int e = tid; e < rows * (DH / 8); e += kThreads) {
-    const int i = e / (DH / 8), c = 8 * (e % (DH / 8));
+  for (int e = tid; e < rows * (dims / 8); e += kThreads) {
+    const int i = e / (dims / 8), c = d0 + 8 * (e % (dims / 8));
     const bf16x8 v = ldg((const bf16x8*)(a.v + ((size_t)r0 + i) * a.v_stride + (size_t)kh * DH + c));
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
@@ -432,9 +433,9 @@ __device__ __forceinline__ void write_values(const StoreArgs& a, int block, int 
   // Whole pieces go line by line (64 prompts of 128 rows, 8 K/V heads: 46 us for 48), parts
   // dim by dim (64 trees of up to 31 rows, 32 heads: 14.3 for 15.8).
   if (all_whole) {
-    for (int e = tid; e < pieces * DH; e += kThreads) write_piece(e % pieces, e / pieces, true);
+    for (int e = tid; e < pieces * dims; e += kThreads) write_piece(e % pieces, d0 + e / pieces, true);
   } else {
-    for (int e = tid; e < pieces * DH; e += kThreads) write_piece(e / DH, e % DH, false);
+    for (int e = tid; e < pieces * dims; e += kThreads) write_piece(e / dims, d0 + e % dims, false);
   }
 }
 
@@ -445,7 +446,7 @@ __global__ __launch_bounds__(kThreads) void store_kernel(StoreArgs a, int turn_b
   if (x < turns)
     turn_rows<DH, NORM>(a, x % turn_blocks, x / turn_blocks * a.heads_per);
   else
-    write_values<DH>(a, (x - turns) / a.Hkv, (x - turns) % a.Hkv);
+    write_values<DH>(a, (x - turns) / a.dim_parts / a.Hkv, (x - turns) / a.dim_parts % a.Hkv, (x - turns) % a.dim_parts);
 }
 
 // ---------------------------------------------------------------- rollback
@@ -561,7 +562,10 @@ hipError_t launch_store(const StoreArgs& args, hipStream_t st) {
   a.heads_per = (int)((long long)turn_blocks * heads / 128);
   a.heads_per = a.heads_per < 1 ? 1 : a.heads_per > 8 ? 8 : a.heads_per;
   const int head_blocks = cdiv(heads, a.heads_per);
-  const dim3 grid(turn_blocks * head_blocks + cdiv(a.N, kStoreRows) * a.Hkv);
+  const long long values = (long long)cdiv(a.N, kStoreRows) * a.Hkv;
+  a.dim_parts = 1;
+  while (a.dim_parts < 8 && values * a.dim_parts < 256) a.dim_parts *= 2;
+  const dim3 grid((unsigned)(turn_blocks * head_blocks + values * a.dim_parts));
   if (a.Dh == 128)
     store_kernel<128, NORM><<<grid, dim3(kThreads), 0, st>>>(a, turn_blocks, head_blocks);
   else

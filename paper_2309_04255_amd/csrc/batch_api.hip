@@ -80,7 +80,7 @@ int store_args(const llmcad_config* cfg, int32_t n_kv_heads, int32_t layer, cons
   a.Hkv = n_kv_heads;
   a.Dh = cfg->head_dim;
   a.n_pages = n_pages;
-  a.heads_per = 0;
+  a.heads_per = a.dim_parts = 0;
   a.q_gain = a.k_gain = nullptr;
   a.q_gain_stride = a.k_gain_stride = 0;
   a.eps = 0.0f;
