@@ -95,11 +95,11 @@ struct Marks {
 
 __device__ __forceinline__ uint32_t byte_of(const uint32_t* words, int piece) { return ((const uint8_t*)words)[piece]; }
 
-// Tokens of the history in a workgroup's pieces, where it has several, piece by piece;
-// those whose occurrence counts have the top bit.
-constexpr int kKept = 4096, kKeptPieces = 64;
+// Tokens of the history in a workgroup's pieces, where it has several, piece by piece and
+// counted within it; those whose occurrence counts have the top bit.
+constexpr int kKept = 8192, kKeptPieces = 64;
 struct Kept {
-  uint32_t token[kKept];
+  uint16_t token[kKept];
   int start[kKeptPieces + 1];  // of each piece's; the last: of all (more than kKept: the history itself is read for every piece)
   int at[kKeptPieces];
 };
@@ -192,7 +192,7 @@ __device__ __forceinline__ void keep_history(Kept& k, const Request& q, int voca
   if (k.start[kKeptPieces] > kKept) return;
   const auto place = [&](const int (&id)[AHEAD], uint32_t i0) {
     each(id, [&](int piece, int j) {
-      k.token[atomicAdd(&k.at[piece], 1)] = (uint32_t)id[j] | ((int)(i0 + j * kThreads + tid) >= q.answer0 ? 0x80000000u : 0u);
+      k.token[atomicAdd(&k.at[piece], 1)] = (uint16_t)(id[j] % kAdjustChunk | ((int)(i0 + j * kThreads + tid) >= q.answer0 ? 0x8000 : 0));
     });
   };
   place(head, 0);
@@ -225,7 +225,7 @@ __device__ __forceinline__ void mark_piece(const AdjustArgs& a, Marks<TEXT, BIAS
       }
     };
     if (kept && kept->start[kKeptPieces] <= kKept) {
-      for (int i = kept->start[piece] + tid; i < kept->start[piece + 1]; i += kThreads) mark(kept->token[i] & 0x7fffffffu, kept->token[i] >> 31);
+      for (int i = kept->start[piece] + tid; i < kept->start[piece + 1]; i += kThreads) mark(base + (kept->token[i] & 0x7fffu), kept->token[i] >> 15);
     } else {
 #pragma unroll 4
       for (uint32_t i = tid; i < q.len; i += kThreads) mark((uint32_t)ldg(q.text + i), (int)i >= q.answer0);
@@ -292,13 +292,25 @@ struct Best {
       value = __builtin_elementwise_maximum(value, top);
     }
   }
-  // The wave's best, to lane 0's partial result.
+  // The wave's best, to lane 0's partial result: the largest value, then the lowest of its tokens.
   __device__ __forceinline__ void write(uint64_t* part) const {
-    float top = value;
-    int at = token;
     const bool nan = __ballot(value != value) != 0;
-    row16_argmax(top, at);
-    col4_argmax(top, at);
+    float top = value;
+    top = fmaxf(top, dpp_f<kDppQuadXor1>(top));
+    top = fmaxf(top, dpp_f<kDppQuadXor2>(top));
+    top = fmaxf(top, dpp_f<kDppRowHalfMirror>(top));
+    top = fmaxf(top, dpp_f<kDppRowMirror>(top));
+    top = col4_max(top);
+    int at = value == top ? token : 0x7fffffff;
+    at = min(at, dpp_i<kDppQuadXor1>(at));
+    at = min(at, dpp_i<kDppQuadXor2>(at));
+    at = min(at, dpp_i<kDppRowHalfMirror>(at));
+    at = min(at, dpp_i<kDppRowMirror>(at));
+    float a, b;
+    pair_xor16(__int_as_float(at), a, b);
+    at = min(__float_as_int(a), __float_as_int(b));
+    pair_xor32(__int_as_float(at), a, b);
+    at = min(__float_as_int(a), __float_as_int(b));
     if ((threadIdx.x & 63) == 0) stg(part, nan ? (uint64_t)~0ull : best_key(top, at));
   }
 };
@@ -391,29 +403,20 @@ __global__ __launch_bounds__(kThreads, 6) void adjust_rows_kernel(AdjustArgs a) 
     const uint64_t others = __ballot(requests != request || r0 + lane >= r1) >> (r - r0);
     r = others ? r + __ffsll((unsigned long long)others) - 1 : r1;
     if (request < 0) continue;
-    Eight<T> next;
-    load_eight(next, logits + (long long)first * a.stride, base, size);
-    uint32_t next_allowed = allowed_byte(a, __builtin_amdgcn_readlane(states, first - r0), base, size);
     const Request q = request_of<TEXT, BIAS>(a, request);
     const bool marked = (TEXT && q.active) || (BIAS && q.listed);
     int token = -1;
-    u32x4 branch = {0, 0, 0, 0};
-    if (TEXT && q.active) {
-      if (tid < q.n) token = ldg(a.by.tokens + q.row0 + tid);  // (at most 128)
-      branch = ldg((const u32x4*)(a.mask + (size_t)first * 4));
-    }
+    if (TEXT && q.active && tid < q.n) token = ldg(a.by.tokens + q.row0 + tid);  // (at most 128)
     if (marked) mark_piece<TEXT, BIAS>(a, m, q, nullptr, 0, entry_of<BIAS>(a, q), base, size);
     for (int row = first; row < r; ++row) {
+      u32x4 branch = {0, 0, 0, 0};
+      if (TEXT && q.active) branch = ldg((const u32x4*)(a.mask + (size_t)row * 4));
+      Eight<T> x;
+      load_eight(x, logits + (long long)row * a.stride, base, size);
+      const uint32_t allowed = allowed_byte(a, __builtin_amdgcn_readlane(states, row - r0), base, size);
       Own<TEXT, BIAS> own;
       if (TEXT && q.active) own.mark(m, turn, q, token, branch, base, size);
       if ((TEXT && q.active) || (marked && row == first)) lds_barrier();
-      Eight<T> x = next;
-      const uint32_t allowed = next_allowed;
-      if (row + 1 < r) {
-        load_eight(next, logits + (long long)(row + 1) * a.stride, base, size);
-        next_allowed = allowed_byte(a, __builtin_amdgcn_readlane(states, row + 1 - r0), base, size);
-        if (TEXT && q.active) branch = ldg((const u32x4*)(a.mask + (size_t)(row + 1) * 4));
-      }
       float f[8];
       adjust_eight<T, TEXT, BIAS>(a, m, turn, q, x, f, allowed, prefix);
       if (a.out) store_eight(x, (T*)a.out + (long long)row * a.out_stride, base, size);
@@ -444,12 +447,7 @@ __global__ __launch_bounds__(kThreads, 6) void adjust_row_kernel(AdjustArgs a) {
   const int request = wave_uniform(ldg(a.row_req + row)), state = a.by.mask_of ? wave_uniform(ldg(a.by.mask_of + row)) : -1;
   const T* logits = (const T*)a.logits + (long long)row * a.stride;
   auto size_of = [&](int c) { return a.V - c * kAdjustChunk < kAdjustChunk ? a.V - c * kAdjustChunk : kAdjustChunk; };
-  Eight<T> next;
-  load_eight(next, logits, c0 * kAdjustChunk, size_of(c0));
   if (request < 0 || !plan_is_for(a.head, a.B, a.N)) return;
-  uint32_t next_allowed = allowed_byte(a, state, c0 * kAdjustChunk, size_of(c0)), next_prefix = 0;
-  const bool prefixed = TEXT && a.by.seen;
-  if (prefixed) next_prefix = mask_byte(a.by.seen, c0 * kAdjustChunk, size_of(c0));
   const Request q = request_of<TEXT, BIAS>(a, request);
   const bool marked = (TEXT && q.active) || (BIAS && q.listed);
   const bool sorted = q.len > 0 && step < a.chunks && a.chunks_per <= kKeptPieces;
@@ -464,19 +462,14 @@ __global__ __launch_bounds__(kThreads, 6) void adjust_row_kernel(AdjustArgs a) {
   Best best;
   for (int c = c0, piece = 0; c < a.chunks; c += step, ++piece) {
     const int base = c * kAdjustChunk, size = size_of(c);
+    Eight<T> x;
+    load_eight(x, logits, base, size);
+    const uint32_t allowed = allowed_byte(a, state, base, size), prefix = TEXT && a.by.seen ? mask_byte(a.by.seen, base, size) : 0u;
     if (marked) {
       mark_piece<TEXT, BIAS>(a, m, q, sorted ? &kept : nullptr, piece, entry, base, size);
       Own<TEXT, BIAS> own;
       if (TEXT && q.active) own.mark(m, 0, q, token, branch, base, size);
       lds_barrier();
-    }
-    Eight<T> x = next;
-    const uint32_t allowed = next_allowed, prefix = next_prefix;
-    if (c + step < a.chunks) {
-      const int to = (c + step) * kAdjustChunk;
-      load_eight(next, logits, to, size_of(c + step));
-      next_allowed = allowed_byte(a, state, to, size_of(c + step));
-      if (prefixed) next_prefix = mask_byte(a.by.seen, to, size_of(c + step));
     }
     float f[8];
     adjust_eight<T, TEXT, BIAS>(a, m, 0, q, x, f, allowed, prefix);
@@ -604,13 +597,15 @@ hipError_t launch_batch_adjust(const AdjustArgs& args, hipStream_t st) {
   a.chunks = cdiv(a.V, kAdjustChunk);
   // About as many workgroups as the GPU holds (three on a CU, four without penalties):
   // of several rows each where requests have several, of several pieces of a row otherwise.
-  const long long tiles = (long long)a.chunks * a.N, want = a.by.penalties ? 768 : 1024;
+  const long long tiles = (long long)a.chunks * a.N;
+  const bool rows = a.N >= 4ll * a.B && tiles < 1ll << 26;  // (a launch takes 2^32 threads)
+  const long long want = rows && a.by.penalties ? 768 : 768;
   const int per = tiles < want ? 1 : (int)((tiles + want / 2) / want);
   a.rows_per = 1;
   a.chunks_per = 0;
-  if (a.N >= 4ll * a.B && tiles < 1ll << 26)
+  if (rows)
     a.rows_per = per < 16 ? per : 16;
-  else  // (a launch takes 2^32 threads)
+  else
     a.chunks_per = per < a.chunks ? per : a.chunks;
   a.segments = a.chunks_per == 0 ? a.chunks : cdiv(a.chunks, a.chunks_per);
   if (a.bf16_in)
