@@ -1,6 +1,27 @@
 // The answer side of a step of several requests: the adjustment of its logits
 // rows (penalties for tokens that a row's own sequence holds, biases, masks), the
 // greedy token of every row, and the walk of the requests' trees along them.
+//
+// A logit changes where its token occurs in the row's text, has a bias or is masked; the
+// others are copied.  A workgroup takes pieces of 4096 tokens: it counts the text's tokens
+// in a piece in LDS (4 bytes per token; integer atomics, whose order changes nothing), marks
+// those that occur in a bitmap, and streams the piece, eight tokens a thread, adjusting
+// the marked ones one after the other.  Every operation is a single fp32 one in the stated
+// order, so that nothing depends on how rows are shared; each wave leaves its best token,
+// and a second launch joins a row's.
+//
+// Bytes bound it where little is marked: 255 rows of 128000 bf16 logits are copied in 24 us
+// (5300 GB/s) and their greedy tokens found in 15 (4300).  With all adjustments they take
+// 45: the marked tokens (a tenth of a piece where a text's tokens are near each other) cost
+// about 60 vector instructions each step, a barrier waits for the slowest wave, and three
+// workgroups are on a CU (LDS).  561 rows of 32000 fp32 logits take 27.6 us (14 to read
+// them), a tree of 31 7.2, two launches' latency.
+//
+// Measured and left out: the next tile's loads in flight while one is computed (registers
+// cost more waves than it hides: 27.6 -> 28.6; with two tiles in turn 40); the branch's tokens
+// in registers instead of LDS, without barriers between rows (30.0 -> 30.6); two marked
+// tokens at a time (41.5 -> 43.0); pieces of 2048 (41 -> 43.7 with long histories); 2 KB more
+// LDS (two workgroups on a CU instead of three: 47 -> 61).
 #include "batch.h"
 
 namespace llmcad {
@@ -381,8 +402,7 @@ __device__ __forceinline__ uint32_t allowed_byte(const AdjustArgs& a, int state,
 }
 
 // Where requests have several rows: a workgroup takes one piece of rows [r0, r1).  A
-// request's marks are made once; the next row's logits are on their way while one
-// is computed.
+// request's marks are made once.
 template <class T, bool TEXT, bool BIAS>
 __global__ __launch_bounds__(kThreads, 6) void adjust_rows_kernel(AdjustArgs a) {
   __shared__ Marks<TEXT, BIAS> m;
@@ -437,7 +457,7 @@ __global__ __launch_bounds__(kThreads, 6) void adjust_rows_kernel(AdjustArgs a) 
 
 // Where they have few: a workgroup takes every a.segments-th piece of one row (tokens
 // that a text repeats lie near each other in many vocabularies).  The row's text is read
-// once; the next piece's logits are on their way while one is computed.
+// once and sorted by piece (38 us for 41 where every piece goes through all of it).
 template <class T, bool TEXT, bool BIAS>
 __global__ __launch_bounds__(kThreads, 6) void adjust_row_kernel(AdjustArgs a) {
   __shared__ Marks<TEXT, BIAS> m;
@@ -595,11 +615,13 @@ void launch_adjust(const AdjustArgs& a, hipStream_t st) {
 hipError_t launch_batch_adjust(const AdjustArgs& args, hipStream_t st) {
   AdjustArgs a = args;
   a.chunks = cdiv(a.V, kAdjustChunk);
-  // About as many workgroups as the GPU holds (three on a CU, four without penalties):
-  // of several rows each where requests have several, of several pieces of a row otherwise.
+  // About as many workgroups as the GPU holds (three on a CU, four without penalties): of
+  // several rows each where requests have eight or more (32 trees of up to 41 with histories
+  // of up to 1000: 27.6 us for 32.3), of several pieces of a row otherwise (four rows each
+  // of 64 requests: 20.3 for 21.8; at eight each takes 40).
   const long long tiles = (long long)a.chunks * a.N;
-  const bool rows = a.N >= 4ll * a.B && tiles < 1ll << 26;  // (a launch takes 2^32 threads)
-  const long long want = rows && a.by.penalties ? 768 : 768;
+  const bool rows = a.N >= 8ll * a.B && tiles < 1ll << 26;  // (a launch takes 2^32 threads)
+  const long long want = a.by.penalties ? 768 : 1024;
   const int per = tiles < want ? 1 : (int)((tiles + want / 2) / want);
   a.rows_per = 1;
   a.chunks_per = 0;
