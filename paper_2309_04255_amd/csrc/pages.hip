@@ -173,22 +173,20 @@ struct Fork {
         }
       }
       __syncthreads();
-      // the pages held before, and those that somebody still holds
-      each_page<THREADS>(a, held, widest, [&](int b, int p) {
-        before.set(p);
-        if (alive[b]) after.set(p);
-      });
       // who needs a page of its own for its last tokens
       PageCopy c{};
       bool copies_one = false;
       if (tid < B && from >= 0 && from != tid) {
         c.rows = held[from] % kPage;
-        const bool goes_on = source[from] != from && first[from] == tid;
-        if (c.rows > 0 && !goes_on) {
-          c.src = ldg(a.table + (size_t)from * a.max_pages + held[from] / kPage);
-          copies_one = c.src >= 0 && c.src < a.n_pages;
-        }
+        copies_one = c.rows > 0 && !(source[from] != from && first[from] == tid);  // (the first of a source that moved goes on with it)
+        if (copies_one) c.src = ldg(a.table + (size_t)from * a.max_pages + held[from] / kPage);
       }
+      // the pages held before, and those that somebody still holds
+      each_page<THREADS>(a, held, widest, [&](int b, int p) {
+        before.set(p);
+        if (alive[b]) after.set(p);
+      });
+      if (copies_one) copies_one = c.src >= 0 && c.src < a.n_pages;
       __syncthreads();
       const int n_free = before.count(a.n_pages, lds), k = block_before<THREADS>(copies_one ? 1 : 0, lds, n_copies);
       if (n_copies > n_free) {
