@@ -504,7 +504,8 @@ typedef struct llmcad_adjustments {
   const int32_t* prompt_len; /* [n_requests] the first tokens of the text that are a prompt
                                 (NULL: 0)                                                    */
   const uint32_t* seen;      /* [W] tokens that every text holds besides (the prefix's): bit
-                                t % 32 of word t / 32, W = ceil(vocab / 32)                  */
+                                t % 32 of word t / 32, W = ceil(vocab / 32) (the last word's
+                                other bits are ignored)                                      */
   const float* penalties;    /* [n_requests][3] repetition, presence, frequency              */
   const int32_t* bias_start; /* [n_requests + 1] request b's biases are entries bias_start[b]
                                 .. bias_start[b + 1] - 1 of the next two, those in [0, n_bias) */

@@ -194,6 +194,22 @@ def test_texts_that_repeat_end_and_lie(binding):
     s.check(out, best, s.oracle())
 
 
+@pytest.mark.parametrize("penalty", [(0.0, 0.0, 0.0), (-1.0, 0.0, 0.0), (1.5, 0.0, float("inf")), (float("inf"), 0.0, 0.0)])
+@pytest.mark.parametrize("n,V", [([1, 2], 33), ([1], 1003), ([20, 20], 4099)])
+def test_bits_behind_the_vocabulary(binding, n, V, penalty):
+    """The last word's bits past the vocabulary are nobody's tokens, whatever the penalties make of them."""
+    s = Step(binding, n, [3] * len(n), V, seed=V)
+    s.penalties[:] = penalty
+    s.seen = []
+    s.tokens[:], s.history[:] = -1, -1
+    kw = s.kw("tokens", "history", "penalties", "seen", "mask_of", "allow")
+    last = -(1 << V % 32)  # bits V % 32 ... 31
+    kw["seen"][-1] |= last
+    kw["allow"][:, -1] |= last
+    out, best = s.run(**kw)
+    s.check(out, best, s.oracle("tokens", "history", "penalties", "seen", "mask_of", "allow"))
+
+
 def test_bias_lists(binding):
     """A token more than once (the last entry counts), tokens that are none, lists that reach past the entries, infinities."""
     s = Step(binding, [2, 2, 2], [1, 1, 1], 4200)
