@@ -567,7 +567,7 @@ int llmcad_batch_adjust(const llmcad_config* cfg, const void* plan, size_t plan_
  * too); the rest of its outputs, and padding rows', are left as they were.
  *
  * Errors: LLMCAD_EARG (a NULL or unaligned pointer, a size out of range, a negative
- * history_stride), LLMCAD_EWORKSPACE (plan_bytes).
+ * history_stride, an output that overlaps tokens or greedy), LLMCAD_EWORKSPACE (plan_bytes).
  */
 int llmcad_batch_accept(const llmcad_config* cfg, const void* plan, size_t plan_bytes, int32_t n_requests, int32_t n_rows,
                         const int32_t* tokens, const int32_t* greedy, int32_t* path, int32_t* accept_len,

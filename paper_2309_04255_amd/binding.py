@@ -689,7 +689,8 @@ def batch_adjust(cfg, plan, n_requests: int, logits, tokens=None, history=None, 
         _want(what, "bias[2]", value, torch.float32, None)
         if token.shape != value.shape:
             raise ValueError("batch_adjust: a bias needs a value for each token")
-        by.bias_start, by.bias_token, by.bias_value, by.n_bias = start.data_ptr(), token.data_ptr(), value.data_ptr(), token.shape[0]
+        by.bias_start, by.bias_token, by.bias_value = start.data_ptr(), token.data_ptr(), value.data_ptr()
+        by.n_bias = token.shape[0]
     if allow is not None:
         _want(what, "allow", allow, i32, None, W)
         by.allow, by.n_masks = allow.data_ptr(), allow.shape[0]
@@ -1181,7 +1182,8 @@ class Batch:
         """Request b continues from request source[b], which holds held[source[b]] tokens (itself: it stays; negative:
         it ends; int32 [n_requests] both; see llmcad_batch_fork).  Between steps: after advance (and commit).  Full pages
         are shared from then on (a length must not fall below one's end again: trim refuses it), and pages past the held
-        tokens come back as with trim.  Returns the new lengths; reads the free list's from the device.  Raises, with everything as it was, if pages run out or a length is none."""
+        tokens come back as with trim.  Returns the new lengths; reads the free list's from the device.  Raises, with
+        everything as it was, if pages run out or a length is none."""
         self._between_steps("fork")
         table, lengths = torch.empty_like(self.block_table), torch.empty_like(held)
         free = torch.empty(self.n_pages, dtype=torch.int32, device=held.device)

@@ -378,6 +378,14 @@ int llmcad_batch_accept(const llmcad_config* cfg, const void* plan, size_t plan_
     return LLMCAD_EARG;
   const PlanLayout P(n_requests, n_rows, cfg->head_dim);
   if (plan_bytes < P.total) return LLMCAD_EWORKSPACE;
+  // (a thread writes an entry of the path while another still reads its token)
+  const size_t rows = (size_t)n_rows * 4, requests = (size_t)n_requests * 4;
+  const struct {
+    const void* at;
+    size_t bytes;
+  } outs[] = {{path, rows}, {accept_len, requests}, {next_token, requests}, {history, history ? requests * (size_t)history_stride : 0}};
+  for (const auto& o : outs)
+    if (o.bytes && (overlap(o.at, o.bytes, tokens, rows) || overlap(o.at, o.bytes, greedy, rows))) return LLMCAD_EARG;
   const char* at = (const char*)plan;
   AcceptArgs a;
   a.head = (const int*)(at + P.head);

@@ -82,6 +82,14 @@ def test_accept(binding, cfg, kw, status):
     assert _call(binding, "llmcad_batch_accept", cfg, ACCEPT, ACCEPT, kw) == getattr(binding, status)
 
 
+@pytest.mark.parametrize("out", ["path", "length", "after", "history"])
+@pytest.mark.parametrize("at", [0, 36, 4096, 4132])  # (the first and the last of the tokens and of the greedy ones)
+def test_accept_writes_apart_from_what_it_reads(binding, cfg, out, at):
+    apart = dict(tokens=FAKE, greedy=FAKE + 4096, path=FAR, length=FAR + 4096, after=FAR + 8192, history=FAR + 12288, stride=5)
+    a = {**ACCEPT, **apart, out: FAKE + at}
+    assert _call(binding, "llmcad_batch_accept", cfg, ACCEPT, a, {}) == binding.EARG
+
+
 FORK = dict(Hkv=32, kp=FAKE, vp=FAKE, n_pages=9, B=4, table=FAKE, max_pages=3, held=FAKE, source=FAKE, table_out=FAR, held_out=FAR + 4096,
             free=FAR + 8192, n_free=FAR + 9000, status=FAR + 9004, ws=FAKE, ws_bytes=1 << 20)
 
