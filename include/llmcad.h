@@ -401,6 +401,11 @@ int llmcad_batch_plan_region(const llmcad_config* cfg, int32_t n_requests, int32
  * it was, and the other operators leave its rows out.  Calling again with the
  * same arguments gives the same plan.
  *
+ * A request with rows writes behind its tokens, into their last page if that is
+ * not full: the page must be in no other table (llmcad_batch_fork shares full
+ * pages; a request that is rolled back into one gives it up, or is forked again).
+ * The plan does not look for such pages.
+ *
  * Errors (checked on the host, nothing enqueued): LLMCAD_EARG for a NULL or
  * unaligned pointer or a size out of range, LLMCAD_ECAPACITY for prefix_len not
  * in [0, 2^30], LLMCAD_EWORKSPACE for plan_bytes below llmcad_batch_plan_bytes.

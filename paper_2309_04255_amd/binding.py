@@ -499,7 +499,8 @@ def batch_plan(cfg, row_start, held, parent, prefix_len: int, block_table, free_
                n_rows: int, stream=None):
     """Build a step's plan on the device (see llmcad_batch_plan): row_start [B + 1], held [B], parent
     [n_rows] or None, block_table [B, max_pages] (updated), free_pages [n_free], all int32; plan a uint8
-    tensor of batch_plan_bytes."""
+    tensor of batch_plan_bytes.  A length must not end inside a page that another request holds too (Batch.plan
+    looks after that, this call does not)."""
     what = "batch_plan"
     dev = _on_device(what, row_start, held, parent, block_table, free_pages, plan)
     B = held.shape[0]
@@ -1081,7 +1082,30 @@ class Batch:
             pages = pages[first[pages.long()] == at]
         return pages
 
+    def _cut(self, held, of=None):
+        """Which requests' lengths end inside a page that another request holds too, bool [n_requests] (of: the
+        requests that count, the others hold nothing).  The next step would write into it behind the other's back."""
+        cols = torch.arange(self.block_table.shape[1], device=held.device)
+        kept = (cols * PAGE < held[:, None]) & (self.block_table >= 0) & (self.block_table < self.n_pages)
+        if of is not None:
+            kept &= of[:, None]
+        index = torch.where(kept, self.block_table, self.n_pages).long()
+        holders = torch.zeros(self.n_pages + 1, dtype=torch.int32, device=held.device)
+        holders.scatter_add_(0, index.view(-1), torch.ones_like(index.view(-1), dtype=torch.int32))
+        last = (cols == (held // PAGE)[:, None]) & (held % PAGE > 0)[:, None]
+        return (last & kept & (holders[index] > 1)).any(1)
+
+    def _refuse_cut(self, what, held, of=None):
+        if bool(self._cut(held, of).any()):
+            raise ValueError(f"{what}: a request would end inside a page that another one holds")
+
     def plan(self, row_start, held, parent=None):
+        """batch_plan of the step.  After a fork, a request with rows whose length ends inside a page that another
+        one holds too counts as one of bad length: no request is placed, and advance raises."""
+        if self._shared:  # (on the device: a step waits for nothing here)
+            _want("Batch.plan", "row_start", row_start, torch.int32, self.n_requests + 1)
+            _want("Batch.plan", "held", held, torch.int32, self.n_requests)
+            held = torch.where(self._cut(held) & (row_start[1:] > row_start[:-1]), -1, held)
         if self._planned:
             self._undo()
         self._planned = True
@@ -1149,14 +1173,7 @@ class Batch:
         rollback; reads how many from the device).  Without it the next plan overwrites their entries.  A length
         that ends inside a page which another request holds too is refused: the next step would write there."""
         if self._shared:
-            cols = torch.arange(self.block_table.shape[1], device=held.device)
-            cut = (cols == (held // PAGE)[:, None]) & (held % PAGE > 0)[:, None] & (self.block_table >= 0)
-            kept = torch.where(cols * PAGE < held[:, None], self.block_table, -1)
-            index = torch.where((kept >= 0) & (kept < self.n_pages), kept, self.n_pages).long()
-            holders = torch.zeros(self.n_pages + 1, dtype=torch.int32, device=held.device)
-            holders.scatter_add_(0, index.view(-1), torch.ones_like(index.view(-1), dtype=torch.int32))
-            if bool((cut & (holders[index] > 1) & (index < self.n_pages)).any()):
-                raise ValueError("trim: a request would end inside a page that another one holds")
+            self._refuse_cut("trim", held)
         pages = self._give_back(torch.arange(self.block_table.shape[1], device=held.device) * PAGE >= held[:, None])
         self.free_pages = torch.cat([pages, self.free_pages])
 
@@ -1181,10 +1198,17 @@ class Batch:
     def fork(self, source, held):
         """Request b continues from request source[b], which holds held[source[b]] tokens (itself: it stays; negative:
         it ends; int32 [n_requests] both; see llmcad_batch_fork).  Between steps: after advance (and commit).  Full pages
-        are shared from then on (a length must not fall below one's end again: trim refuses it), and pages past the held
-        tokens come back as with trim.  Returns the new lengths; reads the free list's from the device.  Raises, with
-        everything as it was, if pages run out or a length is none."""
+        are shared from then on, and pages past the held tokens come back as with trim.  Returns the new lengths; reads
+        the free list's from the device.  Raises, with everything as it was, if pages run out, a length is none, or that
+        of a request which somebody continues from ends inside a page that another such one holds (plan, trim and
+        compact refuse such a length too)."""
         self._between_steps("fork")
+        if self._shared:
+            _want("Batch.fork", "source", source, torch.int32, self.n_requests)
+            _want("Batch.fork", "held", held, torch.int32, self.n_requests)
+            alive = torch.zeros(self.n_requests + 1, dtype=torch.bool, device=held.device)
+            alive[torch.where((source >= 0) & (source < self.n_requests), source, self.n_requests).long()] = True
+            self._refuse_cut("fork", held, alive[:-1])
         table, lengths = torch.empty_like(self.block_table), torch.empty_like(held)
         free = torch.empty(self.n_pages, dtype=torch.int32, device=held.device)
         n_free, status = batch_fork(self.cfg, self.n_kv_heads, self.k_pages, self.v_pages, self.block_table, held, source,
@@ -1199,8 +1223,12 @@ class Batch:
 
     def compact(self, held):
         """Moves the pages that requests hold (held int32 [n_requests]) to the front of the pool, between steps; pages
-        past the held tokens come back as with trim.  Returns their number, read from the device."""
+        past the held tokens come back as with trim, which refuses the same lengths.  Returns their number, read from
+        the device."""
         self._between_steps("compact")
+        if self._shared:
+            _want("Batch.compact", "held", held, torch.int32, self.n_requests)
+            self._refuse_cut("compact", held)
         table = torch.empty_like(self.block_table)
         n_used = int(batch_compact(self.cfg, self.n_kv_heads, self.k_pages, self.v_pages, self.block_table, held, table,
                                    self._pages_workspace()))

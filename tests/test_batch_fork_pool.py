@@ -218,3 +218,106 @@ def test_a_random_program(pool, seed):
         else:
             p.b.compact(p.held)
         p.check()
+
+
+def _i(v):
+    return torch.tensor(v, dtype=torch.int32)
+
+
+def _shared(pool):
+    """Two requests that share two full pages, request 1 rolled back into the second one without a trim."""
+    p = pool(2, 260, 8, 4)
+    assert p.step([128, 0])
+    p.fork([0, 0])
+    p.text[1] = p.text[1][:100]
+    return p, (p.b.block_table.clone(), p.b.free_pages.clone())
+
+
+def _unchanged(p, before):
+    assert torch.equal(p.b.block_table, before[0]) and torch.equal(p.b.free_pages, before[1])
+    p.check()
+
+
+def test_a_step_does_not_write_into_a_shared_page(pool):
+    p, before = _shared(pool)
+    assert not p.step([0, 5])  # (rows of request 1 would be tokens 100 to 104 of request 0)
+    assert p.b.status.tolist() == [ob.BAD_LENGTHS] * 2 and p.b.slot.max() < 0
+    _unchanged(p, before)
+    assert p.step([5, 0])  # (the one that ends inside gets no rows)
+    p.check()
+    p.b.release(0)
+    p.text[0] = []
+    assert p.step([0, 5])  # (nobody else holds the page any more)
+    p.check()
+
+
+def test_a_step_of_a_request_that_shares_whole_pages_only(pool):
+    p, _ = _shared(pool)
+    p.text[1] = p.text[1][:64]
+    assert p.step([3, 40])
+    p.b.trim(p.held)
+    p.check(exact=True)
+    assert p.step([1, 1])  # (the pages that it ends in are its own)
+    p.check()
+
+
+def test_a_fork_does_not_keep_a_shared_page_that_is_cut(pool):
+    p, before = _shared(pool)
+    for source in ([0, 1], [1, 0], [1, 0], [0, 1]):
+        with pytest.raises(ValueError, match="another one holds"):
+            p.fork(source)
+        _unchanged(p, before)
+    p.fork([0, 0])  # (what request 1 held is given up)
+    p.check(exact=True)
+    p, _ = _shared(pool)
+    p.fork([-1, 1])  # (request 0 ends: the page is request 1's alone)
+    assert p.step([3, 5])
+    p.check()
+    p, _ = _shared(pool)
+    p.fork([1, 1])  # (one goes on with the page, the other with a copy)
+    assert p.step([3, 5])
+    p.check()
+    with pytest.raises(RuntimeError, match="not forked"):
+        p.b.fork(_i([0, 2]), p.held)
+
+
+def test_a_compaction_does_not_cut_a_shared_page(pool):
+    p, before = _shared(pool)
+    with pytest.raises(ValueError, match="another one holds"):
+        p.b.compact(p.held)
+    _unchanged(p, before)
+    p.text[1] = p.text[1][:64]
+    p.b.compact(p.held)
+    p.check(exact=True)
+
+
+@pytest.mark.parametrize("seed", range(8))
+def test_a_random_program_that_rolls_back(pool, seed):
+    """As test_a_random_program, with requests that step back anywhere and nothing trimmed: a call is refused and
+    changes nothing, or every request reads its own tokens after it."""
+    rng = np.random.default_rng(100 + seed)
+    B, refused = 4, 0
+    p = pool(B, B * 128, 60, 8)
+    assert p.step([128, 100, 0, 0])
+    for _ in range(60):
+        do = rng.integers(4)
+        before = p.b.block_table.clone(), p.b.free_pages.clone()
+        if rng.random() < 0.3:
+            b = int(rng.integers(B))
+            p.text[b] = p.text[b][:int(rng.integers(0, len(p.text[b]) + 1))]
+        try:
+            if do <= 1:
+                n = [int(m) if len(t) + m <= 500 else 0 for m, t in zip(rng.integers(0, 70, B), p.text)]
+                ok = p.step(n)
+                refused += not ok
+            elif do == 2:
+                p.fork([int(s) for s in rng.integers(-1 if rng.random() < 0.2 else 0, B, B)])
+            else:
+                p.b.compact(p.held)
+        except (ValueError, RuntimeError):
+            refused += 1
+            assert torch.equal(p.b.block_table, before[0]) and torch.equal(p.b.free_pages, before[1])
+        for b, text in enumerate(p.text):
+            pages = p.b.block_table[b, :-(-len(text) // PAGE)].numpy()
+            assert list(p.slots[pages].reshape(-1)[:len(text)] if len(pages) else []) == text, b
+    assert refused

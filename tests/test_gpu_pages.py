@@ -248,3 +248,61 @@ def test_refusals(binding, name, make, match):
     with pytest.raises(binding.LlmcadError):  # (tables in place)
         t = _dev(pool.table)
         binding.batch_compact(pool.cfg, pool.Hkv, pool.k, pool.v, t, _dev(pool.held), t, pool.work)
+
+
+def test_a_plan_that_would_write_into_a_shared_page(binding):
+    """After a fork, a request rolled back into a page that another one holds: no request is placed, nothing is
+    written, in a captured plan too; a request that ends on the page's border goes on."""
+    import workloads
+
+    shape = workloads.MODELS["tiny"]
+    b = binding.Batch(shape, 2, 140, n_pages=8, max_pages=4)
+    b.plan(_dev([0, 128, 128]), _dev([0, 0]))
+    b.advance()
+    b.k_pages.normal_()
+    b.v_pages.normal_()
+    held = b.fork(_dev([0, 0]), _dev([128, 0]))
+    assert held.tolist() == [128, 128] and torch.equal(b.block_table[0], b.block_table[1])
+    before = b.k_pages.clone(), b.v_pages.clone(), b.block_table.clone(), b.free_pages.clone()
+    H, Dh = shape.n_heads, shape.head_dim
+    q = torch.randn(140, H, Dh, device="cuda").to(torch.bfloat16)
+
+    def untouched():
+        torch.cuda.synchronize()
+        b.store(0, q, q, q, torch.empty_like(q))
+        for now, old in zip((b.k_pages, b.v_pages, b.block_table, b.free_pages), before):
+            assert torch.equal(now, old)
+
+    start, held = _dev([0, 0, 5]), _dev([128, 100])
+    b.plan(start, held)
+    assert b.status.tolist() == [binding.PLAN_BAD_LENGTHS] * 2
+    untouched()
+    with pytest.raises(RuntimeError, match="not placed"):
+        b.advance()
+    assert held.tolist() == [128, 100]
+    with pytest.raises(ValueError, match="another one holds"):
+        b.fork(_dev([0, 1]), held)
+    with pytest.raises(ValueError, match="another one holds"):
+        b.compact(held)
+    untouched()
+    b.plan(_dev([0, 5, 5]), held)  # (the one that ends inside has no rows)
+    assert not b.status.any() and int(b.taken) == 1
+    b.plan(start, _dev([128, 64]))
+    assert not b.status.any() and int(b.taken) == 1
+    b.block_table.copy_(before[2])  # (as if the last two had not been)
+    b.plan(start, held)
+    with pytest.raises(RuntimeError, match="not placed"):
+        b.advance()
+    untouched()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        b.plan(start, held)
+    for length, status in ((100, 1), (128, 0), (127, 1), (64, 0), (1, 1)):
+        held.copy_(_dev([128, length]))
+        b.block_table.copy_(before[2])
+        graph.replay()
+        torch.cuda.synchronize()
+        assert b.status.tolist() == [status] * 2, length
+        if status:
+            untouched()
