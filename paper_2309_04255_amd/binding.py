@@ -399,6 +399,7 @@ PLAN_OK = 0
 PLAN_BAD_LENGTHS = 1
 PLAN_NO_PAGES = 2
 PLAN_BAD_TREE = 3
+PLAN_MOVED = 4  # (Batch alone: a fork or compaction moved the plan's pages)
 _PLAN_REGIONS = ("slot", "position", "mask", "rope", "status", "taken")
 
 
@@ -1017,7 +1018,10 @@ class Batch:
     Until advance, a plan's new pages are in the block tables and on the free list both.  Where it did not
     place every request, advance (which raises), release and trim take them out of the tables, and the step can
     be planned anew; so does another plan, which replaces one that was not advanced.  release and trim after a
-    good plan give back the requests' own pages alone, and advance drops those that the tables still hold."""
+    good plan give back the requests' own pages alone, and advance drops those that the tables still hold.
+
+    fork and compact come between steps: they end the last plan (its slots become -1), and store, attention and
+    commit raise until there is another."""
 
     def __init__(self, shape, n_requests: int, n_rows: int, n_pages: int, max_pages: int, prefix_len: int = 0,
                  k_cache=None, v_cache=None, n_kv_heads=None, device="cuda"):
@@ -1044,6 +1048,7 @@ class Batch:
             setattr(self, name, view)  # slot, position, mask, rope, status, taken
         self._planned = False  # the last plan's pages are on the free list still
         self._shared = False   # some pages may be in several tables (fork)
+        self._moved = False    # no plan was made here since the last fork or compaction
         self._more_workspaces = {}  # of adjust, fork and compact, made when first used
         self._changed = False  # ... and some of them have left the tables
 
@@ -1108,7 +1113,7 @@ class Batch:
             held = torch.where(self._cut(held) & (row_start[1:] > row_start[:-1]), -1, held)
         if self._planned:
             self._undo()
-        self._planned = True
+        self._planned, self._moved = True, False
         batch_plan(self.cfg, row_start, held, parent, self.prefix_len, self.block_table, self.free_pages,
                    self.n_pages, self.plan_buffer, self.n_rows)
 
@@ -1118,17 +1123,36 @@ class Batch:
             if t.dim() == 0 or t.shape[0] != self.n_rows:
                 raise ValueError(f"Batch.{what}: {name} must have {self.n_rows} rows, padding included, got {tuple(t.shape)}")
 
+    def _void_plan(self):
+        """After a fork or compaction: the last plan's rows have no slots any more (a commit would write into pages
+        that are others' now)."""
+        self.slot.fill_(-1)
+        self.status.fill_(PLAN_MOVED)
+        self._moved = True
+
+    def _live_plan(self, what):
+        """There was a plan since the last fork or compaction: Batch.plan's, or one that a program (or a graph) made
+        in plan_buffer itself, which the device knows.  (A call that is captured does not ask: it may follow such a
+        plan, and without one finds no slots.)"""
+        if self._moved and not (self.status.is_cuda and torch.cuda.is_current_stream_capturing()):
+            if int(self.status[0]) == PLAN_MOVED:
+                raise RuntimeError(f"Batch.{what}: the pages moved since the last plan (fork, compact)")
+            self._moved = False
+
     def store(self, layer, q, k, v, q_out):
+        self._live_plan("store")
         self._rows("store", q=q, k=k, v=v, q_out=q_out)
         batch_store(self.cfg, self.n_kv_heads, layer, q, k, v, q_out, self.k_pages, self.v_pages, self.plan_buffer,
                     self.n_requests)
 
     def norm_store(self, layer, q, k, v, q_gain, k_gain, q_out):
+        self._live_plan("norm_store")
         self._rows("norm_store", q=q, k=k, v=v, q_out=q_out)
         batch_norm_store(self.cfg, self.n_kv_heads, layer, q, k, v, q_gain, k_gain, q_out, self.k_pages, self.v_pages,
                          self.plan_buffer, self.n_requests)
 
     def attention(self, layer, q, out):
+        self._live_plan("attention")
         self._rows("attention", q=q, out=out)
         batch_attention(self.cfg, self.n_kv_heads, layer, q, self.k_cache, self.v_cache, self.prefix_len, self.k_pages,
                         self.v_pages, self.block_table, self.plan_buffer, out, self.workspace)
@@ -1145,6 +1169,7 @@ class Batch:
         batch_accept(self.cfg, self.plan_buffer, self.n_requests, tokens, greedy, path, accept_len, next_token, history)
 
     def commit(self, path, accept_len):
+        self._live_plan("commit")
         self._rows("commit", path=path)
         batch_commit(self.cfg, self.n_kv_heads, self.k_pages, self.v_pages, self.plan_buffer, self.n_requests, path,
                      accept_len)
@@ -1219,6 +1244,7 @@ class Batch:
         self.block_table.copy_(table)
         self.free_pages = free[:n_free].clone()
         self._shared = True
+        self._void_plan()
         return lengths
 
     def compact(self, held):
@@ -1234,4 +1260,5 @@ class Batch:
                                    self._pages_workspace()))
         self.block_table.copy_(table)
         self.free_pages = torch.arange(n_used, self.n_pages, dtype=torch.int32, device=held.device)
+        self._void_plan()
         return n_used

@@ -321,3 +321,77 @@ def test_a_random_program_that_rolls_back(pool, seed):
             pages = p.b.block_table[b, :-(-len(text) // PAGE)].numpy()
             assert list(p.slots[pages].reshape(-1)[:len(text)] if len(pages) else []) == text, b
     assert refused
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    """Names of the step's operators that reached the library."""
+    from paper_2309_04255_amd import binding
+
+    made = []
+    for name in ("store", "norm_store", "attention", "commit"):
+        monkeypatch.setattr(binding, f"batch_{name}", lambda *a, name=name: made.append(name))
+    return made
+
+
+def _operators(b):
+    x, i = torch.zeros(b.n_rows, 4, 64), _i([0] * b.n_rows)
+    return {"store": lambda: b.store(0, x, x, x, x), "norm_store": lambda: b.norm_store(0, x, x, x, None, None, x),
+            "attention": lambda: b.attention(0, x, x), "commit": lambda: b.commit(i, _i([0] * b.n_requests))}
+
+
+@pytest.mark.parametrize("name", ["store", "norm_store", "attention", "commit"])
+@pytest.mark.parametrize("move", ["fork", "compact"])
+def test_a_plan_from_before_its_pages_moved(pool, calls, name, move):
+    from paper_2309_04255_amd import binding
+
+    p = pool(3, 300, 12, 4)
+    call = _operators(p.b)[name]
+    assert p.step([70, 80, 90])
+    call()
+    p.b.release(0)
+    p.text[0] = []
+    p.fork([0, 1, 1]) if move == "fork" else p.b.compact(p.held)
+    del calls[:]
+    for _ in range(2):
+        with pytest.raises(RuntimeError, match="pages moved"):
+            call()
+    assert not calls and p.b.slot.max() < 0
+    p.check(exact=True)
+    free = p.b.free_pages.clone()
+    with pytest.raises(RuntimeError):
+        p.b.advance()  # (no plan: no pages to drop)
+    assert torch.equal(p.b.free_pages, free)
+    # a plan made without Batch.plan, as a captured step does
+    start = _i([0, 1, 2, 3])
+    binding.batch_plan(p.b.cfg, start, p.held, None, 0, p.b.block_table, p.b.free_pages, 12, p.b.plan_buffer, 300)
+    call()
+    p.fork([0, 1, 2]) if move == "fork" else p.b.compact(p.held)
+    with pytest.raises(RuntimeError, match="pages moved"):
+        call()
+    assert p.step([1, 1, 1])
+    call()
+    assert calls == [name] * 2
+
+
+@pytest.mark.parametrize("fails", ["no room", "cut", "not advanced"])
+def test_a_fork_or_compaction_that_was_refused_leaves_the_plan(pool, calls, fails):
+    p = pool(3, 300, 4 if fails == "no room" else 12, 4)
+    if fails == "cut":
+        assert p.step([128, 0, 0])
+        p.fork([0, 0, 0])
+        p.text[1] = p.text[1][:100]
+        assert p.step([70, 0, 0])
+    else:
+        assert p.step([70, 80, 0])
+    if fails == "not advanced":
+        p.b.plan(_i([0, 1, 2, 3]), p.held)
+    slot = p.b.slot.clone()
+    with pytest.raises((RuntimeError, ValueError)):
+        p.fork([0, 1, 1])
+    if fails != "no room":
+        with pytest.raises((RuntimeError, ValueError)):
+            p.b.compact(p.held)
+    for call in _operators(p.b).values():
+        call()
+    assert len(calls) == 4 and torch.equal(p.b.slot, slot)

@@ -306,3 +306,64 @@ def test_a_plan_that_would_write_into_a_shared_page(binding):
         assert b.status.tolist() == [status] * 2, length
         if status:
             untouched()
+
+
+@pytest.mark.parametrize("move", ["fork", "compact"])
+def test_a_commit_after_its_pages_moved(binding, move):
+    """It raises, and what reaches the device with that plan (a captured commit) moves nothing; a captured step that
+    plans for itself works on after it."""
+    import workloads
+
+    shape = workloads.MODELS["tiny"]
+    N, H, Dh = 40, shape.n_heads, shape.head_dim
+    b = binding.Batch(shape, 2, N, n_pages=9, max_pages=4)
+    q = torch.randn(N, H, Dh, device="cuda").to(torch.bfloat16)
+    start, held, parent = _dev([0, 20, 40]), _dev([50, 0]), _dev([-1] + [0] * 19 + [-1] + [0] * 19)
+    b.block_table[0, 0] = 8
+    b.free_pages = b.free_pages[:8].clone()
+    path, accept = _dev([0, 7] + [-1] * 18 + [0, 9] + [-1] * 18), _dev([1, 1])
+    b.plan(start, held, parent)
+    for layer in range(shape.n_layers):
+        b.store(layer, q, q, q, torch.empty_like(q))
+    b.advance()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        b.commit(path, accept)
+    held += 20
+    b.release(0)  # (so that the other's page moves, or somebody else gets this one's)
+    held[0] = 0
+    if move == "fork":
+        held = b.fork(_dev([1, 1]), held)
+    else:
+        b.compact(held)
+    before = b.k_pages.clone(), b.v_pages.clone()
+    with pytest.raises(RuntimeError, match="pages moved"):
+        b.commit(path, accept)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(b.k_pages, before[0]) and torch.equal(b.v_pages, before[1])
+    free = b.free_pages.clone()
+
+    def step():
+        binding.batch_plan(b.cfg, start, held, parent, 0, b.block_table, free, b.n_pages, b.plan_buffer, N)
+        for layer in range(shape.n_layers):
+            b.store(layer, q, q, q, torch.empty_like(q))
+        b.commit(path, accept)
+
+    again = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(again):
+        step()
+    table = b.block_table.clone()
+    again.replay()
+    torch.cuda.synchronize()
+    assert not b.status.any()
+    once = b.k_pages.clone(), b.v_pages.clone(), b.block_table.clone()
+    assert not torch.equal(once[0], before[0])
+    b.commit(path, _dev([0, 0]))  # (an eager call after a replayed plan is no refusal)
+    for t, old in zip((b.k_pages, b.v_pages, b.block_table), (*before, table)):
+        t.copy_(old)
+    step()
+    torch.cuda.synchronize()
+    for t, want in zip((b.k_pages, b.v_pages, b.block_table), once):
+        assert torch.equal(t, want)
