@@ -1044,13 +1044,14 @@ class Batch:
         self.free_pages = torch.arange(self.n_pages, dtype=torch.int32, device=dev)
         self.plan_buffer = torch.zeros(size, dtype=torch.uint8, device=dev)
         self.workspace = torch.zeros(work, dtype=torch.uint8, device=dev)
+        self.adjust_workspace = torch.empty(batch_adjust_workspace_bytes(self.cfg, self.n_rows), dtype=torch.uint8, device=dev)
+        self.pages_workspace = torch.empty(batch_pages_workspace_bytes(self.n_requests, self.n_pages), dtype=torch.uint8, device=dev)
         for name, view in batch_plan_views(self.cfg, self.n_requests, self.n_rows, self.plan_buffer).items():
             setattr(self, name, view)  # slot, position, mask, rope, status, taken
         self._planned = False  # the last plan's pages are on the free list still
+        self._changed = False  # ... and some of them have left the tables
         self._shared = False   # some pages may be in several tables (fork)
         self._moved = False    # no plan was made here since the last fork or compaction
-        self._more_workspaces = {}  # of adjust, fork and compact, made when first used
-        self._changed = False  # ... and some of them have left the tables
 
     def _among(self, ids, others):
         """Which of ids are pages that others hold too (what is no page is not)."""
@@ -1158,10 +1159,11 @@ class Batch:
                         self.v_pages, self.block_table, self.plan_buffer, out, self.workspace)
 
     def adjust(self, logits, tokens=None, out=None, greedy=None, **by):
-        """batch_adjust of the step's rows (by: history, prompt_len, seen, penalties, bias, allow, mask_of)."""
+        """batch_adjust of the step's rows (by: history, prompt_len, seen, penalties, bias, allow, mask_of, stream).
+        Its workspace is the Batch's: two of its calls must not overlap."""
         self._rows("adjust", logits=logits)
         batch_adjust(self.cfg, self.plan_buffer, self.n_requests, logits, tokens=tokens, out=out, greedy=greedy,
-                     workspace=self._workspace("adjust", batch_adjust_workspace_bytes(self.cfg, self.n_rows)), **by)
+                     workspace=self.adjust_workspace, **by)
 
     def accept(self, tokens, greedy, path, accept_len, next_token, history=None):
         """The accept walk of every request's tree: what commit takes, and the tokens after it."""
@@ -1212,14 +1214,6 @@ class Batch:
         if self._planned:
             raise RuntimeError(f"Batch.{what}: a plan was not advanced")
 
-    def _workspace(self, what, size):
-        if what not in self._more_workspaces:
-            self._more_workspaces[what] = torch.empty(size, dtype=torch.uint8, device=self.block_table.device)
-        return self._more_workspaces[what]
-
-    def _pages_workspace(self):
-        return self._workspace("pages", batch_pages_workspace_bytes(self.n_requests, self.n_pages))
-
     def fork(self, source, held):
         """Request b continues from request source[b], which holds held[source[b]] tokens (itself: it stays; negative:
         it ends; int32 [n_requests] both; see llmcad_batch_fork).  Between steps: after advance (and commit).  Full pages
@@ -1237,7 +1231,7 @@ class Batch:
         table, lengths = torch.empty_like(self.block_table), torch.empty_like(held)
         free = torch.empty(self.n_pages, dtype=torch.int32, device=held.device)
         n_free, status = batch_fork(self.cfg, self.n_kv_heads, self.k_pages, self.v_pages, self.block_table, held, source,
-                                    table, lengths, free, self._pages_workspace())
+                                    table, lengths, free, self.pages_workspace)
         n_free, status = torch.cat([n_free, status]).tolist()
         if status != PLAN_OK:
             raise RuntimeError(f"the requests were not forked (plan status {status})")
@@ -1257,7 +1251,7 @@ class Batch:
             self._refuse_cut("compact", held)
         table = torch.empty_like(self.block_table)
         n_used = int(batch_compact(self.cfg, self.n_kv_heads, self.k_pages, self.v_pages, self.block_table, held, table,
-                                   self._pages_workspace()))
+                                   self.pages_workspace))
         self.block_table.copy_(table)
         self.free_pages = torch.arange(n_used, self.n_pages, dtype=torch.int32, device=held.device)
         self._void_plan()

@@ -395,3 +395,24 @@ def test_a_fork_or_compaction_that_was_refused_leaves_the_plan(pool, calls, fail
     for call in _operators(p.b).values():
         call()
     assert len(calls) == 4 and torch.equal(p.b.slot, slot)
+
+
+def test_workspaces_are_made_with_the_batch(pool, monkeypatch):
+    """No call takes memory of whatever stream it runs on: adjust, fork and compact find their workspaces made."""
+    from paper_2309_04255_amd import binding
+
+    p = pool(2, 40, 6, 3)
+    b, seen = p.b, []
+    adjust = lambda *a, workspace, **kw: seen.append(workspace)  # noqa: E731
+    pages = lambda name, inner: lambda *a, **kw: (seen.append(a[-1]), inner(*a, **kw))[1]  # noqa: E731
+    monkeypatch.setattr(binding, "batch_adjust", adjust)
+    for name in ("batch_fork", "batch_compact"):
+        monkeypatch.setattr(binding, name, pages(name, getattr(binding, name)))
+    made = {t.data_ptr(): t.numel() for t in vars(b).values() if isinstance(t, torch.Tensor)}
+    b.adjust(torch.zeros(40, b.cfg.vocab), greedy=_i([0] * 40))
+    assert p.step([20, 20])
+    p.fork([0, 0])
+    b.compact(p.held)
+    want = [binding.batch_adjust_workspace_bytes(b.cfg, 40)] + [binding.batch_pages_workspace_bytes(2, 6)] * 2
+    assert [t.numel() for t in seen] == want
+    assert [made.get(t.data_ptr()) for t in seen] == want
