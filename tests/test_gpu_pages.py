@@ -367,3 +367,19 @@ def test_a_commit_after_its_pages_moved(binding, move):
     torch.cuda.synchronize()
     for t, want in zip((b.k_pages, b.v_pages, b.block_table), once):
         assert torch.equal(t, want)
+
+
+@pytest.mark.parametrize("held,source,kw", [
+    ([33, 700, 1, 64], [1, 1, 0, 0], {"width": 3000, "L": 3, "Hkv": 3}),       # a wide table
+    ([130, 70, 0, 65] * 20, [4 * g + i for g in range(20) for i in (3, 0, 0, 1)], {"L": 8, "H": 8, "Hkv": 8}),  # many page heads
+])
+def test_forks_of_heads_of_128_in_two_launches(binding, held, source, kw):
+    want = Pool(binding, held, spare=30, Dh=128, **kw).check_fork(source)  # (20 groups: a copy each)
+    assert want["copies"] and want["status"] == ob.OK
+
+
+@pytest.mark.parametrize("held,kw", [
+    ([100, 0, 700, 64], {"width": 5000, "spare": 11, "L": 3, "H": 6, "Hkv": 3}), ([130] * 300, {"n_pages": 1100, "L": 2, "Hkv": 2, "width": 30}),
+])
+def test_compactions_of_heads_of_128_in_two_launches(binding, held, kw):
+    assert _check_compact(Pool(binding, held, Dh=128, **kw))
