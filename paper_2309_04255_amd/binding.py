@@ -1088,21 +1088,17 @@ class Batch:
             pages = pages[first[pages.long()] == at]
         return pages
 
-    def _cut(self, held, of=None):
-        """Which requests' lengths end inside a page that another request holds too, bool [n_requests] (of: the
-        requests that count, the others hold nothing).  The next step would write into it behind the other's back."""
-        cols = torch.arange(self.block_table.shape[1], device=held.device)
-        kept = (cols * PAGE < held[:, None]) & (self.block_table >= 0) & (self.block_table < self.n_pages)
-        if of is not None:
-            kept &= of[:, None]
-        index = torch.where(kept, self.block_table, self.n_pages).long()
-        holders = torch.zeros(self.n_pages + 1, dtype=torch.int32, device=held.device)
-        holders.scatter_add_(0, index.view(-1), torch.ones_like(index.view(-1), dtype=torch.int32))
-        last = (cols == (held // PAGE)[:, None]) & (held % PAGE > 0)[:, None]
-        return (last & kept & (holders[index] > 1)).any(1)
+    def _cut(self, held):
+        """Which requests' lengths end inside a page that another request holds too, bool [n_requests]: the next step
+        would write into it behind the other's back.  (A page has one column in all tables: its keys are turned.)"""
+        held = held.clamp(min=0)
+        col = held // PAGE
+        last = self.block_table.index_select(1, col.clamp(max=self.block_table.shape[1] - 1))  # [b, c]: b's in c's last column
+        holds = (held[:, None] > col * PAGE) & (last == last.diagonal()) & (last >= 0)
+        return holds.diagonal() & (holds.sum(0) > 1)
 
-    def _refuse_cut(self, what, held, of=None):
-        if bool(self._cut(held, of).any()):
+    def _refuse_cut(self, what, held):
+        if bool(self._cut(held).any()):
             raise ValueError(f"{what}: a request would end inside a page that another one holds")
 
     def plan(self, row_start, held, parent=None):
@@ -1227,7 +1223,7 @@ class Batch:
             _want("Batch.fork", "held", held, torch.int32, self.n_requests)
             alive = torch.zeros(self.n_requests + 1, dtype=torch.bool, device=held.device)
             alive[torch.where((source >= 0) & (source < self.n_requests), source, self.n_requests).long()] = True
-            self._refuse_cut("fork", held, alive[:-1])
+            self._refuse_cut("fork", torch.where(alive[:-1], held, 0))  # (a request that ends holds nothing)
         table, lengths = torch.empty_like(self.block_table), torch.empty_like(held)
         free = torch.empty(self.n_pages, dtype=torch.int32, device=held.device)
         n_free, status = batch_fork(self.cfg, self.n_kv_heads, self.k_pages, self.v_pages, self.block_table, held, source,

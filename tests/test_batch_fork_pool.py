@@ -416,3 +416,24 @@ def test_workspaces_are_made_with_the_batch(pool, monkeypatch):
     want = [binding.batch_adjust_workspace_bytes(b.cfg, 40)] + [binding.batch_pages_workspace_bytes(2, 6)] * 2
     assert [t.numel() for t in seen] == want
     assert [made.get(t.data_ptr()) for t in seen] == want
+
+
+def test_lengths_at_the_ends_of_a_table(pool):
+    """Full tables that share every page, lengths of zero and below, rows of the tables that were given back."""
+    p = pool(4, 260, 16, 2)
+    assert p.step([128, 0, 70, 0])
+    p.fork([0, 0, 2, 2])
+    p.check(exact=True)
+    p.b.trim(p.held)
+    p.b.compact(p.held)
+    p.check(exact=True)
+    p.b.release(3)
+    p.text[3] = []
+    p.b.trim(_i([128, 128, 70, 5]))  # (nothing of the last one's is left)
+    assert not p.step([0, 1, 0, 0])  # (no column is left)
+    assert p.b.status.tolist() == [0, ob.NO_PAGES, 0, 0]
+    p.text[1] = []
+    p.b.trim(_i([128, -1, 70, 0]))
+    p.check(exact=True)
+    assert p.step([0, 100, 1, 9])
+    p.check()
