@@ -12,9 +12,11 @@
 //
 // Bytes bound it where little is marked: 255 rows of 128000 bf16 logits are copied in 24 us
 // (5300 GB/s) and their greedy tokens found in 15 (4300).  With all adjustments they take
-// 45: the marked tokens (a tenth of a piece where a text's tokens are near each other) cost
-// about 60 vector instructions each step, a barrier waits for the slowest wave, and three
-// workgroups are on a CU (LDS).  561 rows of 32000 fp32 logits take 27.6 us (14 to read
+// 45: the marked tokens (a tenth of a piece where a text's tokens are near each other) are
+// taken by each lane from its own eight, so that a wave makes as many steps of about 60 vector
+// instructions as its fullest lane has (three or four, where the mean is 0.8); a barrier waits
+// for the slowest wave, and three workgroups are on a CU (LDS).  That is this loop's price and
+// no limit: marked tokens dealt to all lanes of a wave have not been tried.  561 rows of 32000 fp32 logits take 27.6 us (14 to read
 // them), a tree of 31 7.2, two launches' latency.
 //
 // Measured and left out: the next tile's loads in flight while one is computed (registers
@@ -624,7 +626,9 @@ hipError_t launch_batch_adjust(const AdjustArgs& args, hipStream_t st) {
   // About as many workgroups as the GPU holds (three on a CU, four without penalties): of
   // several rows each where requests have eight or more (32 trees of up to 41 with histories
   // of up to 1000: 27.6 us for 32.3), of several pieces of a row otherwise (four rows each
-  // of 64 requests: 20.3 for 21.8; at eight each takes 40).
+  // of 64 requests: 20.3 for 21.8; at eight each takes 40).  N counts padding and B requests
+  // that sit out (the device alone knows the others): single tokens in a step sized for trees
+  // take the first form, with the same results.
   const long long tiles = (long long)a.chunks * a.N;
   const bool rows = a.N >= 8ll * a.B && tiles < 1ll << 26;  // (a launch takes 2^32 threads)
   const long long want = a.by.penalties ? 768 : 1024;

@@ -9,8 +9,8 @@
 // heads, take two, one that decides and leaves the copies in the workspace, and one that
 // copies.
 //
-// Bound by bytes where pages are whole: a 7B pool's 34 moves (1.15 GB each way) take 459 us
-// (5250 GB/s).  A fork copies parts of pages, and of V^T parts of lines, which memory reads
+// Bound by bytes where pages are whole: a 7B pool's 34 moves (1.14 GB each way) take 453 to 459 us
+// (4970 to 5040 GB/s).  A fork copies parts of pages, and of V^T parts of lines, which memory reads
 // and writes whole: 19 copies of 32 tokens on average of 40 layers of 8 heads, 99 MB, are
 // 229 MB read and 125 written (copies 81 us, deciding 10).  Small ones are a chain of
 // latencies: lengths, tables, two counts, the copies (four requests of the ~1B model 12 us, a
@@ -403,7 +403,8 @@ void launch_copies(const PagesArgs& a, long long most, hipStream_t st) {
 
 hipError_t launch_batch_fork(const PagesArgs& a, hipStream_t st) {
   // (One launch: four requests of 22 layers of 16 heads 11.9 us for 14.6 with two; 64 of 40 layers of 8 heads, where
-  // the deciding part's registers and LDS cost the copies' waves, 99 for 93.)
+  // the deciding part's registers and LDS cost the copies' waves, 99 for 93.  The limits lie between these sizes,
+  // none of which between was timed; the copies may be few, which the device alone knows.)
   if (!is_small(a, 2048) || (long long)a.B * a.L * a.Hkv > 4096) {
     fork_plan_kernel<<<dim3(plan_groups(a)), dim3(kLarge), 0, st>>>(a);
     launch_copies(a, a.B, st);
