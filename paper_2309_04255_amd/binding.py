@@ -1020,8 +1020,8 @@ class Batch:
     be planned anew; so does another plan, which replaces one that was not advanced.  release and trim after a
     good plan give back the requests' own pages alone, and advance drops those that the tables still hold.
 
-    fork and compact come between steps: they end the last plan (its slots become -1), and store, attention and
-    commit raise until there is another."""
+    fork and compact come between steps: they end the last plan (its slots become -1, its status PLAN_MOVED), and
+    store, attention and commit raise until there is another."""
 
     def __init__(self, shape, n_requests: int, n_rows: int, n_pages: int, max_pages: int, prefix_len: int = 0,
                  k_cache=None, v_cache=None, n_kv_heads=None, device="cuda"):
@@ -1110,9 +1110,10 @@ class Batch:
             held = torch.where(self._cut(held) & (row_start[1:] > row_start[:-1]), -1, held)
         if self._planned:
             self._undo()
-        self._planned, self._moved = True, False
+        self._planned = True
         batch_plan(self.cfg, row_start, held, parent, self.prefix_len, self.block_table, self.free_pages,
                    self.n_pages, self.plan_buffer, self.n_rows)
+        self._moved = False
 
     def _rows(self, what, **tensors):
         """Every tensor has the plan's n_rows rows (with another number the kernels would leave all as it was)."""

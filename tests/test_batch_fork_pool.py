@@ -437,3 +437,24 @@ def test_lengths_at_the_ends_of_a_table(pool):
     p.check(exact=True)
     assert p.step([0, 100, 1, 9])
     p.check()
+
+
+def test_a_refused_plan_is_no_plan(pool, calls, monkeypatch):
+    from paper_2309_04255_amd import binding
+
+    p = pool(2, 40, 6, 3)
+    assert p.step([20, 20])
+    p.b.compact(p.held)
+
+    def refuses(*a, **kw):
+        raise ValueError("batch_plan: parent")
+
+    with monkeypatch.context() as m:
+        m.setattr(binding, "batch_plan", refuses)
+        with pytest.raises(ValueError, match="parent"):
+            p.b.plan(_i([0, 1, 2]), p.held)
+    for call in _operators(p.b).values():
+        with pytest.raises(RuntimeError, match="pages moved"):
+            call()
+    assert p.step([1, 1])
+    p.check()
